@@ -1,0 +1,174 @@
+// gate_norm.hip -- the norms after and before a block with its gate, residual scale and sum.
+//
+//   n = post(u) act(gate)   or   post(u act(gate));    y = residual + scale scale_vec n;    h = pre(y)
+//
+// Bound by memory: each tensor is read or written once.  TPR threads hold one group (a row, or a
+// head of it) in registers between the reductions; statistics, products and y stay in fp32 until they are
+// stored.  The mean of a LAYER norm is taken off before the squares are summed, so a large
+// mean costs no digits.
+#include "seqmix_device.h"
+
+namespace cv {
+
+// Sum over the TPR threads of a group; `red` (one float per wave) is used when a group spans waves.
+template <int TPR>
+__device__ __forceinline__ float group_sum(float v, float* red) {
+#pragma unroll
+    for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1) v += __shfl_xor(v, m);
+    if constexpr (TPR > 64) {
+        __syncthreads();  // the previous sum has been read
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) v += red[i];
+    }
+    return v;
+}
+
+// Norms x in place: V * ITEMS values per thread, those at or past `n` being zero.
+template <int TPR, int V, int ITEMS>
+__device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, float eps, const float* w, const float* b,
+                                              int n, float* red) {
+    const int t = threadIdx.x % TPR;
+    const float inv = 1.0f / (float)n;
+    if (kind == SEQMIX_NORM_LAYER) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) s += x[i][v];
+        const float mean = group_sum<TPR>(s, red) * inv;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[i][v] = (i * TPR + t) * V < n ? x[i][v] - mean : 0.0f;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int v = 0; v < V; ++v) s = fmaf(x[i][v], x[i][v], s);
+    const float r = 1.0f / sqrtf(fmaf(group_sum<TPR>(s, red), inv, eps));
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (c < n) {
+            float e[V];
+            load_pack<float, V>(w + c, e);
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[i][v] *= r * e[v];
+            if (b) {
+                load_pack<float, V>(b + c, e);
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[i][v] += e[v];
+            }
+        }
+    }
+}
+
+template <typename T, typename TR, int TPR, int V, int ITEMS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormArgs A) {
+    constexpr int NT = TPR < 256 ? 256 : TPR;
+    __shared__ float red[NT / 64];
+    const int t = threadIdx.x % TPR;
+    int64_t id = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    const bool live = id < A.rows;  // TPR > 64 has one group per block: all its threads agree
+    id = live ? id : A.rows - 1;
+    const int64_t row = id / A.ngroups;
+    const int64_t col = (id - row * A.ngroups) * A.group;
+    const int n = A.group;
+
+    float x[ITEMS][V];
+    Pack<T, V> gate[ITEMS];
+    Pack<TR, V> res[ITEMS];
+    const T* u = static_cast<const T*>(A.u) + row * A.u_row + col;
+    const T* gp = static_cast<const T*>(A.gate) + (A.gate ? (row / A.gate_run) * A.gate_row + col : 0);
+    const TR* rp = static_cast<const TR*>(A.res) + (A.res ? row * A.res_row + col : 0);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[i][v] = 0.0f;
+        if (c < n) {
+            load_pack<T, V>(u + c, x[i]);
+            if (A.gate) gate[i] = *reinterpret_cast<const Pack<T, V>*>(gp + c);
+            if (A.res) res[i] = *reinterpret_cast<const Pack<TR, V>*>(rp + c);
+        }
+    }
+    auto apply_gate = [&] {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if ((i * TPR + t) * V < n) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float z = to_f32(gate[i].e[v]);
+                    x[i][v] *= A.gate_act == SEQMIX_ACT_LINEAR ? z
+                               : A.gate_act == SEQMIX_ACT_SILU ? silu(z)
+                                                               : sigmoid(z);
+                }
+            }
+    };
+    if (A.gate && A.gate_first) apply_gate();
+    if (A.post != SEQMIX_NORM_NONE) norm_in_place<TPR, V, ITEMS>(x, A.post, A.post_eps, A.post_w, A.post_b, n, red);
+    if (A.gate && !A.gate_first) apply_gate();
+
+    TR* yp = static_cast<TR*>(A.y) + (A.y ? row * A.y_row + col : 0);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (c < n) {
+            float e[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) e[v] = 1.0f;
+            if (A.scale_vec) load_pack<float, V>(A.scale_vec + col + c, e);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                x[i][v] *= A.scale * e[v];
+                if (A.res) x[i][v] += to_f32(res[i].e[v]);
+            }
+            if (A.y && live) store_pack<TR, V>(yp + c, x[i]);
+        }
+    }
+    if (A.pre == SEQMIX_NORM_NONE) return;
+    norm_in_place<TPR, V, ITEMS>(x, A.pre, A.pre_eps, A.pre_w, A.pre_b, n, red);
+    T* hp = static_cast<T*>(A.h) + row * A.h_row + col;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (c < n && live) store_pack<T, V>(hp + c, x[i]);
+    }
+}
+
+template <typename T, typename TR, int TPR, int V, int ITEMS>
+static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
+    constexpr int NT = TPR < 256 ? 256 : TPR;
+    const int64_t blocks = (a.rows + NT / TPR - 1) / (NT / TPR);
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
+    return hipGetLastError();
+}
+
+// V values per access.  Groups up to 16 accesses: a quarter wave each; up to 64: a wave; up to 1024: a block of 256
+// with 1 to 4 accesses per thread; above (16384 elements by one element each): 1024 threads.
+template <typename T, typename TR, int V>
+static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
+    const int64_t packs = (a.group + V - 1) / V;
+    if (packs <= 16) return launch_one<T, TR, 16, V, 1>(a, s);
+    if (packs <= 64) return launch_one<T, TR, 64, V, 1>(a, s);
+    if (packs <= 256) return launch_one<T, TR, 256, V, 1>(a, s);
+    if (packs <= 512) return launch_one<T, TR, 256, V, 2>(a, s);
+    if (packs <= 1024) return launch_one<T, TR, 256, V, 4>(a, s);
+    if (packs <= 4096) return launch_one<T, TR, 1024, V, 4>(a, s);
+    if constexpr (V == 1) return launch_one<T, TR, 1024, V, 16>(a, s);
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    if (dt == CONV2D_F32) return a.vec ? launch_v<float, float, 4>(a, s) : launch_v<float, float, 1>(a, s);
+    if (rdt == CONV2D_F32) return a.vec ? launch_v<uint16_t, float, 8>(a, s) : launch_v<uint16_t, float, 1>(a, s);
+    return a.vec ? launch_v<uint16_t, uint16_t, 8>(a, s) : launch_v<uint16_t, uint16_t, 1>(a, s);
+}
+
+}  // namespace cv

@@ -1,0 +1,159 @@
+// linattn.hip -- linear attention with a decay per head, token by token.
+//
+//   S_t = exp(g_t) S_{t-1} + k_t v_t^T        o_t = scale q_t S_t
+#include "seqmix_device.h"
+
+namespace cv {
+
+// Log2 of a decay from its natural log.  Logs below -1000 (-infinity among them) have an
+// exponential of exactly zero in fp32 anyway; the bound keeps differences of sums finite.  NaN stays.
+__device__ __forceinline__ double decay_log2(float g) {
+    return (double)(g < -1000.0f ? -1000.0f : g) * 1.4426950408889634;
+}
+
+// One workgroup runs one sequence, head and block of DVB columns of the state through all tokens, the
+// state in registers: thread (rg, cg) holds RPT neighbouring rows of 4 columns.  Bound by reading and writing the
+// state (8 dk dv bytes per head against 4 dk dv operations per token), so it is the kernel of single
+// tokens and very short sequences.
+template <typename T, typename TO, int DVB, int RPT, bool VEC>
+__global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
+    constexpr int LR = DVB / 4;  // threads across the columns
+    __shared__ float red[2][4][DVB];
+    const int t = threadIdx.x, cg = t % LR, rg = t / LR;
+    const int64_t b = blockIdx.x;
+    const int blk = (int)(b % A.ndvb);
+    const int64_t bh = b / A.ndvb;
+    const int head = (int)(bh % A.heads), seq = (int)(bh / A.heads);
+    const int64_t slot = seq_slot(A.sq, seq);
+    if (slot < 0) return;
+    const SeqRange r = seq_range(A.sq, seq);
+    const int c0 = blk * DVB + cg * 4, r0 = rg * RPT;
+    const int nc = min(4, A.dv - c0);                       // live columns of this thread (may be negative)
+    const int nr = nc > 0 ? max(0, min(RPT, A.dk - r0)) : 0;  // ... and rows
+    const int64_t soff = ((slot * A.heads + head) * A.dk + r0) * A.dv + c0;
+
+    float S[RPT][4];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S[i][j] = 0.0f;
+        if (A.s_in && i < nr) {
+            const float* p = A.s_in + soff + (int64_t)i * A.dv;
+            if (A.svec) {
+                load_pack<float, 4>(p, S[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < nc) S[i][j] = p[j];
+            }
+        }
+    }
+    const int qh = head / A.rep;
+    const T* q = static_cast<const T*>(A.q) + r.first * A.q_row + qh * A.q_head + r0;
+    const T* k = static_cast<const T*>(A.k) + r.first * A.k_row + qh * A.k_head + r0;
+    const T* v = static_cast<const T*>(A.v) + r.first * A.v_row + head * A.v_head + c0;
+    const float* g = A.g ? A.g + r.first * A.g_row + head : nullptr;
+    TO* o = static_cast<TO*>(A.o) + r.first * A.o_row + head * A.o_head + blk * DVB;
+
+#pragma unroll 1
+    for (int64_t n = 0; n < r.len; ++n) {
+        float kk[RPT], qq[RPT], vv[4];
+        if (VEC && nr == RPT) {
+            load_pack<T, RPT>(k, kk);
+            load_pack<T, RPT>(q, qq);
+        } else {
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                kk[i] = i < nr ? to_f32(k[i]) : 0.0f;
+                qq[i] = i < nr ? to_f32(q[i]) : 0.0f;
+            }
+        }
+        if (VEC && nc >= 4) {
+            load_pack<T, 4>(v, vv);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vv[j] = j < nc ? to_f32(v[j]) : 0.0f;
+        }
+        const float d = g ? __builtin_amdgcn_exp2f((float)decay_log2(*g)) : 1.0f;
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto update = [&](int rows) {
+#pragma unroll
+            for (int i = 0; i < RPT; ++i)
+                if (i < rows) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        S[i][j] = fmaf(kk[i], vv[j], S[i][j] * d);
+                        acc[j] = fmaf(qq[i], S[i][j], acc[j]);
+                    }
+                }
+        };
+        if (nr == RPT)
+            update(RPT);
+        else  // rows past dk stay out of the sums: 0 * infinity is no zero
+            update(nr);
+#pragma unroll
+        for (int m = LR; m < 64; m <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], m);
+        float(*rd)[DVB] = red[n & 1];  // two buffers: one barrier per token
+        if ((t & 63) < LR) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) rd[t >> 6][cg * 4 + j] = acc[j];
+        }
+        __syncthreads();
+        if (t < DVB && blk * DVB + t < A.dv)
+            o[t] = from_f32<TO>(A.scale * ((rd[0][t] + rd[1][t]) + (rd[2][t] + rd[3][t])));
+        q += A.q_row;
+        k += A.k_row;
+        v += A.v_row;
+        o += A.o_row;
+        if (g) g += A.g_row;
+    }
+    if (A.s_out) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i)
+            if (i < nr) {
+                float* p = A.s_out + soff + (int64_t)i * A.dv;
+                if (A.svec) {
+                    store_pack<float, 4>(p, S[i]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < nc) p[j] = S[i][j];
+                }
+            }
+    }
+}
+
+int attn_tokens_dvb(int) { return 32; }
+
+template <typename T, typename TO, int RPT>
+static void launch_tokens_r(const AttnArgs& a, dim3 grid, hipStream_t s) {
+    if (a.vec)
+        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, 32, RPT, true>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, 32, RPT, false>), grid, dim3(256), 0, s, a);
+}
+
+template <typename T, typename TO>
+static hipError_t launch_tokens_t(const AttnArgs& a, hipStream_t s) {
+    const int64_t blocks = (int64_t)a.sq.seqs * a.heads * a.ndvb;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks);
+    if (a.dk <= 32)
+        launch_tokens_r<T, TO, 1>(a, grid, s);
+    else if (a.dk <= 64)
+        launch_tokens_r<T, TO, 2>(a, grid, s);
+    else if (a.dk <= 128)
+        launch_tokens_r<T, TO, 4>(a, grid, s);
+    else
+        launch_tokens_r<T, TO, 8>(a, grid, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s) {
+    if (dt == CONV2D_F32) return launch_tokens_t<float, float>(a, s);
+    return odt == CONV2D_F32 ? launch_tokens_t<uint16_t, float>(a, s) : launch_tokens_t<uint16_t, uint16_t>(a, s);
+}
+
+}  // namespace cv

@@ -1,0 +1,292 @@
+// seqmix_api.hip -- C ABI of the token-mixing operators: validation, plans, workspaces, launches.
+#include <new>
+
+#include "seqmix_internal.h"
+
+using namespace cv;
+
+struct seqmix_attn_desc {
+    seqmix_attn_params p;
+    seqmix_attn_plan_info plan;
+    int64_t nseg = 0;  // segment ids at most (0: not cut)
+    // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
+    void* ws = nullptr;
+    int device = -1;
+    hipEvent_t done = nullptr;
+    hipStream_t last_stream = nullptr;
+    bool has_last = false;
+};
+struct seqmix_conv_desc {
+    seqmix_conv_params p;
+};
+struct seqmix_norm_desc {
+    seqmix_norm_params p;
+};
+
+namespace {
+
+#define SM_TRY(e)                       \
+    do {                                \
+        const int st_ = (e);            \
+        if (st_ != CONV2D_OK) return st_; \
+    } while (0)
+
+constexpr int64_t kMaxRows = (1LL << 31) - 1;
+
+bool known_dtype(int d) { return d == CONV2D_F32 || d == CONV2D_BF16; }
+int64_t esize(int d) { return d == CONV2D_BF16 ? 2 : 4; }
+
+// Rows, sequences and slots as every sequence operator has them.
+int check_seqs(int64_t tokens, int64_t seqs, int64_t slots) {
+    if (tokens < 0 || seqs < 1 || slots < 1) return CONV2D_E_INVALID;
+    if (tokens > kMaxRows || seqs > kMaxRows || slots > kMaxRows) return CONV2D_E_UNSUPPORTED;
+    return CONV2D_OK;
+}
+
+int seq_args(int64_t tokens, int64_t seqs, int64_t slots, const int64_t* off, const int32_t* slot, SeqArgs* out) {
+    if (!off && tokens % seqs != 0) return CONV2D_E_INVALID;
+    if (!slot && slots < seqs) return CONV2D_E_INVALID;
+    *out = SeqArgs{off, slot, tokens, off ? 0 : tokens / seqs, slots, (int32_t)seqs};
+    return CONV2D_OK;
+}
+
+bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
+
+// Rows `row` elements apart, heads `head` elements apart, of `dim` elements each, can hold what they should.
+bool strides_ok(int64_t tokens, int64_t row, int64_t heads, int64_t head, int64_t dim) {
+    if (head < dim && heads > 1) return false;
+    if (head < 0 || row < 0) return false;
+    // either order of rows and heads, without overlap
+    const bool rows_outer = row >= (heads - 1) * head + dim;
+    const bool heads_outer = heads > 1 && row >= dim && head >= (tokens - 1) * row + dim;
+    return tokens <= 1 || rows_outer || heads_outer;
+}
+
+hipError_t alloc_ws(seqmix_attn_desc* d) {
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (d->device >= 0) return d->device == dev ? hipSuccess : hipErrorInvalidDevice;
+    e = hipEventCreateWithFlags(&d->done, hipEventDisableTiming);
+    if (e != hipSuccess) return e;
+    e = hipMalloc(&d->ws, (size_t)d->plan.workspace_bytes);
+    if (e != hipSuccess) {
+        (void)hipEventDestroy(d->done);
+        d->done = nullptr;
+        d->ws = nullptr;
+        return e;
+    }
+    d->device = dev;
+    return hipSuccess;
+}
+
+int ensure_ws(seqmix_attn_desc* d) {
+    if (d->plan.workspace_bytes == 0) return CONV2D_OK;
+    switch (alloc_ws(d)) {
+        case hipSuccess: return CONV2D_OK;
+        case hipErrorOutOfMemory: (void)hipGetLastError(); return CONV2D_E_ALLOC;
+        case hipErrorInvalidDevice: return CONV2D_E_UNSUPPORTED;
+        default: return CONV2D_E_HIP;
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+// ------------------------------------------------------------------ attention
+int seqmix_attn_desc_create(const seqmix_attn_params* params, seqmix_attn_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_attn_params& p = *params;
+    SM_TRY(check_seqs(p.tokens, p.seqs, p.slots));
+    if (p.heads < 1 || p.qk_heads < 1 || p.heads % p.qk_heads != 0 || p.dk < 1 || p.dv < 1) return CONV2D_E_INVALID;
+    if (!strides_ok(p.tokens, p.q_row, p.qk_heads, p.q_head, p.dk) ||
+        !strides_ok(p.tokens, p.k_row, p.qk_heads, p.k_head, p.dk) ||
+        !strides_ok(p.tokens, p.v_row, p.heads, p.v_head, p.dv) ||
+        !strides_ok(p.tokens, p.o_row, p.heads, p.o_head, p.dv))
+        return CONV2D_E_INVALID;
+    if (!known_dtype(p.dtype) || !known_dtype(p.o_dtype) || (p.dtype == CONV2D_F32 && p.o_dtype != CONV2D_F32))
+        return CONV2D_E_UNSUPPORTED;
+    if (p.decay != SEQMIX_DECAY_NONE && p.decay != SEQMIX_DECAY_HEAD && p.decay != SEQMIX_DECAY_TOKEN)
+        return CONV2D_E_INVALID;
+    if (p.dk > SEQMIX_MAX_HEAD_DIM || p.dv > SEQMIX_MAX_HEAD_DIM) return CONV2D_E_UNSUPPORTED;
+    seqmix_attn_desc* d = new (std::nothrow) seqmix_attn_desc;
+    if (!d) return CONV2D_E_ALLOC;
+    d->p = p;
+    d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_attn_desc_destroy(seqmix_attn_desc* d) {
+    if (!d) return CONV2D_OK;
+    if (d->ws) (void)hipFree(d->ws);
+    if (d->done) (void)hipEventDestroy(d->done);
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_attn_plan_query(const seqmix_attn_desc* d, seqmix_attn_plan_info* out) {
+    if (!d || !out) return CONV2D_E_NULL;
+    *out = d->plan;
+    return CONV2D_OK;
+}
+
+int seqmix_attn_reserve(seqmix_attn_desc* d) {
+    if (!d) return CONV2D_E_NULL;
+    return ensure_ws(d);
+}
+
+int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const void* v, const float* decay,
+                    const int64_t* offsets, const int32_t* slot_index, const float* state_in, float* state_out, void* o,
+                    void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_attn_params& p = d->p;
+    if (p.tokens > 0 && (!q || !k || !v || !o || (p.decay != SEQMIX_DECAY_NONE && !decay))) return CONV2D_E_NULL;
+    AttnArgs a{};
+    SM_TRY(seq_args(p.tokens, p.seqs, p.slots, offsets, slot_index, &a.sq));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.g = p.decay == SEQMIX_DECAY_NONE ? nullptr : decay;
+    a.s_in = state_in;
+    a.s_out = state_out;
+    a.o = o;
+    a.q_row = p.q_row, a.q_head = p.q_head, a.k_row = p.k_row, a.k_head = p.k_head;
+    a.v_row = p.v_row, a.v_head = p.v_head, a.o_row = p.o_row, a.o_head = p.o_head;
+    a.g_row = p.decay == SEQMIX_DECAY_TOKEN ? p.heads : 0;
+    a.heads = p.heads;
+    a.rep = p.heads / p.qk_heads;
+    a.dk = p.dk;
+    a.dv = p.dv;
+    a.scale = p.scale;
+    const int64_t unit = 16 / esize(p.dtype);
+    a.vec = p.dk % unit == 0 && p.dv % unit == 0 && p.q_row % unit == 0 && p.q_head % unit == 0 && p.k_row % unit == 0 &&
+            p.k_head % unit == 0 && p.v_row % unit == 0 && p.v_head % unit == 0 && p.o_row % unit == 0 &&
+            p.o_head % unit == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(o, 16);
+    a.svec = p.dv % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
+    a.ndvb = (p.dv + 31) / 32;
+    return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+}
+
+// ------------------------------------------------------------------ causal convolution
+int seqmix_conv_desc_create(const seqmix_conv_params* params, seqmix_conv_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_conv_params& p = *params;
+    SM_TRY(check_seqs(p.tokens, p.seqs, p.slots));
+    if (p.channels < 1 || p.width < 1) return CONV2D_E_INVALID;
+    if (p.tokens > 1 && (p.x_row < p.channels || p.y_row < p.channels)) return CONV2D_E_INVALID;
+    if (!known_dtype(p.dtype) || (p.act != SEQMIX_ACT_NONE && p.act != SEQMIX_ACT_SILU) ||
+        p.width > SEQMIX_MAX_CONV_WIDTH || p.channels > kMaxRows - 4096)
+        return CONV2D_E_UNSUPPORTED;
+    seqmix_conv_desc* d = new (std::nothrow) seqmix_conv_desc{p};
+    if (!d) return CONV2D_E_ALLOC;
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_conv_desc_destroy(seqmix_conv_desc* d) {
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_conv_fwd(const seqmix_conv_desc* d, const void* x, const void* w, const float* bias, const int64_t* offsets,
+                    const int32_t* slot_index, const void* window_in, void* window_out, void* y, void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_conv_params& p = d->p;
+    if (!w || (p.has_bias && !bias) || (p.tokens > 0 && (!x || !y))) return CONV2D_E_NULL;
+    ConvArgs a{};
+    SM_TRY(seq_args(p.tokens, p.seqs, p.slots, offsets, slot_index, &a.sq));
+    a.x = x;
+    a.w = w;
+    a.bias = p.has_bias ? bias : nullptr;
+    a.win_in = p.width > 1 ? window_in : nullptr;
+    a.win_out = p.width > 1 ? window_out : nullptr;
+    a.y = y;
+    a.x_row = p.x_row;
+    a.y_row = p.y_row;
+    a.channels = (int32_t)p.channels;
+    a.width = p.width;
+    a.silu = p.act == SEQMIX_ACT_SILU;
+    const int64_t unit = 16 / esize(p.dtype);
+    a.vec = p.channels % unit == 0 && p.x_row % unit == 0 && p.y_row % unit == 0 && aligned(x, 16) && aligned(y, 16) &&
+            aligned(a.win_in, 16) && aligned(a.win_out, 16);
+    return launch_token_conv(a, p.dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+}
+
+// ------------------------------------------------------------------ norms
+int seqmix_norm_desc_create(const seqmix_norm_params* params, seqmix_norm_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_norm_params& p = *params;
+    if (p.rows < 0 || p.width < 1 || p.group < 1 || p.width % p.group != 0 || p.gate_run < 1) return CONV2D_E_INVALID;
+    if (!(p.post_eps >= 0.0f) || !(p.pre_eps >= 0.0f)) return CONV2D_E_INVALID;
+    if (p.u_row < p.width || (p.gate != SEQMIX_ACT_NONE && p.gate_row < p.width) ||
+        (p.residual && p.res_row < p.width) || p.y_row < p.width ||
+        (p.pre != SEQMIX_NORM_NONE && p.h_row < p.width))
+        return CONV2D_E_INVALID;
+    if (!known_dtype(p.dtype) || !known_dtype(p.res_dtype) || (p.dtype == CONV2D_F32 && p.res_dtype != CONV2D_F32) ||
+        p.post < SEQMIX_NORM_NONE || p.post > SEQMIX_NORM_LAYER || p.pre < SEQMIX_NORM_NONE ||
+        p.pre > SEQMIX_NORM_LAYER || p.gate < SEQMIX_ACT_NONE || p.gate > SEQMIX_ACT_LINEAR)
+        return CONV2D_E_UNSUPPORTED;
+    if (p.group > SEQMIX_MAX_NORM_WIDTH || p.rows > kMaxRows || p.width > kMaxRows ||
+        (p.pre != SEQMIX_NORM_NONE && p.group != p.width))
+        return CONV2D_E_UNSUPPORTED;
+    seqmix_norm_desc* d = new (std::nothrow) seqmix_norm_desc{p};
+    if (!d) return CONV2D_E_ALLOC;
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_norm_desc_destroy(seqmix_norm_desc* d) {
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_norm_fwd(const seqmix_norm_desc* d, const void* u, const float* post_w, const float* post_b, const void* gate,
+                    const void* residual, const float* scale_vec, const float* pre_w, const float* pre_b, void* y,
+                    void* h, void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_norm_params& p = d->p;
+    const bool post = p.post != SEQMIX_NORM_NONE, pre = p.pre != SEQMIX_NORM_NONE;
+    if ((post && (!post_w || (p.post_bias && !post_b))) || (p.scale_vec && !scale_vec) ||
+        (pre && (!pre_w || (p.pre_bias && !pre_b))))
+        return CONV2D_E_NULL;
+    if (p.rows > 0 && (!u || (p.gate != SEQMIX_ACT_NONE && !gate) || (p.residual && !residual) || (pre && !h) ||
+                       (!pre && !y)))
+        return CONV2D_E_NULL;
+    if (pre && h == y && p.rows > 0) return CONV2D_E_INVALID;
+    NormArgs a{};
+    a.u = u;
+    a.post_w = post ? post_w : nullptr;
+    a.post_b = post && p.post_bias ? post_b : nullptr;
+    a.gate = p.gate != SEQMIX_ACT_NONE ? gate : nullptr;
+    a.res = p.residual ? residual : nullptr;
+    a.scale_vec = p.scale_vec ? scale_vec : nullptr;
+    a.pre_w = pre ? pre_w : nullptr;
+    a.pre_b = pre && p.pre_bias ? pre_b : nullptr;
+    a.y = y;
+    a.h = pre ? h : nullptr;
+    a.ngroups = (int32_t)(p.width / p.group);
+    a.rows = p.rows * a.ngroups;
+    a.group = (int32_t)p.group;
+    a.gate_run = p.gate_run;
+    a.u_row = p.u_row, a.gate_row = p.gate_row, a.res_row = p.res_row, a.y_row = p.y_row, a.h_row = p.h_row;
+    a.post = p.post;
+    a.gate_act = p.gate;
+    a.gate_first = p.gate_first;
+    a.pre = p.pre;
+    a.scale = p.scale;
+    a.post_eps = p.post_eps;
+    a.pre_eps = p.pre_eps;
+    const int64_t unit = 16 / esize(p.dtype);
+    a.vec = p.group % unit == 0 && aligned(a.post_w, 16) && aligned(a.post_b, 16) && aligned(a.scale_vec, 16) &&
+            aligned(a.pre_w, 16) && aligned(a.pre_b, 16) && aligned(u, 16) && p.u_row % unit == 0 &&
+            (!a.gate || (aligned(gate, 16) && p.gate_row % unit == 0)) &&
+            (!a.res || (aligned(residual, 16) && p.res_row % unit == 0)) &&
+            (!y || (aligned(y, 16) && p.y_row % unit == 0)) && (!a.h || (aligned(h, 16) && p.h_row % unit == 0));
+    return launch_norm(a, p.dtype, p.res_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK
+                                                                                               : CONV2D_E_HIP;
+}
+
+}  // extern "C"

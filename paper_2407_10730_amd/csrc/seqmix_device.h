@@ -1,0 +1,93 @@
+// seqmix_device.h -- device helpers of the token-mixing kernels.
+#pragma once
+
+#include "device_common.h"
+#include "seqmix_internal.h"
+
+namespace cv {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 16-bit storage stands for bf16 throughout (uint16_t).
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) {  // the hardware's conversion: nearest even, NaN kept
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// N consecutive elements as they lie in memory, `Bytes` of them moved per access.
+template <typename T, int N>
+struct alignas(sizeof(T) * N <= 16 ? sizeof(T) * N : 16) Pack {
+    T e[N];
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_pack(const T* p, float (&out)[N]) {
+    const Pack<T, N> v = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = to_f32(v.e[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_pack(T* p, const float (&in)[N]) {
+    Pack<T, N> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.e[i] = from_f32<T>(in[i]);
+    *reinterpret_cast<Pack<T, N>*>(p) = v;
+}
+
+// Rows [first, first + len) of sequence i, clamped so that no offsets lead outside the call's rows.
+struct SeqRange {
+    int64_t first, len;
+};
+__device__ __forceinline__ int64_t clamp_row(int64_t r, int64_t tokens) { return r < 0 ? 0 : r > tokens ? tokens : r; }
+__device__ __forceinline__ SeqRange seq_range(const SeqArgs& a, int i) {
+    if (!a.off) return {(int64_t)i * a.seq_len, a.seq_len};
+    const int64_t b = clamp_row(a.off[i], a.tokens), e = clamp_row(a.off[i + 1], a.tokens);
+    return {b, e > b ? e - b : 0};
+}
+// Pool entry of sequence i, -1: the sequence is skipped.
+__device__ __forceinline__ int64_t seq_slot(const SeqArgs& a, int i) {
+    if (!a.slot) return i;
+    const int64_t s = a.slot[i];
+    return s >= 0 && s < a.slots ? s : -1;
+}
+
+// Parts of `size` tokens of all sequences, numbered so that no prefix sum over the sequences is needed:
+// sequence i owns the ids [offsets[i] / size + i, offsets[i+1] / size + i + 1), at least
+// ceil(len / size) and at least one, so the ids of a call are below tokens / size + seqs.
+struct SeqPart {
+    int seq;
+    int64_t part, first_id;  // number of the part within the sequence, id of its part 0
+};
+__device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, int64_t id, int64_t size) {
+    if (!a.off) {
+        const int64_t per = a.seq_len / size + 1;
+        const int64_t i = id / per;
+        return {(int)i, id - i * per, i * per};
+    }
+    int lo = 0, hi = a.seqs - 1;  // the last sequence whose first id is at most `id`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (clamp_row(a.off[mid], a.tokens) / size + mid <= id)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    const int64_t first = clamp_row(a.off[lo], a.tokens) / size + lo;
+    return {lo, id - first, first};
+}
+inline int64_t seq_part_ids(const SeqArgs& a, int64_t size) {
+    return a.off ? a.tokens / size + a.seqs : (int64_t)a.seqs * (a.seq_len / size + 1);
+}
+
+// 1 / (1 + exp(-x)) on the hardware's exponential and reciprocal (each within 1 ulp of fp32).
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
+}
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
+
+}  // namespace cv

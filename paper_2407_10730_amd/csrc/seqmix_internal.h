@@ -1,0 +1,71 @@
+// seqmix_internal.h -- shared declarations of the token-mixing operators (seqmix.h).
+#pragma once
+
+#include "conv2d_internal.h"
+#include "seqmix.h"
+
+namespace cv {
+
+constexpr int kSeqmixCUs = 256;  // plans are made without a GPU: MI355X has 256 CUs
+
+// How the rows of a call divide into sequences, and which pool entry each has.
+struct SeqArgs {
+    const int64_t* off;   // [seqs + 1] or NULL: seq_len rows each
+    const int32_t* slot;  // [seqs] or NULL: slot i
+    int64_t tokens, seq_len, slots;
+    int32_t seqs;
+};
+
+struct AttnArgs {
+    SeqArgs sq;
+    const void *q, *k, *v;
+    const float* g;
+    const float* s_in;
+    float* s_out;
+    void* o;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+    int64_t g_row;        // heads (a decay for each token) or 0
+    int32_t heads, rep;   // rep heads share a q/k head
+    int32_t dk, dv, ndvb; // dv blocks per head
+    float scale;
+    int32_t vec;          // pointers and strides allow wide loads of q, k, v; stores of o
+    int32_t svec;         // ... of the states
+    // segments: `segment` tokens each; ids offsets[i] / segment + i + (segment of sequence i)
+    int64_t segment, nseg;
+    float* ws_state;      // [nseg][heads][dk][dv]
+    float* ws_decay;      // [nseg][heads]: log of a segment's whole decay, times log2(e)
+};
+
+hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s);
+int attn_tokens_dvb(int dv);
+
+struct ConvArgs {
+    SeqArgs sq;
+    const void *x, *w;
+    const float* bias;
+    const void* win_in;
+    void* win_out;
+    void* y;
+    int64_t x_row, y_row;
+    int32_t channels, width, silu;
+    int32_t vec;          // 16-byte accesses of x, y and the windows are aligned
+};
+hipError_t launch_token_conv(const ConvArgs& a, int dt, hipStream_t s);
+
+struct NormArgs {
+    const void* u;
+    const float *post_w, *post_b;
+    const void* gate;
+    const void* res;
+    const float *scale_vec, *pre_w, *pre_b;
+    void *y, *h;
+    int64_t rows;         // rows * groups of the call
+    int32_t group, ngroups;
+    int64_t gate_run, u_row, gate_row, res_row, y_row, h_row;
+    int32_t post, gate_act, gate_first, pre;
+    float scale, post_eps, pre_eps;
+    int32_t vec;
+};
+hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s);
+
+}  // namespace cv

@@ -1,0 +1,117 @@
+// token_conv.hip -- causal depthwise convolution over tokens with a carried window.
+//
+//   y[t,c] = act(bias[c] + sum_i w[c,i] x[t - W + 1 + i, c])
+//
+// Bound by memory: x is read and y written once, 2W operations per value.  A thread owns V
+// neighbouring channels and walks along a tile of tokens with the last W - 1 rows in registers,
+// so each row of x is loaded once per tile (and W - 1 of them once more by the next tile).
+// A tile lies within one sequence, so the window pool is read by each sequence's tile 0 alone; that
+// tile also writes the new window, after its read, which makes the update in place free of races.
+#include "seqmix_device.h"
+
+namespace cv {
+
+constexpr int kConvTile = 32;  // tokens per tile: at width 4 the rows loaded twice are under a tenth
+
+template <typename T, int W, int V>
+__global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
+    if (c >= A.channels) return;
+    const SeqPart sp = seq_part(A.sq, blockIdx.y + (int64_t)blockIdx.z * 65535, tile);
+    if (sp.seq >= A.sq.seqs) return;
+    const SeqRange r = seq_range(A.sq, sp.seq);
+    const int64_t t0 = sp.part * tile;
+    if (sp.part < 0 || (sp.part > 0 && t0 >= r.len)) return;
+    const int64_t slot = seq_slot(A.sq, sp.seq);
+    if (slot < 0) return;
+    const int n = (int)min<int64_t>(r.len - t0, tile);
+    const T* __restrict__ x = static_cast<const T*>(A.x) + (r.first + t0) * A.x_row + c;
+    T* __restrict__ y = static_cast<T*>(A.y) + (r.first + t0) * A.y_row + c;
+
+    float w[V][W], bias[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[v][i] = to_f32(static_cast<const T*>(A.w)[(int64_t)(c + v) * W + i]);
+        bias[v] = A.bias ? A.bias[c + v] : 0.0f;
+    }
+    float row[W][V];  // row[i]: x of tap i
+    if constexpr (W > 1) {
+        const T* win = static_cast<const T*>(A.win_in) + (slot * (W - 1)) * A.channels + c;
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+            const int64_t t = t0 - (W - 1) + i;
+            if (t >= 0) {
+                load_pack<T, V>(x + (int64_t)(i - (W - 1)) * A.x_row, row[i]);
+            } else if (A.win_in) {
+                load_pack<T, V>(win + (int64_t)i * A.channels, row[i]);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) row[i][v] = 0.0f;
+            }
+        }
+        if (sp.part == 0 && A.win_out) {  // rows len .. len + W - 2 of window and sequence together
+            T* out = static_cast<T*>(A.win_out) + (slot * (W - 1)) * A.channels + c;
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i) {
+                const int64_t t = r.len + i - (W - 1);
+                float e[V];
+                if (t >= 0) {
+                    load_pack<T, V>(x + t * A.x_row, e);
+                } else {  // row i + len of the window, in registers
+#pragma unroll
+                    for (int j = 0; j < W - 1; ++j)
+                        if (j == i + r.len) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v) e[v] = row[j][v];
+                        }
+                }
+                store_pack<T, V>(out + (int64_t)i * A.channels, e);
+            }
+        }
+    }
+#pragma unroll 4
+    for (int t = 0; t < n; ++t) {
+        load_pack<T, V>(x + (int64_t)t * A.x_row, row[W - 1]);
+        float o[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            o[v] = bias[v];
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[v] = fmaf(w[v][i], row[i][v], o[v]);
+            if (A.silu) o[v] = silu(o[v]);
+        }
+        store_pack<T, V>(y + (int64_t)t * A.y_row, o);
+#pragma unroll
+        for (int i = 0; i + 1 < W; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) row[i][v] = row[i + 1][v];
+    }
+}
+
+template <typename T, int V>
+static hipError_t launch_conv_w(const ConvArgs& a, hipStream_t s) {
+    const int tile = kConvTile;
+    const int64_t ids = seq_part_ids(a.sq, tile);
+    const int64_t gz = (ids + 65534) / 65535;
+    if (gz > 65535) return hipErrorInvalidValue;
+    const int64_t per = (a.channels + V - 1) / V;
+    const dim3 grid((unsigned)((per + 255) / 256), (unsigned)(gz > 1 ? 65535 : ids), (unsigned)gz);
+    switch (a.width) {
+#define CASE(W)                                                                            \
+    case W:                                                                                \
+        hipLaunchKernelGGL((token_conv_kernel<T, W, V>), grid, dim3(256), 0, s, a, tile); \
+        break;
+        CASE(1) CASE(2) CASE(3) CASE(4) CASE(5) CASE(6) CASE(7) CASE(8)
+#undef CASE
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_token_conv(const ConvArgs& a, int dt, hipStream_t s) {
+    if (dt == CONV2D_BF16) return a.vec ? launch_conv_w<uint16_t, 8>(a, s) : launch_conv_w<uint16_t, 1>(a, s);
+    return a.vec ? launch_conv_w<float, 4>(a, s) : launch_conv_w<float, 1>(a, s);
+}
+
+}  // namespace cv
