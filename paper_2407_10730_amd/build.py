@@ -11,8 +11,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libconv2d.so")
 HARNESS = os.path.join(HERE, "convbench")
 SOURCES = ["conv2d_api.hip", "gemm_mfma.hip", "pack_kernels.hip", "direct_kernels.hip", "slice_conv.hip",
-           "probes.hip", "winograd.hip", "patch_conv.hip", "seqmix_api.hip", "linattn.hip", "token_conv.hip",
-           "gate_norm.hip"]
+           "probes.hip", "winograd.hip", "patch_conv.hip", "seqmix_api.hip", "linattn.hip",
+           "linattn_chunks.hip", "token_conv.hip", "gate_norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

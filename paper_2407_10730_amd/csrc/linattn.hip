@@ -1,15 +1,9 @@
-// linattn.hip -- linear attention with a decay per head, token by token.
+// linattn.hip -- linear attention with a decay per head, token by token, and the joining of segments.
 //
 //   S_t = exp(g_t) S_{t-1} + k_t v_t^T        o_t = scale q_t S_t
 #include "seqmix_device.h"
 
 namespace cv {
-
-// Log2 of a decay from its natural log.  Logs below -1000 (-infinity among them) have an
-// exponential of exactly zero in fp32 anyway; the bound keeps differences of sums finite.  NaN stays.
-__device__ __forceinline__ double decay_log2(float g) {
-    return (double)(g < -1000.0f ? -1000.0f : g) * 1.4426950408889634;
-}
 
 // One workgroup runs one sequence, head and block of DVB columns of the state through all tokens, the
 // state in registers: thread (rg, cg) holds RPT neighbouring rows of 4 columns.  Bound by reading and writing the
@@ -125,8 +119,6 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     }
 }
 
-int attn_tokens_dvb(int) { return 32; }
-
 template <typename T, typename TO, int RPT>
 static void launch_tokens_r(const AttnArgs& a, dim3 grid, hipStream_t s) {
     if (a.vec)
@@ -154,6 +146,60 @@ static hipError_t launch_tokens_t(const AttnArgs& a, hipStream_t s) {
 hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s) {
     if (dt == CONV2D_F32) return launch_tokens_t<float, float>(a, s);
     return odt == CONV2D_F32 ? launch_tokens_t<uint16_t, float>(a, s) : launch_tokens_t<uint16_t, uint16_t>(a, s);
+}
+
+// Joins the segments of each sequence: ws_state holds the state that each segment but the last adds from
+// zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring
+// elements of a state and walks along the segments, four loads ahead of the sum.
+template <int V>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
+    const int64_t size = (int64_t)A.dk * A.dv;
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+    if (e >= size) return;
+    const int head = blockIdx.y;
+    const int seq = blockIdx.z;
+    const SeqRange r = seq_range(A.sq, seq);
+    const int64_t slot = seq_slot(A.sq, seq);
+    if (slot < 0) return;
+    const int64_t first = A.sq.off ? r.first / A.segment + seq : seq * seq_parts(A.sq.seq_len, A.segment);
+    const int64_t parts = min(seq_parts(r.len, A.segment), A.nseg - first);  // (offsets that lie)
+    float S[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) S[v] = 0.0f;
+    if (A.s_in) load_pack<float, V>(A.s_in + (slot * A.heads + head) * size + e, S);
+    const int64_t pitch = (int64_t)A.heads * size;
+    float* ws = A.ws_state + (first * A.heads + head) * size + e;
+    const float* wd = A.ws_decay + first * A.heads + head;
+    for (int64_t p = 0; p < parts; p += 4) {
+        float add[4][V], d[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p + u + 1 < parts) {
+                load_pack<float, V>(ws + (p + u) * pitch, add[u]);
+                d[u] = wd[(p + u) * A.heads];
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (p + u < parts) store_pack<float, V>(ws + (p + u) * pitch, S);
+            if (p + u + 1 < parts) {
+                const float f = __builtin_amdgcn_exp2f(d[u]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) S[v] = fmaf(f, S[v], add[u][v]);
+            }
+        }
+    }
+}
+
+hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s) {
+    const int64_t size = (int64_t)a.dk * a.dv;
+    const int V = a.svec ? 4 : 1;
+    if (a.sq.seqs > 65535) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((size / V + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
+    if (V == 4)
+        hipLaunchKernelGGL((attn_join_kernel<4>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<1>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace cv

@@ -1,0 +1,382 @@
+// linattn_chunks.hip -- linear attention with a decay per head in chunks of 64 tokens, bf16 operands.
+//
+// With b_i the sum of a chunk's first i log decays and S the state it starts from,
+//
+//   o_i = scale ( exp(b_i) q_i S + sum_{j <= i} exp(b_i - b_j) (q_i . k_j) v_j )
+//   S'  = exp(b_C) S + sum_j exp(b_C - b_j) k_j v_j^T
+//
+// are four matrix products per chunk.  One workgroup (4 waves) runs a sequence's chunks in order, for one head and
+// 64 NT columns of v.  Each wave owns 16 NT of the columns: its part of S stays in the accumulator
+// registers from chunk to chunk and is itself an operand of q S (the rows that a lane holds as a result
+// are the reduction indices that it feeds as an operand; q is read from LDS in the same order), so S never
+// passes through LDS.  The scores are shared: each wave computes 16 rows of them into LDS.  Products over
+// tokens read k and v from LDS through the transposing load.
+//
+// Rounding: the scores and, as an operand of q S, the state are rounded to bf16 once (o is bf16 itself, or
+// as exact as bf16 operands make it); the state's own update multiplies exact k by exp(b_C - b_j) v_j
+// as three bf16 planes, which hold all 24 bits, so states keep fp32 accuracy over any length.
+#include "seqmix_device.h"
+
+namespace cv {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Four rows of 16 columns transposed: lane l of each 16 gives the address of row l / 4, columns 4 (l % 4) .. + 3,
+// and receives column l of the four rows.
+__device__ __forceinline__ u32x2 lds_tr(const uint16_t* p) {
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p)));
+}
+__device__ __forceinline__ bf16x8 join8(u32x2 a, u32x2 b) {
+    return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// 8 consecutive elements of a row, those at or past `n` zero.
+__device__ __forceinline__ u32x4 load8(const uint16_t* p, int n, bool vec) {
+    if (n <= 0) return u32x4{0, 0, 0, 0};
+    if (vec) return *reinterpret_cast<const u32x4*>(p);
+    u32x4 r{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    return r;
+}
+
+template <int DKT, int NT, bool STATE_ONLY>
+__global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
+    constexpr int C = kChunk, DKP = 32 * DKT, DVB = 64 * NT;
+    constexpr int QP = DKP + 8, VP = DVB + 8, PP = C + 8;  // LDS row pitches: 16 bytes off the bank period
+    constexpr int MT = 2 * DKT;                            // 16-row tiles of the state
+    __shared__ __align__(16) uint16_t sQ[STATE_ONLY ? 1 : C * QP];
+    __shared__ __align__(16) uint16_t sK[C * QP];
+    __shared__ __align__(16) uint16_t sV[C * VP];
+    __shared__ __align__(16) uint16_t sP[STATE_ONLY ? 1 : C * PP];
+    __shared__ __align__(16) double sB[C];
+    __shared__ __align__(16) float sE[C], sD[C];
+    __shared__ float sTot;
+
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l16 = lane & 15, quad = lane >> 4;
+    const int bid = xcd_remap(blockIdx.x, gridDim.x);
+    const int blk = bid % A.ndvb;
+    const int hid = bid / A.ndvb;
+    const int head = hid % A.heads;
+    const int64_t id = hid / A.heads;
+    SeqPart sp{(int)id, 0, id};
+    if (A.segment) sp = seq_part(A.sq, id, A.segment);
+    if (sp.seq >= A.sq.seqs || sp.part < 0) return;
+    const SeqRange r = seq_range(A.sq, sp.seq);
+    const int64_t start = sp.part * A.segment;
+    if (sp.part > 0 && start >= r.len) return;
+    const bool last = !A.segment || r.len - start <= A.segment;
+    if (STATE_ONLY && last) return;
+    const int64_t slot = seq_slot(A.sq, sp.seq);
+    if (slot < 0) return;
+    const int64_t len = last ? r.len - start : A.segment;
+
+    const int c0 = blk * DVB;             // first column of the workgroup
+    const int wc = wave * 16 * NT;        // ... of the wave, within the workgroup's
+    const int64_t row0 = r.first + start;
+    const int qh = head / A.rep;
+    const bool vec = A.vec;
+
+    // The state: tile (m, n) of the wave holds rows 16 m + 4 quad + i and column wc + col(l16, n).
+    // Columns are dealt so that a lane's results of all n tiles are 4 NT neighbours.
+    auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
+    f32x4 S[MT][NT];
+    const float* s_init = STATE_ONLY ? nullptr
+                          : A.segment ? A.ws_state + (id * A.heads + head) * (int64_t)A.dk * A.dv
+                          : A.s_in ? A.s_in + (slot * A.heads + head) * (int64_t)A.dk * A.dv
+                                   : nullptr;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
+                S[m][n][i] = s_init && rr < A.dk && cc < A.dv ? s_init[(int64_t)rr * A.dv + cc] : 0.0f;
+            }
+
+    // Loads: thread t takes 8 elements of row t / (DKP / 8) + i * RS of q and k, likewise of v
+    constexpr int RS = 256 / (DKP / 8), RSV = 256 / (DVB / 8);
+    const int lr = t / (DKP / 8), lc = t % (DKP / 8) * 8, lrv = t / (DVB / 8), lcv = t % (DVB / 8) * 8;
+    const uint16_t* gq = static_cast<const uint16_t*>(A.q) + (row0 + lr) * A.q_row + qh * A.q_head + lc;
+    const uint16_t* gk = static_cast<const uint16_t*>(A.k) + (row0 + lr) * A.k_row + qh * A.k_head + lc;
+    const uint16_t* gv = static_cast<const uint16_t*>(A.v) + (row0 + lrv) * A.v_row + head * A.v_head + c0 + lcv;
+    const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
+    u32x4 rq[STATE_ONLY ? 1 : DKT], rk[DKT], rv[2 * NT];
+    float rg = 0.0f;
+    auto load = [&](int64_t c) {  // chunk starting at token c of the segment into registers
+        const int n = (int)min<int64_t>(C, len - c);
+#pragma unroll
+        for (int i = 0; i < DKT; ++i) {
+            const bool ok = lr + i * RS < n;
+            if constexpr (!STATE_ONLY) rq[i] = load8(gq + (c + i * RS) * A.q_row, ok ? A.dk - lc : 0, vec);
+            rk[i] = load8(gk + (c + i * RS) * A.k_row, ok ? A.dk - lc : 0, vec);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i)
+            rv[i] = load8(gv + (c + i * RSV) * A.v_row, lrv + i * RSV < n ? A.dv - c0 - lcv : 0, vec);
+        if (wave == 0) rg = gg && lane < n ? gg[(c + lane) * A.g_row] : 0.0f;
+    };
+
+    double whole = 0.0;  // log2 of the segment's decay (wave 0)
+    if (len > 0) load(0);
+    for (int64_t c = 0; c < len; c += C) {
+        const int n = (int)min<int64_t>(C, len - c);
+        // registers to LDS; decays
+#pragma unroll
+        for (int i = 0; i < DKT; ++i) {
+            if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
+            *reinterpret_cast<u32x4*>(&sK[(lr + i * RS) * QP + lc]) = rk[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
+        if (wave == 0) {
+            // running sums in 64 bits: differences of sums stay exact after decays that clear the state
+            double b = decay_log2(rg);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const double up = __shfl_up(b, d);
+                if (lane >= d) b += up;
+            }
+            const double tot = __shfl(b, 63);
+            sB[lane] = b;
+            sD[lane] = __builtin_amdgcn_exp2f((float)b);
+            sE[lane] = __builtin_amdgcn_exp2f((float)(tot - b));
+            if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);
+            whole += tot;
+        }
+        __syncthreads();
+        if (c + C < len) load(c + C);
+
+        f32x4 O[4][NT];
+        if constexpr (!STATE_ONLY) {
+            // scores, rows 16 wave .. + 15, transposed: a lane holds 4 neighbouring j of one i
+            bf16x8 qf[DKT];
+#pragma unroll
+            for (int k = 0; k < DKT; ++k)
+                qf[k] = *reinterpret_cast<const bf16x8*>(&sQ[(16 * wave + l16) * QP + 32 * k + 8 * quad]);
+            const int i = 16 * wave + l16;
+            const double bi = sB[i];
+            const int jt_end = wave | 1;  // tiles beyond the diagonal that the products below read: zeros
+            for (int jt = 0; jt <= jt_end; ++jt) {
+                u32x2 p{0, 0};
+                if (jt <= wave) {
+                    f32x4 s{0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < DKT; ++k)
+                        s = mfma16(*reinterpret_cast<const bf16x8*>(&sK[(16 * jt + l16) * QP + 32 * k + 8 * quad]), qf[k],
+                                   s);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int j = 16 * jt + 4 * quad + u;
+                        const float f = __builtin_amdgcn_exp2f((float)(bi - sB[j]));
+                        s[u] = j <= i ? s[u] * f : 0.0f;
+                    }
+                    p = u32x2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+                }
+                *reinterpret_cast<u32x2*>(&sP[i * PP + 16 * jt + 4 * quad]) = p;
+            }
+        }
+        // exp(b_i) q_i S, transposed: rows are columns of v, columns the 16 tokens of a tile
+        auto inter = [&] {
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) O[it][nt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < DKT; ++k) {
+                bf16x8 sf[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const f32x4 a = S[2 * k][nt], b = S[2 * k + 1][nt];
+                    sf[nt] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]),
+                                                              pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])});
+                }
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const uint16_t* p = &sQ[(16 * it + l16) * QP + 32 * k + 4 * quad];
+                    const bf16x8 qf = join8(*reinterpret_cast<const u32x2*>(p), *reinterpret_cast<const u32x2*>(p + 16));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) O[it][nt] = mfma16(sf[nt], qf, O[it][nt]);
+                }
+            }
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const float d = sD[16 * it + l16];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) O[it][nt] *= d;
+            }
+        };
+        if constexpr (!STATE_ONLY) {
+            inter();
+            __syncthreads();
+        }
+        // v as an operand: 8 tokens of one column per lane
+        u32x4 vf[2][NT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint16_t* p = &sV[(32 * s + 8 * quad + (l16 >> 2)) * VP + wc + 4 * NT * (l16 & 3) + 4 * nt];
+                const u32x2 a = lds_tr(p), b = lds_tr(p + 4 * VP);
+                vf[s][nt] = u32x4{a[0], a[1], b[0], b[1]};
+            }
+        if constexpr (!STATE_ONLY) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int it = 2 * s; it < 4; ++it) {
+                    const bf16x8 pf =
+                        *reinterpret_cast<const bf16x8*>(&sP[(16 * it + l16) * PP + 32 * s + 8 * quad]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        O[it][nt] = mfma16(__builtin_bit_cast(bf16x8, vf[s][nt]), pf, O[it][nt]);
+                }
+            // A later token's infinite or NaN v times its score of zero has made every earlier token NaN too, the
+            // first of the 32 that share a product step among them: such chunks are summed again
+            // without the masked terms.
+            bool bad = false;
+            if (l16 == 0) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        bad |= !(fabsf(O[0][nt][u]) < __builtin_inff()) || !(fabsf(O[2][nt][u]) < __builtin_inff());
+            }
+            if (__any(bad)) {
+                inter();
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int i = 16 * it + l16;
+                    for (int j = 0; j <= i; ++j) {
+                        const float p = to_f32(sP[i * PP + j]);
+                        const uint16_t* v = &sV[j * VP + wc + 4 * NT * quad];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) O[it][nt][u] = fmaf(p, to_f32(v[4 * nt + u]), O[it][nt][u]);
+                    }
+                }
+            }
+            const int oc = c0 + wc + 4 * NT * quad;
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int i = 16 * it + l16;
+                if (i < n && oc < A.dv) {
+                    const int64_t at = (row0 + c + i) * A.o_row + head * A.o_head + oc;
+                    float e[4 * NT];
+#pragma unroll
+                    for (int x = 0; x < 4 * NT; ++x) e[x] = A.scale * O[it][x / 4][x % 4];
+                    if (o_f32) {
+                        float* o = static_cast<float*>(A.o) + at;
+                        if (vec) {
+                            store_pack<float, 4 * NT>(o, e);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 4 * NT; ++x)
+                                if (oc + x < A.dv) o[x] = e[x];
+                        }
+                    } else {
+                        uint16_t* o = static_cast<uint16_t*>(A.o) + at;
+                        if (vec) {
+                            store_pack<uint16_t, 4 * NT>(o, e);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 4 * NT; ++x)
+                                if (oc + x < A.dv) o[x] = from_f32<uint16_t>(e[x]);
+                        }
+                    }
+                }
+            }
+        }
+        // the state moves on
+        const float tot = sTot;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[m][nt] *= tot;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 vp[NT][3];  // planes of exp(b_C - b_j) v_j
+            const f32x4 e0 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad]);
+            const f32x4 e1 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad + 4]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                u32x4 pl[3];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    float lo = __builtin_bit_cast(float, vf[s][nt][w] << 16) * (w < 2 ? e0[2 * w] : e1[2 * w - 4]);
+                    float hi = __builtin_bit_cast(float, vf[s][nt][w] & 0xffff0000u) *
+                               (w < 2 ? e0[2 * w + 1] : e1[2 * w - 3]);
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) {
+                        const uint32_t p = pack_bf16(lo, hi);
+                        pl[x][w] = p;
+                        lo -= __builtin_bit_cast(float, p << 16);
+                        hi -= __builtin_bit_cast(float, p & 0xffff0000u);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 3; ++x) vp[nt][x] = __builtin_bit_cast(bf16x8, pl[x]);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const uint16_t* p = &sK[(32 * s + 8 * quad + (l16 >> 2)) * QP + 16 * m + 4 * (l16 & 3)];
+                const bf16x8 kf = join8(lds_tr(p), lds_tr(p + 4 * QP));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 2; x >= 0; --x) S[m][nt] = mfma16(kf, vp[nt][x], S[m][nt]);
+            }
+        }
+        __syncthreads();
+    }
+
+    float* s_left = STATE_ONLY ? A.ws_state + (id * A.heads + head) * (int64_t)A.dk * A.dv
+                    : last && A.s_out ? A.s_out + (slot * A.heads + head) * (int64_t)A.dk * A.dv
+                                      : nullptr;
+    if (s_left) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
+                    if (rr < A.dk && cc < A.dv) s_left[(int64_t)rr * A.dv + cc] = S[m][n][i];
+                }
+    }
+    if (STATE_ONLY && blk == 0 && t == 0) A.ws_decay[id * A.heads + head] = (float)whole;
+}
+
+template <int DKT, int NT>
+static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
+    const int64_t ids = a.segment ? a.nseg : a.sq.seqs;
+    const int64_t blocks = ids * a.heads * a.ndvb;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (state_only)
+        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, 0);
+    else
+        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false>), dim3((unsigned)blocks), dim3(256), 0, s, a,
+                           odt == CONV2D_F32);
+    return hipGetLastError();
+}
+
+hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
+    if (a.dk > 128) return launch_one<8, 1>(a, odt, state_only, s);  // two column tiles would not fit the registers
+    if (chunk_block(a.dk, a.dv) == 64)
+        return a.dk <= 64 ? launch_one<2, 1>(a, odt, state_only, s) : launch_one<4, 1>(a, odt, state_only, s);
+    return a.dk <= 64 ? launch_one<2, 2>(a, odt, state_only, s) : launch_one<4, 2>(a, odt, state_only, s);
+}
+
+}  // namespace cv

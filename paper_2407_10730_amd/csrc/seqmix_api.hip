@@ -1,4 +1,5 @@
 // seqmix_api.hip -- C ABI of the token-mixing operators: validation, plans, workspaces, launches.
+#include <algorithm>
 #include <new>
 
 #include "seqmix_internal.h"
@@ -8,7 +9,6 @@ using namespace cv;
 struct seqmix_attn_desc {
     seqmix_attn_params p;
     seqmix_attn_plan_info plan;
-    int64_t nseg = 0;  // segment ids at most (0: not cut)
     // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
     void* ws = nullptr;
     int device = -1;
@@ -90,6 +90,38 @@ int ensure_ws(seqmix_attn_desc* d) {
     }
 }
 
+int order_after_last(seqmix_attn_desc* d, hipStream_t s) {
+    if (d->has_last && s != d->last_stream) {
+        if (hipEventRecord(d->done, d->last_stream) != hipSuccess || hipStreamWaitEvent(s, d->done, 0) != hipSuccess)
+            return CONV2D_E_HIP;
+    }
+    d->last_stream = s;
+    d->has_last = true;
+    return CONV2D_OK;
+}
+
+// Sequences of this many tokens or fewer on average go token by token.
+constexpr int64_t kTokensMost = 8;
+
+// Kernel, and where sequences are cut: about two workgroups per CU over all heads and column blocks, in segments of
+// at least 128 tokens (below that the segments' states cost more than their tokens).
+void plan_attn(seqmix_attn_desc* d) {
+    const seqmix_attn_params& p = d->p;
+    d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
+    if (p.tokens <= kTokensMost * p.seqs || p.dtype != CONV2D_BF16) return;
+    d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
+    d->plan.chunk = kChunk;
+    const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv));
+    if (p.seqs * across >= 2 * kSeqmixCUs) return;
+    int64_t seg = (p.tokens * across + 2 * kSeqmixCUs - 1) / (2 * kSeqmixCUs);
+    seg = (std::max<int64_t>(seg, 128) + kChunk - 1) / kChunk * kChunk;
+    if (seg >= p.tokens) return;
+    const int64_t ids = p.tokens / seg + p.seqs;
+    const int64_t state = (int64_t)p.dk * p.dv * 4;
+    d->plan.segment = seg;
+    d->plan.workspace_bytes = ids * p.heads * (state + 4);
+}
+
 }  // namespace
 
 extern "C" {
@@ -113,7 +145,7 @@ int seqmix_attn_desc_create(const seqmix_attn_params* params, seqmix_attn_desc**
     seqmix_attn_desc* d = new (std::nothrow) seqmix_attn_desc;
     if (!d) return CONV2D_E_ALLOC;
     d->p = p;
-    d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
+    plan_attn(d);
     *out = d;
     return CONV2D_OK;
 }
@@ -166,8 +198,23 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
             p.k_head % unit == 0 && p.v_row % unit == 0 && p.v_head % unit == 0 && p.o_row % unit == 0 &&
             p.o_head % unit == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(o, 16);
     a.svec = p.dv % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
-    a.ndvb = (p.dv + 31) / 32;
-    return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+    if (d->plan.kernel == SEQMIX_KERNEL_TOKENS) {
+        a.ndvb = (p.dv + kTokensBlock - 1) / kTokensBlock;
+        return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+    }
+    a.ndvb = (p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv);
+    if (d->plan.segment == 0 || (!offsets && a.sq.seq_len <= d->plan.segment))  // no sequence is cut
+        return launch_attn_chunks_bf16(a, p.o_dtype, false, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+    SM_TRY(ensure_ws(d));
+    SM_TRY(order_after_last(d, s));
+    a.segment = d->plan.segment;
+    a.nseg = seq_part_ids(a.sq, a.segment);
+    a.ws_state = static_cast<float*>(d->ws);
+    a.ws_decay = a.ws_state + (p.tokens / a.segment + p.seqs) * p.heads * p.dk * p.dv;
+    if (launch_attn_chunks_bf16(a, p.o_dtype, true, s) != hipSuccess || launch_attn_join(a, s) != hipSuccess ||
+        launch_attn_chunks_bf16(a, p.o_dtype, false, s) != hipSuccess)
+        return CONV2D_E_HIP;
+    return CONV2D_OK;
 }
 
 // ------------------------------------------------------------------ causal convolution

@@ -58,14 +58,15 @@ __device__ __forceinline__ int64_t seq_slot(const SeqArgs& a, int i) {
 
 // Parts of `size` tokens of all sequences, numbered so that no prefix sum over the sequences is needed:
 // sequence i owns the ids [offsets[i] / size + i, offsets[i+1] / size + i + 1), at least
-// ceil(len / size) and at least one, so the ids of a call are below tokens / size + seqs.
+// ceil(len / size) and at least one, so the ids of a call are below tokens / size + seqs.  Sequences of
+// equal length own exactly as many as they have parts (seq_parts).
 struct SeqPart {
     int seq;
     int64_t part, first_id;  // number of the part within the sequence, id of its part 0
 };
 __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, int64_t id, int64_t size) {
     if (!a.off) {
-        const int64_t per = a.seq_len / size + 1;
+        const int64_t per = seq_parts(a.seq_len, size);
         const int64_t i = id / per;
         return {(int)i, id - i * per, i * per};
     }
@@ -80,8 +81,11 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, int64_t id, int64_
     const int64_t first = clamp_row(a.off[lo], a.tokens) / size + lo;
     return {lo, id - first, first};
 }
-inline int64_t seq_part_ids(const SeqArgs& a, int64_t size) {
-    return a.off ? a.tokens / size + a.seqs : (int64_t)a.seqs * (a.seq_len / size + 1);
+
+// Log2 of a decay from its natural log.  Logs below -1000 (-infinity among them) have an
+// exponential of exactly zero in fp32 anyway; the bound keeps differences of sums finite.  NaN stays.
+__device__ __forceinline__ double decay_log2(float g) {
+    return (double)(g < -1000.0f ? -1000.0f : g) * 1.4426950408889634;
 }
 
 // 1 / (1 + exp(-x)) on the hardware's exponential and reciprocal (each within 1 ulp of fp32).

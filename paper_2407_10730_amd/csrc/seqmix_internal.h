@@ -16,6 +16,14 @@ struct SeqArgs {
     int32_t seqs;
 };
 
+// Parts of `size` tokens of a sequence (an empty one has one), and the ids that number the parts of all sequences.
+__host__ __device__ inline int64_t seq_parts(int64_t len, int64_t size) {
+    return len > size ? (len + size - 1) / size : 1;
+}
+inline int64_t seq_part_ids(const SeqArgs& a, int64_t size) {
+    return a.off ? a.tokens / size + a.seqs : (int64_t)a.seqs * seq_parts(a.seq_len, size);
+}
+
 struct AttnArgs {
     SeqArgs sq;
     const void *q, *k, *v;
@@ -36,8 +44,16 @@ struct AttnArgs {
     float* ws_decay;      // [nseg][heads]: log of a segment's whole decay, times log2(e)
 };
 
+constexpr int kTokensBlock = 32;  // state columns of a workgroup of the token kernel
 hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s);
-int attn_tokens_dvb(int dv);
+
+// Chunk kernels: chunk_block() state columns per workgroup.  state_only: the states that segments add from zero
+// (all but the last of each sequence) into ws_state / ws_decay; launch_attn_join turns them into
+// the states that the segments start from, which the full pass reads.
+constexpr int kChunk = 64;
+inline int chunk_block(int dk, int dv) { return dv <= 64 || dk > 128 ? 64 : 128; }
+hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s);
+hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s);
 
 struct ConvArgs {
     SeqArgs sq;
