@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libconv2d.so")
 HARNESS = os.path.join(HERE, "convbench")
 SOURCES = ["conv2d_api.hip", "gemm_mfma.hip", "pack_kernels.hip", "direct_kernels.hip", "slice_conv.hip",
            "probes.hip", "winograd.hip", "patch_conv.hip", "seqmix_api.hip", "linattn.hip",
-           "linattn_chunks.hip", "token_conv.hip", "gate_norm.hip"]
+           "linattn_chunks.hip", "linattn_chunks_f32.hip", "token_conv.hip", "gate_norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -15,7 +15,7 @@
 // Rounding: the scores and, as an operand of q S, the state are rounded to bf16 once (o is bf16 itself, or
 // as exact as bf16 operands make it); the state's own update multiplies exact k by exp(b_C - b_j) v_j
 // as three bf16 planes, which hold all 24 bits, so states keep fp32 accuracy over any length.
-#include "seqmix_device.h"
+#include "linattn_device.h"
 
 namespace cv {
 
@@ -64,26 +64,12 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
     __shared__ float sTot;
 
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l16 = lane & 15, quad = lane >> 4;
-    const int bid = xcd_remap(blockIdx.x, gridDim.x);
-    const int blk = bid % A.ndvb;
-    const int hid = bid / A.ndvb;
-    const int head = hid % A.heads;
-    const int64_t id = hid / A.heads;
-    SeqPart sp{(int)id, 0, id};
-    if (A.segment) sp = seq_part(A.sq, id, A.segment);
-    if (sp.seq >= A.sq.seqs || sp.part < 0) return;
-    const SeqRange r = seq_range(A.sq, sp.seq);
-    const int64_t start = sp.part * A.segment;
-    if (sp.part > 0 && start >= r.len) return;
-    const bool last = !A.segment || r.len - start <= A.segment;
-    if (STATE_ONLY && last) return;
-    const int64_t slot = seq_slot(A.sq, sp.seq);
-    if (slot < 0) return;
-    const int64_t len = last ? r.len - start : A.segment;
-
-    const int c0 = blk * DVB;             // first column of the workgroup
+    AttnPlace pl;
+    if (!attn_place(A, STATE_ONLY, &pl)) return;
+    const int head = pl.head;
+    const int64_t row0 = pl.row0, len = pl.len;
+    const int c0 = pl.blk * DVB;          // first column of the workgroup
     const int wc = wave * 16 * NT;        // ... of the wave, within the workgroup's
-    const int64_t row0 = r.first + start;
     const int qh = head / A.rep;
     const bool vec = A.vec;
 
@@ -91,10 +77,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
     // Columns are dealt so that a lane's results of all n tiles are 4 NT neighbours.
     auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
     f32x4 S[MT][NT];
-    const float* s_init = STATE_ONLY ? nullptr
-                          : A.segment ? A.ws_state + (id * A.heads + head) * (int64_t)A.dk * A.dv
-                          : A.s_in ? A.s_in + (slot * A.heads + head) * (int64_t)A.dk * A.dv
-                                   : nullptr;
+    const float* s_init = STATE_ONLY ? nullptr : attn_first_state(A, pl);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -141,17 +124,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
         if (wave == 0) {
-            // running sums in 64 bits: differences of sums stay exact after decays that clear the state
-            double b = decay_log2(rg);
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double up = __shfl_up(b, d);
-                if (lane >= d) b += up;
-            }
-            const double tot = __shfl(b, 63);
-            sB[lane] = b;
-            sD[lane] = __builtin_amdgcn_exp2f((float)b);
-            sE[lane] = __builtin_amdgcn_exp2f((float)(tot - b));
+            const double tot = chunk_decays(rg, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);
             whole += tot;
         }
@@ -251,7 +224,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        bad |= !(fabsf(O[0][nt][u]) < __builtin_inff()) || !(fabsf(O[2][nt][u]) < __builtin_inff());
+                        bad |= !finite(O[0][nt][u]) || !finite(O[2][nt][u]);
             }
             if (__any(bad)) {
                 inter();
@@ -273,29 +246,10 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
             for (int it = 0; it < 4; ++it) {
                 const int i = 16 * it + l16;
                 if (i < n && oc < A.dv) {
-                    const int64_t at = (row0 + c + i) * A.o_row + head * A.o_head + oc;
                     float e[4 * NT];
 #pragma unroll
-                    for (int x = 0; x < 4 * NT; ++x) e[x] = A.scale * O[it][x / 4][x % 4];
-                    if (o_f32) {
-                        float* o = static_cast<float*>(A.o) + at;
-                        if (vec) {
-                            store_pack<float, 4 * NT>(o, e);
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 4 * NT; ++x)
-                                if (oc + x < A.dv) o[x] = e[x];
-                        }
-                    } else {
-                        uint16_t* o = static_cast<uint16_t*>(A.o) + at;
-                        if (vec) {
-                            store_pack<uint16_t, 4 * NT>(o, e);
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 4 * NT; ++x)
-                                if (oc + x < A.dv) o[x] = from_f32<uint16_t>(e[x]);
-                        }
-                    }
+                    for (int x = 0; x < 4 * NT; ++x) e[x] = O[it][x / 4][x % 4];
+                    attn_store<4 * NT>(A, o_f32, row0 + c + i, head, oc, e);
                 }
             }
         }
@@ -342,9 +296,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
         __syncthreads();
     }
 
-    float* s_left = STATE_ONLY ? A.ws_state + (id * A.heads + head) * (int64_t)A.dk * A.dv
-                    : last && A.s_out ? A.s_out + (slot * A.heads + head) * (int64_t)A.dk * A.dv
-                                      : nullptr;
+    float* s_left = attn_last_state(A, pl, STATE_ONLY);
     if (s_left) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -356,7 +308,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
                     if (rr < A.dk && cc < A.dv) s_left[(int64_t)rr * A.dv + cc] = S[m][n][i];
                 }
     }
-    if (STATE_ONLY && blk == 0 && t == 0) A.ws_decay[id * A.heads + head] = (float)whole;
+    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[pl.id * A.heads + head] = (float)whole;
 }
 
 template <int DKT, int NT>

@@ -108,9 +108,9 @@ constexpr int64_t kTokensMost = 8;
 void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
-    if (p.tokens <= kTokensMost * p.seqs || p.dtype != CONV2D_BF16) return;
+    if (p.tokens <= kTokensMost * p.seqs) return;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
-    d->plan.chunk = kChunk;
+    d->plan.chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv));
     if (p.seqs * across >= 2 * kSeqmixCUs) return;
     int64_t seg = (p.tokens * across + 2 * kSeqmixCUs - 1) / (2 * kSeqmixCUs);
@@ -203,16 +203,19 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
         return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     }
     a.ndvb = (p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv);
+    auto chunks = [&](bool state_only) {
+        return p.dtype == CONV2D_BF16 ? launch_attn_chunks_bf16(a, p.o_dtype, state_only, s)
+                                      : launch_attn_chunks_f32(a, state_only, s);
+    };
     if (d->plan.segment == 0 || (!offsets && a.sq.seq_len <= d->plan.segment))  // no sequence is cut
-        return launch_attn_chunks_bf16(a, p.o_dtype, false, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+        return chunks(false) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     SM_TRY(ensure_ws(d));
     SM_TRY(order_after_last(d, s));
     a.segment = d->plan.segment;
     a.nseg = seq_part_ids(a.sq, a.segment);
     a.ws_state = static_cast<float*>(d->ws);
     a.ws_decay = a.ws_state + (p.tokens / a.segment + p.seqs) * p.heads * p.dk * p.dv;
-    if (launch_attn_chunks_bf16(a, p.o_dtype, true, s) != hipSuccess || launch_attn_join(a, s) != hipSuccess ||
-        launch_attn_chunks_bf16(a, p.o_dtype, false, s) != hipSuccess)
+    if (chunks(true) != hipSuccess || launch_attn_join(a, s) != hipSuccess || chunks(false) != hipSuccess)
         return CONV2D_E_HIP;
     return CONV2D_OK;
 }
