@@ -161,8 +161,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
     const SeqRange r = seq_range(A.sq, seq);
     const int64_t slot = seq_slot(A.sq, seq);
     if (slot < 0) return;
-    const int64_t first = A.sq.off ? r.first / A.segment + seq : seq * seq_parts(A.sq.seq_len, A.segment);
-    const int64_t parts = min(seq_parts(r.len, A.segment), A.nseg - first);  // (offsets that lie)
+    const uint32_t seg = (uint32_t)A.segment;
+    const uint32_t len = (uint32_t)r.len, own = len > seg ? (len + seg - 1) / seg : 1;
+    const int64_t first = A.sq.off ? (uint32_t)r.first / seg + seq : (int64_t)seq * own;
+    const int64_t parts = min<int64_t>(own, A.nseg - first);  // (offsets that lie)
     float S[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) S[v] = 0.0f;

@@ -39,18 +39,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// 8 consecutive elements of a row, those at or past `n` zero.
-__device__ __forceinline__ u32x4 load8(const uint16_t* p, int n, bool vec) {
-    if (n <= 0) return u32x4{0, 0, 0, 0};
-    if (vec) return *reinterpret_cast<const u32x4*>(p);
-    u32x4 r{0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
-    return r;
-}
-
-template <int DKT, int NT, bool STATE_ONLY>
+template <int DKT, int NT, bool STATE_ONLY, bool VEC>
 __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
     constexpr int C = kChunk, DKP = 32 * DKT, DVB = 64 * NT;
     constexpr int QP = DKP + 8, VP = DVB + 8, PP = C + 8;  // LDS row pitches: 16 bytes off the bank period
@@ -71,43 +60,40 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
     const int c0 = pl.blk * DVB;          // first column of the workgroup
     const int wc = wave * 16 * NT;        // ... of the wave, within the workgroup's
     const int qh = head / A.rep;
-    const bool vec = A.vec;
 
     // The state: tile (m, n) of the wave holds rows 16 m + 4 quad + i and column wc + col(l16, n).
     // Columns are dealt so that a lane's results of all n tiles are 4 NT neighbours.
     auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
     f32x4 S[MT][NT];
-    const float* s_init = STATE_ONLY ? nullptr : attn_first_state(A, pl);
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
-                S[m][n][i] = s_init && rr < A.dk && cc < A.dv ? s_init[(int64_t)rr * A.dv + cc] : 0.0f;
-            }
+    auto scol = [&](int n) { return c0 + col(l16, n); };
+    load_state<MT, NT>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), scol, quad, S);
 
     // Loads: thread t takes 8 elements of row t / (DKP / 8) + i * RS of q and k, likewise of v
     constexpr int RS = 256 / (DKP / 8), RSV = 256 / (DVB / 8);
     const int lr = t / (DKP / 8), lc = t % (DKP / 8) * 8, lrv = t / (DVB / 8), lcv = t % (DVB / 8) * 8;
-    const uint16_t* gq = static_cast<const uint16_t*>(A.q) + (row0 + lr) * A.q_row + qh * A.q_head + lc;
-    const uint16_t* gk = static_cast<const uint16_t*>(A.k) + (row0 + lr) * A.k_row + qh * A.k_head + lc;
-    const uint16_t* gv = static_cast<const uint16_t*>(A.v) + (row0 + lrv) * A.v_row + head * A.v_head + c0 + lcv;
+    const uint16_t* gq = static_cast<const uint16_t*>(A.q) + row0 * A.q_row + qh * A.q_head;
+    const uint16_t* gk = static_cast<const uint16_t*>(A.k) + row0 * A.k_row + qh * A.k_head;
+    const uint16_t* gv = static_cast<const uint16_t*>(A.v) + row0 * A.v_row + head * A.v_head + c0;
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
+    const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
+    const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
+    const uint32_t q_at = live > 0 ? (lr * q_row + lc) * 2 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 2 : OOB_OFF;
+    const uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 2 : OOB_OFF;
     u32x4 rq[STATE_ONLY ? 1 : DKT], rk[DKT], rv[2 * NT];
     float rg = 0.0f;
     auto load = [&](int64_t c) {  // chunk starting at token c of the segment into registers
         const int n = (int)min<int64_t>(C, len - c);
+        if constexpr (!STATE_ONLY) {
+            const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gq + c * A.q_row, n, q_row, A.dk);
 #pragma unroll
-        for (int i = 0; i < DKT; ++i) {
-            const bool ok = lr + i * RS < n;
-            if constexpr (!STATE_ONLY) rq[i] = load8(gq + (c + i * RS) * A.q_row, ok ? A.dk - lc : 0, vec);
-            rk[i] = load8(gk + (c + i * RS) * A.k_row, ok ? A.dk - lc : 0, vec);
+            for (int i = 0; i < DKT; ++i) rq[i] = load_row<uint16_t, VEC>(r, q_at + i * (RS * 2) * q_row, live);
         }
+        const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gk + c * A.k_row, n, k_row, A.dk);
+        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv - c0);
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i)
-            rv[i] = load8(gv + (c + i * RSV) * A.v_row, lrv + i * RSV < n ? A.dv - c0 - lcv : 0, vec);
+        for (int i = 0; i < DKT; ++i) rk[i] = load_row<uint16_t, VEC>(r, k_at + i * (RS * 2) * k_row, live);
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) rv[i] = load_row<uint16_t, VEC>(rr, v_at + i * (RSV * 2) * v_row, live_v);
         if (wave == 0) rg = gg && lane < n ? gg[(c + lane) * A.g_row] : 0.0f;
     };
 
@@ -133,31 +119,35 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
 
         f32x4 O[4][NT];
         if constexpr (!STATE_ONLY) {
-            // scores, rows 16 wave .. + 15, transposed: a lane holds 4 neighbouring j of one i
-            bf16x8 qf[DKT];
+            // Scores, transposed (a lane holds 4 neighbouring j of one i).  10 of the 16 tiles are on or below the
+            // diagonal and 2 above it are read as zeros: 3 per wave, (it, jt) =
+            // (0,0) (3,0) (3,1) | (1,0) (1,1) (3,2) | (2,0) (2,1) (2,2) | (3,3) (0,1) (2,3)
+            constexpr uint32_t kIt[3] = {0x3210, 0x0213, 0x2233}, kJt[3] = {0x3000, 0x1110, 0x3221};
+            f32x4 sc[3];
+            int row[3], krow[3];
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {
+                sc[x] = f32x4{0, 0, 0, 0};
+                row[x] = 16 * ((kIt[x] >> (4 * wave)) & 15) + l16;
+                krow[x] = 16 * ((kJt[x] >> (4 * wave)) & 15);
+            }
 #pragma unroll
             for (int k = 0; k < DKT; ++k)
-                qf[k] = *reinterpret_cast<const bf16x8*>(&sQ[(16 * wave + l16) * QP + 32 * k + 8 * quad]);
-            const int i = 16 * wave + l16;
-            const double bi = sB[i];
-            const int jt_end = wave | 1;  // tiles beyond the diagonal that the products below read: zeros
-            for (int jt = 0; jt <= jt_end; ++jt) {
-                u32x2 p{0, 0};
-                if (jt <= wave) {
-                    f32x4 s{0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < DKT; ++k)
-                        s = mfma16(*reinterpret_cast<const bf16x8*>(&sK[(16 * jt + l16) * QP + 32 * k + 8 * quad]), qf[k],
-                                   s);
+                for (int x = 0; x < 3; ++x)
+                    sc[x] = mfma16(*reinterpret_cast<const bf16x8*>(&sK[(krow[x] + l16) * QP + 32 * k + 8 * quad]),
+                                   *reinterpret_cast<const bf16x8*>(&sQ[row[x] * QP + 32 * k + 8 * quad]), sc[x]);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int j = 16 * jt + 4 * quad + u;
-                        const float f = __builtin_amdgcn_exp2f((float)(bi - sB[j]));
-                        s[u] = j <= i ? s[u] * f : 0.0f;
-                    }
-                    p = u32x2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+            for (int x = 0; x < 3; ++x) {
+                const int i = row[x], j = krow[x] + 4 * quad;
+                const double bi = sB[i];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const bool on = j + u <= i;
+                    const float f = __builtin_amdgcn_exp2f(on ? (float)(bi - sB[j + u]) : 0.0f);
+                    sc[x][u] = (on ? sc[x][u] : 0.0f) * f;
                 }
-                *reinterpret_cast<u32x2*>(&sP[i * PP + 16 * jt + 4 * quad]) = p;
+                *reinterpret_cast<u32x2*>(&sP[i * PP + j]) = u32x2{pack_bf16(sc[x][0], sc[x][1]), pack_bf16(sc[x][2], sc[x][3])};
             }
         }
         // exp(b_i) q_i S, transposed: rows are columns of v, columns the 16 tokens of a tile
@@ -249,7 +239,7 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
                     float e[4 * NT];
 #pragma unroll
                     for (int x = 0; x < 4 * NT; ++x) e[x] = O[it][x / 4][x % 4];
-                    attn_store<4 * NT>(A, o_f32, row0 + c + i, head, oc, e);
+                    attn_store<4 * NT, VEC>(A, o_f32, row0 + c + i, head, oc, e);
                 }
             }
         }
@@ -297,30 +287,27 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
     }
 
     float* s_left = attn_last_state(A, pl, STATE_ONLY);
-    if (s_left) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
-                    if (rr < A.dk && cc < A.dv) s_left[(int64_t)rr * A.dv + cc] = S[m][n][i];
-                }
-    }
-    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[pl.id * A.heads + head] = (float)whole;
+    if (s_left) store_state<MT, NT>(A, s_left, scol, quad, S);
+    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
 }
 
 template <int DKT, int NT>
 static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
-    const int64_t ids = a.segment ? a.nseg : a.sq.seqs;
-    const int64_t blocks = ids * a.heads * a.ndvb;
+    const int64_t blocks = (a.segment ? a.nseg : a.sq.seqs) * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    if (state_only)
-        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, 0);
-    else
-        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false>), dim3((unsigned)blocks), dim3(256), 0, s, a,
-                           odt == CONV2D_F32);
+    const dim3 grid((unsigned)blocks), block(256);
+    const int f32 = odt == CONV2D_F32;
+    if (state_only) {
+        if (a.vec)
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true, true>), grid, block, 0, s, a, f32);
+        else
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true, false>), grid, block, 0, s, a, f32);
+    } else {
+        if (a.vec)
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false, true>), grid, block, 0, s, a, f32);
+        else
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false, false>), grid, block, 0, s, a, f32);
+    }
     return hipGetLastError();
 }
 

@@ -13,19 +13,8 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// 4 consecutive elements of a row, those at or past `n` zero.
-__device__ __forceinline__ f32x4 load4(const float* p, int n, bool vec) {
-    if (n <= 0) return f32x4{0, 0, 0, 0};
-    if (vec) return *reinterpret_cast<const f32x4*>(p);
-    f32x4 r{0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < n) r[i] = p[i];
-    return r;
-}
-
 // dk up to 64 DKT, 64 NT columns of v per workgroup
-template <int DKT, int NT, bool STATE_ONLY>
+template <int DKT, int NT, bool STATE_ONLY, bool VEC>
 __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
     constexpr int C = kChunkF32, DKP = 64 * DKT, DVB = 64 * NT;
     constexpr int QP = DKP + 4, VP = DVB + 4, PP = C + 4;  // LDS row pitches in floats
@@ -46,42 +35,39 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
     const int c0 = pl.blk * DVB;      // first column of the workgroup
     const int wc = wave * 16 * NT;    // ... of the wave, within the workgroup's
     const int qh = head / A.rep;
-    const bool vec = A.vec;
 
     // tile (m, n): rows 16 m + 4 quad + i, column col(l16, n); a lane's results of all n tiles are 4 NT neighbours
     auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
     f32x4 S[MT][NT];
-    const float* s_init = STATE_ONLY ? nullptr : attn_first_state(A, pl);
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
-                S[m][n][i] = s_init && rr < A.dk && cc < A.dv ? s_init[(int64_t)rr * A.dv + cc] : 0.0f;
-            }
+    auto scol = [&](int n) { return c0 + col(l16, n); };
+    load_state<MT, NT>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), scol, quad, S);
 
     constexpr int NQ = C * DKP / 4 / 256, NV = C * DVB / 4 / 256;  // 16-byte loads per thread
     constexpr int RS = 256 / (DKP / 4), RSV = 256 / (DVB / 4);
     const int lr = t / (DKP / 4), lc = t % (DKP / 4) * 4, lrv = t / (DVB / 4), lcv = t % (DVB / 4) * 4;
-    const float* gq = static_cast<const float*>(A.q) + (row0 + lr) * A.q_row + qh * A.q_head + lc;
-    const float* gk = static_cast<const float*>(A.k) + (row0 + lr) * A.k_row + qh * A.k_head + lc;
-    const float* gv = static_cast<const float*>(A.v) + (row0 + lrv) * A.v_row + head * A.v_head + c0 + lcv;
+    const float* gq = static_cast<const float*>(A.q) + row0 * A.q_row + qh * A.q_head;
+    const float* gk = static_cast<const float*>(A.k) + row0 * A.k_row + qh * A.k_head;
+    const float* gv = static_cast<const float*>(A.v) + row0 * A.v_row + head * A.v_head + c0;
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
-    f32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
+    const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
+    const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
+    const uint32_t q_at = live > 0 ? (lr * q_row + lc) * 4 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 4 : OOB_OFF;
+    const uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 4 : OOB_OFF;
+    u32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
     float rg = 0.0f;
     auto load = [&](int64_t c) {
         const int n = (int)min<int64_t>(C, len - c);
+        if constexpr (!STATE_ONLY) {
+            const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gq + c * A.q_row, n, q_row, A.dk);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const bool ok = lr + i * RS < n;
-            if constexpr (!STATE_ONLY) rq[i] = load4(gq + (c + i * RS) * A.q_row, ok ? A.dk - lc : 0, vec);
-            rk[i] = load4(gk + (c + i * RS) * A.k_row, ok ? A.dk - lc : 0, vec);
+            for (int i = 0; i < NQ; ++i) rq[i] = load_row<float, VEC>(r, q_at + i * (RS * 4) * q_row, live);
         }
+        const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gk + c * A.k_row, n, k_row, A.dk);
+        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv - c0);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            rv[i] = load4(gv + (c + i * RSV) * A.v_row, lrv + i * RSV < n ? A.dv - c0 - lcv : 0, vec);
+        for (int i = 0; i < NQ; ++i) rk[i] = load_row<float, VEC>(r, k_at + i * (RS * 4) * k_row, live);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) rv[i] = load_row<float, VEC>(rr, v_at + i * (RSV * 4) * v_row, live_v);
         if (wave == 0) rg = gg && lane < n ? gg[(c + lane) * A.g_row] : 0.0f;
     };
 
@@ -91,11 +77,11 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
         const int n = (int)min<int64_t>(C, len - c);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-            if constexpr (!STATE_ONLY) *reinterpret_cast<f32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
-            *reinterpret_cast<f32x4*>(&sK[(lr + i * RS) * QP + lc]) = rk[i];
+            if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
+            *reinterpret_cast<u32x4*>(&sK[(lr + i * RS) * QP + lc]) = rk[i];
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) *reinterpret_cast<f32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
+        for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
         if (wave == 0) {
             const double tot = chunk_decays(rg, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);
@@ -123,8 +109,9 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int j = 16 * jt + 4 * quad + u;
-                    const float f = __builtin_amdgcn_exp2f((float)(bi - sB[j]));
-                    s[u] = j <= i ? s[u] * f : 0.0f;
+                    const bool on = j <= i;
+                    const float f = __builtin_amdgcn_exp2f(on ? (float)(bi - sB[j]) : 0.0f);
+                    s[u] = (on ? s[u] : 0.0f) * f;
                 }
                 *reinterpret_cast<f32x4*>(&sP[i * PP + 16 * jt + 4 * quad]) = s;
             }
@@ -204,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
                     float e[4 * NT];
 #pragma unroll
                     for (int x = 0; x < 4 * NT; ++x) e[x] = O[it][x / 4][x % 4];
-                    attn_store<4 * NT>(A, 1, row0 + c + i, head, oc, e);
+                    attn_store<4 * NT, VEC>(A, 1, row0 + c + i, head, oc, e);
                 }
             }
         }
@@ -233,28 +220,26 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
     }
 
     float* s_left = attn_last_state(A, pl, STATE_ONLY);
-    if (s_left) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int rr = 16 * m + 4 * quad + i, cc = c0 + col(l16, n);
-                    if (rr < A.dk && cc < A.dv) s_left[(int64_t)rr * A.dv + cc] = S[m][n][i];
-                }
-    }
-    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[pl.id * A.heads + head] = (float)whole;
+    if (s_left) store_state<MT, NT>(A, s_left, scol, quad, S);
+    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
 }
 
 template <int DKT, int NT>
 static hipError_t launch_one(const AttnArgs& a, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.segment ? a.nseg : a.sq.seqs) * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    if (state_only)
-        hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+    const dim3 grid((unsigned)blocks), block(256);
+    if (state_only) {
+        if (a.vec)
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, true, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, true, false>), grid, block, 0, s, a);
+    } else {
+        if (a.vec)
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, false, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, false, false>), grid, block, 0, s, a);
+    }
     return hipGetLastError();
 }
 

@@ -8,7 +8,8 @@ namespace cv {
 // What a workgroup of a chunk kernel runs: tokens [row0, row0 + len) for one head and block of columns.
 struct AttnPlace {
     int head, blk;
-    int64_t id, slot, row0, len;
+    int id;
+    int64_t slot, row0, len;
     bool last;  // the end of its sequence
 };
 // False: nothing (in all threads of the workgroup).  Consecutive ids (column blocks, then heads, of the same tokens)
@@ -18,9 +19,9 @@ __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, A
     const int hid = bid / A.ndvb;
     out->blk = bid - hid * A.ndvb;
     out->id = hid / A.heads;
-    out->head = hid - (int)out->id * A.heads;
-    SeqPart sp{(int)out->id, 0, out->id};
-    if (A.segment) sp = seq_part(A.sq, out->id, A.segment);
+    out->head = hid - out->id * A.heads;
+    SeqPart sp{out->id, 0};
+    if (A.segment) sp = seq_part(A.sq, out->id, (uint32_t)A.segment);
     if (sp.seq >= A.sq.seqs || sp.part < 0) return false;
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t start = sp.part * A.segment;
@@ -34,12 +35,12 @@ __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, A
 }
 __device__ __forceinline__ const float* attn_first_state(const AttnArgs& A, const AttnPlace& p) {
     const int64_t size = (int64_t)A.dk * A.dv;
-    if (A.segment) return A.ws_state + (p.id * A.heads + p.head) * size;
+    if (A.segment) return A.ws_state + ((int64_t)p.id * A.heads + p.head) * size;
     return A.s_in ? A.s_in + (p.slot * A.heads + p.head) * size : nullptr;
 }
 __device__ __forceinline__ float* attn_last_state(const AttnArgs& A, const AttnPlace& p, bool state_only) {
     const int64_t size = (int64_t)A.dk * A.dv;
-    if (state_only) return A.ws_state + (p.id * A.heads + p.head) * size;
+    if (state_only) return A.ws_state + ((int64_t)p.id * A.heads + p.head) * size;
     return p.last && A.s_out ? A.s_out + (p.slot * A.heads + p.head) * size : nullptr;
 }
 
@@ -49,12 +50,23 @@ __device__ __forceinline__ float* attn_last_state(const AttnArgs& A, const AttnP
 __device__ __forceinline__ double chunk_decays(float g, double* sB, float* sD, float* sE, int size) {
     const int lane = threadIdx.x & 63;
     double b = decay_log2(g);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double up = __shfl_up(b, d);
-        if (lane >= d) b += up;
+    // inclusive scan by lane moves: 1, 2, 4 and 8 lanes up within rows of 16, then the rows' sums
+#define SCAN_STEP(ctrl, rows)                                                                            \
+    {                                                                                                    \
+        const u32x2 w = __builtin_bit_cast(u32x2, b);                                                    \
+        b += __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_update_dpp(0, w[0], ctrl, rows, 0xf, false),  \
+                                              (uint32_t)__builtin_amdgcn_update_dpp(0, w[1], ctrl, rows, 0xf, false)}); \
     }
-    const double tot = __shfl(b, 63);
+    SCAN_STEP(0x111, 0xf)
+    SCAN_STEP(0x112, 0xf)
+    SCAN_STEP(0x114, 0xf)
+    SCAN_STEP(0x118, 0xf)
+    SCAN_STEP(0x142, 0xa)
+    SCAN_STEP(0x143, 0xc)
+#undef SCAN_STEP
+    const u32x2 w = __builtin_bit_cast(u32x2, b);
+    const double tot = __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_readlane(w[0], 63),
+                                                        (uint32_t)__builtin_amdgcn_readlane(w[1], 63)});
     if (lane < size) {
         sB[lane] = b;
         sD[lane] = __builtin_amdgcn_exp2f((float)b);
@@ -63,17 +75,77 @@ __device__ __forceinline__ double chunk_decays(float g, double* sB, float* sD, f
     return tot;
 }
 
+// Rows of a chunk are loaded through range-checked buffers, which read zero outside their range: the range ends with
+// the chunk's last row, and columns past the end go to OOB_OFF, so no load needs a branch or a mask and all
+// loads of a chunk are in flight together.  `n` rows of `dim` elements, `row` elements apart (row >= dim).
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rsrc(const T* p, int n, uint32_t row, int dim) {
+    return make_rsrc(p, ((uint32_t)(n - 1) * row + (uint32_t)dim) * (uint32_t)sizeof(T));
+}
+
+// 16 bytes of a row, its first element at byte `off`; `live` elements of them are columns (VEC: all, or off is OOB_OFF
+// or above).
+template <typename T, bool VEC>
+__device__ __forceinline__ u32x4 load_row(__amdgpu_buffer_rsrc_t r, uint32_t off, int live) {
+    if constexpr (VEC) {
+        return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    } else {
+        u32x4 v;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = __builtin_amdgcn_raw_buffer_load_b32(r, i < live ? off + 4 * i : OOB_OFF, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = (uint32_t)ld_u16(r, 2 * i < live ? off + 4 * i : OOB_OFF) |
+                       (uint32_t)ld_u16(r, 2 * i + 1 < live ? off + 4 * i + 2 : OOB_OFF) << 16;
+        }
+        return v;
+    }
+}
+
+// A state as MFMA results hold it: tile (m, n) has rows 16 m + 4 quad + i and column c(n).  Rows past dk lie past the
+// buffer's range.
+template <int MT, int NT, typename Col>
+__device__ __forceinline__ void load_state(const AttnArgs& A, const float* p, Col c, int quad, f32x4 (&S)[MT][NT]) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, p ? (uint32_t)(A.dk * A.dv * 4) : 0u);
+    const uint32_t row = (uint32_t)A.dv * 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t at = c(n) < A.dv ? 4 * quad * row + c(n) * 4 : OOB_OFF;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[m][n][i] = ld_f32(r, at + (16 * m + i) * row);
+    }
+}
+template <int MT, int NT, typename Col>
+__device__ __forceinline__ void store_state(const AttnArgs& A, float* p, Col c, int quad, const f32x4 (&S)[MT][NT]) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, (uint32_t)(A.dk * A.dv * 4));
+    uint32_t row = (uint32_t)A.dv * 4;
+    asm volatile("" : "+s"(row));  // or the addresses of the load would be kept in registers until here
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t at = c(n) < A.dv ? 4 * quad * row + c(n) * 4 : OOB_OFF;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st_f32(r, at + (16 * m + i) * row, S[m][n][i]);
+    }
+}
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 
 // N results of one token, scaled and rounded, to columns c .. c + N - 1 (those at or past dv are none).
-template <int N>
+template <int N, bool VEC>
 __device__ __forceinline__ void attn_store(const AttnArgs& A, int o_f32, int64_t row, int head, int c, float (&e)[N]) {
     const int64_t at = row * A.o_row + head * A.o_head + c;
 #pragma unroll
     for (int x = 0; x < N; ++x) e[x] *= A.scale;
     if (o_f32) {
         float* o = static_cast<float*>(A.o) + at;
-        if (A.vec) {
+        if constexpr (VEC) {
             store_pack<float, N>(o, e);
         } else {
 #pragma unroll
@@ -82,7 +154,7 @@ __device__ __forceinline__ void attn_store(const AttnArgs& A, int o_f32, int64_t
         }
     } else {
         uint16_t* o = static_cast<uint16_t*>(A.o) + at;
-        if (A.vec) {
+        if constexpr (VEC) {
             store_pack<uint16_t, N>(o, e);
         } else {
 #pragma unroll

@@ -103,12 +103,18 @@ int order_after_last(seqmix_attn_desc* d, hipStream_t s) {
 // Sequences of this many tokens or fewer on average go token by token.
 constexpr int64_t kTokensMost = 8;
 
+// The chunk kernels address the rows of a chunk by 32-bit byte offsets from its first: rows further apart go
+// token by token.
+bool chunk_rows_near(const seqmix_attn_params& p) {
+    return std::max({p.q_row, p.k_row, p.v_row}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
+}
+
 // Kernel, and where sequences are cut: about two workgroups per CU over all heads and column blocks, in segments of
 // at least 128 tokens (below that the segments' states cost more than their tokens).
 void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
-    if (p.tokens <= kTokensMost * p.seqs) return;
+    if (p.tokens <= kTokensMost * p.seqs || !chunk_rows_near(p)) return;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
     d->plan.chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv));

@@ -39,11 +39,14 @@ __device__ __forceinline__ void store_pack(T* p, const float (&in)[N]) {
     *reinterpret_cast<Pack<T, N>*>(p) = v;
 }
 
-// Rows [first, first + len) of sequence i, clamped so that no offsets lead outside the call's rows.
+// Rows [first, first + len) of sequence i, clamped so that no offsets lead outside the call's rows.  Row numbers, slots
+// and parts are below 2^31 (the descriptors refuse more), so their divisions are 32-bit ones.
 struct SeqRange {
     int64_t first, len;
 };
-__device__ __forceinline__ int64_t clamp_row(int64_t r, int64_t tokens) { return r < 0 ? 0 : r > tokens ? tokens : r; }
+__device__ __forceinline__ uint32_t clamp_row(int64_t r, int64_t tokens) {
+    return (uint32_t)(r < 0 ? 0 : r > tokens ? tokens : r);
+}
 __device__ __forceinline__ SeqRange seq_range(const SeqArgs& a, int i) {
     if (!a.off) return {(int64_t)i * a.seq_len, a.seq_len};
     const int64_t b = clamp_row(a.off[i], a.tokens), e = clamp_row(a.off[i + 1], a.tokens);
@@ -62,13 +65,13 @@ __device__ __forceinline__ int64_t seq_slot(const SeqArgs& a, int i) {
 // equal length own exactly as many as they have parts (seq_parts).
 struct SeqPart {
     int seq;
-    int64_t part, first_id;  // number of the part within the sequence, id of its part 0
+    int part;  // number of the part within the sequence; negative: none (offsets that lie)
 };
-__device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, int64_t id, int64_t size) {
+__device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint32_t size) {
     if (!a.off) {
-        const int64_t per = seq_parts(a.seq_len, size);
-        const int64_t i = id / per;
-        return {(int)i, id - i * per, i * per};
+        const uint32_t len = (uint32_t)a.seq_len, per = len > size ? (len + size - 1) / size : 1;
+        const uint32_t i = id / per;
+        return {(int)i, (int)(id - i * per)};
     }
     int lo = 0, hi = a.seqs - 1;  // the last sequence whose first id is at most `id`
     while (lo < hi) {
@@ -78,8 +81,7 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, int64_t id, int64_
         else
             hi = mid - 1;
     }
-    const int64_t first = clamp_row(a.off[lo], a.tokens) / size + lo;
-    return {lo, id - first, first};
+    return {lo, (int)id - (int)(clamp_row(a.off[lo], a.tokens) / size + lo)};
 }
 
 // Log2 of a decay from its natural log.  Logs below -1000 (-infinity among them) have an

@@ -17,7 +17,7 @@ struct SeqArgs {
 };
 
 // Parts of `size` tokens of a sequence (an empty one has one), and the ids that number the parts of all sequences.
-__host__ __device__ inline int64_t seq_parts(int64_t len, int64_t size) {
+inline int64_t seq_parts(int64_t len, int64_t size) {
     return len > size ? (len + size - 1) / size : 1;
 }
 inline int64_t seq_part_ids(const SeqArgs& a, int64_t size) {

@@ -17,10 +17,10 @@ template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
     const int c = (blockIdx.x * 256 + threadIdx.x) * V;
     if (c >= A.channels) return;
-    const SeqPart sp = seq_part(A.sq, blockIdx.y + (int64_t)blockIdx.z * 65535, tile);
+    const SeqPart sp = seq_part(A.sq, blockIdx.y + blockIdx.z * 65535u, tile);
     if (sp.seq >= A.sq.seqs) return;
     const SeqRange r = seq_range(A.sq, sp.seq);
-    const int64_t t0 = sp.part * tile;
+    const int64_t t0 = (int64_t)sp.part * tile;
     if (sp.part < 0 || (sp.part > 0 && t0 >= r.len)) return;
     const int64_t slot = seq_slot(A.sq, sp.seq);
     if (slot < 0) return;
