@@ -42,7 +42,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 template <int DKT, int NT, bool STATE_ONLY, bool VEC>
 __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
     constexpr int C = kChunk, DKP = 32 * DKT, DVB = 64 * NT;
-    constexpr int QP = DKP + 8, VP = DVB + 8, PP = C + 8;  // LDS row pitches: 16 bytes off the bank period
+    // LDS row pitches.  Of the 64 banks, rows of q and k are 12 apart (or -12): 8 rows of 16 bytes, 16 of 8, and the 4
+    // rows that a transposing load takes 8 banks of are free of conflicts; rows of v, of which it takes
+    // every other 8 bytes with NT = 2, are 16 apart then.
+    constexpr int QP = DKP + (DKP == 64 ? 40 : 24), VP = DVB + (NT == 1 ? 40 : 32), PP = C + 8;
     constexpr int MT = 2 * DKT;                            // 16-row tiles of the state
     __shared__ __align__(16) uint16_t sQ[STATE_ONLY ? 1 : C * QP];
     __shared__ __align__(16) uint16_t sK[C * QP];
@@ -274,13 +277,19 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
                 for (int x = 0; x < 3; ++x) vp[nt][x] = __builtin_bit_cast(bf16x8, pl[x]);
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const uint16_t* p = &sK[(32 * s + 8 * quad + (l16 >> 2)) * QP + 16 * m + 4 * (l16 & 3)];
-                const bf16x8 kf = join8(lds_tr(p), lds_tr(p + 4 * QP));
+            for (int m = 0; m < MT; m += 2) {
+                bf16x8 kf[2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int y = 0; y < 2; ++y) {
+                    const uint16_t* p = &sK[(32 * s + 8 * quad + (l16 >> 2)) * QP + 16 * (m + y) + 4 * (l16 & 3)];
+                    kf[y] = join8(lds_tr(p), lds_tr(p + 4 * QP));
+                }
 #pragma unroll
-                    for (int x = 2; x >= 0; --x) S[m][nt] = mfma16(kf, vp[nt][x], S[m][nt]);
+                for (int x = 2; x >= 0; --x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) S[m + y][nt] = mfma16(kf[y], vp[nt][x], S[m + y][nt]);
             }
         }
         __syncthreads();
