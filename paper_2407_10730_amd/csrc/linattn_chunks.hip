@@ -5,13 +5,12 @@
 //   o_i = scale ( exp(b_i) q_i S + sum_{j <= i} exp(b_i - b_j) (q_i . k_j) v_j )
 //   S'  = exp(b_C) S + sum_j exp(b_C - b_j) k_j v_j^T
 //
-// are four matrix products per chunk.  One workgroup (4 waves) runs a sequence's chunks in order, for one head and
-// 64 NT columns of v.  Each wave owns 16 NT of the columns: its part of S stays in the accumulator
-// registers from chunk to chunk and is itself an operand of q S (the rows that a lane holds as a result
-// are the reduction indices that it feeds as an operand; q is read from LDS in the same order), so S never
-// passes through LDS.  The scores are shared: each wave computes 16 rows of them into LDS.  Products over
-// tokens read k and v from LDS through the transposing load.
-//
+// are four matrix products per chunk.  One workgroup runs a sequence's chunks in order, for one head and 64 or 128 columns
+// of v, 16 per wave.  A wave's part of S stays in its accumulator registers from chunk to chunk and is itself an
+// operand of q S (the rows that a lane holds as a result are the reduction indices that it feeds as an
+// operand; q is read from LDS in the same order), so S never passes through LDS.  The scores are shared: the waves
+// divide their 16x16 tiles and exchange them through LDS.  Products over tokens read k and v from LDS through the
+// transposing load.
 // Rounding: the scores and, as an operand of q S, the state are rounded to bf16 once (o is bf16 itself, or
 // as exact as bf16 operands make it); the state's own update multiplies exact k by exp(b_C - b_j) v_j
 // as three bf16 planes, which hold all 24 bits, so states keep fp32 accuracy over any length.
@@ -28,51 +27,71 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
 
 // Four rows of 16 columns transposed: lane l of each 16 gives the address of row l / 4, columns 4 (l % 4) .. + 3,
 // and receives column l of the four rows.
-__device__ __forceinline__ u32x2 lds_tr(const uint16_t* p) {
+__device__ __forceinline__ u32x2 lds_tr(const uint16_t* base, uint32_t off) {
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p)));
+    return __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(reinterpret_cast<const char*>(base) + off)));
 }
 __device__ __forceinline__ bf16x8 join8(u32x2 a, u32x2 b) {
     return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
 }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+// Where LDS holds element (row, c) of a tile of P columns (q, k: 64, 128 or 256; v: 64 or 128; scores: 64).  The 16-byte
+// units of a row are permuted by an exclusive or with a number of the row, so that without padding (a row is a
+// multiple of half the 64 banks) these take distinct banks: 16 rows of one unit, whether the 16 lanes served
+// together are of one quad or of two (8 rows each, of neighbouring units: rows r < 4 and r >= 12 of a tile, or the
+// others); 16 rows of half a unit; and 4 rows, r % 4 = 0 .. 3, of two units or of half of each of four, which the
+// transposing loads of v and k take.  Counted: 0 conflict cycles in the state pass (a third of its LDS cycles with padded rows).
+// The number depends on row % 16 only, so 16 rows or 64 bytes (32 bytes ...) further on is an addition or an exclusive
+// or with a constant: the kernel keeps one byte offset per access pattern (swz_at) and derives the others.
+template <int P>
+__device__ __forceinline__ uint32_t swz(int row) {
+    const int h0 = row >> 2 & 1, h1 = row >> 3 & 1;
+    return P == 64 ? (row & 2) << 1 | (h0 ^ h1) << 1 | h1  // two rows per 64 banks
+                   : (row & 3) << 2 | (h0 ^ h1) << 1 | h1;
+}
+template <int P>
+__device__ __forceinline__ uint32_t swz_at(int row, int c) {
+    return row * (2 * P) + ((((uint32_t)c >> 3) ^ swz<P>(row)) << 4) + (c & 7) * 2;
+}
+template <typename V>
+__device__ __forceinline__ V lds_read(const uint16_t* base, uint32_t off) {
+    return *reinterpret_cast<const V*>(reinterpret_cast<const char*>(base) + off);
+}
+template <typename V>
+__device__ __forceinline__ void lds_write(uint16_t* base, uint32_t off, V v) {
+    *reinterpret_cast<V*>(reinterpret_cast<char*>(base) + off) = v;
 }
 
-template <int DKT, int NT, bool STATE_ONLY, bool VEC>
-__global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
-    constexpr int C = kChunk, DKP = 32 * DKT, DVB = 64 * NT;
-    // LDS row pitches.  Of the 64 banks, rows of q and k are 12 apart (or -12): 8 rows of 16 bytes, 16 of 8, and the 4
-    // rows that a transposing load takes 8 banks of are free of conflicts; rows of v, of which it takes
-    // every other 8 bytes with NT = 2, are 16 apart then.
-    constexpr int QP = DKP + (DKP == 64 ? 40 : 24), VP = DVB + (NT == 1 ? 40 : 32), PP = C + 8;
+// waves per SIMD that LDS leaves room for
+constexpr int chunk_occupancy(int dkt, int waves) { return waves == 8 ? (dkt <= 4 ? 4 : 2) : dkt <= 2 ? 4 : dkt <= 4 ? 3 : 1; }
+
+template <int DKT, int WAVES, bool STATE_ONLY, bool VEC>
+__global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
+    constexpr int C = kChunk, DKP = 32 * DKT, DVB = 16 * WAVES, NTHR = 64 * WAVES;
     constexpr int MT = 2 * DKT;                            // 16-row tiles of the state
-    __shared__ __align__(16) uint16_t sQ[STATE_ONLY ? 1 : C * QP];
-    __shared__ __align__(16) uint16_t sK[C * QP];
-    __shared__ __align__(16) uint16_t sV[C * VP];
-    __shared__ __align__(16) uint16_t sP[STATE_ONLY ? 1 : C * PP];
+    __shared__ __align__(16) uint16_t sQ[STATE_ONLY ? 1 : C * DKP];
+    __shared__ __align__(16) uint16_t sK[C * DKP];
+    __shared__ __align__(16) uint16_t sV[C * DVB];
+    __shared__ __align__(16) uint16_t sP[STATE_ONLY ? 1 : C * C];
     __shared__ __align__(16) double sB[C];
     __shared__ __align__(16) float sE[C], sD[C];
     __shared__ float sTot;
 
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l16 = lane & 15, quad = lane >> 4;
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    int lane = t & 63, l16 = lane & 15, quad = lane >> 4;
     AttnPlace pl;
     if (!attn_place(A, STATE_ONLY, &pl)) return;
     const int head = pl.head;
     const int64_t row0 = pl.row0, len = pl.len;
     const int c0 = pl.blk * DVB;          // first column of the workgroup
-    const int wc = wave * 16 * NT;        // ... of the wave, within the workgroup's
+    const int wc = wave * 16;             // ... of the wave, within the workgroup's
     const int qh = head / A.rep;
 
-    // The state: tile (m, n) of the wave holds rows 16 m + 4 quad + i and column wc + col(l16, n).
-    // Columns are dealt so that a lane's results of all n tiles are 4 NT neighbours.
-    auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
-    f32x4 S[MT][NT];
-    auto scol = [&](int n) { return c0 + col(l16, n); };
-    load_state<MT, NT>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), scol, quad, S);
+    f32x4 S[MT];  // tile m: rows 32 (m / 2) + 8 quad + 4 (m % 2) + i, column c0 + wc + l16
+    load_state<8, 4>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), c0 + wc + l16, quad, S);
 
     // Loads: thread t takes 8 elements of row t / (DKP / 8) + i * RS of q and k, likewise of v
-    constexpr int RS = 256 / (DKP / 8), RSV = 256 / (DVB / 8);
+    constexpr int RS = NTHR / (DKP / 8), RSV = NTHR / (DVB / 8), NQ = C / RS, NV = C / RSV;
     const int lr = t / (DKP / 8), lc = t % (DKP / 8) * 8, lrv = t / (DVB / 8), lcv = t % (DVB / 8) * 8;
     const uint16_t* gq = static_cast<const uint16_t*>(A.q) + row0 * A.q_row + qh * A.q_head;
     const uint16_t* gk = static_cast<const uint16_t*>(A.k) + row0 * A.k_row + qh * A.k_head;
@@ -80,251 +99,213 @@ __global__ __launch_bounds__(256, DKT <= 4 ? 2 : 1) void attn_chunks_bf16_kernel
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
     const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
     const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
-    const uint32_t q_at = live > 0 ? (lr * q_row + lc) * 2 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 2 : OOB_OFF;
-    const uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 2 : OOB_OFF;
-    u32x4 rq[STATE_ONLY ? 1 : DKT], rk[DKT], rv[2 * NT];
+    uint32_t q_at = live > 0 ? (lr * q_row + lc) * 2 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 2 : OOB_OFF;
+    uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 2 : OOB_OFF;
+    u32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
     float rg = 0.0f;
     auto load = [&](int64_t c) {  // chunk starting at token c of the segment into registers
         const int n = (int)min<int64_t>(C, len - c);
         if constexpr (!STATE_ONLY) {
             const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gq + c * A.q_row, n, q_row, A.dk);
 #pragma unroll
-            for (int i = 0; i < DKT; ++i) rq[i] = load_row<uint16_t, VEC>(r, q_at + i * (RS * 2) * q_row, live);
+            for (int i = 0; i < NQ; ++i) rq[i] = load_row<uint16_t, VEC>(r, q_at + i * (RS * 2) * q_row, live);
         }
         const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gk + c * A.k_row, n, k_row, A.dk);
         const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv - c0);
 #pragma unroll
-        for (int i = 0; i < DKT; ++i) rk[i] = load_row<uint16_t, VEC>(r, k_at + i * (RS * 2) * k_row, live);
+        for (int i = 0; i < NQ; ++i) rk[i] = load_row<uint16_t, VEC>(r, k_at + i * (RS * 2) * k_row, live);
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) rv[i] = load_row<uint16_t, VEC>(rr, v_at + i * (RSV * 2) * v_row, live_v);
-        if (wave == 0) rg = gg && lane < n ? gg[(c + lane) * A.g_row] : 0.0f;
+        for (int i = 0; i < NV; ++i) rv[i] = load_row<uint16_t, VEC>(rr, v_at + i * (RSV * 2) * v_row, live_v);
+        if (wave == WAVES - 1) rg = load_decay(A, gg, c, lane, n);
     };
 
-    double whole = 0.0;  // log2 of the segment's decay (wave 0)
+    // byte offsets in LDS of this thread's accesses: stores of a chunk's rows; rows of q and k as operands; k and v
+    // transposed (tokens 0-3 and 4-7 of a quad's 8); scores
+    uint32_t o_st = swz_at<DKP>(lr, lc), o_stv = swz_at<DVB>(lrv, lcv);
+    uint32_t o_row = swz_at<DKP>(l16, 8 * quad);
+    const int tr = 8 * quad + (l16 >> 2), tc = 4 * (l16 & 3);
+    uint32_t o_k0 = swz_at<DKP>(tr, 2 * tc), o_k1 = swz_at<DKP>(tr + 4, 2 * tc);
+    uint32_t o_v0 = swz_at<DVB>(tr, wc + tc), o_v1 = swz_at<DVB>(tr + 4, wc + tc);
+    uint32_t o_pw = swz_at<C>(l16, 4 * quad), o_pr = swz_at<C>(l16, 8 * quad);
+
+    double whole = 0.0;  // log2 of the segment's decay (last wave)
     if (len > 0) load(0);
     for (int64_t c = 0; c < len; c += C) {
         const int n = (int)min<int64_t>(C, len - c);
+        // what follows from these offsets is cheaper computed again than kept in registers over the loop
+        asm volatile("" : "+v"(o_st), "+v"(o_stv), "+v"(o_row), "+v"(o_k0), "+v"(o_k1), "+v"(o_pw), "+v"(o_pr),
+                     "+v"(o_v0), "+v"(o_v1));
+        asm volatile("" : "+v"(q_at), "+v"(k_at), "+v"(v_at), "+v"(l16), "+v"(quad), "+v"(lane));
         // registers to LDS; decays
 #pragma unroll
-        for (int i = 0; i < DKT; ++i) {
-            if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
-            *reinterpret_cast<u32x4*>(&sK[(lr + i * RS) * QP + lc]) = rk[i];
+        for (int i = 0; i < NQ; ++i) {
+            // 8 rows further on the number of the row differs in its two low bits
+            const uint32_t off = (RS == 8 && i % 2 ? o_st ^ (3u << 4) : o_st) + i * RS * 2 * DKP;
+            if constexpr (!STATE_ONLY) lds_write(sQ, off, rq[i]);
+            lds_write(sK, off, rk[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
-        if (wave == 0) {
-            const double tot = chunk_decays(rg, sB, sD, sE, C);
+        for (int i = 0; i < NV; ++i) lds_write(sV, o_stv + i * RSV * 2 * DVB, rv[i]);
+        if (wave == WAVES - 1) {
+            const double tot = chunk_decays(rg, lane, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);
             whole += tot;
         }
         __syncthreads();
-        if (c + C < len) load(c + C);
+        if (STATE_ONLY && c + C < len) load(c + C);
 
-        f32x4 O[4][NT];
         if constexpr (!STATE_ONLY) {
-            // Scores, transposed (a lane holds 4 neighbouring j of one i).  10 of the 16 tiles are on or below the
-            // diagonal and 2 above it are read as zeros: 3 per wave, (it, jt) =
-            // (0,0) (3,0) (3,1) | (1,0) (1,1) (3,2) | (2,0) (2,1) (2,2) | (3,3) (0,1) (2,3)
-            constexpr uint32_t kIt[3] = {0x3210, 0x0213, 0x2233}, kJt[3] = {0x3000, 0x1110, 0x3221};
-            f32x4 sc[3];
-            int row[3], krow[3];
+            // Scores, transposed (a lane holds 4 neighbouring j of one i): the 10 of 16 tiles on or below the diagonal, and
+            // the 2 above it that are read as zeros, dealt to the waves in turn: (it, jt) = (0,0) (1,0) (1,1) (2,0)
+            // (2,1) (2,2) (0,1) (2,3) (3,0) (3,1) (3,2) (3,3)
+            constexpr uint64_t kIt = 0x333320222110, kJt = 0x321031210100;
 #pragma unroll
-            for (int x = 0; x < 3; ++x) {
-                sc[x] = f32x4{0, 0, 0, 0};
-                row[x] = 16 * ((kIt[x] >> (4 * wave)) & 15) + l16;
-                krow[x] = 16 * ((kJt[x] >> (4 * wave)) & 15);
-            }
+            for (int x = 0; x < 12; x += WAVES) {
+                if (x + WAVES > 12 && x + wave >= 12) break;
+                const int it = (int)(kIt >> (4 * (x + wave))) & 15, jt = (int)(kJt >> (4 * (x + wave))) & 15;
+                f32x4 sc{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < DKT; ++k)
-#pragma unroll
-                for (int x = 0; x < 3; ++x)
-                    sc[x] = mfma16(*reinterpret_cast<const bf16x8*>(&sK[(krow[x] + l16) * QP + 32 * k + 8 * quad]),
-                                   *reinterpret_cast<const bf16x8*>(&sQ[row[x] * QP + 32 * k + 8 * quad]), sc[x]);
-#pragma unroll
-            for (int x = 0; x < 3; ++x) {
-                const int i = row[x], j = krow[x] + 4 * quad;
+                for (int k = 0; k < DKT; ++k)
+                    sc = mfma16(lds_read<bf16x8>(sK, (o_row + jt * (32 * DKP)) ^ (k << 6)),
+                                lds_read<bf16x8>(sQ, (o_row + it * (32 * DKP)) ^ (k << 6)), sc);
+                const int i = 16 * it + l16, j = 16 * jt + 4 * quad;
                 const double bi = sB[i];
+                const f64x2 b01 = *reinterpret_cast<const f64x2*>(&sB[j]), b23 = *reinterpret_cast<const f64x2*>(&sB[j + 2]);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const bool on = j + u <= i;
-                    const float f = __builtin_amdgcn_exp2f(on ? (float)(bi - sB[j + u]) : 0.0f);
-                    sc[x][u] = (on ? sc[x][u] : 0.0f) * f;
+                    const float f = (float)(bi - (u < 2 ? b01[u] : b23[u - 2]));
+                    sc[u] = (on ? sc[u] : 0.0f) * __builtin_amdgcn_exp2f(on ? f : 0.0f);
                 }
-                *reinterpret_cast<u32x2*>(&sP[i * PP + j]) = u32x2{pack_bf16(sc[x][0], sc[x][1]), pack_bf16(sc[x][2], sc[x][3])};
+                lds_write(sP, (o_pw ^ (jt << 5)) + it * (32 * C), u32x2{pack_bf16(sc[0], sc[1]), pack_bf16(sc[2], sc[3])});
             }
         }
-        // exp(b_i) q_i S, transposed: rows are columns of v, columns the 16 tokens of a tile
-        auto inter = [&] {
+        if constexpr (!STATE_ONLY) __syncthreads();
+        // v as an operand: 8 tokens of one column per lane
+        u32x4 vf[2];
 #pragma unroll
-            for (int it = 0; it < 4; ++it)
+        for (int s = 0; s < 2; ++s) {
+            const u32x2 a = lds_tr(sV, o_v0 + 32 * s * 2 * DVB), b = lds_tr(sV, o_v1 + 32 * s * 2 * DVB);
+            vf[s] = u32x4{a[0], a[1], b[0], b[1]};
+        }
+        if constexpr (!STATE_ONLY) {
+            f32x4 O[4];  // transposed: rows are columns of v, columns the 16 tokens of a tile
+            // exp(b_i) q_i S
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) O[it][nt] = f32x4{0, 0, 0, 0};
+            for (int it = 0; it < 4; ++it) O[it] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < DKT; ++k) {
-                bf16x8 sf[NT];
+                const f32x4 a = S[2 * k], b = S[2 * k + 1];
+                const bf16x8 sf = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]),
+                                                                   pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])});
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const f32x4 a = S[2 * k][nt], b = S[2 * k + 1][nt];
-                    sf[nt] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]),
-                                                              pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])});
-                }
-#pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    const uint16_t* p = &sQ[(16 * it + l16) * QP + 32 * k + 4 * quad];
-                    const bf16x8 qf = join8(*reinterpret_cast<const u32x2*>(p), *reinterpret_cast<const u32x2*>(p + 16));
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) O[it][nt] = mfma16(sf[nt], qf, O[it][nt]);
-                }
+                for (int it = 0; it < 4; ++it)
+                    O[it] = mfma16(sf, lds_read<bf16x8>(sQ, (o_row ^ (k << 6)) + it * (32 * DKP)), O[it]);
             }
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const float d = sD[16 * it + l16];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) O[it][nt] *= d;
-            }
-        };
-        if constexpr (!STATE_ONLY) {
-            inter();
-            __syncthreads();
-        }
-        // v as an operand: 8 tokens of one column per lane
-        u32x4 vf[2][NT];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const uint16_t* p = &sV[(32 * s + 8 * quad + (l16 >> 2)) * VP + wc + 4 * NT * (l16 & 3) + 4 * nt];
-                const u32x2 a = lds_tr(p), b = lds_tr(p + 4 * VP);
-                vf[s][nt] = u32x4{a[0], a[1], b[0], b[1]};
-            }
-        if constexpr (!STATE_ONLY) {
+            for (int it = 0; it < 4; ++it) O[it] *= sD[16 * it + l16];
+            const f32x4 inter[4] = {O[0], O[1], O[2], O[3]};
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int it = 2 * s; it < 4; ++it) {
-                    const bf16x8 pf =
-                        *reinterpret_cast<const bf16x8*>(&sP[(16 * it + l16) * PP + 32 * s + 8 * quad]);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        O[it][nt] = mfma16(__builtin_bit_cast(bf16x8, vf[s][nt]), pf, O[it][nt]);
-                }
+                for (int it = 2 * s; it < 4; ++it)
+                    O[it] = mfma16(__builtin_bit_cast(bf16x8, vf[s]),
+                                   lds_read<bf16x8>(sP, (o_pr ^ (s << 6)) + it * (32 * C)), O[it]);
             // A later token's infinite or NaN v times its score of zero has made every earlier token NaN too, the
-            // first of the 32 that share a product step among them: such chunks are summed again
-            // without the masked terms.
+            // first of the 32 that share a product step among them: such chunks are summed again without the
+            // masked terms.
             bool bad = false;
-            if (l16 == 0) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        bad |= !finite(O[0][nt][u]) || !finite(O[2][nt][u]);
-            }
-            if (__any(bad)) {
-                inter();
+            for (int u = 0; u < 4; ++u) bad = bad || !finite(O[0][u]) || !finite(O[2][u]);
+            if (__any(bad && l16 == 0)) {
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
                     const int i = 16 * it + l16;
+                    O[it] = inter[it];
                     for (int j = 0; j <= i; ++j) {
-                        const float p = to_f32(sP[i * PP + j]);
-                        const uint16_t* v = &sV[j * VP + wc + 4 * NT * quad];
+                        const float p = to_f32(lds_read<uint16_t>(sP, swz_at<C>(i, j)));
+                        const uint32_t v = swz_at<DVB>(j, wc + 4 * quad);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) O[it][nt][u] = fmaf(p, to_f32(v[4 * nt + u]), O[it][nt][u]);
+                        for (int u = 0; u < 4; ++u) O[it][u] = fmaf(p, to_f32(lds_read<uint16_t>(sV, v + 2 * u)), O[it][u]);
                     }
                 }
             }
-            const int oc = c0 + wc + 4 * NT * quad;
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const int i = 16 * it + l16;
-                if (i < n && oc < A.dv) {
-                    float e[4 * NT];
-#pragma unroll
-                    for (int x = 0; x < 4 * NT; ++x) e[x] = O[it][x / 4][x % 4];
-                    attn_store<4 * NT, VEC>(A, o_f32, row0 + c + i, head, oc, e);
-                }
-            }
+            // the next chunk's rows travel under the state's products (any earlier, and their registers would spill)
+            if (c + C < len) load(c + C);
+            attn_store<4, VEC>(A, o_f32, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         // the state moves on
         const float tot = sTot;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[m][nt] *= tot;
+        for (int m = 0; m < MT; ++m) S[m] *= tot;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            bf16x8 vp[NT][3];  // planes of exp(b_C - b_j) v_j
+            u32x4 vp[3];  // planes of exp(b_C - b_j) v_j
             const f32x4 e0 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad]);
             const f32x4 e1 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad + 4]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                u32x4 pl[3];
+            for (int w = 0; w < 4; ++w) {
+                float lo = __builtin_bit_cast(float, vf[s][w] << 16) * (w < 2 ? e0[2 * w] : e1[2 * w - 4]);
+                float hi = __builtin_bit_cast(float, vf[s][w] & 0xffff0000u) * (w < 2 ? e0[2 * w + 1] : e1[2 * w - 3]);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    float lo = __builtin_bit_cast(float, vf[s][nt][w] << 16) * (w < 2 ? e0[2 * w] : e1[2 * w - 4]);
-                    float hi = __builtin_bit_cast(float, vf[s][nt][w] & 0xffff0000u) *
-                               (w < 2 ? e0[2 * w + 1] : e1[2 * w - 3]);
-#pragma unroll
-                    for (int x = 0; x < 3; ++x) {
-                        const uint32_t p = pack_bf16(lo, hi);
-                        pl[x][w] = p;
-                        lo -= __builtin_bit_cast(float, p << 16);
-                        hi -= __builtin_bit_cast(float, p & 0xffff0000u);
-                    }
+                for (int x = 0; x < 3; ++x) {
+                    const uint32_t p = pack_bf16(lo, hi);
+                    vp[x][w] = p;
+                    lo -= __builtin_bit_cast(float, p << 16);
+                    hi -= __builtin_bit_cast(float, p & 0xffff0000u);
                 }
-#pragma unroll
-                for (int x = 0; x < 3; ++x) vp[nt][x] = __builtin_bit_cast(bf16x8, pl[x]);
             }
 #pragma unroll
-            for (int m = 0; m < MT; m += 2) {
+            for (int m = 0; m < MT; m += 2) {  // two tiles side by side: a product does not wait for the one before
                 bf16x8 kf[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const uint16_t* p = &sK[(32 * s + 8 * quad + (l16 >> 2)) * QP + 16 * (m + y) + 4 * (l16 & 3)];
-                    kf[y] = join8(lds_tr(p), lds_tr(p + 4 * QP));
+                    const uint32_t at = m << 5, down = 32 * s * 2 * DKP + 8 * y;
+                    kf[y] = join8(lds_tr(sK, (o_k0 ^ at) + down), lds_tr(sK, (o_k1 ^ at) + down));
                 }
 #pragma unroll
                 for (int x = 2; x >= 0; --x)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) S[m + y][nt] = mfma16(kf[y], vp[nt][x], S[m + y][nt]);
+                    for (int y = 0; y < 2; ++y) S[m + y] = mfma16(kf[y], __builtin_bit_cast(bf16x8, vp[x]), S[m + y]);
             }
         }
         __syncthreads();
     }
 
     float* s_left = attn_last_state(A, pl, STATE_ONLY);
-    if (s_left) store_state<MT, NT>(A, s_left, scol, quad, S);
-    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
+    if (s_left) store_state<8, 4>(A, s_left, c0 + wc + l16, quad, S);
+    if (STATE_ONLY && pl.blk == 0 && t == NTHR - 1) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
 }
 
-template <int DKT, int NT>
+template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.segment ? a.nseg : a.sq.seqs) * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid((unsigned)blocks), block(64 * WAVES);
     const int f32 = odt == CONV2D_F32;
     if (state_only) {
         if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true, true>), grid, block, 0, s, a, f32);
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, true, true>), grid, block, 0, s, a, f32);
         else
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, true, false>), grid, block, 0, s, a, f32);
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, true, false>), grid, block, 0, s, a, f32);
     } else {
         if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false, true>), grid, block, 0, s, a, f32);
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, false, true>), grid, block, 0, s, a, f32);
         else
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, NT, false, false>), grid, block, 0, s, a, f32);
+            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, false, false>), grid, block, 0, s, a, f32);
     }
     return hipGetLastError();
 }
 
 hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
-    if (a.dk > 128) return launch_one<8, 1>(a, odt, state_only, s);  // two column tiles would not fit the registers
-    if (chunk_block(a.dk, a.dv) == 64)
-        return a.dk <= 64 ? launch_one<2, 1>(a, odt, state_only, s) : launch_one<4, 1>(a, odt, state_only, s);
-    return a.dk <= 64 ? launch_one<2, 2>(a, odt, state_only, s) : launch_one<4, 2>(a, odt, state_only, s);
+    const int dkt = a.dk <= 64 ? 2 : a.dk <= 128 ? 4 : 8;
+    if (chunk_block(a.dv) == 64)
+        return dkt == 2 ? launch_one<2, 4>(a, odt, state_only, s)
+               : dkt == 4 ? launch_one<4, 4>(a, odt, state_only, s)
+                          : launch_one<8, 4>(a, odt, state_only, s);
+    return dkt == 2 ? launch_one<2, 8>(a, odt, state_only, s)
+           : dkt == 4 ? launch_one<4, 8>(a, odt, state_only, s)
+                      : launch_one<8, 8>(a, odt, state_only, s);
 }
 
 }  // namespace cv

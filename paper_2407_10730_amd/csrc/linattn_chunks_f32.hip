@@ -13,10 +13,12 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// dk up to 64 DKT, 64 NT columns of v per workgroup
-template <int DKT, int NT, bool STATE_ONLY, bool VEC>
-__global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
-    constexpr int C = kChunkF32, DKP = 64 * DKT, DVB = 64 * NT;
+// dk up to 64 DKT, 16 WAVES columns of v per workgroup; waves per SIMD that LDS leaves room for
+constexpr int chunk_f32_occupancy(int dkt, int waves) { return waves == 8 ? (dkt <= 2 ? 4 : 2) : dkt <= 2 ? 3 : 2; }
+
+template <int DKT, int WAVES, bool STATE_ONLY, bool VEC>
+__global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void attn_chunks_f32_kernel(AttnArgs A) {
+    constexpr int C = kChunkF32, DKP = 64 * DKT, DVB = 16 * WAVES, NTHR = 64 * WAVES;
     constexpr int QP = DKP + 4, VP = DVB + 4, PP = C + 4;  // LDS row pitches in floats
     constexpr int MT = DKP / 16;
     __shared__ __align__(16) float sQ[STATE_ONLY ? 1 : C * QP];
@@ -27,23 +29,21 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
     __shared__ __align__(16) float sE[C], sD[C];
     __shared__ float sTot;
 
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, l16 = lane & 15, quad = lane >> 4;
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    int lane = t & 63, l16 = lane & 15, quad = lane >> 4;
     AttnPlace pl;
     if (!attn_place(A, STATE_ONLY, &pl)) return;
     const int head = pl.head;
     const int64_t row0 = pl.row0, len = pl.len;
     const int c0 = pl.blk * DVB;      // first column of the workgroup
-    const int wc = wave * 16 * NT;    // ... of the wave, within the workgroup's
+    const int wc = wave * 16;         // ... of the wave, within the workgroup's
     const int qh = head / A.rep;
 
-    // tile (m, n): rows 16 m + 4 quad + i, column col(l16, n); a lane's results of all n tiles are 4 NT neighbours
-    auto col = [&](int x, int n) { return wc + 4 * NT * (x >> 2) + 4 * n + (x & 3); };
-    f32x4 S[MT][NT];
-    auto scol = [&](int n) { return c0 + col(l16, n); };
-    load_state<MT, NT>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), scol, quad, S);
+    f32x4 S[MT];  // tile m: rows 16 m + 4 quad + i, column c0 + wc + l16
+    load_state<4, 16>(A, STATE_ONLY ? nullptr : attn_first_state(A, pl), c0 + wc + l16, quad, S);
 
-    constexpr int NQ = C * DKP / 4 / 256, NV = C * DVB / 4 / 256;  // 16-byte loads per thread
-    constexpr int RS = 256 / (DKP / 4), RSV = 256 / (DVB / 4);
+    constexpr int NQ = C * DKP / 4 / NTHR, NV = C * DVB / 4 / NTHR;  // 16-byte loads per thread
+    constexpr int RS = NTHR / (DKP / 4), RSV = NTHR / (DVB / 4);
     const int lr = t / (DKP / 4), lc = t % (DKP / 4) * 4, lrv = t / (DVB / 4), lcv = t % (DVB / 4) * 4;
     const float* gq = static_cast<const float*>(A.q) + row0 * A.q_row + qh * A.q_head;
     const float* gk = static_cast<const float*>(A.k) + row0 * A.k_row + qh * A.k_head;
@@ -51,8 +51,8 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
     const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
     const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
-    const uint32_t q_at = live > 0 ? (lr * q_row + lc) * 4 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 4 : OOB_OFF;
-    const uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 4 : OOB_OFF;
+    uint32_t q_at = live > 0 ? (lr * q_row + lc) * 4 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 4 : OOB_OFF;
+    uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 4 : OOB_OFF;
     u32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
     float rg = 0.0f;
     auto load = [&](int64_t c) {
@@ -68,13 +68,15 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
         for (int i = 0; i < NQ; ++i) rk[i] = load_row<float, VEC>(r, k_at + i * (RS * 4) * k_row, live);
 #pragma unroll
         for (int i = 0; i < NV; ++i) rv[i] = load_row<float, VEC>(rr, v_at + i * (RSV * 4) * v_row, live_v);
-        if (wave == 0) rg = gg && lane < n ? gg[(c + lane) * A.g_row] : 0.0f;
+        if (wave == WAVES - 1) rg = load_decay(A, gg, c, lane, n);
     };
 
     double whole = 0.0;
     if (len > 0) load(0);
     for (int64_t c = 0; c < len; c += C) {
         const int n = (int)min<int64_t>(C, len - c);
+        // what follows from these is cheaper computed again than kept in registers over the loop
+        asm volatile("" : "+v"(q_at), "+v"(k_at), "+v"(v_at), "+v"(l16), "+v"(quad), "+v"(lane));
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
@@ -82,15 +84,14 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
-        if (wave == 0) {
-            const double tot = chunk_decays(rg, sB, sD, sE, C);
+        if (wave == WAVES - 1) {
+            const double tot = chunk_decays(rg, lane, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);
             whole += tot;
         }
         __syncthreads();
-        if (c + C < len) load(c + C);
+        if (STATE_ONLY && c + C < len) load(c + C);
 
-        f32x4 O[2][NT];
         if constexpr (!STATE_ONLY) {
             // one 16x16 tile of scores per wave, transposed (a lane holds 4 neighbouring j of one i); the one above
             // the diagonal is never read
@@ -106,148 +107,123 @@ __global__ __launch_bounds__(256, 2) void attn_chunks_f32_kernel(AttnArgs A) {
                 }
                 const int i = 16 * it + l16;
                 const double bi = sB[i];
+                const int j = 16 * jt + 4 * quad;
+                const f64x2 b01 = *reinterpret_cast<const f64x2*>(&sB[j]), b23 = *reinterpret_cast<const f64x2*>(&sB[j + 2]);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const int j = 16 * jt + 4 * quad + u;
-                    const bool on = j <= i;
-                    const float f = __builtin_amdgcn_exp2f(on ? (float)(bi - sB[j]) : 0.0f);
-                    s[u] = (on ? s[u] : 0.0f) * f;
+                    const bool on = j + u <= i;
+                    const float f = (float)(bi - (u < 2 ? b01[u] : b23[u - 2]));
+                    s[u] = (on ? s[u] : 0.0f) * __builtin_amdgcn_exp2f(on ? f : 0.0f);
                 }
-                *reinterpret_cast<f32x4*>(&sP[i * PP + 16 * jt + 4 * quad]) = s;
+                *reinterpret_cast<f32x4*>(&sP[i * PP + j]) = s;
             }
         }
-        auto inter = [&] {  // exp(b_i) q_i S, transposed
-#pragma unroll
-            for (int it = 0; it < 2; ++it)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) O[it][nt] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int it = 0; it < 2; ++it) {
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(&sQ[(16 * it + l16) * QP + 16 * m + 4 * quad]);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) O[it][nt] = mfma_f32(S[m][nt][u], b[u], O[it][nt]);
-                }
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const float d = sD[16 * it + l16];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) O[it][nt] *= d;
-            }
-        };
-        if constexpr (!STATE_ONLY) {
-            inter();
-            __syncthreads();
-        }
-        float vf[2][4][NT];  // v of token 16 h + 4 quad + u
+        if constexpr (!STATE_ONLY) __syncthreads();
+        float vf[2][4];  // v of token 16 h + 4 quad + u
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) vf[h][u][nt] = sV[(16 * h + 4 * quad + u) * VP + col(l16, nt)];
+            for (int u = 0; u < 4; ++u) vf[h][u] = sV[(16 * h + 4 * quad + u) * VP + wc + l16];
         if constexpr (!STATE_ONLY) {
+            f32x4 O[2];  // transposed: rows are columns of v, columns the 16 tokens of a tile
+            // exp(b_i) q_i S
+#pragma unroll
+            for (int it = 0; it < 2; ++it) O[it] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                f32x4 b[2];
+#pragma unroll
+                for (int it = 0; it < 2; ++it)
+                    b[it] = *reinterpret_cast<const f32x4*>(&sQ[(16 * it + l16) * QP + 16 * m + 4 * quad]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int it = 0; it < 2; ++it) O[it] = mfma_f32(S[m][u], b[it][u], O[it]);
+            }
+#pragma unroll
+            for (int it = 0; it < 2; ++it) O[it] *= sD[16 * it + l16];
+            const f32x4 inter[2] = {O[0], O[1]};
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int it = h; it < 2; ++it) {
                     const f32x4 p = *reinterpret_cast<const f32x4*>(&sP[(16 * it + l16) * PP + 16 * h + 4 * quad]);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) O[it][nt] = mfma_f32(vf[h][u][nt], p[u], O[it][nt]);
+                    for (int u = 0; u < 4; ++u) O[it] = mfma_f32(vf[h][u], p[u], O[it]);
                 }
             // an infinite or NaN v of a later token has reached the first token of the 16: sum without the masked terms
             bool bad = false;
-            if (l16 == 0) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) bad |= !finite(O[0][nt][u]) || !finite(O[1][nt][u]);
-            }
-            if (__any(bad)) {
-                inter();
+            for (int u = 0; u < 4; ++u) bad = bad || !finite(O[0][u]) || !finite(O[1][u]);
+            if (__any(bad && l16 == 0)) {
 #pragma unroll
                 for (int it = 0; it < 2; ++it) {
                     const int i = 16 * it + l16;
+                    O[it] = inter[it];
                     for (int j = 0; j <= i; ++j) {
                         const float p = sP[i * PP + j];
-                        const float* v = &sV[j * VP + wc + 4 * NT * quad];
+                        const float* v = &sV[j * VP + wc + 4 * quad];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) O[it][nt][u] = fmaf(p, v[4 * nt + u], O[it][nt][u]);
+                        for (int u = 0; u < 4; ++u) O[it][u] = fmaf(p, v[u], O[it][u]);
                     }
                 }
             }
-            const int oc = c0 + wc + 4 * NT * quad;
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int i = 16 * it + l16;
-                if (i < n && oc < A.dv) {
-                    float e[4 * NT];
-#pragma unroll
-                    for (int x = 0; x < 4 * NT; ++x) e[x] = O[it][x / 4][x % 4];
-                    attn_store<4 * NT, VEC>(A, 1, row0 + c + i, head, oc, e);
-                }
-            }
+            // the next chunk's rows travel under the state's products (any earlier, and their registers would spill)
+            if (c + C < len) load(c + C);
+            attn_store<2, VEC>(A, 1, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         const float tot = sTot;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[m][nt] *= tot;
+        for (int m = 0; m < MT; ++m) S[m] *= tot;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 e = *reinterpret_cast<const f32x4*>(&sE[16 * h + 4 * quad]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 4; ++u) vf[h][u] *= e[u];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) vf[h][u][nt] *= e[u];
+            for (int m = 0; m < MT; m += 4)  // four tiles side by side: a product does not wait for the one before
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float k = sK[(16 * h + 4 * quad + u) * QP + 16 * m + l16];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) S[m][nt] = mfma_f32(k, vf[h][u][nt], S[m][nt]);
-                }
+                    for (int y = 0; y < 4; ++y)
+                        S[m + y] = mfma_f32(sK[(16 * h + 4 * quad + u) * QP + 16 * (m + y) + l16], vf[h][u], S[m + y]);
         }
         __syncthreads();
     }
 
     float* s_left = attn_last_state(A, pl, STATE_ONLY);
-    if (s_left) store_state<MT, NT>(A, s_left, scol, quad, S);
-    if (STATE_ONLY && pl.blk == 0 && t == 0) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
+    if (s_left) store_state<4, 16>(A, s_left, c0 + wc + l16, quad, S);
+    if (STATE_ONLY && pl.blk == 0 && t == NTHR - 1) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
 }
 
-template <int DKT, int NT>
+template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.segment ? a.nseg : a.sq.seqs) * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid((unsigned)blocks), block(64 * WAVES);
     if (state_only) {
         if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, true, true>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, WAVES, true, true>), grid, block, 0, s, a);
         else
-            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, true, false>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, WAVES, true, false>), grid, block, 0, s, a);
     } else {
         if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, false, true>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, WAVES, false, true>), grid, block, 0, s, a);
         else
-            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, NT, false, false>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((attn_chunks_f32_kernel<DKT, WAVES, false, false>), grid, block, 0, s, a);
     }
     return hipGetLastError();
 }
 
 hipError_t launch_attn_chunks_f32(const AttnArgs& a, bool state_only, hipStream_t s) {
-    if (a.dk > 128) return launch_one<4, 1>(a, state_only, s);
-    if (chunk_block(a.dk, a.dv) == 64)
-        return a.dk <= 64 ? launch_one<1, 1>(a, state_only, s) : launch_one<2, 1>(a, state_only, s);
-    return a.dk <= 64 ? launch_one<1, 2>(a, state_only, s) : launch_one<2, 2>(a, state_only, s);
+    const int dkt = a.dk <= 64 ? 1 : a.dk <= 128 ? 2 : 4;
+    if (chunk_block(a.dv) == 64)
+        return dkt == 1 ? launch_one<1, 4>(a, state_only, s)
+               : dkt == 2 ? launch_one<2, 4>(a, state_only, s)
+                          : launch_one<4, 4>(a, state_only, s);
+    return dkt == 1 ? launch_one<1, 8>(a, state_only, s)
+           : dkt == 2 ? launch_one<2, 8>(a, state_only, s)
+                      : launch_one<4, 8>(a, state_only, s);
 }
 
 }  // namespace cv

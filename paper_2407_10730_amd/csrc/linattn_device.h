@@ -5,6 +5,8 @@
 
 namespace cv {
 
+typedef double f64x2 __attribute__((ext_vector_type(2)));
+
 // What a workgroup of a chunk kernel runs: tokens [row0, row0 + len) for one head and block of columns.
 struct AttnPlace {
     int head, blk;
@@ -44,11 +46,16 @@ __device__ __forceinline__ float* attn_last_state(const AttnArgs& A, const AttnP
     return p.last && A.s_out ? A.s_out + (p.slot * A.heads + p.head) * size : nullptr;
 }
 
+// Log decay of the lane's token in a chunk of n tokens that starts at g; 0 past its end and without decays.
+__device__ __forceinline__ float load_decay(const AttnArgs& A, const float* g, int64_t c, int lane, int n) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(g + c * A.g_row, g ? OOB_OFF - 1 : 0u);
+    return ld_f32(r, lane < n ? (uint32_t)lane * (uint32_t)A.g_row * 4u : OOB_OFF);
+}
+
 // One wave: the decays of a chunk of up to 64 tokens (g of this lane's token, 0 past the chunk).  sB: running sums in
 // log2, in 64 bits, so that differences of sums stay exact after decays that clear the state; sD their
 // exponentials; sE the exponentials of what is left to the chunk's end.  Returns the whole chunk's.
-__device__ __forceinline__ double chunk_decays(float g, double* sB, float* sD, float* sE, int size) {
-    const int lane = threadIdx.x & 63;
+__device__ __forceinline__ double chunk_decays(float g, int lane, double* sB, float* sD, float* sE, int size) {
     double b = decay_log2(g);
     // inclusive scan by lane moves: 1, 2, 4 and 8 lanes up within rows of 16, then the rows' sums
 #define SCAN_STEP(ctrl, rows)                                                                            \
@@ -73,6 +80,10 @@ __device__ __forceinline__ double chunk_decays(float g, double* sB, float* sD, f
         sE[lane] = __builtin_amdgcn_exp2f((float)(tot - b));
     }
     return tot;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 // Rows of a chunk are loaded through range-checked buffers, which read zero outside their range: the range ends with
@@ -105,61 +116,66 @@ __device__ __forceinline__ u32x4 load_row(__amdgpu_buffer_rsrc_t r, uint32_t off
     }
 }
 
-// A state as MFMA results hold it: tile (m, n) has rows 16 m + 4 quad + i and column c(n).  Rows past dk lie past the
-// buffer's range.
-template <int MT, int NT, typename Col>
-__device__ __forceinline__ void load_state(const AttnArgs& A, const float* p, Col c, int quad, f32x4 (&S)[MT][NT]) {
+// Column c of a state as MFMA results hold it: tile m has rows QS quad + i from its first row on; odd tiles begin TS rows
+// after even ones, pairs 32 rows apart.  Rows past dk lie past the buffer's range.
+template <int QS, int TS, int MT>
+__device__ __forceinline__ void load_state(const AttnArgs& A, const float* p, int c, int quad, f32x4 (&S)[MT]) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, p ? (uint32_t)(A.dk * A.dv * 4) : 0u);
     const uint32_t row = (uint32_t)A.dv * 4;
+    const uint32_t at = c < A.dv ? QS * quad * row + c * 4 : OOB_OFF;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint32_t at = c(n) < A.dv ? 4 * quad * row + c(n) * 4 : OOB_OFF;
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) S[m][n][i] = ld_f32(r, at + (16 * m + i) * row);
-    }
+        for (int i = 0; i < 4; ++i) S[m][i] = ld_f32(r, at + (m / 2 * 32 + m % 2 * TS + i) * row);
 }
-template <int MT, int NT, typename Col>
-__device__ __forceinline__ void store_state(const AttnArgs& A, float* p, Col c, int quad, const f32x4 (&S)[MT][NT]) {
+template <int QS, int TS, int MT>
+__device__ __forceinline__ void store_state(const AttnArgs& A, float* p, int c, int quad, const f32x4 (&S)[MT]) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, (uint32_t)(A.dk * A.dv * 4));
     uint32_t row = (uint32_t)A.dv * 4;
     asm volatile("" : "+s"(row));  // or the addresses of the load would be kept in registers until here
+    const uint32_t at = c < A.dv ? QS * quad * row + c * 4 : OOB_OFF;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint32_t at = c(n) < A.dv ? 4 * quad * row + c(n) * 4 : OOB_OFF;
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st_f32(r, at + (16 * m + i) * row, S[m][n][i]);
-    }
+        for (int i = 0; i < 4; ++i) st_f32(r, at + (m / 2 * 32 + m % 2 * TS + i) * row, S[m][i]);
 }
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 
-// N results of one token, scaled and rounded, to columns c .. c + N - 1 (those at or past dv are none).
-template <int N, bool VEC>
-__device__ __forceinline__ void attn_store(const AttnArgs& A, int o_f32, int64_t row, int head, int c, float (&e)[N]) {
-    const int64_t at = row * A.o_row + head * A.o_head + c;
-#pragma unroll
-    for (int x = 0; x < N; ++x) e[x] *= A.scale;
+// Results of a chunk of n tokens that starts at token c of the segment, scaled and rounded: tile it holds tokens 16 it + l16,
+// columns col .. col + 3 (those at or past dv are none).
+template <int IT, bool VEC>
+__device__ __forceinline__ void attn_store(const AttnArgs& A, int o_f32, const AttnPlace& pl, int64_t c, int n, int col,
+                                           int l16, const f32x4 (&O)[IT]) {
+    const int64_t first = (pl.row0 + c) * A.o_row + pl.head * A.o_head;
+    const uint32_t row = (uint32_t)A.o_row, at = (uint32_t)l16 * row + col;
+    const int live = A.dv - col;
     if (o_f32) {
-        float* o = static_cast<float*>(A.o) + at;
-        if constexpr (VEC) {
-            store_pack<float, N>(o, e);
-        } else {
+        const __amdgpu_buffer_rsrc_t r = chunk_rsrc(static_cast<float*>(A.o) + first, n, row, A.dv);
 #pragma unroll
-            for (int x = 0; x < N; ++x)
-                if (c + x < A.dv) o[x] = e[x];
+        for (int it = 0; it < IT; ++it) {
+            const f32x4 v = O[it] * A.scale;
+            if constexpr (VEC) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r,
+                                                       live > 0 ? (at + it * 16 * row) * 4 : OOB_OFF, 0, 0);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) st_f32(r, x < live ? (at + it * 16 * row + x) * 4 : OOB_OFF, v[x]);
+            }
         }
     } else {
-        uint16_t* o = static_cast<uint16_t*>(A.o) + at;
-        if constexpr (VEC) {
-            store_pack<uint16_t, N>(o, e);
-        } else {
+        const __amdgpu_buffer_rsrc_t r = chunk_rsrc(static_cast<uint16_t*>(A.o) + first, n, row, A.dv);
 #pragma unroll
-            for (int x = 0; x < N; ++x)
-                if (c + x < A.dv) o[x] = from_f32<uint16_t>(e[x]);
+        for (int it = 0; it < IT; ++it) {
+            const f32x4 v = O[it] * A.scale;
+            const u32x2 w{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            if constexpr (VEC) {
+                __builtin_amdgcn_raw_buffer_store_b64(w, r, live > 0 ? (at + it * 16 * row) * 2 : OOB_OFF, 0, 0);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    st_u16(r, x < live ? (at + it * 16 * row + x) * 2 : OOB_OFF, (uint16_t)(w[x / 2] >> (16 * (x & 1))));
+            }
         }
     }
 }

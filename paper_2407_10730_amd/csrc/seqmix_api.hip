@@ -106,7 +106,7 @@ constexpr int64_t kTokensMost = 8;
 // The chunk kernels address the rows of a chunk by 32-bit byte offsets from its first: rows further apart go
 // token by token.
 bool chunk_rows_near(const seqmix_attn_params& p) {
-    return std::max({p.q_row, p.k_row, p.v_row}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
+    return std::max({p.q_row, p.k_row, p.v_row, p.o_row, (int64_t)p.heads}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
 }
 
 // Kernel, and where sequences are cut: about two workgroups per CU over all heads and column blocks, in segments of
@@ -117,7 +117,7 @@ void plan_attn(seqmix_attn_desc* d) {
     if (p.tokens <= kTokensMost * p.seqs || !chunk_rows_near(p)) return;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
     d->plan.chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
-    const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv));
+    const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dv) - 1) / chunk_block(p.dv));
     if (p.seqs * across >= 2 * kSeqmixCUs) return;
     int64_t seg = (p.tokens * across + 2 * kSeqmixCUs - 1) / (2 * kSeqmixCUs);
     seg = (std::max<int64_t>(seg, 128) + kChunk - 1) / kChunk * kChunk;
@@ -208,7 +208,7 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
         a.ndvb = (p.dv + kTokensBlock - 1) / kTokensBlock;
         return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     }
-    a.ndvb = (p.dv + chunk_block(p.dk, p.dv) - 1) / chunk_block(p.dk, p.dv);
+    a.ndvb = (p.dv + chunk_block(p.dv) - 1) / chunk_block(p.dv);
     auto chunks = [&](bool state_only) {
         return p.dtype == CONV2D_BF16 ? launch_attn_chunks_bf16(a, p.o_dtype, state_only, s)
                                       : launch_attn_chunks_f32(a, state_only, s);

@@ -51,7 +51,7 @@ hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s)
 // (all but the last of each sequence) into ws_state / ws_decay; launch_attn_join turns them into
 // the states that the segments start from, which the full pass reads.
 constexpr int kChunk = 64, kChunkF32 = 32;
-inline int chunk_block(int dk, int dv) { return dv <= 64 || dk > 128 ? 64 : 128; }
+inline int chunk_block(int dv) { return dv <= 64 ? 64 : 128; }
 hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s);
 hipError_t launch_attn_chunks_f32(const AttnArgs& a, bool state_only, hipStream_t s);
 hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s);
