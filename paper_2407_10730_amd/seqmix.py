@@ -142,8 +142,20 @@ def _pick(names, value, what):
         raise ValueError(f"{what} is one of {', '.join(names)}: got {value!r}") from None
 
 
+def _torch_hooks():
+    """torch's own checks and stream lookup without their Python wrappers, where this torch has them (a
+    call on a few tokens is bound by its host side)."""
+    import torch
+    try:
+        from torch._C._dynamo.guards import assert_size_stride
+    except ImportError:
+        assert_size_stride = None
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return assert_size_stride, raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 class _Operator:
-    """A descriptor, and what each tensor argument has to be: name -> (dtype, shape, strides)."""
+    """A descriptor, and what each tensor argument of a call has to be, in the order of the C call."""
 
     op = ""
 
@@ -154,7 +166,8 @@ class _Operator:
         self.params = params
         self.desc = _create(self.op, params)
         self._fwd = getattr(load(), f"seqmix_{self.op}_fwd")
-        self._want = {}
+        self._fits, self._raw_stream = _torch_hooks()
+        self._want = []
 
     def _expect(self, name, dtype, shape, strides=None):
         if strides is None:
@@ -162,33 +175,40 @@ class _Operator:
             for d in reversed(shape):
                 strides.insert(0, n)
                 n *= d
-        # an extent of one (or an empty tensor) leaves the strides open
-        fixed = 0 not in shape and tuple(i for i, d in enumerate(shape) if d > 1)
-        self._want[name] = (dtype, tuple(shape), tuple(strides), fixed)
+        self._want.append((dtype, tuple(shape), tuple(strides), name))
 
-    def _arg(self, t, name, dev):
-        """Device address of argument `name`; refuses a tensor that is not what the descriptor says."""
-        dtype, shape, strides, fixed = self._want[name]
+    def _refuse(self, t, want, dev):
+        """Raises unless the tensor fits after all (the strides of extents of one and of empty tensors are open)."""
+        dtype, shape, strides, name = want
+        who = f"{type(self).__name__}: {name}"
         if t.dtype is not dtype or t.shape != shape:
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{type(self).__name__}: {name} is {tuple(t.shape)} {t.dtype}, "
-                                                  f"not {shape} {dtype}")
-        have = t.stride()
-        if have != strides and fixed is not False and any(have[i] != strides[i] for i in fixed):
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{type(self).__name__}: {name} has strides {have}, not {strides}")
-        if t.get_device() != dev or dev < 0:
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{type(self).__name__}: {name} is on {t.device}: all arguments are "
-                                                  "on one GPU")
-        return t.data_ptr()
+            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}")
+        if 0 not in shape and any(d > 1 and a != b for d, a, b in zip(shape, t.stride(), strides)):
+            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} has strides {t.stride()}, not {strides}")
+        if dev < 0 or t.get_device() != dev:
+            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} is on {t.device}: all arguments are on one GPU")
 
-    def _launch(self, dev, stream, *args):
-        torch = self._torch
-        if stream is None:
-            stream = torch.cuda.current_stream(dev)
-        if dev == torch.cuda.current_device():
-            st = self._fwd(self.desc, *args, _stream(stream))
+    def _launch(self, dev, stream, tensors):
+        """Checks the tensors (None: not given) and calls the library with their addresses."""
+        args, fits = [self.desc], self._fits
+        for t, want in zip(tensors, self._want):
+            if t is None:
+                args.append(None)
+                continue
+            if fits is None or dev < 0 or t.dtype is not want[0] or t.get_device() != dev:
+                self._refuse(t, want, dev)
+            else:
+                try:
+                    fits(t, want[1], want[2])
+                except AssertionError:
+                    self._refuse(t, want, dev)
+            args.append(t.data_ptr())
+        args.append(self._raw_stream(dev) if stream is None else _stream(stream))
+        if dev == self._torch.cuda.current_device():
+            st = self._fwd(*args)
         else:
-            with torch.cuda.device(dev):
-                st = self._fwd(self.desc, *args, _stream(stream))
+            with self._torch.cuda.device(dev):
+                st = self._fwd(*args)
         if st:
             raise Conv2dError(st, f"seqmix_{self.op}_fwd")
 
@@ -229,22 +249,17 @@ class LinearAttention(_Operator):
             decay=kind, scale=scale, **{f"{n}_{d}": s[i] for n, s in strides.items() for i, d in
                                         enumerate(("row", "head"))}))
         td, torch = self._td, self._torch
-        for n, h, d in (("q", qk_heads, dk), ("k", qk_heads, dk), ("v", heads, dv), ("o", heads, dv)):
-            self._expect(n, td[odt if n == "o" else dt], (tokens, h, d), (*strides[n], 1))
+        for n, h, d in (("q", qk_heads, dk), ("k", qk_heads, dk), ("v", heads, dv)):
+            self._expect(n, td[dt], (tokens, h, d), (*strides[n], 1))
         self._expect("decay", torch.float32, (tokens, heads) if decay == "token" else (heads,))
-        self._expect("state", torch.float32, (slots, heads, dk, dv))
         self._expect("offsets", torch.int64, (seqs + 1,))
         self._expect("slot_index", torch.int32, (seqs,))
+        self._expect("state_in", torch.float32, (slots, heads, dk, dv))
+        self._expect("state_out", torch.float32, (slots, heads, dk, dv))
+        self._expect("o", td[odt], (tokens, heads, dv), (*strides["o"], 1))
 
     def run(self, q, k, v, decay, state_in, state_out, o, offsets=None, slot_index=None, stream=None):
-        dev = o.get_device()
-        arg = self._arg
-        self._launch(dev, stream, arg(q, "q", dev), arg(k, "k", dev), arg(v, "v", dev),
-                     None if decay is None else arg(decay, "decay", dev),
-                     None if offsets is None else arg(offsets, "offsets", dev),
-                     None if slot_index is None else arg(slot_index, "slot_index", dev),
-                     None if state_in is None else arg(state_in, "state", dev),
-                     None if state_out is None else arg(state_out, "state", dev), arg(o, "o", dev))
+        self._launch(o.get_device(), stream, (q, k, v, decay, offsets, slot_index, state_in, state_out, o))
 
     def plan(self):
         return seqmix_attn_plan_query(self.desc)
@@ -272,21 +287,16 @@ class TokenConv(_Operator):
             x_row=x_row, y_row=y_row))
         td, torch = self._td[dt], self._torch
         self._expect("x", td, (tokens, channels), (x_row, 1))
-        self._expect("y", td, (tokens, channels), (y_row, 1))
         self._expect("w", td, (channels, width))
         self._expect("bias", torch.float32, (channels,))
-        self._expect("window", td, (slots, width - 1, channels))
         self._expect("offsets", torch.int64, (seqs + 1,))
         self._expect("slot_index", torch.int32, (seqs,))
+        self._expect("window_in", td, (slots, width - 1, channels))
+        self._expect("window_out", td, (slots, width - 1, channels))
+        self._expect("y", td, (tokens, channels), (y_row, 1))
 
     def run(self, x, w, bias, window_in, window_out, y, offsets=None, slot_index=None, stream=None):
-        dev = y.get_device()
-        arg = self._arg
-        self._launch(dev, stream, arg(x, "x", dev), arg(w, "w", dev), None if bias is None else arg(bias, "bias", dev),
-                     None if offsets is None else arg(offsets, "offsets", dev),
-                     None if slot_index is None else arg(slot_index, "slot_index", dev),
-                     None if window_in is None else arg(window_in, "window", dev),
-                     None if window_out is None else arg(window_out, "window", dev), arg(y, "y", dev))
+        self._launch(y.get_device(), stream, (x, w, bias, offsets, slot_index, window_in, window_out, y))
 
 
 class GateNorm(_Operator):
@@ -315,24 +325,15 @@ class GateNorm(_Operator):
             pre_eps=eps if pre_eps is None else pre_eps, **row))
         td, torch = self._td, self._torch
         self._expect("u", td[dt], (rows, width), (row["u_row"], 1))
-        self._expect("h", td[dt], (rows, width), (row["h_row"], 1))
+        self._expect("post_w", torch.float32, (group,))
+        self._expect("post_b", torch.float32, (group,))
         self._expect("gate", td[dt], (-(-rows // gate_run), width), (row["gate_row"], 1))
         self._expect("residual", td[rdt], (rows, width), (row["res_row"], 1))
-        self._expect("y", td[rdt], (rows, width), (row["y_row"], 1))
-        for n in ("post_w", "post_b"):
-            self._expect(n, torch.float32, (group,))
         for n in ("scale_vec", "pre_w", "pre_b"):
             self._expect(n, torch.float32, (width,))
+        self._expect("y", td[rdt], (rows, width), (row["y_row"], 1))
+        self._expect("h", td[dt], (rows, width), (row["h_row"], 1))
 
     def run(self, u, post_w=None, post_b=None, gate=None, residual=None, scale_vec=None, pre_w=None, pre_b=None,
             y=None, h=None, stream=None):
-        dev = u.get_device()
-        arg = self._arg
-        self._launch(dev, stream, arg(u, "u", dev), None if post_w is None else arg(post_w, "post_w", dev),
-                     None if post_b is None else arg(post_b, "post_b", dev),
-                     None if gate is None else arg(gate, "gate", dev),
-                     None if residual is None else arg(residual, "residual", dev),
-                     None if scale_vec is None else arg(scale_vec, "scale_vec", dev),
-                     None if pre_w is None else arg(pre_w, "pre_w", dev),
-                     None if pre_b is None else arg(pre_b, "pre_b", dev), None if y is None else arg(y, "y", dev),
-                     None if h is None else arg(h, "h", dev))
+        self._launch(u.get_device(), stream, (u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h))
