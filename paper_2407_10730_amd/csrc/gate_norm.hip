@@ -13,8 +13,7 @@ namespace cv {
 // Sum over the TPR threads of a group; `red` (one float per wave) is used when a group spans waves.
 template <int TPR>
 __device__ __forceinline__ float group_sum(float v, float* red) {
-#pragma unroll
-    for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1) v += __shfl_xor(v, m);
+    v = lanes_sum<(TPR < 64 ? TPR : 64)>(v);
     if constexpr (TPR > 64) {
         __syncthreads();  // the previous sum has been read
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
@@ -26,10 +25,35 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
     return v;
 }
 
+// fp32 values [width] that a thread needs at its places.  EARLY loads them before the reductions that they wait for.
+template <int TPR, int V, int ITEMS, bool EARLY>
+struct Vec {
+    static constexpr bool kEarly = EARLY;
+    const float* p;
+    float e[kEarly ? ITEMS : 1][V];
+    __device__ __forceinline__ Vec(const float* q, int n) : p(q) {
+        if constexpr (kEarly) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = (i * TPR + threadIdx.x % TPR) * V;
+                if (p && c < n) load_pack<float, V>(p + c, e[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void get(int i, int c, float (&out)[V]) const {
+        if constexpr (kEarly) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) out[v] = e[i][v];
+        } else {
+            load_pack<float, V>(p + c, out);
+        }
+    }
+};
+
 // Norms x in place: V * ITEMS values per thread, those at or past `n` being zero.
-template <int TPR, int V, int ITEMS>
-__device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, float eps, const float* w, const float* b,
-                                              int n, float* red) {
+template <int TPR, int V, int ITEMS, bool EARLY>
+__device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, float eps, const Vec<TPR, V, ITEMS, EARLY>& w,
+                                              const Vec<TPR, V, ITEMS, EARLY>& b, int n, float* red) {
     const int t = threadIdx.x % TPR;
     const float inv = 1.0f / (float)n;
     if (kind == SEQMIX_NORM_LAYER) {
@@ -55,11 +79,11 @@ __device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, fl
         const int c = (i * TPR + t) * V;
         if (c < n) {
             float e[V];
-            load_pack<float, V>(w + c, e);
+            w.get(i, c, e);
 #pragma unroll
             for (int v = 0; v < V; ++v) x[i][v] *= r * e[v];
-            if (b) {
-                load_pack<float, V>(b + c, e);
+            if (b.p) {
+                b.get(i, c, e);
 #pragma unroll
                 for (int v = 0; v < V; ++v) x[i][v] += e[v];
             }
@@ -67,7 +91,7 @@ __device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, fl
     }
 }
 
-template <typename T, typename TR, int TPR, int V, int ITEMS>
+template <typename T, typename TR, int TPR, int V, int ITEMS, bool EARLY>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormArgs A) {
     constexpr int NT = TPR < 256 ? 256 : TPR;
     __shared__ float red[NT / 64];
@@ -96,6 +120,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
             if (A.res) res[i] = *reinterpret_cast<const Pack<TR, V>*>(rp + c);
         }
     }
+    const Vec<TPR, V, ITEMS, EARLY> post_w(A.post_w, n), post_b(A.post_b, n), scale_vec(A.scale_vec ? A.scale_vec + col : nullptr, n),
+        pre_w(A.pre_w, n), pre_b(A.pre_b, n);
     auto apply_gate = [&] {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -110,7 +136,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
             }
     };
     if (A.gate && A.gate_first) apply_gate();
-    if (A.post != SEQMIX_NORM_NONE) norm_in_place<TPR, V, ITEMS>(x, A.post, A.post_eps, A.post_w, A.post_b, n, red);
+    if (A.post != SEQMIX_NORM_NONE) norm_in_place<TPR, V, ITEMS, EARLY>(x, A.post, A.post_eps, post_w, post_b, n, red);
     if (A.gate && !A.gate_first) apply_gate();
 
     TR* yp = static_cast<TR*>(A.y) + (A.y ? row * A.y_row + col : 0);
@@ -121,7 +147,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
             float e[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) e[v] = 1.0f;
-            if (A.scale_vec) load_pack<float, V>(A.scale_vec + col + c, e);
+            if (scale_vec.p) scale_vec.get(i, c, e);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 x[i][v] *= A.scale * e[v];
@@ -131,7 +157,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
         }
     }
     if (A.pre == SEQMIX_NORM_NONE) return;
-    norm_in_place<TPR, V, ITEMS>(x, A.pre, A.pre_eps, A.pre_w, A.pre_b, n, red);
+    norm_in_place<TPR, V, ITEMS, EARLY>(x, A.pre, A.pre_eps, pre_w, pre_b, n, red);
     T* hp = static_cast<T*>(A.h) + row * A.h_row + col;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
@@ -145,20 +171,26 @@ static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
     constexpr int NT = TPR < 256 ? 256 : TPR;
     const int64_t blocks = (a.rows + NT / TPR - 1) / (NT / TPR);
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
+    // With fewer than two blocks per CU the time is one block's chain of loads: weights early take one wait out of it (13 rows of
+    // 1537 fp32 6.5 -> 5.1 us).  With many, their registers cost waves (8192 x 2048 bf16 by heads of 128: 26 us, late 23.5).
+    if (ITEMS * V <= 8 && blocks < 2 * kSeqmixCUs)
+        hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS, (ITEMS * V <= 8)>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
+    else
+        hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS, false>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
 
-// V values per access.  Groups up to 16 accesses: a quarter wave each; up to 64: a wave; up to 1024: a block of 256
-// with 1 to 4 accesses per thread; above (16384 elements by one element each): 1024 threads.
+// V values per access.  Groups up to 16 accesses: 16 lanes each; up to 64: a wave; above, a block of 256 to 1024 threads with as
+// few accesses per thread as that allows, up to 4 (16384 elements by one element each: 16).
 template <typename T, typename TR, int V>
 static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
     const int64_t packs = (a.group + V - 1) / V;
     if (packs <= 16) return launch_one<T, TR, 16, V, 1>(a, s);
     if (packs <= 64) return launch_one<T, TR, 64, V, 1>(a, s);
     if (packs <= 256) return launch_one<T, TR, 256, V, 1>(a, s);
-    if (packs <= 512) return launch_one<T, TR, 256, V, 2>(a, s);
-    if (packs <= 1024) return launch_one<T, TR, 256, V, 4>(a, s);
+    if (packs <= 512) return launch_one<T, TR, 512, V, 1>(a, s);
+    if (packs <= 1024) return launch_one<T, TR, 1024, V, 1>(a, s);
+    if (packs <= 2048) return launch_one<T, TR, 1024, V, 2>(a, s);
     if (packs <= 4096) return launch_one<T, TR, 1024, V, 4>(a, s);
     if constexpr (V == 1) return launch_one<T, TR, 1024, V, 16>(a, s);
     return hipErrorInvalidValue;

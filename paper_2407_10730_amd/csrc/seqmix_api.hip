@@ -267,7 +267,7 @@ int seqmix_conv_fwd(const seqmix_conv_desc* d, const void* x, const void* w, con
     a.silu = p.act == SEQMIX_ACT_SILU;
     const int64_t unit = 16 / esize(p.dtype);
     a.vec = p.channels % unit == 0 && p.x_row % unit == 0 && p.y_row % unit == 0 && aligned(x, 16) && aligned(y, 16) &&
-            aligned(a.win_in, 16) && aligned(a.win_out, 16);
+            aligned(w, 16) && aligned(a.bias, 16) && aligned(a.win_in, 16) && aligned(a.win_out, 16);
     return launch_token_conv(a, p.dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
 

@@ -20,9 +20,9 @@ __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) {  // the hardwa
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// N consecutive elements as they lie in memory, `Bytes` of them moved per access.
+// N consecutive elements as they lie in memory, aligned to the largest power of two (16 at most) that divides their size.
 template <typename T, int N>
-struct alignas(sizeof(T) * N <= 16 ? sizeof(T) * N : 16) Pack {
+struct alignas((sizeof(T) * N & -(sizeof(T) * N)) < 16 ? (sizeof(T) * N & -(sizeof(T) * N)) : 16) Pack {
     T e[N];
 };
 template <typename T, int N>
@@ -73,14 +73,18 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint3
         const uint32_t i = id / per;
         return {(int)i, (int)(id - i * per)};
     }
-    int lo = 0, hi = a.seqs - 1;  // the last sequence whose first id is at most `id`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (clamp_row(a.off[mid], a.tokens) / size + mid <= id)
-            lo = mid;
-        else
-            hi = mid - 1;
+    // the last sequence whose first id is at most `id`: a wave's lanes look at 64 of them at a time, so that the
+    // search waits for memory once up to 64 sequences and twice up to 4096 (all lanes of the wave take part)
+    int lo = 0;
+    const int lane = threadIdx.x & 63;
+    for (int n = a.seqs; n > 1;) {
+        const int step = (n + 63) / 64, i = lane * step;
+        const bool at_most = i < n && clamp_row(a.off[lo + i], a.tokens) / size + (lo + i) <= id;
+        const int k = max(__popcll(__ballot(at_most)) - 1, 0);
+        lo += k * step;
+        n = min(step, n - k * step);
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);
     return {lo, (int)id - (int)(clamp_row(a.off[lo], a.tokens) / size + lo)};
 }
 
@@ -88,6 +92,22 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint3
 // exponential of exactly zero in fp32 anyway; the bound keeps differences of sums finite.  NaN stays.
 __device__ __forceinline__ double decay_log2(float g) {
     return (double)(g < -1000.0f ? -1000.0f : g) * 1.4426950408889634;
+}
+
+// Sum over groups of N lanes (16 or 64), in every lane.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
+#define ROTATE_ADD(n) v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + n, 0xf, 0xf, false))
+    ROTATE_ADD(8);
+    ROTATE_ADD(4);
+    ROTATE_ADD(2);
+    ROTATE_ADD(1);
+#undef ROTATE_ADD
+    if constexpr (N == 16) return v;
+    auto row = [&](int lane) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    };
+    return (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // 1 / (1 + exp(-x)) on the hardware's exponential and reciprocal (each within 1 ulp of fp32).

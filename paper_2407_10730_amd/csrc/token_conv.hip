@@ -11,14 +11,15 @@
 
 namespace cv {
 
-constexpr int kConvTile = 32;  // tokens per tile: at width 4 the rows loaded twice are under a tenth
+// Tokens per tile: at width 4 the rows loaded twice are under a tenth of 32; with fewer than two workgroups per CU of
+// those, tiles of 8 (shorter chains of loads).  8192 x 4096 bf16: 32 as good as 64, 16 a tenth slower.
+constexpr int kConvTile = 32, kConvTileFew = 8, kConvAhead = 8;
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
-    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
-    if (c >= A.channels) return;
     const SeqPart sp = seq_part(A.sq, blockIdx.y + blockIdx.z * 65535u, tile);
-    if (sp.seq >= A.sq.seqs) return;
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
+    if (c >= A.channels || sp.seq >= A.sq.seqs) return;
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t t0 = (int64_t)sp.part * tile;
     if (sp.part < 0 || (sp.part > 0 && t0 >= r.len)) return;
@@ -28,12 +29,23 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
     const T* __restrict__ x = static_cast<const T*>(A.x) + (r.first + t0) * A.x_row + c;
     T* __restrict__ y = static_cast<T*>(A.y) + (r.first + t0) * A.y_row + c;
 
-    float w[V][W], bias[V];
+    // the first rows are on their way while weights and window arrive
+    Pack<T, V> next[kConvAhead];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
+    for (int u = 0; u < kConvAhead; ++u)
+        if (u < n) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)u * A.x_row);
+    float w[V * W], bias[V];
+    if constexpr (V > 1) {
+        load_pack<T, V * W>(static_cast<const T*>(A.w) + (int64_t)c * W, w);
+    } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[v][i] = to_f32(static_cast<const T*>(A.w)[(int64_t)(c + v) * W + i]);
-        bias[v] = A.bias ? A.bias[c + v] : 0.0f;
+        for (int i = 0; i < W; ++i) w[i] = to_f32(static_cast<const T*>(A.w)[(int64_t)c * W + i]);
+    }
+    if (A.bias) {
+        load_pack<float, V>(A.bias + c, bias);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) bias[v] = 0.0f;
     }
     float row[W][V];  // row[i]: x of tap i
     if constexpr (W > 1) {
@@ -70,33 +82,44 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
             }
         }
     }
-#pragma unroll 4
-    for (int t = 0; t < n; ++t) {
-        load_pack<T, V>(x + (int64_t)t * A.x_row, row[W - 1]);
-        float o[V];
+    for (int t = 0; t < n; t += kConvAhead) {
+        Pack<T, V> now[kConvAhead];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            o[v] = bias[v];
-#pragma unroll
-            for (int i = 0; i < W; ++i) o[v] = fmaf(w[v][i], row[i][v], o[v]);
-            if (A.silu) o[v] = silu(o[v]);
+        for (int u = 0; u < kConvAhead; ++u) {
+            now[u] = next[u];
+            if (t + kConvAhead + u < n)
+                next[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)(t + kConvAhead + u) * A.x_row);
         }
-        store_pack<T, V>(y + (int64_t)t * A.y_row, o);
 #pragma unroll
-        for (int i = 0; i + 1 < W; ++i)
+        for (int u = 0; u < kConvAhead; ++u) {
+            if (t + u < n) {
+                float o[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) row[i][v] = row[i + 1][v];
+                for (int v = 0; v < V; ++v) {
+                    row[W - 1][v] = to_f32(now[u].e[v]);
+                    o[v] = bias[v];
+#pragma unroll
+                    for (int i = 0; i < W; ++i) o[v] = fmaf(w[v * W + i], row[i][v], o[v]);
+                    if (A.silu) o[v] = silu(o[v]);
+                }
+                store_pack<T, V>(y + (int64_t)(t + u) * A.y_row, o);
+#pragma unroll
+                for (int i = 0; i + 1 < W; ++i)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) row[i][v] = row[i + 1][v];
+            }
+        }
     }
 }
 
 template <typename T, int V>
 static hipError_t launch_conv_w(const ConvArgs& a, hipStream_t s) {
-    const int tile = kConvTile;
+    const int64_t across = (a.channels + 256 * V - 1) / (256 * V);
+    const int tile = a.sq.tokens / kConvTile * across < 2 * kSeqmixCUs ? kConvTileFew : kConvTile;
     const int64_t ids = seq_part_ids(a.sq, tile);
     const int64_t gz = (ids + 65534) / 65535;
     if (gz > 65535) return hipErrorInvalidValue;
-    const int64_t per = (a.channels + V - 1) / V;
-    const dim3 grid((unsigned)((per + 255) / 256), (unsigned)(gz > 1 ? 65535 : ids), (unsigned)gz);
+    const dim3 grid((unsigned)across, (unsigned)(gz > 1 ? 65535 : ids), (unsigned)gz);
     switch (a.width) {
 #define CASE(W)                                                                            \
     case W:                                                                                \

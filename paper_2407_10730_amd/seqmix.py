@@ -149,7 +149,8 @@ def _torch_hooks():
     try:
         from torch._C._dynamo.guards import assert_size_stride
     except ImportError:
-        assert_size_stride = None
+        def assert_size_stride(t, shape, strides):
+            assert t.shape == shape and t.stride() == strides
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return assert_size_stride, raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
@@ -191,18 +192,18 @@ class _Operator:
     def _launch(self, dev, stream, tensors):
         """Checks the tensors (None: not given) and calls the library with their addresses."""
         args, fits = [self.desc], self._fits
-        for t, want in zip(tensors, self._want):
+        add = args.append
+        for t, (dtype, shape, strides, _) in zip(tensors, self._want):
             if t is None:
-                args.append(None)
+                add(None)
                 continue
-            if fits is None or dev < 0 or t.dtype is not want[0] or t.get_device() != dev:
-                self._refuse(t, want, dev)
-            else:
-                try:
-                    fits(t, want[1], want[2])
-                except AssertionError:
-                    self._refuse(t, want, dev)
-            args.append(t.data_ptr())
+            try:
+                fits(t, shape, strides)
+                if t.dtype is not dtype or t.get_device() != dev or dev < 0:
+                    raise AssertionError
+            except AssertionError:
+                self._refuse(t, self._want[len(args) - 1], dev)
+            add(t.data_ptr())
         args.append(self._raw_stream(dev) if stream is None else _stream(stream))
         if dev == self._torch.cuda.current_device():
             st = self._fwd(*args)
