@@ -149,12 +149,13 @@ hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s)
 }
 
 // Joins the segments of each sequence: ws_state holds the state that each segment but the last adds from
-// zero; afterwards it holds the state that each segment starts from.  One thread owns one element of a state (more per
-// thread left too few threads to cover the latency) and walks along the segments, 8 loads ahead of the sum.
+// zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring elements of a state and
+// walks along the segments, AHEAD loads ahead of the sum.  Bound by its bytes, 8 dk dv per segment and head.
+template <int V>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
     constexpr int AHEAD = 8;
     const int64_t size = (int64_t)A.dk * A.dv;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
     if (e >= size) return;
     const int head = blockIdx.y;
     const int seq = blockIdx.z;
@@ -164,38 +165,42 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
     const uint32_t seg = (uint32_t)A.segment;
     const uint32_t len = (uint32_t)r.len, own = len > seg ? (len + seg - 1) / seg : 1;
     const int64_t first = A.sq.off ? (uint32_t)r.first / seg + seq : (int64_t)seq * own;
-    const int64_t parts = min<int64_t>(own, A.nseg - first);  // (offsets that lie)
-    float S = A.s_in ? A.s_in[(slot * A.heads + head) * size + e] : 0.0f;
+    const int parts = (int)min<int64_t>(own, A.nseg - first);  // (offsets that lie)
+    float S[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) S[v] = 0.0f;
+    if (A.s_in) load_pack<float, V>(A.s_in + (slot * A.heads + head) * size + e, S);
     const int64_t pitch = (int64_t)A.heads * size;
     float* ws = A.ws_state + (first * A.heads + head) * size + e;
     const float* wd = A.ws_decay + first * A.heads + head;
-    int64_t p = 0;
-    for (; p + AHEAD < parts; p += AHEAD) {
-        float add[AHEAD], d[AHEAD];
+    for (int p = 0; p < parts; p += AHEAD) {
+        float add[AHEAD][V], d[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            add[u] = ws[(p + u) * pitch];
-            d[u] = wd[(p + u) * A.heads];
+        for (int u = 0; u < AHEAD; ++u) {  // (past the last that counts: that one again)
+            const int from = max(min(p + u, parts - 2), 0);
+            load_pack<float, V>(ws + from * pitch, add[u]);
+            d[u] = wd[(int64_t)from * A.heads];
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            ws[(p + u) * pitch] = S;
-            S = fmaf(__builtin_amdgcn_exp2f(d[u]), S, add[u]);
-        }
-    }
-    for (; p < parts; ++p) {
-        const bool more = p + 1 < parts;
-        const float add = more ? ws[p * pitch] : 0.0f, d = more ? wd[p * A.heads] : 0.0f;
-        ws[p * pitch] = S;
-        S = fmaf(__builtin_amdgcn_exp2f(d), S, add);
+        for (int u = 0; u < AHEAD; ++u)
+            if (p + u < parts) {
+                store_pack<float, V>(ws + (p + u) * pitch, S);
+                const float f = __builtin_amdgcn_exp2f(d[u]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) S[v] = fmaf(f, S[v], add[u][v]);
+            }
     }
 }
 
 hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s) {
     const int64_t size = (int64_t)a.dk * a.dv;
+    const int V = a.svec ? 4 : 1;
     if (a.sq.seqs > 65535 || a.heads > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((size + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
-    hipLaunchKernelGGL(attn_join_kernel, grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((size / V + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
+    if (V == 4)
+        hipLaunchKernelGGL((attn_join_kernel<4>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<1>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

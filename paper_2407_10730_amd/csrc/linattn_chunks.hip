@@ -299,7 +299,7 @@ static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStr
 
 hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
     const int dkt = a.dk <= 64 ? 2 : a.dk <= 128 ? 4 : 8;
-    if (chunk_block(a.dv) == 64)
+    if (a.block == 64)
         return dkt == 2 ? launch_one<2, 4>(a, odt, state_only, s)
                : dkt == 4 ? launch_one<4, 4>(a, odt, state_only, s)
                           : launch_one<8, 4>(a, odt, state_only, s);

@@ -217,7 +217,7 @@ static hipError_t launch_one(const AttnArgs& a, bool state_only, hipStream_t s) 
 
 hipError_t launch_attn_chunks_f32(const AttnArgs& a, bool state_only, hipStream_t s) {
     const int dkt = a.dk <= 64 ? 1 : a.dk <= 128 ? 2 : 4;
-    if (chunk_block(a.dv) == 64)
+    if (a.block == 64)
         return dkt == 1 ? launch_one<1, 4>(a, state_only, s)
                : dkt == 2 ? launch_one<2, 4>(a, state_only, s)
                           : launch_one<4, 4>(a, state_only, s);

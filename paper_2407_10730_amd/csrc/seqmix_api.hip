@@ -9,6 +9,7 @@ using namespace cv;
 struct seqmix_attn_desc {
     seqmix_attn_params p;
     seqmix_attn_plan_info plan;
+    int32_t block = 0;  // state columns per workgroup
     // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
     void* ws = nullptr;
     int device = -1;
@@ -109,23 +110,43 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
     return std::max({p.q_row, p.k_row, p.v_row, p.o_row, (int64_t)p.heads}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
 }
 
-// Kernel, and where sequences are cut: about two workgroups per CU over all heads and column blocks, in segments of
-// at least 128 tokens (below that the segments' states cost more than their tokens).
+// Kernel, state columns per workgroup (block) and where sequences are cut.
+//
+// A workgroup takes its chunks one after the other, about 5 us each (dk = dv = 128) with one workgroup per CU and 8 with two.
+// Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the segments are as
+// long as 256 workgroups allow, or 512 where those still have 8 chunks each: 8192 tokens, 16 heads of 128 x 128 bf16:
+// 71 us in segments of 512, 75 of 256, 78 of 384 (a part of the CUs has two), 110 of 1024; 65536 tokens, 8 heads: 227 us
+// in segments of 1024, 237 of 2048, 242 of 512.  Packed sequences of unknown lengths take 512 (5664 tokens in 10 sequences, 12
+// heads of 64 x 128: 41 us in segments of 192, 45 of 256, 50 of 512).
+// Sequences of up to 5 chunks are not cut (100 tokens: 7.6 us, cut 13.6; 300: 17.4 either way).
+// Where 128-column blocks leave half of the CUs empty, blocks of 64 (1024 tokens, 8 heads: 19.7 us, 21.4; 300 tokens:
+// 17.3, 21.8).
 void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
+    d->block = kTokensBlock;
     if (p.tokens <= kTokensMost * p.seqs || !chunk_rows_near(p)) return;
+    const int64_t chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
-    d->plan.chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
-    const int64_t across = (int64_t)p.heads * ((p.dv + chunk_block(p.dv) - 1) / chunk_block(p.dv));
-    if (p.seqs * across >= 2 * kSeqmixCUs) return;
-    int64_t seg = (p.tokens * across + 2 * kSeqmixCUs - 1) / (2 * kSeqmixCUs);
-    seg = (std::max<int64_t>(seg, 128) + kChunk - 1) / kChunk * kChunk;
-    if (seg >= p.tokens) return;
-    const int64_t ids = p.tokens / seg + p.seqs;
-    const int64_t state = (int64_t)p.dk * p.dv * 4;
-    d->plan.segment = seg;
-    d->plan.workspace_bytes = ids * p.heads * (state + 4);
+    d->plan.chunk = (int32_t)chunk;
+    const int64_t wide = p.dv <= 64 ? 64 : 128;
+    const int64_t across = p.heads * ((p.dv + wide - 1) / wide);
+    int64_t groups = p.seqs * across;  // workgroups
+    if (p.tokens > 5 * chunk * p.seqs && groups < 2 * kSeqmixCUs) {
+        auto length = [&](int64_t want) {  // of segments, such that there are about `want` workgroups
+            const int64_t parts = std::max<int64_t>(want / across - (p.seqs > 1 ? p.seqs : 0), 1);
+            return ((p.tokens + parts - 1) / parts + kChunk - 1) / kChunk * kChunk;
+        };
+        int64_t seg = length(2 * kSeqmixCUs);
+        if (p.seqs == 1 && seg < 8 * chunk) seg = length(kSeqmixCUs);
+        const int64_t ids = p.tokens / seg + p.seqs;
+        if (seg < p.tokens) {
+            d->plan.segment = seg;
+            d->plan.workspace_bytes = ids * p.heads * ((int64_t)p.dk * p.dv * 4 + 4);
+            groups = (p.seqs == 1 ? (p.tokens + seg - 1) / seg : ids) * across;
+        }
+    }
+    d->block = (int32_t)(groups * 2 <= kSeqmixCUs ? 64 : wide);
 }
 
 }  // namespace
@@ -204,16 +225,18 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
             p.k_head % unit == 0 && p.v_row % unit == 0 && p.v_head % unit == 0 && p.o_row % unit == 0 &&
             p.o_head % unit == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(o, 16);
     a.svec = p.dv % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
+    a.block = d->block;
+    a.ndvb = (p.dv + d->block - 1) / d->block;
     if (d->plan.kernel == SEQMIX_KERNEL_TOKENS) {
-        a.ndvb = (p.dv + kTokensBlock - 1) / kTokensBlock;
         return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     }
-    a.ndvb = (p.dv + chunk_block(p.dv) - 1) / chunk_block(p.dv);
     auto chunks = [&](bool state_only) {
         return p.dtype == CONV2D_BF16 ? launch_attn_chunks_bf16(a, p.o_dtype, state_only, s)
                                       : launch_attn_chunks_f32(a, state_only, s);
     };
-    if (d->plan.segment == 0 || (!offsets && a.sq.seq_len <= d->plan.segment))  // no sequence is cut
+    // sequences of known length are cut where that shortens the chain of their chunks by more than it costs
+    if (d->plan.segment == 0 ||
+        (!offsets && (a.sq.seq_len <= d->plan.segment || 2 * a.sq.seq_len <= 3 * d->plan.segment + 10 * d->plan.chunk)))
         return chunks(false) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     SM_TRY(ensure_ws(d));
     SM_TRY(order_after_last(d, s));

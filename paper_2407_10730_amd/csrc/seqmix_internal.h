@@ -34,7 +34,8 @@ struct AttnArgs {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
     int64_t g_row;        // heads (a decay for each token) or 0
     int32_t heads, rep;   // rep heads share a q/k head
-    int32_t dk, dv, ndvb; // dv blocks per head
+    int32_t dk, dv;
+    int32_t block, ndvb;  // state columns per workgroup, such blocks per head
     float scale;
     int32_t vec;          // pointers and strides allow wide loads of q, k, v; stores of o
     int32_t svec;         // ... of the states
@@ -47,11 +48,10 @@ struct AttnArgs {
 constexpr int kTokensBlock = 32;  // state columns of a workgroup of the token kernel
 hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s);
 
-// Chunk kernels: chunk_block() state columns per workgroup.  state_only: the states that segments add from zero
+// Chunk kernels: 64 or 128 state columns per workgroup.  state_only: the states that segments add from zero
 // (all but the last of each sequence) into ws_state / ws_decay; launch_attn_join turns them into
 // the states that the segments start from, which the full pass reads.
 constexpr int kChunk = 64, kChunkF32 = 32;
-inline int chunk_block(int dv) { return dv <= 64 ? 64 : 128; }
 hipError_t launch_attn_chunks_bf16(const AttnArgs& a, int odt, bool state_only, hipStream_t s);
 hipError_t launch_attn_chunks_f32(const AttnArgs& a, bool state_only, hipStream_t s);
 hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s);

@@ -150,7 +150,8 @@ def _torch_hooks():
         from torch._C._dynamo.guards import assert_size_stride
     except ImportError:
         def assert_size_stride(t, shape, strides):
-            assert t.shape == shape and t.stride() == strides
+            if t.shape != shape or t.stride() != strides:
+                raise AssertionError
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return assert_size_stride, raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
