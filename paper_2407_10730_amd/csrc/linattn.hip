@@ -7,8 +7,7 @@ namespace cv {
 
 // One workgroup runs one sequence, head and block of DVB columns of the state through all tokens, the
 // state in registers: thread (rg, cg) holds RPT neighbouring rows of 4 columns.  Bound by reading and writing the
-// state (8 dk dv bytes per head against 4 dk dv operations per token), so it is the kernel of single
-// tokens and very short sequences.
+// state (8 dk dv bytes per head against 4 dk dv operations per token), so it is the kernel of one or two tokens.
 template <typename T, typename TO, int DVB, int RPT, bool VEC>
 __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     constexpr int LR = DVB / 4;  // threads across the columns
@@ -25,22 +24,19 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     const int nc = min(4, A.dv - c0);                       // live columns of this thread (may be negative)
     const int nr = nc > 0 ? max(0, min(RPT, A.dk - r0)) : 0;  // ... and rows
     const int64_t soff = ((slot * A.heads + head) * A.dk + r0) * A.dv + c0;
+    const bool whole = A.svec && nr == RPT;  // (svec: dv is a multiple of 4, so nc is 4 too)
 
     float S[RPT][4];
+    if (A.s_in && whole) {  // no branch between the loads: all are in flight together
+        const float* p = A.s_in + soff;
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) {
+        for (int i = 0; i < RPT; ++i) load_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) S[i][j] = 0.0f;
-        if (A.s_in && i < nr) {
-            const float* p = A.s_in + soff + (int64_t)i * A.dv;
-            if (A.svec) {
-                load_pack<float, 4>(p, S[i]);
-            } else {
+        for (int i = 0; i < RPT; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < nc) S[i][j] = p[j];
-            }
-        }
+            for (int j = 0; j < 4; ++j)
+                S[i][j] = A.s_in && i < nr && j < nc ? A.s_in[soff + (int64_t)i * A.dv + j] : 0.0f;
     }
     const int qh = head / A.rep;
     const T* q = static_cast<const T*>(A.q) + r.first * A.q_row + qh * A.q_head + r0;
@@ -103,44 +99,48 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
         o += A.o_row;
         if (g) g += A.g_row;
     }
-    if (A.s_out) {
+    if (A.s_out && whole) {
+        float* p = A.s_out + soff;
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) store_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
+    } else if (A.s_out) {
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
-            if (i < nr) {
-                float* p = A.s_out + soff + (int64_t)i * A.dv;
-                if (A.svec) {
-                    store_pack<float, 4>(p, S[i]);
-                } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (j < nc) p[j] = S[i][j];
-                }
-            }
+            for (int j = 0; j < 4; ++j)
+                if (i < nr && j < nc) A.s_out[soff + (int64_t)i * A.dv + j] = S[i][j];
     }
 }
 
-template <typename T, typename TO, int RPT>
+template <typename T, typename TO, int DVB, int DK>
 static void launch_tokens_r(const AttnArgs& a, dim3 grid, hipStream_t s) {
+    constexpr int RPT = DK * DVB / 1024;
     if (a.vec)
-        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, 32, RPT, true>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, DVB, RPT, true>), grid, dim3(256), 0, s, a);
     else
-        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, 32, RPT, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, DVB, RPT, false>), grid, dim3(256), 0, s, a);
 }
 
-template <typename T, typename TO>
-static hipError_t launch_tokens_t(const AttnArgs& a, hipStream_t s) {
+template <typename T, typename TO, int DVB>
+static hipError_t launch_tokens_b(const AttnArgs& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.sq.seqs * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
     if (a.dk <= 32)
-        launch_tokens_r<T, TO, 1>(a, grid, s);
+        launch_tokens_r<T, TO, DVB, 32>(a, grid, s);
     else if (a.dk <= 64)
-        launch_tokens_r<T, TO, 2>(a, grid, s);
+        launch_tokens_r<T, TO, DVB, 64>(a, grid, s);
     else if (a.dk <= 128)
-        launch_tokens_r<T, TO, 4>(a, grid, s);
+        launch_tokens_r<T, TO, DVB, 128>(a, grid, s);
     else
-        launch_tokens_r<T, TO, 8>(a, grid, s);
+        launch_tokens_r<T, TO, DVB, 256>(a, grid, s);
     return hipGetLastError();
+}
+
+template <typename T, typename TO>
+static hipError_t launch_tokens_t(const AttnArgs& a, hipStream_t s) {
+    return a.block == kTokensBlock ? launch_tokens_b<T, TO, kTokensBlock>(a, s)
+                                   : launch_tokens_b<T, TO, kTokensWide>(a, s);
 }
 
 hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s) {

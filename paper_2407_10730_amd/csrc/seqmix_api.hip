@@ -101,9 +101,6 @@ int order_after_last(seqmix_attn_desc* d, hipStream_t s) {
     return CONV2D_OK;
 }
 
-// Sequences of this many tokens or fewer on average go token by token.
-constexpr int64_t kTokensMost = 8;
-
 // The chunk kernels address the rows of a chunk by 32-bit byte offsets from its first: rows further apart go
 // token by token.
 bool chunk_rows_near(const seqmix_attn_params& p) {
@@ -111,6 +108,12 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 }
 
 // Kernel, state columns per workgroup (block) and where sequences are cut.
+//
+// Up to 2 tokens per sequence (fp32: 4) go token by token.  A chunk costs the same for 1 token as for 64, the token kernel
+// more with each: 8 sequences, 16 heads of 128 x 128 bf16: 6.5, 7.5 and 7.6 us for 1, 2 and 3 tokens, a chunk 8.0; 256 sequences:
+// 113, 118 and 123 us, a chunk 116; fp32, 128 sequences: 58 to 69 us for 1 to 4 tokens, a chunk 78.
+// Its blocks have 32 columns (more workgroups; 64 sequences of 16 heads of 64 x 64: 10.9 us, with 128 columns 11.6) until
+// there are 8 such per CU, then 128 (256 sequences as above: 113 us, with 32 columns 116).
 //
 // A workgroup takes its chunks one after the other, about 5 us each (dk = dv = 128) with one workgroup per CU and 8 with two.
 // Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the segments are as
@@ -124,8 +127,9 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
-    d->block = kTokensBlock;
-    if (p.tokens <= kTokensMost * p.seqs || !chunk_rows_near(p)) return;
+    const int64_t narrow = p.seqs * p.heads * ((p.dv + kTokensBlock - 1) / kTokensBlock);
+    d->block = narrow > 8 * kSeqmixCUs ? kTokensWide : kTokensBlock;
+    if (p.tokens <= (p.dtype == CONV2D_BF16 ? 2 : 4) * p.seqs || !chunk_rows_near(p)) return;
     const int64_t chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
     d->plan.chunk = (int32_t)chunk;

@@ -45,7 +45,7 @@ struct AttnArgs {
     float* ws_decay;      // [nseg][heads]: log of a segment's whole decay, times log2(e)
 };
 
-constexpr int kTokensBlock = 32;  // state columns of a workgroup of the token kernel
+constexpr int kTokensBlock = 32, kTokensWide = 128;  // state columns of a workgroup of the token kernel
 hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s);
 
 // Chunk kernels: 64 or 128 state columns per workgroup.  state_only: the states that segments add from zero
