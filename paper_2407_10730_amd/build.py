@@ -10,6 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libconv2d.so")
 HARNESS = os.path.join(HERE, "convbench")
+PYCALL = os.path.join(HERE, "_seqmix.so")
 SOURCES = ["conv2d_api.hip", "gemm_mfma.hip", "pack_kernels.hip", "direct_kernels.hip", "slice_conv.hip",
            "probes.hip", "winograd.hip", "patch_conv.hip", "seqmix_api.hip", "linattn.hip",
            "linattn_chunks.hip", "linattn_chunks_f32.hip", "token_conv.hip", "gate_norm.hip"]
@@ -33,6 +34,26 @@ def _compile(src, verbose):
     out = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
                     if "packed-fp32-ops" not in l and "is not a recognized feature" not in l)
     return src, r.returncode, out, obj
+
+
+def _build_pycall(verbose):
+    """The Python side of seqmix.py's calls (host code against the installed torch)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension as ce
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *["-I" + p for p in ce.include_paths()], "-I" + sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "seqmix_py.cpp"), *["-L" + p for p in ce.library_paths()[:1]],
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", PYCALL + ".tmp"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        print(r.stdout + r.stderr, file=sys.stderr)
+        raise RuntimeError("g++ failed for seqmix_py.cpp")
+    os.replace(PYCALL + ".tmp", PYCALL)
 
 
 def build(verbose: bool = False) -> str:
@@ -62,6 +83,7 @@ def build(verbose: bool = False) -> str:
         print(r.stdout + r.stderr, file=sys.stderr)
         raise RuntimeError("hipcc failed for convbench.cpp")
     os.replace(tmp, HARNESS)
+    _build_pycall(verbose)
     return LIB
 
 

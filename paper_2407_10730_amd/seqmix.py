@@ -53,6 +53,7 @@ class seqmix_norm_params(ctypes.Structure):
 
 
 _lib = None
+_pycall = None
 
 
 def load():
@@ -142,20 +143,6 @@ def _pick(names, value, what):
         raise ValueError(f"{what} is one of {', '.join(names)}: got {value!r}") from None
 
 
-def _torch_hooks():
-    """torch's own checks and stream lookup without their Python wrappers, where this torch has them (a
-    call on a few tokens is bound by its host side)."""
-    import torch
-    try:
-        from torch._C._dynamo.guards import assert_size_stride
-    except ImportError:
-        def assert_size_stride(t, shape, strides):
-            if t.shape != shape or t.stride() != strides:
-                raise AssertionError
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return assert_size_stride, raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-
-
 class _Operator:
     """A descriptor, and what each tensor argument of a call has to be, in the order of the C call."""
 
@@ -167,9 +154,11 @@ class _Operator:
         self._td = {B.CONV2D_F32: torch.float32, B.CONV2D_BF16: torch.bfloat16}
         self.params = params
         self.desc = _create(self.op, params)
-        self._fwd = getattr(load(), f"seqmix_{self.op}_fwd")
-        self._fits, self._raw_stream = _torch_hooks()
         self._want = []
+        self._call = None
+        # torch's stream lookup without its Python wrapper (1 us), where this torch has it
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
     def _expect(self, name, dtype, shape, strides=None):
         if strides is None:
@@ -179,44 +168,50 @@ class _Operator:
                 n *= d
         self._want.append((dtype, tuple(shape), tuple(strides), name))
 
+    def _ready(self):
+        """The checks and the C function as one call of the extension module."""
+        global _pycall
+        if _pycall is None:
+            from . import _seqmix as _pycall  # after torch
+        fn = ctypes.cast(getattr(load(), f"seqmix_{self.op}_fwd"), ctypes.c_void_p).value
+        like = {d: self._torch.empty(0, dtype=d) for d in {w[0] for w in self._want}}
+        self._call = _pycall.make(fn, self.desc, [(like[d], shape, strides) for d, shape, strides, _ in self._want])
+        return self._call
+
     def _refuse(self, t, want, dev):
-        """Raises unless the tensor fits after all (the strides of extents of one and of empty tensors are open)."""
         dtype, shape, strides, name = want
         who = f"{type(self).__name__}: {name}"
+        if not isinstance(t, self._torch.Tensor):
+            raise TypeError(f"{who} is a tensor or None: got {type(t).__name__}")
         if t.dtype is not dtype or t.shape != shape:
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}")
-        if 0 not in shape and any(d > 1 and a != b for d, a, b in zip(shape, t.stride(), strides)):
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} has strides {t.stride()}, not {strides}")
-        if dev < 0 or t.get_device() != dev:
-            raise Conv2dError(B.CONV2D_E_INVALID, f"{who} is on {t.device}: all arguments are on one GPU")
-
-    def _launch(self, dev, stream, tensors):
-        """Checks the tensors (None: not given) and calls the library with their addresses."""
-        args, fits = [self.desc], self._fits
-        add = args.append
-        for t, (dtype, shape, strides, _) in zip(tensors, self._want):
-            if t is None:
-                add(None)
-                continue
-            try:
-                fits(t, shape, strides)
-                if t.dtype is not dtype or t.get_device() != dev or dev < 0:
-                    raise AssertionError
-            except AssertionError:
-                self._refuse(t, self._want[len(args) - 1], dev)
-            add(t.data_ptr())
-        args.append(self._raw_stream(dev) if stream is None else _stream(stream))
-        if dev == self._torch.cuda.current_device():
-            st = self._fwd(*args)
+            what = f"is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}"
+        elif not t.is_cuda or t.get_device() != dev:
+            what = f"is on {t.device}: all arguments are on one GPU"
         else:
-            with self._torch.cuda.device(dev):
-                st = self._fwd(*args)
+            what = f"has strides {t.stride()}, not {strides}"
+        raise Conv2dError(B.CONV2D_E_INVALID, f"{who} {what}")
+
+    def _launch(self, dev, stream, *tensors):
+        """Checks the tensors (None: not given) and calls the library with their addresses."""
+        cuda = self._torch.cuda
+        call = self._call or self._ready()
+        if dev < 0:  # no GPU, no stream: let the checks say which tensor is wrong
+            st = _pycall.run(call, dev, 0, *tensors)
+        else:
+            raw = self._raw_stream(dev) if stream is None else _stream(stream)
+            if dev == cuda.current_device():
+                st = _pycall.run(call, dev, raw, *tensors)
+            else:
+                with cuda.device(dev):
+                    st = _pycall.run(call, dev, raw, *tensors)
+        if st > 0:
+            self._refuse(tensors[st - 1], self._want[st - 1], dev)
         if st:
             raise Conv2dError(st, f"seqmix_{self.op}_fwd")
 
     def close(self):
         if self.desc:
-            desc, self.desc = self.desc, 0
+            desc, self.desc, self._call = self.desc, 0, None
             _check(getattr(load(), f"seqmix_{self.op}_desc_destroy")(desc), f"seqmix_{self.op}_desc_destroy")
 
     def __del__(self):
@@ -261,7 +256,7 @@ class LinearAttention(_Operator):
         self._expect("o", td[odt], (tokens, heads, dv), (*strides["o"], 1))
 
     def run(self, q, k, v, decay, state_in, state_out, o, offsets=None, slot_index=None, stream=None):
-        self._launch(o.get_device(), stream, (q, k, v, decay, offsets, slot_index, state_in, state_out, o))
+        self._launch(o.get_device(), stream, q, k, v, decay, offsets, slot_index, state_in, state_out, o)
 
     def plan(self):
         return seqmix_attn_plan_query(self.desc)
@@ -298,7 +293,7 @@ class TokenConv(_Operator):
         self._expect("y", td, (tokens, channels), (y_row, 1))
 
     def run(self, x, w, bias, window_in, window_out, y, offsets=None, slot_index=None, stream=None):
-        self._launch(y.get_device(), stream, (x, w, bias, offsets, slot_index, window_in, window_out, y))
+        self._launch(y.get_device(), stream, x, w, bias, offsets, slot_index, window_in, window_out, y)
 
 
 class GateNorm(_Operator):
@@ -338,4 +333,4 @@ class GateNorm(_Operator):
 
     def run(self, u, post_w=None, post_b=None, gate=None, residual=None, scale_vec=None, pre_w=None, pre_b=None,
             y=None, h=None, stream=None):
-        self._launch(u.get_device(), stream, (u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h))
+        self._launch(u.get_device(), stream, u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h)
