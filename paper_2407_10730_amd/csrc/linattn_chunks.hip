@@ -19,6 +19,7 @@
 namespace cv {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
             whole += tot;
         }
         __syncthreads();
-        if (STATE_ONLY && c + C < len) load(c + C);
+        if (c + C < len) load(c + C);
 
         if constexpr (!STATE_ONLY) {
             // Scores, transposed (a lane holds 4 neighbouring j of one i): the 10 of 16 tiles on or below the diagonal, and
@@ -204,24 +205,18 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
             }
 #pragma unroll
             for (int it = 0; it < 4; ++it) O[it] *= sD[16 * it + l16];
-            const f32x4 inter[4] = {O[0], O[1], O[2], O[3]};
+            // The scores above the diagonal are zeros, but zero times an infinite or NaN v is NaN: a chunk with such a v
+            // among the wave's is summed without those terms.
+            u16x2 top{0, 0};
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int it = 2 * s; it < 4; ++it)
-                    O[it] = mfma16(__builtin_bit_cast(bf16x8, vf[s]),
-                                   lds_read<bf16x8>(sP, (o_pr ^ (s << 6)) + it * (32 * C)), O[it]);
-            // A later token's infinite or NaN v times its score of zero has made every earlier token NaN too, the
-            // first of the 32 that share a product step among them: such chunks are summed again without the
-            // masked terms.
-            bool bad = false;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) bad = bad || !finite(O[0][u]) || !finite(O[2][u]);
-            if (__any(bad && l16 == 0)) {
+                for (int w = 0; w < 4; ++w)
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[s][w] & 0x7fff7fffu));
+            if (__any(max(top[0], top[1]) >= 0x7f80)) {
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
                     const int i = 16 * it + l16;
-                    O[it] = inter[it];
                     for (int j = 0; j <= i; ++j) {
                         const float p = to_f32(lds_read<uint16_t>(sP, swz_at<C>(i, j)));
                         const uint32_t v = swz_at<DVB>(j, wc + 4 * quad);
@@ -229,9 +224,14 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
                         for (int u = 0; u < 4; ++u) O[it][u] = fmaf(p, to_f32(lds_read<uint16_t>(sV, v + 2 * u)), O[it][u]);
                     }
                 }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int it = 2 * s; it < 4; ++it)
+                        O[it] = mfma16(__builtin_bit_cast(bf16x8, vf[s]),
+                                       lds_read<bf16x8>(sP, (o_pr ^ (s << 6)) + it * (32 * C)), O[it]);
             }
-            // the next chunk's rows travel under the state's products (any earlier, and their registers would spill)
-            if (c + C < len) load(c + C);
             attn_store<4, VEC>(A, o_f32, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         // the state moves on
@@ -240,6 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
         for (int m = 0; m < MT; ++m) S[m] *= tot;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+            __builtin_amdgcn_sched_barrier(0);  // (operands of both steps at once would spill)
             u32x4 vp[3];  // planes of exp(b_C - b_j) v_j
             const f32x4 e0 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad]);
             const f32x4 e1 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad + 4]);

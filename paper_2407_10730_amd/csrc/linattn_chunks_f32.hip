@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
             whole += tot;
         }
         __syncthreads();
-        if (STATE_ONLY && c + C < len) load(c + C);
+        if (c + C < len) load(c + C);
 
         if constexpr (!STATE_ONLY) {
             // one 16x16 tile of scores per wave, transposed (a lane holds 4 neighbouring j of one i); the one above
@@ -142,24 +142,16 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
             }
 #pragma unroll
             for (int it = 0; it < 2; ++it) O[it] *= sD[16 * it + l16];
-            const f32x4 inter[2] = {O[0], O[1]};
+            // zero scores above the diagonal times an infinite or NaN v are NaN: sum without those terms
+            uint32_t top = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int it = h; it < 2; ++it) {
-                    const f32x4 p = *reinterpret_cast<const f32x4*>(&sP[(16 * it + l16) * PP + 16 * h + 4 * quad]);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) O[it] = mfma_f32(vf[h][u], p[u], O[it]);
-                }
-            // an infinite or NaN v of a later token has reached the first token of the 16: sum without the masked terms
-            bool bad = false;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) bad = bad || !finite(O[0][u]) || !finite(O[1][u]);
-            if (__any(bad && l16 == 0)) {
+                for (int u = 0; u < 4; ++u) top = max(top, __builtin_bit_cast(uint32_t, vf[h][u]) & 0x7fffffffu);
+            if (__any(top >= 0x7f800000u)) {
 #pragma unroll
                 for (int it = 0; it < 2; ++it) {
                     const int i = 16 * it + l16;
-                    O[it] = inter[it];
                     for (int j = 0; j <= i; ++j) {
                         const float p = sP[i * PP + j];
                         const float* v = &sV[j * VP + wc + 4 * quad];
@@ -167,9 +159,16 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
                         for (int u = 0; u < 4; ++u) O[it][u] = fmaf(p, v[u], O[it][u]);
                     }
                 }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int it = h; it < 2; ++it) {
+                        const f32x4 p = *reinterpret_cast<const f32x4*>(&sP[(16 * it + l16) * PP + 16 * h + 4 * quad]);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) O[it] = mfma_f32(vf[h][u], p[u], O[it]);
+                    }
             }
-            // the next chunk's rows travel under the state's products (any earlier, and their registers would spill)
-            if (c + C < len) load(c + C);
             attn_store<2, VEC>(A, 1, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         const float tot = sTot;

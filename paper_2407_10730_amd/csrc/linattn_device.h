@@ -140,8 +140,6 @@ __device__ __forceinline__ void store_state(const AttnArgs& A, float* p, int c, 
         for (int i = 0; i < 4; ++i) st_f32(r, at + (m / 2 * 32 + m % 2 * TS + i) * row, S[m][i]);
 }
 
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) < __builtin_inff(); }
-
 // Results of a chunk of n tokens that starts at token c of the segment, scaled and rounded: tile it holds tokens 16 it + l16,
 // columns col .. col + 3 (those at or past dv are none).
 template <int IT, bool VEC>
