@@ -51,7 +51,7 @@ extern "C" {
  *   S_t = exp(g_t) S_{t-1} + k_t v_t^T      (dk x dv)        o_t = scale * q_t S_t
  *
  * g is the log of the decay.  -infinity clears the state (a document that starts inside a sequence);
- * values above 0 let it grow.  What a token holds never reaches the outputs of tokens before it, also where
+ * values above 0 let it grow (by less than 2^100 over any 64 tokens, or results are not finite).  What a token holds never reaches the outputs of tokens before it, also where
  * it is infinite or NaN. */
 enum {
     SEQMIX_DECAY_NONE = 0,  /* g = 0 */

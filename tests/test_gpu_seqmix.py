@@ -165,6 +165,40 @@ def test_attention(kw, carry):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_many_sequences(dtype):
+    """More sequences than a wave looks up at once, and than one step of its search covers; some of them cut."""
+    rng = np.random.default_rng(2)
+    lens = [int(t) for t in rng.integers(0, 12, 150)]
+    lens[70] = 400
+    a = Attn(lens, 1, 1, 32, 32, dtype=dtype, uniform=False, pool=4)
+    left = a.state.clone()
+    a.run(left, left).check(left)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,uniform", [([2000], None), ([900, 900], None), ([1500, 0, 800, 1], False)])
+def test_attention_in_segments(dtype, lens, uniform):
+    """Long enough to be cut, also where the last segment is short."""
+    a = Attn(lens, 2, 2, 64, 96, dtype=dtype, uniform=uniform)
+    plan = a.op.plan()
+    assert plan.kernel == M.SEQMIX_KERNEL_CHUNKS and 0 < plan.segment < max(lens) and plan.workspace_bytes > 0
+    left = torch.empty_like(a.state)
+    a.run(a.state, left).check(left)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[3], [100]])
+def test_attention_growing_decays(dtype, lens):
+    """Log decays above 0, growing by far more than a chunk's terms are of."""
+    def edit(a):
+        a.g.uniform_(-0.2, 0.6, generator=torch.Generator(device="cuda").manual_seed(1))
+
+    a = Attn(lens, 2, 2, 64, 64, dtype=dtype, edit=edit)
+    left = torch.empty_like(a.state)
+    a.run(a.state, left).check(left)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[1, 1], [150, 40]])
 @pytest.mark.parametrize("kw", [dict(shift=1), dict(pad=24), dict(pad=3), dict(heads_outer=True),
                                 dict(heads_outer=True, shift=3, pad=1)], ids=str)
@@ -432,6 +466,22 @@ def test_token_conv_keeps_sequences_apart():
     y2.fill_(4.0)
     op.run(x, w, b, pool, left2, y2, slot_index=torch.tensor([2, -1, 1], dtype=torch.int32, device="cuda"))
     assert bool((y2[40:80] == 4.0).all())
+
+
+def test_token_conv_many_sequences():
+    """More sequences than two steps of a wave's search cover."""
+    rng = np.random.default_rng(4)
+    lens = [int(t) for t in rng.integers(0, 3, 5000)]
+    c = 40
+    x = torch.randn(sum(lens), c, device="cuda")
+    w = torch.randn(c, 3, device="cuda")
+    pool = torch.randn(5000, 2, c, device="cuda")
+    y, left = torch.empty_like(x), pool.clone()
+    op = M.TokenConv(tokens=len(x), seqs=5000, channels=c, width=3, dtype="f32", bias=False, act="none")
+    op.run(x, w, None, left, left, y, offsets=torch.tensor([0] + lens, device="cuda").cumsum(0))
+    want, size, after = ref.token_conv(_host(x), _host(w), 0.0, lens, _host(pool), "none")
+    _near(_host(y), want, 5 * U * size, 1.0, "y")
+    assert np.array_equal(_host(left), after)
 
 
 def test_token_conv_rows_past_32_bits():

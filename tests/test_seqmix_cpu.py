@@ -118,6 +118,28 @@ def test_calls_refuse_missing_pointers_and_bad_packing():
     M.seqmix_norm_desc_destroy(n)
 
 
+def _plan(**kw):
+    d = M.seqmix_attn_desc_create(_attn(**kw))
+    p = M.seqmix_attn_plan_query(d)
+    M.seqmix_attn_desc_destroy(d)
+    return p
+
+
+def test_attention_plans():
+    dims = dict(dk=128, dv=128, heads=8, qk_heads=8, q_row=1024, q_head=128, k_row=1024, k_head=128, v_row=1024,
+                v_head=128, o_row=1024, o_head=128)
+    one = _plan(tokens=64, seqs=64, slots=64, **dims)
+    assert (one.kernel, one.segment, one.workspace_bytes) == (M.SEQMIX_KERNEL_TOKENS, 0, 0)
+    assert _plan(tokens=5 * 64, seqs=64, slots=64, **dims).kernel == M.SEQMIX_KERNEL_CHUNKS
+    assert _plan(tokens=300, seqs=1, slots=1, **dims).segment == 0        # a few chunks: not worth a second pass
+    assert _plan(tokens=1 << 16, seqs=64, slots=64, **dims).segment == 0  # enough sequences side by side
+    cut = _plan(tokens=1 << 16, seqs=1, slots=1, **dims)
+    assert cut.segment % cut.chunk == 0 and 0 < cut.segment < 1 << 16
+    assert cut.workspace_bytes >= (1 << 16) // cut.segment * 8 * 128 * 128 * 4
+    # rows too far apart for the chunk kernels' 32-bit offsets
+    assert _plan(tokens=1 << 10, seqs=1, slots=1, **dict(dims, q_row=1 << 24)).kernel == M.SEQMIX_KERNEL_TOKENS
+
+
 def test_helpers_refuse_tensors_that_do_not_fit():
     op = M.TokenConv(tokens=4, seqs=1, channels=8, width=3, dtype="f32")
     x = torch.zeros(4, 8)
@@ -129,6 +151,8 @@ def test_helpers_refuse_tensors_that_do_not_fit():
         with pytest.raises(B.Conv2dError) as e:
             op.run(*args)
         assert e.value.status == B.CONV2D_E_INVALID
+    with pytest.raises(TypeError):
+        op.run(x.tolist(), *ok[1:])
     op.close()
     for make in (lambda: M.TokenConv(tokens=4, seqs=1, channels=8, width=3, dtype="f16"),
                  lambda: M.TokenConv(tokens=4, seqs=1, channels=8, width=3, act="relu"),
