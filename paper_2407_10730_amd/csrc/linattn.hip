@@ -17,37 +17,19 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     const int blk = (int)(b % A.ndvb);
     const int64_t bh = b / A.ndvb;
     const int head = (int)(bh % A.heads), seq = (int)(bh / A.heads);
-    const int64_t slot = seq_slot(A.sq, seq);
-    if (slot < 0) return;
     const SeqRange r = seq_range(A.sq, seq);
     const int c0 = blk * DVB + cg * 4, r0 = rg * RPT;
     const int nc = min(4, A.dv - c0);                       // live columns of this thread (may be negative)
     const int nr = nc > 0 ? max(0, min(RPT, A.dk - r0)) : 0;  // ... and rows
-    const int64_t soff = ((slot * A.heads + head) * A.dk + r0) * A.dv + c0;
-    const bool whole = A.svec && nr == RPT;  // (svec: dv is a multiple of 4, so nc is 4 too)
 
-    float S[RPT][4];
-    if (A.s_in && whole) {  // no branch between the loads: all are in flight together
-        const float* p = A.s_in + soff;
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) load_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < RPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                S[i][j] = A.s_in && i < nr && j < nc ? A.s_in[soff + (int64_t)i * A.dv + j] : 0.0f;
-    }
     const int qh = head / A.rep;
     const T* q = static_cast<const T*>(A.q) + r.first * A.q_row + qh * A.q_head + r0;
     const T* k = static_cast<const T*>(A.k) + r.first * A.k_row + qh * A.k_head + r0;
     const T* v = static_cast<const T*>(A.v) + r.first * A.v_row + head * A.v_head + c0;
     const float* g = A.g ? A.g + r.first * A.g_row + head : nullptr;
     TO* o = static_cast<TO*>(A.o) + r.first * A.o_row + head * A.o_head + blk * DVB;
-
-#pragma unroll 1
-    for (int64_t n = 0; n < r.len; ++n) {
-        float kk[RPT], qq[RPT], vv[4];
+    float kk[RPT], qq[RPT], vv[4], gg = 0.0f;
+    auto load = [&] {  // the token at the pointers
         if (VEC && nr == RPT) {
             load_pack<T, RPT>(k, kk);
             load_pack<T, RPT>(q, qq);
@@ -64,7 +46,30 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) vv[j] = j < nc ? to_f32(v[j]) : 0.0f;
         }
-        const float d = g ? __builtin_amdgcn_exp2f((float)decay_log2(*g)) : 1.0f;
+        if (g) gg = *g;
+    };
+    if (r.len > 0) load();  // under way while the slot, and then the state, are looked up
+
+    const int64_t slot = seq_slot(A.sq, seq);
+    if (slot < 0) return;
+    const int64_t soff = ((slot * A.heads + head) * A.dk + r0) * A.dv + c0;
+    const bool whole = A.svec && nr == RPT;  // (svec: dv is a multiple of 4, so nc is 4 too)
+    float S[RPT][4];
+    if (A.s_in && whole) {  // no branch between the loads: all are in flight together
+        const float* p = A.s_in + soff;
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) load_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                S[i][j] = A.s_in && i < nr && j < nc ? A.s_in[soff + (int64_t)i * A.dv + j] : 0.0f;
+    }
+
+#pragma unroll 1
+    for (int64_t n = 0; n < r.len; ++n) {
+        const float d = g ? __builtin_amdgcn_exp2f((float)decay_log2(gg)) : 1.0f;
         float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         auto update = [&](int rows) {
 #pragma unroll
@@ -81,6 +86,13 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
             update(RPT);
         else  // rows past dk stay out of the sums: 0 * infinity is no zero
             update(nr);
+        if (n + 1 < r.len) {
+            q += A.q_row;
+            k += A.k_row;
+            v += A.v_row;
+            if (g) g += A.g_row;
+            load();
+        }
 #pragma unroll
         for (int m = LR; m < 64; m <<= 1)
 #pragma unroll
@@ -93,11 +105,7 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
         __syncthreads();
         if (t < DVB && blk * DVB + t < A.dv)
             o[t] = from_f32<TO>(A.scale * ((rd[0][t] + rd[1][t]) + (rd[2][t] + rd[3][t])));
-        q += A.q_row;
-        k += A.k_row;
-        v += A.v_row;
         o += A.o_row;
-        if (g) g += A.g_row;
     }
     if (A.s_out && whole) {
         float* p = A.s_out + soff;

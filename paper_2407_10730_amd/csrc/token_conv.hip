@@ -23,13 +23,11 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t t0 = (int64_t)sp.part * tile;
     if (sp.part < 0 || (sp.part > 0 && t0 >= r.len)) return;
-    const int64_t slot = seq_slot(A.sq, sp.seq);
-    if (slot < 0) return;
     const int n = (int)min<int64_t>(r.len - t0, tile);
     const T* __restrict__ x = static_cast<const T*>(A.x) + (r.first + t0) * A.x_row + c;
     T* __restrict__ y = static_cast<T*>(A.y) + (r.first + t0) * A.y_row + c;
 
-    // the first rows are on their way while weights and window arrive
+    // the first rows and the weights are on their way while the slot, and then the window, are looked up
     Pack<T, V> next[kConvAhead];
 #pragma unroll
     for (int u = 0; u < kConvAhead; ++u)
@@ -47,6 +45,8 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
 #pragma unroll
         for (int v = 0; v < V; ++v) bias[v] = 0.0f;
     }
+    const int64_t slot = seq_slot(A.sq, sp.seq);
+    if (slot < 0) return;
     float row[W][V];  // row[i]: x of tap i
     if constexpr (W > 1) {
         const T* win = static_cast<const T*>(A.win_in) + (slot * (W - 1)) * A.channels + c;
