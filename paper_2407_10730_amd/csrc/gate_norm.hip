@@ -153,7 +153,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
                 x[i][v] *= A.scale * e[v];
                 if (A.res) x[i][v] += to_f32(res[i].e[v]);
             }
-            if (A.y && live) store_pack<TR, V>(yp + c, x[i]);
+            if (A.y && live) store_result<TR, V>(yp + c, x[i], A.past);
         }
     }
     if (A.pre == SEQMIX_NORM_NONE) return;
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int c = (i * TPR + t) * V;
-        if (c < n && live) store_pack<T, V>(hp + c, x[i]);
+        if (c < n && live) store_result<T, V>(hp + c, x[i], A.past);
     }
 }
 

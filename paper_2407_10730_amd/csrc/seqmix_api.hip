@@ -295,6 +295,7 @@ int seqmix_conv_fwd(const seqmix_conv_desc* d, const void* x, const void* w, con
     const int64_t unit = 16 / esize(p.dtype);
     a.vec = p.channels % unit == 0 && p.x_row % unit == 0 && p.y_row % unit == 0 && aligned(x, 16) && aligned(y, 16) &&
             aligned(w, 16) && aligned(a.bias, 16) && aligned(a.win_in, 16) && aligned(a.win_out, 16);
+    a.past = p.tokens * p.channels * esize(p.dtype) >= kPastBytes;
     return launch_token_conv(a, p.dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
 
@@ -368,6 +369,7 @@ int seqmix_norm_fwd(const seqmix_norm_desc* d, const void* u, const float* post_
             (!a.gate || (aligned(gate, 16) && p.gate_row % unit == 0)) &&
             (!a.res || (aligned(residual, 16) && p.res_row % unit == 0)) &&
             (!y || (aligned(y, 16) && p.y_row % unit == 0)) && (!a.h || (aligned(h, 16) && p.h_row % unit == 0));
+    a.past = p.rows * p.width * ((y ? esize(p.res_dtype) : 0) + (pre ? esize(p.dtype) : 0)) >= kPastBytes;
     return launch_norm(a, p.dtype, p.res_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK
                                                                                                : CONV2D_E_HIP;
 }

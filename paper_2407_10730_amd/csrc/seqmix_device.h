@@ -39,6 +39,24 @@ __device__ __forceinline__ void store_pack(T* p, const float (&in)[N]) {
     *reinterpret_cast<Pack<T, N>*>(p) = v;
 }
 
+// ... past the caches where `past` (full 16-byte stores only): results larger than the L2s push out what is still to be
+// read, and their lines are not fetched for writing.
+template <typename T, int N>
+__device__ __forceinline__ void store_result(T* p, const float (&in)[N], bool past) {
+    Pack<T, N> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.e[i] = from_f32<T>(in[i]);
+    if constexpr (sizeof(v) == 16) {
+        if (past) {
+            asm volatile("" ::: "memory");  // or the two stores become one, without the hint
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
+            asm volatile("" ::: "memory");
+            return;
+        }
+    }
+    *reinterpret_cast<Pack<T, N>*>(p) = v;
+}
+
 // Rows [first, first + len) of sequence i, clamped so that no offsets lead outside the call's rows.  Row numbers, slots
 // and parts are below 2^31 (the descriptors refuse more), so their divisions are 32-bit ones.
 struct SeqRange {

@@ -6,6 +6,9 @@
 
 namespace cv {
 
+// Results of this many bytes or more are written past the caches (8 L2s of 4 MiB): 8192 x 4096 bf16 convolution 31.8 -> 26.5 us,
+// 8192 x 2048 norm with residual 34.0 -> 26.2 us; below, the next operator still finds them there.
+constexpr int64_t kPastBytes = 32LL << 20;
 constexpr int kSeqmixCUs = 256;  // plans are made without a GPU: MI355X has 256 CUs
 
 // How the rows of a call divide into sequences, and which pool entry each has.
@@ -66,6 +69,7 @@ struct ConvArgs {
     int64_t x_row, y_row;
     int32_t channels, width, silu;
     int32_t vec;          // 16-byte accesses of x, y and the windows are aligned
+    int32_t past;         // y is written past the caches
 };
 hipError_t launch_token_conv(const ConvArgs& a, int dt, hipStream_t s);
 
@@ -81,7 +85,7 @@ struct NormArgs {
     int64_t gate_run, u_row, gate_row, res_row, y_row, h_row;
     int32_t post, gate_act, gate_first, pre;
     float scale, post_eps, pre_eps;
-    int32_t vec;
+    int32_t vec, past;
 };
 hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s);
 

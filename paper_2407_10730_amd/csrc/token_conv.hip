@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
                     for (int i = 0; i < W; ++i) o[v] = fmaf(w[v * W + i], row[i][v], o[v]);
                     if (A.silu) o[v] = silu(o[v]);
                 }
-                store_pack<T, V>(y + (int64_t)(t + u) * A.y_row, o);
+                store_result<T, V>(y + (int64_t)(t + u) * A.y_row, o, A.past);
 #pragma unroll
                 for (int i = 0; i + 1 < W; ++i)
 #pragma unroll
