@@ -6,9 +6,10 @@
 
 namespace cv {
 
-// Results of this many bytes or more are written past the caches (8 L2s of 4 MiB): 8192 x 4096 bf16 convolution 31.8 -> 26.5 us,
-// 8192 x 2048 norm with residual 34.0 -> 26.2 us; below, the next operator still finds them there.
-constexpr int64_t kPastBytes = 32LL << 20;
+// Results of this many bytes or more are written past the caches: 8192 x 4096 bf16 convolution 31.8 -> 26.3 us, 8192 x 2048 norm
+// with residual 34.0 -> 26.4 us, 2048 rows of the two 12.4 -> 10.6 and 11.3 -> 9.6 us.  The operators after them do
+// not miss it (a layer over 8496 tokens 297 us, 296 with it): the XCDs' L2s hold little of what others wrote.
+constexpr int64_t kPastBytes = 4LL << 20;
 constexpr int kSeqmixCUs = 256;  // plans are made without a GPU: MI355X has 256 CUs
 
 // How the rows of a call divide into sequences, and which pool entry each has.
