@@ -3,6 +3,8 @@
 The library (libconv2d.so, HIP) exports the C ABI declared in
 include/conv2d.h; ``binding`` mirrors it function by function and
 ``runner`` drives one operation with torch-owned device memory.
+``seqmix`` does both for the token-mixing operators of include/seqmix.h,
+and ``mixer`` is a layer of them.
 """
 from .binding import (  # noqa: F401
     ALGO_NAMES, CONV2D_ALGO_AUTO, CONV2D_ALGO_DIRECT, CONV2D_ALGO_IM2COL_GEMM,
