@@ -8,7 +8,10 @@ namespace cv {
 // One workgroup runs one sequence, head and block of DVB columns of the state through all tokens, the
 // state in registers: thread (rg, cg) holds RPT neighbouring rows of 4 columns.  Bound by reading and writing the
 // state (8 dk dv bytes per head against 4 dk dv operations per token), so it is the kernel of one or two tokens.
-template <typename T, typename TO, int DVB, int RPT, bool VEC>
+// All loads are wide at any alignment: a thread whose columns pass the last one moves down to the last four, and owns
+// those from `skip` on only; what it computes of the others is not used (128 sequences, 16 heads of 128 x 189: 101 us, with
+// such rows read by elements 170; of 131 x 130: 90, 262).
+template <typename T, typename TO, int DVB, int RPT>
 __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     constexpr int LR = DVB / 4;  // threads across the columns
     __shared__ float red[2][4][DVB];
@@ -18,9 +21,10 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     const int64_t bh = b / A.ndvb;
     const int head = (int)(bh % A.heads), seq = (int)(bh / A.heads);
     const SeqRange r = seq_range(A.sq, seq);
-    const int c0 = blk * DVB + cg * 4, r0 = rg * RPT;
-    const int nc = min(4, A.dv - c0);                       // live columns of this thread (may be negative)
-    const int nr = nc > 0 ? max(0, min(RPT, A.dk - r0)) : 0;  // ... and rows
+    const int r0 = rg * RPT, nc = min(4, A.dv - blk * DVB - cg * 4);  // owned columns (none: below 1)
+    const int skip = A.dv >= 4 && nc > 0 ? 4 - nc : 0, jend = skip + nc;
+    const int c0 = blk * DVB + cg * 4 - skip;
+    const int nr = nc > 0 ? max(0, min(RPT, A.dk - r0)) : 0;  // owned rows
 
     const int qh = head / A.rep;
     const T* q = static_cast<const T*>(A.q) + r.first * A.q_row + qh * A.q_head + r0;
@@ -30,7 +34,7 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     TO* o = static_cast<TO*>(A.o) + r.first * A.o_row + head * A.o_head + blk * DVB;
     float kk[RPT], qq[RPT], vv[4], gg = 0.0f;
     auto load = [&] {  // the token at the pointers
-        if (VEC && nr == RPT) {
+        if (nr == RPT) {
             load_pack<T, RPT>(k, kk);
             load_pack<T, RPT>(q, qq);
         } else {
@@ -40,11 +44,11 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
                 qq[i] = i < nr ? to_f32(q[i]) : 0.0f;
             }
         }
-        if (VEC && nc >= 4) {
+        if (jend == 4) {
             load_pack<T, 4>(v, vv);
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vv[j] = j < nc ? to_f32(v[j]) : 0.0f;
+            for (int j = 0; j < 4; ++j) vv[j] = j < jend ? to_f32(v[j]) : 0.0f;
         }
         if (g) gg = *g;
     };
@@ -52,19 +56,20 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
 
     const int64_t slot = seq_slot(A.sq, seq);
     if (slot < 0) return;
-    const int64_t soff = ((slot * A.heads + head) * A.dk + r0) * A.dv + c0;
-    const bool whole = A.svec && nr == RPT;  // (svec: dv is a multiple of 4, so nc is 4 too)
-    float S[RPT][4];
-    if (A.s_in && whole) {  // no branch between the loads: all are in flight together
-        const float* p = A.s_in + soff;
+    const int64_t soff = (slot * A.heads + head) * A.dk * A.dv;
+    const uint32_t row = (uint32_t)A.dv * 4, size = (uint32_t)A.dk * row;  // bytes; rows past dk are out of range
+    const uint32_t at = nc > 0 ? (uint32_t)r0 * row + c0 * 4 : OOB_OFF;
+    const __amdgpu_buffer_rsrc_t rin = make_rsrc(A.s_in ? A.s_in + soff : nullptr, A.s_in ? size : 0u);
+    f32x4 S[RPT];
+    if (A.dv >= 4) {
 #pragma unroll
-        for (int i = 0; i < RPT; ++i) load_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
+        for (int i = 0; i < RPT; ++i)
+            S[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rin, at + i * row, 0, 0));
     } else {
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                S[i][j] = A.s_in && i < nr && j < nc ? A.s_in[soff + (int64_t)i * A.dv + j] : 0.0f;
+            for (int j = 0; j < 4; ++j) S[i][j] = ld_f32(rin, j < jend ? at + i * row + j * 4 : OOB_OFF);
     }
 
 #pragma unroll 1
@@ -100,33 +105,32 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
         float(*rd)[DVB] = red[n & 1];  // two buffers: one barrier per token
         if ((t & 63) < LR) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) rd[t >> 6][cg * 4 + j] = acc[j];
+            for (int j = 0; j < 4; ++j)
+                if (j >= skip) rd[t >> 6][cg * 4 + j - skip] = acc[j];
         }
         __syncthreads();
         if (t < DVB && blk * DVB + t < A.dv)
             o[t] = from_f32<TO>(A.scale * ((rd[0][t] + rd[1][t]) + (rd[2][t] + rd[3][t])));
         o += A.o_row;
     }
-    if (A.s_out && whole) {
-        float* p = A.s_out + soff;
+    if (!A.s_out) return;
+    const __amdgpu_buffer_rsrc_t rout = make_rsrc(A.s_out + soff, size);
+    if (nc >= 4) {
 #pragma unroll
-        for (int i = 0; i < RPT; ++i) store_pack<float, 4>(p + (int64_t)i * A.dv, S[i]);
-    } else if (A.s_out) {
+        for (int i = 0; i < RPT; ++i)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, S[i]), rout, at + i * row, 0, 0);
+    } else if (nc > 0) {
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (i < nr && j < nc) A.s_out[soff + (int64_t)i * A.dv + j] = S[i][j];
+            for (int j = 0; j < 4; ++j) st_f32(rout, j >= skip && j < jend ? at + i * row + j * 4 : OOB_OFF, S[i][j]);
     }
 }
 
 template <typename T, typename TO, int DVB, int DK>
 static void launch_tokens_r(const AttnArgs& a, dim3 grid, hipStream_t s) {
     constexpr int RPT = DK * DVB / 1024;
-    if (a.vec)
-        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, DVB, RPT, true>), grid, dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((attn_tokens_kernel<T, TO, DVB, RPT, false>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attn_tokens_kernel<T, TO, DVB, RPT>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T, typename TO, int DVB>
@@ -157,14 +161,12 @@ hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s)
 }
 
 // Joins the segments of each sequence: ws_state holds the state that each segment but the last adds from
-// zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring elements of a state and
-// walks along the segments, AHEAD loads ahead of the sum.  Bound by its bytes, 8 dk dv per segment and head.
+// zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring elements of a state (from
+// e on) and walks along the segments, AHEAD loads ahead of the sum.  Bound by its bytes, 8 dk dv per segment and head.
 template <int V>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
+__device__ __forceinline__ void join_elements(const AttnArgs& A, int64_t e) {
     constexpr int AHEAD = 8;
     const int64_t size = (int64_t)A.dk * A.dv;
-    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
-    if (e >= size) return;
     const int head = blockIdx.y;
     const int seq = blockIdx.z;
     const SeqRange r = seq_range(A.sq, seq);
@@ -200,15 +202,20 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
     }
 }
 
+// Four elements per thread, and one in the threads of the last three.
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
+    const int size = A.dk * A.dv, i = blockIdx.x * 256 + threadIdx.x, packs = size / 4;
+    if (i < packs)
+        join_elements<4>(A, 4 * i);
+    else if (i < packs + size % 4)
+        join_elements<1>(A, 3 * packs + i);
+}
+
 hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s) {
-    const int64_t size = (int64_t)a.dk * a.dv;
-    const int V = a.svec ? 4 : 1;
+    const int size = a.dk * a.dv;
     if (a.sq.seqs > 65535 || a.heads > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((size / V + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
-    if (V == 4)
-        hipLaunchKernelGGL((attn_join_kernel<4>), grid, dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((attn_join_kernel<1>), grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((size / 4 + size % 4 + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
+    hipLaunchKernelGGL(attn_join_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -105,12 +105,13 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
     const int lr = t / (DKP / 8), lc = t % (DKP / 8) * 8, lrv = t / (DVB / 8), lcv = t % (DVB / 8) * 8;
     const uint16_t* gq = static_cast<const uint16_t*>(A.q) + row0 * A.q_row + qh * A.q_head;
     const uint16_t* gk = static_cast<const uint16_t*>(A.k) + row0 * A.k_row + qh * A.k_head;
-    const uint16_t* gv = static_cast<const uint16_t*>(A.v) + row0 * A.v_row + head * A.v_head + c0;
+    const uint16_t* gv = static_cast<const uint16_t*>(A.v) + row0 * A.v_row + head * A.v_head;
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
     const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
-    const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
-    uint32_t q_at = live > 0 ? (lr * q_row + lc) * 2 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 2 : OOB_OFF;
-    uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 2 : OOB_OFF;
+    uint32_t cut, cut_v;  // (of q, k and of v: row_part)
+    uint32_t q_at = row_part<uint16_t, VEC>(lr * q_row, lc, A.dk, &cut);
+    uint32_t k_at = row_part<uint16_t, VEC>(lr * k_row, lc, A.dk, &cut);
+    uint32_t v_at = row_part<uint16_t, VEC>(lrv * v_row, c0 + lcv, A.dv, &cut_v);
     u32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
     float rg = 0.0f;
     auto load = [&](int64_t c) {  // chunk starting at token c of the segment into registers
@@ -118,14 +119,14 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
         if constexpr (!STATE_ONLY) {
             const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gq + c * A.q_row, n, q_row, A.dk);
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) rq[i] = load_row<uint16_t, VEC>(r, q_at + i * (RS * 2) * q_row, live);
+            for (int i = 0; i < NQ; ++i) rq[i] = load_row<uint16_t, VEC>(r, q_at + i * (RS * 2) * q_row, A.dk);
         }
         const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gk + c * A.k_row, n, k_row, A.dk);
-        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv - c0);
+        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) rk[i] = load_row<uint16_t, VEC>(r, k_at + i * (RS * 2) * k_row, live);
+        for (int i = 0; i < NQ; ++i) rk[i] = load_row<uint16_t, VEC>(r, k_at + i * (RS * 2) * k_row, A.dk);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) rv[i] = load_row<uint16_t, VEC>(rr, v_at + i * (RSV * 2) * v_row, live_v);
+        for (int i = 0; i < NV; ++i) rv[i] = load_row<uint16_t, VEC>(rr, v_at + i * (RSV * 2) * v_row, A.dv);
         if (wave == WAVES - 1) rg = load_decay(A, gg, c, lane, n);
     };
 
@@ -146,16 +147,17 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
         asm volatile("" : "+v"(o_st), "+v"(o_stv), "+v"(o_row), "+v"(o_k0), "+v"(o_k1), "+v"(o_pw), "+v"(o_pr),
                      "+v"(o_v0), "+v"(o_v1));
         asm volatile("" : "+v"(q_at), "+v"(k_at), "+v"(v_at), "+v"(l16), "+v"(quad), "+v"(lane));
+        if constexpr (!VEC) asm volatile("" : "+v"(cut), "+v"(cut_v));
         // registers to LDS; decays
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             // 8 rows further on the number of the row differs in its two low bits
             const uint32_t off = (RS == 8 && i % 2 ? o_st ^ (3u << 4) : o_st) + i * RS * 2 * DKP;
-            if constexpr (!STATE_ONLY) lds_write(sQ, off, rq[i]);
-            lds_write(sK, off, rk[i]);
+            if constexpr (!STATE_ONLY) lds_write(sQ, off, row_part_of<uint16_t, VEC>(rq[i], cut));
+            lds_write(sK, off, row_part_of<uint16_t, VEC>(rk[i], cut));
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) lds_write(sV, o_stv + i * RSV * 2 * DVB, rv[i]);
+        for (int i = 0; i < NV; ++i) lds_write(sV, o_stv + i * RSV * 2 * DVB, row_part_of<uint16_t, VEC>(rv[i], cut_v));
         if (wave == WAVES - 1) {
             const double tot = chunk_decays(rg, lane, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);

@@ -47,12 +47,14 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
     const int lr = t / (DKP / 4), lc = t % (DKP / 4) * 4, lrv = t / (DVB / 4), lcv = t % (DVB / 4) * 4;
     const float* gq = static_cast<const float*>(A.q) + row0 * A.q_row + qh * A.q_head;
     const float* gk = static_cast<const float*>(A.k) + row0 * A.k_row + qh * A.k_head;
-    const float* gv = static_cast<const float*>(A.v) + row0 * A.v_row + head * A.v_head + c0;
+    const float* gv = static_cast<const float*>(A.v) + row0 * A.v_row + head * A.v_head;
     const float* gg = A.g ? A.g + row0 * A.g_row + head : nullptr;
     const uint32_t q_row = (uint32_t)A.q_row, k_row = (uint32_t)A.k_row, v_row = (uint32_t)A.v_row;
-    const int live = A.dk - lc, live_v = A.dv - c0 - lcv;
-    uint32_t q_at = live > 0 ? (lr * q_row + lc) * 4 : OOB_OFF, k_at = live > 0 ? (lr * k_row + lc) * 4 : OOB_OFF;
-    uint32_t v_at = live_v > 0 ? (lrv * v_row + lcv) * 4 : OOB_OFF;
+    uint32_t cut, cut_v;  // (of q, k and of v: row_part)
+    uint32_t q_at = row_part<float, VEC>(lr * q_row, lc, A.dk, &cut);
+    uint32_t k_at = row_part<float, VEC>(lr * k_row, lc, A.dk, &cut);
+    uint32_t v_at = row_part<float, VEC>(lrv * v_row, c0 + lcv, A.dv, &cut_v);
+    auto part_of = [](u32x4 v, uint32_t c) { return row_part_of<float, VEC>(v, c); };
     u32x4 rq[STATE_ONLY ? 1 : NQ], rk[NQ], rv[NV];
     float rg = 0.0f;
     auto load = [&](int64_t c) {
@@ -60,14 +62,14 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
         if constexpr (!STATE_ONLY) {
             const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gq + c * A.q_row, n, q_row, A.dk);
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) rq[i] = load_row<float, VEC>(r, q_at + i * (RS * 4) * q_row, live);
+            for (int i = 0; i < NQ; ++i) rq[i] = load_row<float, VEC>(r, q_at + i * (RS * 4) * q_row, A.dk);
         }
         const __amdgpu_buffer_rsrc_t r = chunk_rsrc(gk + c * A.k_row, n, k_row, A.dk);
-        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv - c0);
+        const __amdgpu_buffer_rsrc_t rr = chunk_rsrc(gv + c * A.v_row, n, v_row, A.dv);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) rk[i] = load_row<float, VEC>(r, k_at + i * (RS * 4) * k_row, live);
+        for (int i = 0; i < NQ; ++i) rk[i] = load_row<float, VEC>(r, k_at + i * (RS * 4) * k_row, A.dk);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) rv[i] = load_row<float, VEC>(rr, v_at + i * (RSV * 4) * v_row, live_v);
+        for (int i = 0; i < NV; ++i) rv[i] = load_row<float, VEC>(rr, v_at + i * (RSV * 4) * v_row, A.dv);
         if (wave == WAVES - 1) rg = load_decay(A, gg, c, lane, n);
     };
 
@@ -77,13 +79,14 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
         const int n = (int)min<int64_t>(C, len - c);
         // what follows from these is cheaper computed again than kept in registers over the loop
         asm volatile("" : "+v"(q_at), "+v"(k_at), "+v"(v_at), "+v"(l16), "+v"(quad), "+v"(lane));
+        if constexpr (!VEC) asm volatile("" : "+v"(cut), "+v"(cut_v));
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-            if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = rq[i];
-            *reinterpret_cast<u32x4*>(&sK[(lr + i * RS) * QP + lc]) = rk[i];
+            if constexpr (!STATE_ONLY) *reinterpret_cast<u32x4*>(&sQ[(lr + i * RS) * QP + lc]) = part_of(rq[i], cut);
+            *reinterpret_cast<u32x4*>(&sK[(lr + i * RS) * QP + lc]) = part_of(rk[i], cut);
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = rv[i];
+        for (int i = 0; i < NV; ++i) *reinterpret_cast<u32x4*>(&sV[(lrv + i * RSV) * VP + lcv]) = part_of(rv[i], cut_v);
         if (wave == WAVES - 1) {
             const double tot = chunk_decays(rg, lane, sB, sD, sE, C);
             if (lane == 0) sTot = __builtin_amdgcn_exp2f((float)tot);

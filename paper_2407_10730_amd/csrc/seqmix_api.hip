@@ -113,7 +113,9 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 // more with each: 8 sequences, 16 heads of 128 x 128 bf16: 6.5, 7.5 and 7.6 us for 1, 2 and 3 tokens, a chunk 8.0; 256 sequences:
 // 113, 118 and 123 us, a chunk 116; fp32, 128 sequences: 58 to 69 us for 1 to 4 tokens, a chunk 78.
 // Its blocks have 32 columns (more workgroups; 64 sequences of 16 heads of 64 x 64: 10.9 us, with 128 columns 11.6) until
-// there are 8 such per CU, then 128 (256 sequences as above: 113 us, with 32 columns 116).
+// there are 8 such per CU, then 128 (256 sequences as above: 113 us, with 32 columns 116).  Where dv is no multiple of 32, blocks
+// share cache lines at their ends, and 128 are better from one per CU on (16 heads of 127 x 127, 4, 8 and 64 sequences: 7.9, 12.1 and
+// 43.8 us with 32 columns, 8.4, 9.3 and 24.7 with 128).
 //
 // A workgroup takes its chunks one after the other, about 5 us each (dk = dv = 128) with one workgroup per CU and 8 with two.
 // Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the segments are as
@@ -128,7 +130,7 @@ void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};
     const int64_t narrow = p.seqs * p.heads * ((p.dv + kTokensBlock - 1) / kTokensBlock);
-    d->block = narrow > 8 * kSeqmixCUs ? kTokensWide : kTokensBlock;
+    d->block = narrow > (p.dv % kTokensBlock ? 1 : 8) * kSeqmixCUs ? kTokensWide : kTokensBlock;
     if (p.tokens <= (p.dtype == CONV2D_BF16 ? 2 : 4) * p.seqs || !chunk_rows_near(p)) return;
     const int64_t chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
@@ -225,10 +227,7 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
     a.dv = p.dv;
     a.scale = p.scale;
     const int64_t unit = 16 / esize(p.dtype);
-    a.vec = p.dk % unit == 0 && p.dv % unit == 0 && p.q_row % unit == 0 && p.q_head % unit == 0 && p.k_row % unit == 0 &&
-            p.k_head % unit == 0 && p.v_row % unit == 0 && p.v_head % unit == 0 && p.o_row % unit == 0 &&
-            p.o_head % unit == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(o, 16);
-    a.svec = p.dv % 4 == 0 && aligned(state_in, 16) && aligned(state_out, 16);
+    a.vec = p.dk % unit == 0 && p.dv % unit == 0;
     a.block = d->block;
     a.ndvb = (p.dv + d->block - 1) / d->block;
     if (d->plan.kernel == SEQMIX_KERNEL_TOKENS) {

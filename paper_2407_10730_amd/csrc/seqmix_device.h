@@ -20,9 +20,10 @@ __device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) {  // the hardwa
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// N consecutive elements as they lie in memory, aligned to the largest power of two (16 at most) that divides their size.
+// N consecutive elements as they lie in memory, at any address that an element may have: 8 and 16 bytes are still one load
+// or store.
 template <typename T, int N>
-struct alignas((sizeof(T) * N & -(sizeof(T) * N)) < 16 ? (sizeof(T) * N & -(sizeof(T) * N)) : 16) Pack {
+struct Pack {
     T e[N];
 };
 template <typename T, int N>

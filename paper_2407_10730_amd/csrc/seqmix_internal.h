@@ -41,8 +41,7 @@ struct AttnArgs {
     int32_t dk, dv;
     int32_t block, ndvb;  // state columns per workgroup, such blocks per head
     float scale;
-    int32_t vec;          // pointers and strides allow wide loads of q, k, v; stores of o
-    int32_t svec;         // ... of the states
+    int32_t vec;          // dk and dv are multiples of 16 bytes of q, k and v
     // segments: `segment` tokens each; ids offsets[i] / segment + i + (segment of sequence i)
     int64_t segment, nseg;
     float* ws_state;      // [nseg][heads][dk][dv]

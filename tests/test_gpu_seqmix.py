@@ -209,6 +209,28 @@ def test_attention_strides(dtype, lens, kw):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[1] * 2, [3] * 160, [150, 0, 40], [700]], ids=["1x2", "3x160", "150,0,40", "700"])
+@pytest.mark.parametrize("dk,dv", [(9, 8), (8, 13), (3, 5), (7, 130), (131, 2), (15, 129), (127, 3), (250, 67), (2, 1),
+                                   (36, 189), (68, 98)])
+def test_attention_odd_heads_between_nan(dtype, lens, dk, dv):
+    """Rows end inside a load, and what lies beside them is no operand and stays as it is."""
+    def edit(a):
+        for t in (a.q, a.k, a.v):
+            keep = t.clone()
+            t._base.fill_(float("nan"))
+            t.copy_(keep)
+        a.o._base.fill_(5.0)
+
+    a = Attn(lens, 2, 1, dk, dv, dtype=dtype, pad=3, shift=1, edit=edit, uniform=False)
+    left = torch.full((a.slots + 1, a.heads, dk, dv), 3.0, device="cuda")
+    a.run(a.state, left[:-1]).check(left[:-1])
+    a.o.fill_(5.0)
+    assert bool((a.o._base == 5.0).all()) and bool((left[-1] == 3.0).all())
+    left[:-1] = a.state  # in place
+    a.run(left[:-1], left[:-1]).check(left[:-1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[1, 1, 1], [4, 4, 4], [150, 70, 0], [700]])
 def test_attention_decays_that_clear_the_state(dtype, lens):
     """-infinity (and the type's lowest value) as the log of a decay, also many of them and of other sizes between."""
