@@ -164,18 +164,17 @@ hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s)
 // zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring elements of a state (from
 // e on) and walks along the segments, AHEAD loads ahead of the sum.  Bound by its bytes, 8 dk dv per segment and head.
 template <int V>
-__device__ __forceinline__ void join_elements(const AttnArgs& A, int64_t e) {
+__device__ __forceinline__ void join_elements(const AttnArgs& A, int seq, int64_t e) {
     constexpr int AHEAD = 8;
     const int64_t size = (int64_t)A.dk * A.dv;
     const int head = blockIdx.y;
-    const int seq = blockIdx.z;
     const SeqRange r = seq_range(A.sq, seq);
+    const uint32_t seg = (uint32_t)A.segment;
+    if (r.len <= A.alone) return;  // starts from its own state
     const int64_t slot = seq_slot(A.sq, seq);
     if (slot < 0) return;
-    const uint32_t seg = (uint32_t)A.segment;
-    const uint32_t len = (uint32_t)r.len, own = len > seg ? (len + seg - 1) / seg : 1;
-    const int64_t first = A.sq.off ? (uint32_t)r.first / seg + seq : (int64_t)seq * own;
-    const int parts = (int)min<int64_t>(own, A.nseg - first);  // (offsets that lie)
+    const int64_t first = (uint32_t)A.ws_mul * (uint32_t)r.first / seg;
+    const int parts = (int)min<int64_t>(((uint32_t)r.len + seg - 1) / seg, A.nws - first);
     float S[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) S[v] = 0.0f;
@@ -205,16 +204,21 @@ __device__ __forceinline__ void join_elements(const AttnArgs& A, int64_t e) {
 // Four elements per thread, and one in the threads of the last three.
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs A) {
     const int size = A.dk * A.dv, i = blockIdx.x * 256 + threadIdx.x, packs = size / 4;
-    if (i < packs)
-        join_elements<4>(A, 4 * i);
-    else if (i < packs + size % 4)
-        join_elements<1>(A, 3 * packs + i);
+    for (int seq = blockIdx.z; seq < A.sq.seqs; seq += gridDim.z) {
+        if (i < packs)
+            join_elements<4>(A, seq, 4 * i);
+        else if (i < packs + size % 4)
+            join_elements<1>(A, seq, 3 * packs + i);
+    }
 }
 
 hipError_t launch_attn_join(const AttnArgs& a, hipStream_t s) {
     const int size = a.dk * a.dv;
-    if (a.sq.seqs > 65535 || a.heads > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((size / 4 + size % 4 + 255) / 256), (unsigned)a.heads, (unsigned)a.sq.seqs);
+    if (a.heads > 65535) return hipErrorInvalidValue;
+    // (most sequences of a large batch are not cut: 16 workgroups per CU share them)
+    const int blocks = (size / 4 + size % 4 + 255) / 256;
+    const int64_t across = std::max<int64_t>(16 * kSeqmixCUs / ((int64_t)blocks * a.heads), 1);
+    const dim3 grid((unsigned)blocks, (unsigned)a.heads, (unsigned)std::min<int64_t>(across, a.sq.seqs));
     hipLaunchKernelGGL(attn_join_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }

@@ -286,12 +286,12 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
 
     float* s_left = attn_last_state(A, pl, STATE_ONLY);
     if (s_left) store_state<8, 4>(A, s_left, c0 + wc + l16, quad, S);
-    if (STATE_ONLY && pl.blk == 0 && t == NTHR - 1) A.ws_decay[(int64_t)pl.id * A.heads + head] = (float)whole;
+    if (STATE_ONLY && pl.blk == 0 && t == NTHR - 1) A.ws_decay[pl.ws * A.heads + head] = (float)whole;
 }
 
 template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
-    const int64_t blocks = (a.segment ? a.nseg : a.sq.seqs) * a.heads * a.ndvb;
+    const int64_t blocks = (a.ids * a.units + 7) / 8 * 8 * a.unit;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(64 * WAVES);
     const int f32 = odt == CONV2D_F32;

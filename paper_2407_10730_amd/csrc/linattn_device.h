@@ -10,25 +10,29 @@ typedef double f64x2 __attribute__((ext_vector_type(2)));
 // What a workgroup of a chunk kernel runs: tokens [row0, row0 + len) for one head and block of columns.
 struct AttnPlace {
     int head, blk;
-    int id;
+    int64_t ws;  // place in the workspace (of a cut sequence)
     int64_t slot, row0, len;
-    bool last;  // the end of its sequence
+    bool cut, last;  // a segment; the end of its sequence
 };
-// False: nothing (in all threads of the workgroup).  Consecutive ids (column blocks, then heads, of the same tokens)
-// go to the same XCD, where they share q and k in its L2.
+// False: nothing (in all threads of the workgroup).  Heads that share q and k, and their column blocks, go to the same XCD,
+// where they share them in its L2; these units go to the XCDs in turn, as ids without work may lie side by side (8 sequences of 200
+// tokens, 16 heads of 128 x 128: 27 us, with neighbouring ids on one XCD 34).
 __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, AttnPlace* out) {
-    const int bid = xcd_remap(blockIdx.x, gridDim.x);
-    const int hid = bid / A.ndvb;
-    out->blk = bid - hid * A.ndvb;
-    out->id = hid / A.heads;
-    out->head = hid - out->id * A.heads;
-    SeqPart sp{out->id, 0};
-    if (A.segment) sp = seq_part(A.sq, out->id, (uint32_t)A.segment);
+    const uint32_t j = blockIdx.x / 8, round = j / (uint32_t)A.unit, u = blockIdx.x % 8 + 8 * round;
+    const int id = u / (uint32_t)A.units;
+    if (id >= A.ids) return false;
+    const uint32_t at = (u - id * A.units) * A.unit + (j - round * A.unit);
+    out->head = at / (uint32_t)A.ndvb;
+    out->blk = at - out->head * A.ndvb;
+    SeqPart sp{id, 0};
+    if (A.segment) sp = seq_part(A.sq, id, (uint32_t)A.segment, A.places, A.ws_mul);
     if (sp.seq >= A.sq.seqs || sp.part < 0) return false;
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t start = sp.part * A.segment;
-    if (sp.part > 0 && start >= r.len) return false;
-    out->last = !A.segment || r.len - start <= A.segment;
+    out->cut = A.segment && r.len > A.alone;
+    if (sp.part > 0 && (!out->cut || start >= r.len)) return false;  // (the first of these where none is left)
+    out->last = !out->cut || r.len - start <= A.segment;
+    out->ws = out->cut ? (uint32_t)A.ws_mul * (uint32_t)r.first / (uint32_t)A.segment + sp.part : 0;
     if (state_only && out->last) return false;
     out->slot = seq_slot(A.sq, sp.seq);
     out->len = out->last ? r.len - start : A.segment;
@@ -37,12 +41,12 @@ __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, A
 }
 __device__ __forceinline__ const float* attn_first_state(const AttnArgs& A, const AttnPlace& p) {
     const int64_t size = (int64_t)A.dk * A.dv;
-    if (A.segment) return A.ws_state + ((int64_t)p.id * A.heads + p.head) * size;
+    if (p.cut) return A.ws_state + (p.ws * A.heads + p.head) * size;
     return A.s_in ? A.s_in + (p.slot * A.heads + p.head) * size : nullptr;
 }
 __device__ __forceinline__ float* attn_last_state(const AttnArgs& A, const AttnPlace& p, bool state_only) {
     const int64_t size = (int64_t)A.dk * A.dv;
-    if (state_only) return A.ws_state + ((int64_t)p.id * A.heads + p.head) * size;
+    if (state_only) return A.ws_state + (p.ws * A.heads + p.head) * size;
     return p.last && A.s_out ? A.s_out + (p.slot * A.heads + p.head) * size : nullptr;
 }
 

@@ -9,7 +9,8 @@ using namespace cv;
 struct seqmix_attn_desc {
     seqmix_attn_params p;
     seqmix_attn_plan_info plan;
-    int32_t block = 0;  // state columns per workgroup
+    int32_t block = 0, block_uncut = 0;  // state columns per workgroup; of chunk kernels where no sequence is cut
+    int64_t alone = 0;  // packed sequences of up to this many tokens are not cut
     // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
     void* ws = nullptr;
     int device = -1;
@@ -107,6 +108,29 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
     return std::max({p.q_row, p.k_row, p.v_row, p.o_row, (int64_t)p.heads}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
 }
 
+// Sequences of one length up to this are not cut: the chain of their chunks would be shortened by less than cutting costs.
+int64_t alone(int64_t segment, int64_t chunk) { return (3 * segment + 10 * chunk) / 2; }
+
+// ... of packed sequences, where a longer one may make the other launches necessary in any case: those of up to a segment and a chunk, and
+// those near the average where that is short or where the sequences fill half of the CUs as they are (8 of 500, 16 heads of 128 x 128: 40
+// us, all cut in segments of 192: 57).
+int64_t alone_packed(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64_t groups) {
+    const bool even = p.tokens <= 5 * chunk * p.seqs || 2 * groups >= kSeqmixCUs;
+    return std::max(segment + chunk, even ? p.tokens / p.seqs * 9 / 8 : 0);
+}
+
+// State columns of a workgroup of the chunk kernels, of which there are `groups` with the wider blocks: 64 also where the last 128 would be
+// half empty (8192 tokens, 16 heads of 128 x 192: 97 us, 100; fp32, 4096 tokens: 130, 148).
+int64_t chunk_columns(const seqmix_attn_params& p) { return (p.dv - 1) % 128 < 64 ? 64 : 128; }
+int32_t chunk_block(const seqmix_attn_params& p, int64_t groups) {
+    return (int32_t)(groups * 2 <= kSeqmixCUs ? 64 : chunk_columns(p));
+}
+
+// Places for segments' states in the workspace.
+int64_t ws_places(const seqmix_attn_params& p, int64_t segment) {
+    return p.seqs == 1 ? (p.tokens + segment - 1) / segment : 2 * p.tokens / segment;
+}
+
 // Kernel, state columns per workgroup (block) and where sequences are cut.
 //
 // Up to 2 tokens per sequence (fp32: 4) go token by token.  A chunk costs the same for 1 token as for 64, the token kernel
@@ -121,9 +145,12 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 // Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the segments are as
 // long as 256 workgroups allow, or 512 where those still have 8 chunks each: 8192 tokens, 16 heads of 128 x 128 bf16:
 // 71 us in segments of 512, 75 of 256, 78 of 384 (a part of the CUs has two), 110 of 1024; 65536 tokens, 8 heads: 227 us
-// in segments of 1024, 237 of 2048, 242 of 512.  Packed sequences of unknown lengths take 512 (5664 tokens in 10 sequences, 12
-// heads of 64 x 128: 41 us in segments of 192, 45 of 256, 50 of 512).
-// Sequences of up to 5 chunks are not cut (100 tokens: 7.6 us, cut 13.6; 300: 17.4 either way).
+// in segments of 1024, 237 of 2048, 242 of 512.  Sequences of up to 5 chunks are not cut (100 tokens: 7.6 us, cut 13.6; 300: 17.4
+// either way).
+// Packed sequences, whose lengths the host does not know, take 512 (5664 tokens in 10 sequences, 12 heads of 64 x 128: 41 us in segments of 192,
+// 45 of 256, 50 of 512); the kernels cut the longer ones (alone_packed).  They may be one long prompt among single tokens
+// (1, 570, 3, 1 tokens, 1 head of 191 x 128: 22 us, uncut 61; 64 of 1 and one of 1000, 16 heads of 128 x 128: 57, uncut 78) or of one
+// length, where the other launches are wasted (4 of 150, 4 heads: 17 us, uncut 12.4).
 // Where 128-column blocks leave half of the CUs empty, blocks of 64 (1024 tokens, 8 heads: 19.7 us, 21.4; 300 tokens:
 // 17.3, 21.8).
 void plan_attn(seqmix_attn_desc* d) {
@@ -135,24 +162,23 @@ void plan_attn(seqmix_attn_desc* d) {
     const int64_t chunk = p.dtype == CONV2D_BF16 ? kChunk : kChunkF32;
     d->plan.kernel = SEQMIX_KERNEL_CHUNKS;
     d->plan.chunk = (int32_t)chunk;
-    const int64_t wide = p.dv <= 64 ? 64 : 128;
-    const int64_t across = p.heads * ((p.dv + wide - 1) / wide);
-    int64_t groups = p.seqs * across;  // workgroups
-    if (p.tokens > 5 * chunk * p.seqs && groups < 2 * kSeqmixCUs) {
+    const int64_t across = p.heads * ((p.dv + 127) / 128);
+    const int64_t groups = p.seqs * across;  // workgroups, uncut
+    d->block = d->block_uncut = chunk_block(p, groups);
+    if (groups < 2 * kSeqmixCUs || p.tokens < chunk * p.seqs) {
         auto length = [&](int64_t want) {  // of segments, such that there are about `want` workgroups
-            const int64_t parts = std::max<int64_t>(want / across - (p.seqs > 1 ? p.seqs : 0), 1);
+            const int64_t all = want / across, parts = std::max<int64_t>(p.seqs > 1 ? std::max(all - p.seqs, all / 2) : all, 1);
             return ((p.tokens + parts - 1) / parts + kChunk - 1) / kChunk * kChunk;
         };
         int64_t seg = length(2 * kSeqmixCUs);
         if (p.seqs == 1 && seg < 8 * chunk) seg = length(kSeqmixCUs);
-        const int64_t ids = p.tokens / seg + p.seqs;
-        if (seg < p.tokens) {
+        if (p.tokens > alone(seg, chunk)) {
             d->plan.segment = seg;
-            d->plan.workspace_bytes = ids * p.heads * ((int64_t)p.dk * p.dv * 4 + 4);
-            groups = (p.seqs == 1 ? (p.tokens + seg - 1) / seg : ids) * across;
+            d->alone = alone_packed(p, seg, chunk, groups);
+            d->plan.workspace_bytes = ws_places(p, seg) * p.heads * ((int64_t)p.dk * p.dv * 4 + 4);
+            d->block = chunk_block(p, std::max<int64_t>((p.tokens + seg - 1) / seg, p.seqs) * across);
         }
     }
-    d->block = (int32_t)(groups * 2 <= kSeqmixCUs ? 64 : wide);
 }
 
 }  // namespace
@@ -228,25 +254,32 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
     a.scale = p.scale;
     const int64_t unit = 16 / esize(p.dtype);
     a.vec = p.dk % unit == 0 && p.dv % unit == 0;
-    a.block = d->block;
-    a.ndvb = (p.dv + d->block - 1) / d->block;
-    if (d->plan.kernel == SEQMIX_KERNEL_TOKENS) {
+    const bool chunked = d->plan.kernel == SEQMIX_KERNEL_CHUNKS;
+    const bool cut = d->plan.segment > 0 && (offsets || a.sq.seq_len > alone(d->plan.segment, d->plan.chunk));
+    a.block = chunked && !cut ? d->block_uncut : d->block;
+    a.ndvb = (p.dv + a.block - 1) / a.block;
+    if (!chunked) {
         return launch_attn_tokens(a, p.dtype, p.o_dtype, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     }
     auto chunks = [&](bool state_only) {
+        a.places = state_only && offsets && a.nws < a.nseg;
+        a.ids = !cut ? p.seqs : a.places ? a.nws : a.nseg;
+        // heads that share q and k, and their column blocks, stay together where there are units for all XCDs
+        a.unit = a.ids * p.qk_heads >= 16 ? a.rep * a.ndvb : 1;
+        a.units = p.heads * a.ndvb / a.unit;
         return p.dtype == CONV2D_BF16 ? launch_attn_chunks_bf16(a, p.o_dtype, state_only, s)
                                       : launch_attn_chunks_f32(a, state_only, s);
     };
-    // sequences of known length are cut where that shortens the chain of their chunks by more than it costs
-    if (d->plan.segment == 0 ||
-        (!offsets && (a.sq.seq_len <= d->plan.segment || 2 * a.sq.seq_len <= 3 * d->plan.segment + 10 * d->plan.chunk)))
-        return chunks(false) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+    if (!cut) return chunks(false) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
     SM_TRY(ensure_ws(d));
     SM_TRY(order_after_last(d, s));
     a.segment = d->plan.segment;
+    a.alone = offsets ? d->alone : a.segment;
     a.nseg = seq_part_ids(a.sq, a.segment);
+    a.ws_mul = p.seqs == 1 ? 1 : 2;
+    a.nws = ws_places(p, a.segment);
     a.ws_state = static_cast<float*>(d->ws);
-    a.ws_decay = a.ws_state + (p.tokens / a.segment + p.seqs) * p.heads * p.dk * p.dv;
+    a.ws_decay = a.ws_state + a.nws * p.heads * p.dk * p.dv;
     if (chunks(true) != hipSuccess || launch_attn_join(a, s) != hipSuccess || chunks(false) != hipSuccess)
         return CONV2D_E_HIP;
     return CONV2D_OK;

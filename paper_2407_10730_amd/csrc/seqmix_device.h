@@ -82,11 +82,13 @@ __device__ __forceinline__ int64_t seq_slot(const SeqArgs& a, int i) {
 // sequence i owns the ids [offsets[i] / size + i, offsets[i+1] / size + i + 1), at least
 // ceil(len / size) and at least one, so the ids of a call are below tokens / size + seqs.  Sequences of
 // equal length own exactly as many as they have parts (seq_parts).
+// `places` (with offsets): from mul offsets[i] / size on instead, without an id of their own for sequences without parts.
 struct SeqPart {
     int seq;
     int part;  // number of the part within the sequence; negative: none (offsets that lie)
 };
-__device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint32_t size) {
+__device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint32_t size, bool places = false,
+                                            uint32_t mul = 1) {
     if (!a.off) {
         const uint32_t len = (uint32_t)a.seq_len, per = len > size ? (len + size - 1) / size : 1;
         const uint32_t i = id / per;
@@ -94,17 +96,18 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint3
     }
     // the last sequence whose first id is at most `id`: a wave's lanes look at 64 of them at a time, so that the
     // search waits for memory once up to 64 sequences and twice up to 4096 (all lanes of the wave take part)
+    auto first_id = [&](int i) { return (places ? mul : 1u) * clamp_row(a.off[i], a.tokens) / size + (places ? 0 : i); };
     int lo = 0;
     const int lane = threadIdx.x & 63;
     for (int n = a.seqs; n > 1;) {
         const int step = (n + 63) / 64, i = lane * step;
-        const bool at_most = i < n && clamp_row(a.off[lo + i], a.tokens) / size + (lo + i) <= id;
+        const bool at_most = i < n && first_id(lo + i) <= id;
         const int k = max(__popcll(__ballot(at_most)) - 1, 0);
         lo += k * step;
         n = min(step, n - k * step);
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    return {lo, (int)id - (int)(clamp_row(a.off[lo], a.tokens) / size + lo)};
+    return {lo, (int)id - (int)first_id(lo)};
 }
 
 // Log2 of a decay from its natural log.  Logs below -1000 (-infinity among them) have an

@@ -42,10 +42,17 @@ struct AttnArgs {
     int32_t block, ndvb;  // state columns per workgroup, such blocks per head
     float scale;
     int32_t vec;          // dk and dv are multiples of 16 bytes of q, k and v
-    // segments: `segment` tokens each; ids offsets[i] / segment + i + (segment of sequence i)
-    int64_t segment, nseg;
-    float* ws_state;      // [nseg][heads][dk][dv]
-    float* ws_decay;      // [nseg][heads]: log of a segment's whole decay, times log2(e)
+    // Sequences of more than `alone` tokens (more than `segment`) are cut in segments: ids offsets[i] / segment + i + (segment
+    // of sequence i), of which only the first has work where a sequence is not cut.  Only cut ones have a place in the
+    // workspace, ws_mul * offsets[i] / segment + (segment of sequence i): with ws_mul 2 the ranges of two cut sequences are apart, as
+    // 2 len / segment, rounded down, is at least len / segment, rounded up.
+    int64_t segment, alone, nseg, nws;
+    int32_t ws_mul;
+    int32_t places;       // the ids of this pass number places of the workspace
+    int64_t ids;          // of this pass: sequences, segments or places
+    int32_t unit, units;  // workgroups of an id that stay on one XCD, such units per id
+    float* ws_state;      // [nws][heads][dk][dv]
+    float* ws_decay;      // [nws][heads]: log of a segment's whole decay, times log2(e)
 };
 
 constexpr int kTokensBlock = 32, kTokensWide = 128;  // state columns of a workgroup of the token kernel

@@ -187,6 +187,20 @@ def test_attention_in_segments(dtype, lens, uniform):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,qk_heads", [(2, 1), (16, 16)])
+@pytest.mark.parametrize("lens", [[1] * 64 + [1000], [1] * 20 + [700, 0, 0, 650] + [1] * 30 + [129], [570, 1, 3],
+                                  [64, 65, 96, 97, 127, 128, 129, 130, 191, 192, 193, 300]], ids=lambda x: f"{len(x)}-{sum(x)}")
+def test_attention_some_cut(dtype, heads, qk_heads, lens):
+    """Packs of which the long sequences are cut and the others are not, in place in a pool."""
+    a = Attn(lens, heads, qk_heads, 64, 72, dtype=dtype, pool=3, uniform=False)
+    plan = a.op.plan()
+    assert plan.kernel == M.SEQMIX_KERNEL_CHUNKS and 0 < plan.segment < max(lens)
+    left, other = a.state.clone(), np.setdiff1d(np.arange(a.slots), a.index)
+    a.run(left, left).check(left)
+    assert torch.equal(left[other], a.state[other])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[3], [100]])
 def test_attention_growing_decays(dtype, lens):
     """Log decays above 0, growing by far more than a chunk's terms are of."""
