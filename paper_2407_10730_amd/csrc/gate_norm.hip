@@ -35,8 +35,8 @@ struct Vec {
         if constexpr (kEarly) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                const int c = (i * TPR + threadIdx.x % TPR) * V;
-                if (p && c < n) load_pack<float, V>(p + c, e[i]);
+                const RowPlace<V> at((i * TPR + threadIdx.x % TPR) * V, n);
+                if (p && at.on) load_pack<float, V>(p + at.c, e[i]);
             }
         }
     }
@@ -50,12 +50,25 @@ struct Vec {
     }
 };
 
+// Zeros in the places that the thread does not own.
+template <int TPR, int V, int ITEMS>
+__device__ __forceinline__ void clear_unowned(float (&x)[ITEMS][V], int n) {
+    if (V == 1 || n % V == 0) return;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const RowPlace<V> at((i * TPR + threadIdx.x % TPR) * V, n);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[i][v] = v < at.skip ? 0.0f : x[i][v];
+    }
+}
+
 // Norms x in place: V * ITEMS values per thread, those at or past `n` being zero.
 template <int TPR, int V, int ITEMS, bool EARLY>
 __device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, float eps, const Vec<TPR, V, ITEMS, EARLY>& w,
                                               const Vec<TPR, V, ITEMS, EARLY>& b, int n, float* red) {
     const int t = threadIdx.x % TPR;
     const float inv = 1.0f / (float)n;
+    clear_unowned<TPR, V, ITEMS>(x, n);
     if (kind == SEQMIX_NORM_LAYER) {
         float s = 0.0f;
 #pragma unroll
@@ -67,6 +80,7 @@ __device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, fl
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) x[i][v] = (i * TPR + t) * V < n ? x[i][v] - mean : 0.0f;
+        clear_unowned<TPR, V, ITEMS>(x, n);
     }
     float s = 0.0f;
 #pragma unroll
@@ -76,14 +90,14 @@ __device__ __forceinline__ void norm_in_place(float (&x)[ITEMS][V], int kind, fl
     const float r = 1.0f / sqrtf(fmaf(group_sum<TPR>(s, red), inv, eps));
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + t) * V;
-        if (c < n) {
+        const RowPlace<V> at((i * TPR + t) * V, n);
+        if (at.on) {
             float e[V];
-            w.get(i, c, e);
+            w.get(i, at.c, e);
 #pragma unroll
             for (int v = 0; v < V; ++v) x[i][v] *= r * e[v];
             if (b.p) {
-                b.get(i, c, e);
+                b.get(i, at.c, e);
 #pragma unroll
                 for (int v = 0; v < V; ++v) x[i][v] += e[v];
             }
@@ -111,13 +125,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     const TR* rp = static_cast<const TR*>(A.res) + (A.res ? row * A.res_row + col : 0);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + t) * V;
+        const RowPlace<V> at((i * TPR + t) * V, n);
 #pragma unroll
         for (int v = 0; v < V; ++v) x[i][v] = 0.0f;
-        if (c < n) {
-            load_pack<T, V>(u + c, x[i]);
-            if (A.gate) gate[i] = *reinterpret_cast<const Pack<T, V>*>(gp + c);
-            if (A.res) res[i] = *reinterpret_cast<const Pack<TR, V>*>(rp + c);
+        if (at.on) {
+            load_pack<T, V>(u + at.c, x[i]);
+            if (A.gate) gate[i] = *reinterpret_cast<const Pack<T, V>*>(gp + at.c);
+            if (A.res) res[i] = *reinterpret_cast<const Pack<TR, V>*>(rp + at.c);
         }
     }
     const Vec<TPR, V, ITEMS, EARLY> post_w(A.post_w, n), post_b(A.post_b, n), scale_vec(A.scale_vec ? A.scale_vec + col : nullptr, n),
@@ -142,18 +156,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     TR* yp = static_cast<TR*>(A.y) + (A.y ? row * A.y_row + col : 0);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + t) * V;
-        if (c < n) {
+        const RowPlace<V> at((i * TPR + t) * V, n);
+        if (at.on) {
             float e[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) e[v] = 1.0f;
-            if (scale_vec.p) scale_vec.get(i, c, e);
+            if (scale_vec.p) scale_vec.get(i, at.c, e);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 x[i][v] *= A.scale * e[v];
                 if (A.res) x[i][v] += to_f32(res[i].e[v]);
             }
-            if (A.y && live) store_result<TR, V>(yp + c, x[i], A.past);
+            if (A.y && live) store_owned<TR, V>(yp + at.c, x[i], at.skip, A.past);
         }
     }
     if (A.pre == SEQMIX_NORM_NONE) return;
@@ -161,8 +175,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     T* hp = static_cast<T*>(A.h) + row * A.h_row + col;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + t) * V;
-        if (c < n && live) store_result<T, V>(hp + c, x[i], A.past);
+        const RowPlace<V> at((i * TPR + t) * V, n);
+        if (at.on && live) store_owned<T, V>(hp + at.c, x[i], at.skip, A.past);
     }
 }
 

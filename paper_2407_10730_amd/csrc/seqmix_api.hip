@@ -52,7 +52,6 @@ int seq_args(int64_t tokens, int64_t seqs, int64_t slots, const int64_t* off, co
     return CONV2D_OK;
 }
 
-bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
 
 // Rows `row` elements apart, heads `head` elements apart, of `dim` elements each, can hold what they should.
 bool strides_ok(int64_t tokens, int64_t row, int64_t heads, int64_t head, int64_t dim) {
@@ -324,9 +323,7 @@ int seqmix_conv_fwd(const seqmix_conv_desc* d, const void* x, const void* w, con
     a.channels = (int32_t)p.channels;
     a.width = p.width;
     a.silu = p.act == SEQMIX_ACT_SILU;
-    const int64_t unit = 16 / esize(p.dtype);
-    a.vec = p.channels % unit == 0 && p.x_row % unit == 0 && p.y_row % unit == 0 && aligned(x, 16) && aligned(y, 16) &&
-            aligned(w, 16) && aligned(a.bias, 16) && aligned(a.win_in, 16) && aligned(a.win_out, 16);
+    a.vec = p.channels >= 16 / esize(p.dtype);
     a.past = p.tokens * p.channels * esize(p.dtype) >= kPastBytes;
     return launch_token_conv(a, p.dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
@@ -395,12 +392,7 @@ int seqmix_norm_fwd(const seqmix_norm_desc* d, const void* u, const float* post_
     a.scale = p.scale;
     a.post_eps = p.post_eps;
     a.pre_eps = p.pre_eps;
-    const int64_t unit = 16 / esize(p.dtype);
-    a.vec = p.group % unit == 0 && aligned(a.post_w, 16) && aligned(a.post_b, 16) && aligned(a.scale_vec, 16) &&
-            aligned(a.pre_w, 16) && aligned(a.pre_b, 16) && aligned(u, 16) && p.u_row % unit == 0 &&
-            (!a.gate || (aligned(gate, 16) && p.gate_row % unit == 0)) &&
-            (!a.res || (aligned(residual, 16) && p.res_row % unit == 0)) &&
-            (!y || (aligned(y, 16) && p.y_row % unit == 0)) && (!a.h || (aligned(h, 16) && p.h_row % unit == 0));
+    a.vec = p.group >= 16 / esize(p.dtype);
     a.past = p.rows * p.width * ((y ? esize(p.res_dtype) : 0) + (pre ? esize(p.dtype) : 0)) >= kPastBytes;
     return launch_norm(a, p.dtype, p.res_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK
                                                                                                : CONV2D_E_HIP;

@@ -6,6 +6,8 @@
 
 namespace cv {
 
+typedef u32x4 u32x4_any __attribute__((aligned(2)));  // at any address that an element may have
+
 constexpr float kLog2e = 1.4426950408889634f;
 
 // 16-bit storage stands for bf16 throughout (uint16_t).
@@ -40,6 +42,19 @@ __device__ __forceinline__ void store_pack(T* p, const float (&in)[N]) {
     *reinterpret_cast<Pack<T, N>*>(p) = v;
 }
 
+// The N of a thread's elements of a row of n >= N (N is 1, or fewer than N are one by one): from `first` on, and where that passes
+// the end the row's last N, of which the thread owns those from `skip` on.
+template <int N>
+struct RowPlace {
+    int c, skip;
+    bool on;
+    __device__ __forceinline__ RowPlace(int first, int n) {
+        on = first < n;
+        c = on ? min(first, n - N) : first;
+        skip = first - c;
+    }
+};
+
 // ... past the caches where `past` (full 16-byte stores only): results larger than the L2s push out what is still to be
 // read, and their lines are not fetched for writing.
 template <typename T, int N>
@@ -50,12 +65,24 @@ __device__ __forceinline__ void store_result(T* p, const float (&in)[N], bool pa
     if constexpr (sizeof(v) == 16) {
         if (past) {
             asm volatile("" ::: "memory");  // or the two stores become one, without the hint
-            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4_any, v), reinterpret_cast<u32x4_any*>(p));
             asm volatile("" ::: "memory");
             return;
         }
     }
     *reinterpret_cast<Pack<T, N>*>(p) = v;
+}
+
+// ... of those from `skip` on.
+template <typename T, int N>
+__device__ __forceinline__ void store_owned(T* p, const float (&in)[N], int skip, bool past) {
+    if (N == 1 || skip == 0) {
+        store_result<T, N>(p, in, past);
+    } else {
+#pragma unroll
+        for (int i = 1; i < N; ++i)
+            if (i >= skip) p[i] = from_f32<T>(in[i]);
+    }
 }
 
 // Rows [first, first + len) of sequence i, clamped so that no offsets lead outside the call's rows.  Row numbers, slots

@@ -18,8 +18,9 @@ constexpr int kConvTile = 32, kConvTileFew = 8, kConvAhead = 8;
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
     const SeqPart sp = seq_part(A.sq, blockIdx.y + blockIdx.z * 65535u, tile);
-    const int c = (blockIdx.x * 256 + threadIdx.x) * V;
-    if (c >= A.channels || sp.seq >= A.sq.seqs) return;
+    const RowPlace<V> at((blockIdx.x * 256 + threadIdx.x) * V, A.channels);
+    const int c = at.c;
+    if (!at.on || sp.seq >= A.sq.seqs) return;
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t t0 = (int64_t)sp.part * tile;
     if (sp.part < 0 || (sp.part > 0 && t0 >= r.len)) return;
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
                             for (int v = 0; v < V; ++v) e[v] = row[j][v];
                         }
                 }
-                store_pack<T, V>(out + (int64_t)i * A.channels, e);
+                store_owned<T, V>(out + (int64_t)i * A.channels, e, at.skip, false);
             }
         }
     }
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) void token_conv_kernel(ConvArgs A, int tile) {
                     for (int i = 0; i < W; ++i) o[v] = fmaf(w[v * W + i], row[i][v], o[v]);
                     if (A.silu) o[v] = silu(o[v]);
                 }
-                store_result<T, V>(y + (int64_t)(t + u) * A.y_row, o, A.past);
+                store_owned<T, V>(y + (int64_t)(t + u) * A.y_row, o, at.skip, A.past);
 #pragma unroll
                 for (int i = 0; i + 1 < W; ++i)
 #pragma unroll
