@@ -113,7 +113,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     int64_t id = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     const bool live = id < A.rows;  // TPR > 64 has one group per block: all its threads agree
     id = live ? id : A.rows - 1;
-    const int64_t row = id / A.ngroups;
+    // (64-bit divisions take longer than a small group's sums: 8105 x 4096 bf16 by groups of 128 53.2 us, 49.9; 64 x 200 4.3, 4.0)
+    const bool few = A.rows <= 0x7fffffff;
+    const int64_t row = few ? fdiv((uint32_t)id, A.by_groups) : id / A.ngroups;
     const int64_t col = (id - row * A.ngroups) * A.group;
     const int n = A.group;
 
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     Pack<T, V> gate[ITEMS];
     Pack<TR, V> res[ITEMS];
     const T* u = static_cast<const T*>(A.u) + row * A.u_row + col;
-    const T* gp = static_cast<const T*>(A.gate) + (A.gate ? (row / A.gate_run) * A.gate_row + col : 0);
+    const T* gp = static_cast<const T*>(A.gate) + (A.gate ? (int64_t)fdiv((uint32_t)row, A.by_run) * A.gate_row + col : 0);
     const TR* rp = static_cast<const TR*>(A.res) + (A.res ? row * A.res_row + col : 0);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {

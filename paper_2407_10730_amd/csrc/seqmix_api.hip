@@ -383,7 +383,8 @@ int seqmix_norm_fwd(const seqmix_norm_desc* d, const void* u, const float* post_
     a.ngroups = (int32_t)(p.width / p.group);
     a.rows = p.rows * a.ngroups;
     a.group = (int32_t)p.group;
-    a.gate_run = p.gate_run;
+    a.by_groups = make_fastdiv((uint32_t)a.ngroups);
+    a.by_run = make_fastdiv((uint32_t)std::min(p.gate_run, kMaxRows));
     a.u_row = p.u_row, a.gate_row = p.gate_row, a.res_row = p.res_row, a.y_row = p.y_row, a.h_row = p.h_row;
     a.post = p.post;
     a.gate_act = p.gate;

@@ -89,7 +89,8 @@ struct NormArgs {
     void *y, *h;
     int64_t rows;         // rows * groups of the call
     int32_t group, ngroups;
-    int64_t gate_run, u_row, gate_row, res_row, y_row, h_row;
+    FastDiv by_groups, by_run;  // rows below 2^31
+    int64_t u_row, gate_row, res_row, y_row, h_row;
     int32_t post, gate_act, gate_first, pre;
     float scale, post_eps, pre_eps;
     int32_t vec, past;
