@@ -16,10 +16,9 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     constexpr int LR = DVB / 4;  // threads across the columns
     __shared__ float red[2][4][DVB];
     const int t = threadIdx.x, cg = t % LR, rg = t / LR;
-    const int64_t b = blockIdx.x;
-    const int blk = (int)(b % A.ndvb);
-    const int64_t bh = b / A.ndvb;
-    const int head = (int)(bh % A.heads), seq = (int)(bh / A.heads);
+    const uint32_t bh = blockIdx.x / (uint32_t)A.ndvb;
+    const int blk = (int)(blockIdx.x - bh * A.ndvb);
+    const int seq = (int)(bh / (uint32_t)A.heads), head = (int)(bh - (uint32_t)seq * A.heads);
     const SeqRange r = seq_range(A.sq, seq);
     const int r0 = rg * RPT, nc = min(4, A.dv - blk * DVB - cg * 4);  // owned columns (none: below 1)
     const int skip = A.dv >= 4 && nc > 0 ? 4 - nc : 0, jend = skip + nc;
