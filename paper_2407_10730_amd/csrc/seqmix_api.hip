@@ -10,7 +10,7 @@ struct seqmix_attn_desc {
     seqmix_attn_params p;
     seqmix_attn_plan_info plan;
     int32_t block = 0, block_uncut = 0;  // state columns per workgroup; of chunk kernels where no sequence is cut
-    int64_t alone = 0;  // packed sequences of up to this many tokens are not cut
+    int64_t alone = 0, alone_packed = 0;  // sequences of up to this many tokens are not cut: of one length; packed
     // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
     void* ws = nullptr;
     int device = -1;
@@ -107,8 +107,16 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
     return std::max({p.q_row, p.k_row, p.v_row, p.o_row, (int64_t)p.heads}) <= (1LL << 31) / (kChunk * 4) - SEQMIX_MAX_HEAD_DIM;
 }
 
-// Sequences of one length up to this are not cut: the chain of their chunks would be shortened by less than cutting costs.
-int64_t alone(int64_t segment, int64_t chunk) { return (3 * segment + 10 * chunk) / 2; }
+// Sequences of one length up to this are not cut: the chain of their chunks would be shortened by less than cutting costs, which is 0.6 of
+// the chunks of a segment and 6.5 us.  Chunks take 2.1, 2.9 and 4.5 us for dk up to 64, 128 and 256 (fp32 2.5, 3.9 and 6.9): 256
+// tokens, 2 heads of 256 x 128: 22.1 us, cut 18.2 (fp32 59, 22); 320, of 64 x 64: 13.6, 12.9.  `groups` workgroups of 64 columns are
+// busy uncut; 1.25 times their share of the CUs is what cutting costs in throughput (16 heads of 128 x 128, 4 sequences: 1000 tokens 51 us,
+// cut 54, and 4000 198, 124; 6 of 700 38, 54; 8 of 2000 107, 128).
+int64_t alone(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64_t groups) {
+    const int64_t least = segment * 8 / 5 + chunk * (p.dk <= 64 ? 12 : p.dk <= 128 ? 8 : 5) / 4;
+    const int64_t left = 4 * kSeqmixCUs - 5 * groups;  // of 4 per CU
+    return left > 0 ? least * 4 * kSeqmixCUs / left : INT64_MAX;
+}
 
 // ... of packed sequences, where a longer one may make the other launches necessary in any case: those of up to a segment and a chunk, and
 // those near the average where that is short or where the sequences fill half of the CUs as they are (8 of 500, 16 heads of 128 x 128: 40
@@ -144,8 +152,8 @@ int64_t ws_places(const seqmix_attn_params& p, int64_t segment) {
 // Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the segments are as
 // long as 256 workgroups allow, or 512 where those still have 8 chunks each: 8192 tokens, 16 heads of 128 x 128 bf16:
 // 71 us in segments of 512, 75 of 256, 78 of 384 (a part of the CUs has two), 110 of 1024; 65536 tokens, 8 heads: 227 us
-// in segments of 1024, 237 of 2048, 242 of 512.  Sequences of up to 5 chunks are not cut (100 tokens: 7.6 us, cut 13.6; 300: 17.4
-// either way).
+// in segments of 1024, 237 of 2048, 242 of 512.  In fp32 segments may be one chunk of 32 tokens while they leave half of the CUs empty (512
+// tokens, 2 heads: 18.2 us, of 64 tokens 21.9; 16 heads: 29.4, 26.7).
 // Packed sequences, whose lengths the host does not know, take 512 (5664 tokens in 10 sequences, 12 heads of 64 x 128: 41 us in segments of 192,
 // 45 of 256, 50 of 512); the kernels cut the longer ones (alone_packed).  They may be one long prompt among single tokens
 // (1, 570, 3, 1 tokens, 1 head of 191 x 128: 22 us, uncut 61; 64 of 1 and one of 1000, 16 heads of 128 x 128: 57, uncut 78) or of one
@@ -167,13 +175,15 @@ void plan_attn(seqmix_attn_desc* d) {
     if (groups < 2 * kSeqmixCUs || p.tokens < chunk * p.seqs) {
         auto length = [&](int64_t want) {  // of segments, such that there are about `want` workgroups
             const int64_t all = want / across, parts = std::max<int64_t>(p.seqs > 1 ? std::max(all - p.seqs, all / 2) : all, 1);
-            return ((p.tokens + parts - 1) / parts + kChunk - 1) / kChunk * kChunk;
+            const int64_t unit = (p.tokens / chunk + p.seqs) * across * 2 <= kSeqmixCUs ? chunk : kChunk;
+            return ((p.tokens + parts - 1) / parts + unit - 1) / unit * unit;
         };
         int64_t seg = length(2 * kSeqmixCUs);
         if (p.seqs == 1 && seg < 8 * chunk) seg = length(kSeqmixCUs);
-        if (p.tokens > alone(seg, chunk)) {
+        d->alone = alone(p, seg, chunk, p.seqs * p.heads * ((p.dv + 63) / 64));
+        if (p.tokens > (p.seqs == 1 ? d->alone : alone(p, seg, chunk, 0) + 2 * chunk)) {
             d->plan.segment = seg;
-            d->alone = alone_packed(p, seg, chunk, groups);
+            d->alone_packed = alone_packed(p, seg, chunk, groups);
             d->plan.workspace_bytes = ws_places(p, seg) * p.heads * ((int64_t)p.dk * p.dv * 4 + 4);
             d->block = chunk_block(p, std::max<int64_t>((p.tokens + seg - 1) / seg, p.seqs) * across);
         }
@@ -254,7 +264,7 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
     const int64_t unit = 16 / esize(p.dtype);
     a.vec = p.dk % unit == 0 && p.dv % unit == 0;
     const bool chunked = d->plan.kernel == SEQMIX_KERNEL_CHUNKS;
-    const bool cut = d->plan.segment > 0 && (offsets || a.sq.seq_len > alone(d->plan.segment, d->plan.chunk));
+    const bool cut = d->plan.segment > 0 && (offsets || a.sq.seq_len > d->alone);
     a.block = chunked && !cut ? d->block_uncut : d->block;
     a.ndvb = (p.dv + a.block - 1) / a.block;
     if (!chunked) {
@@ -273,7 +283,7 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
     SM_TRY(ensure_ws(d));
     SM_TRY(order_after_last(d, s));
     a.segment = d->plan.segment;
-    a.alone = offsets ? d->alone : a.segment;
+    a.alone = offsets ? d->alone_packed : a.segment;
     a.nseg = seq_part_ids(a.sq, a.segment);
     a.ws_mul = p.seqs == 1 ? 1 : 2;
     a.nws = ws_places(p, a.segment);
