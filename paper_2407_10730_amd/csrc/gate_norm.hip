@@ -199,11 +199,12 @@ static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
 // V values per access: 16 bytes, or 1 in groups below that.  Groups up to 16 accesses: 16 lanes each; up to 64: a wave; above, a block of
 // 256 to 1024 threads.  The sizes between take half of the threads with two accesses each (fewer idle ones and shorter sums): 8105 x
 // 4096 fp32 by groups of 128 with 64 lanes 117 us, with 16 81; 16000 x 1000 bf16 45.8, 35.1; 2000 x 4096 fp32 34.5, 31.4.  Two
-// accesses of 8 values wait longer for their weights, so in bf16 only where there are rows for all CUs (64 x 1000: 4.4, 6.0 us).
+// accesses of 8 values wait longer for their weights, so in bf16 only where there are rows for all CUs (64 x 1000: 4.4, 6.0 us); in fp32
+// from one row per CU on (64 x 1500: 4.2, 4.4; x 4096: 5.3, 5.1).
 template <typename T, typename TR, int V>
 static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
     const int64_t packs = (a.group + V - 1) / V;
-    const bool two = V <= 4 || a.rows >= 8 * kSeqmixCUs;
+    const bool two = a.rows >= (V <= 4 ? 1 : 8) * kSeqmixCUs;
     if (packs <= 16) return launch_one<T, TR, 16, V, 1>(a, s);
     if constexpr (V > 1) {
         if (packs <= 32 && two) return launch_one<T, TR, 16, V, 2>(a, s);
@@ -211,7 +212,7 @@ static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
         if (packs <= 128 && two) return launch_one<T, TR, 64, V, 2>(a, s);
         if (packs <= 256) return launch_one<T, TR, 256, V, 1>(a, s);
         if (packs <= 512) return two ? launch_one<T, TR, 256, V, 2>(a, s) : launch_one<T, TR, 512, V, 1>(a, s);
-        if (packs <= 1024) return two ? launch_one<T, TR, 512, V, 2>(a, s) : launch_one<T, TR, 1024, V, 1>(a, s);
+        if (packs <= 1024) return two || V <= 4 ? launch_one<T, TR, 512, V, 2>(a, s) : launch_one<T, TR, 1024, V, 1>(a, s);
         if (packs <= 2048) return launch_one<T, TR, 1024, V, 2>(a, s);
         if constexpr (V == 4) return launch_one<T, TR, 1024, V, 4>(a, s);
     }

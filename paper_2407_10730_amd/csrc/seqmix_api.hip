@@ -113,7 +113,8 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 // busy uncut; 1.25 times their share of the CUs is what cutting costs in throughput (16 heads of 128 x 128, 4 sequences: 1000 tokens 51 us,
 // cut 54, and 4000 198, 124; 6 of 700 38, 54; 8 of 2000 107, 128).
 int64_t alone(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64_t groups) {
-    const int64_t least = segment * 8 / 5 + chunk * (p.dk <= 64 ? 12 : p.dk <= 128 ? 8 : 5) / 4;
+    const int quarters[2][3] = {{12, 11, 6}, {11, 7, 4}};  // of a chunk, in 6.5 us and more
+    const int64_t least = segment * 8 / 5 + chunk * quarters[p.dtype == CONV2D_F32][p.dk <= 64 ? 0 : p.dk <= 128 ? 1 : 2] / 4;
     const int64_t left = 4 * kSeqmixCUs - 5 * groups;  // of 4 per CU
     return left > 0 ? least * 4 * kSeqmixCUs / left : INT64_MAX;
 }
@@ -154,8 +155,8 @@ int64_t ws_places(const seqmix_attn_params& p, int64_t segment) {
 // 71 us in segments of 512, 75 of 256, 78 of 384 (a part of the CUs has two), 110 of 1024; 65536 tokens, 8 heads: 227 us
 // in segments of 1024, 237 of 2048, 242 of 512.  In fp32 segments may be one chunk of 32 tokens while they leave half of the CUs empty (512
 // tokens, 2 heads: 18.2 us, of 64 tokens 21.9; 16 heads: 29.4, 26.7).
-// Packed sequences, whose lengths the host does not know, take 512 (5664 tokens in 10 sequences, 12 heads of 64 x 128: 41 us in segments of 192,
-// 45 of 256, 50 of 512); the kernels cut the longer ones (alone_packed).  They may be one long prompt among single tokens
+// Packed sequences, whose lengths the host does not know, take 512 (5664 tokens in 10 sequences, 12 heads of 64 x 128: 41 us in
+// segments of 192, 45 of 256, 50 of 512); the kernels cut the longer ones (alone_packed).  They may be one long prompt among single tokens
 // (1, 570, 3, 1 tokens, 1 head of 191 x 128: 22 us, uncut 61; 64 of 1 and one of 1000, 16 heads of 128 x 128: 57, uncut 78) or of one
 // length, where the other launches are wasted (4 of 150, 4 heads: 17 us, uncut 12.4).
 // Where 128-column blocks leave half of the CUs empty, blocks of 64 (1024 tokens, 8 heads: 19.7 us, 21.4; 300 tokens:
@@ -175,7 +176,7 @@ void plan_attn(seqmix_attn_desc* d) {
     if (groups < 2 * kSeqmixCUs || p.tokens < chunk * p.seqs) {
         auto length = [&](int64_t want) {  // of segments, such that there are about `want` workgroups
             const int64_t all = want / across, parts = std::max<int64_t>(p.seqs > 1 ? std::max(all - p.seqs, all / 2) : all, 1);
-            const int64_t unit = (p.tokens / chunk + p.seqs) * across * 2 <= kSeqmixCUs ? chunk : kChunk;
+            const int64_t unit = (p.tokens / chunk + (p.seqs > 1 ? p.seqs : 0)) * across * 2 <= kSeqmixCUs ? chunk : kChunk;
             return ((p.tokens + parts - 1) / parts + unit - 1) / unit * unit;
         };
         int64_t seg = length(2 * kSeqmixCUs);
