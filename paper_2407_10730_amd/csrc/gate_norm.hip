@@ -221,9 +221,9 @@ static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
 
 hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
-    if (dt == CONV2D_F32) return a.vec ? launch_v<float, float, 4>(a, s) : launch_v<float, float, 1>(a, s);
-    if (rdt == CONV2D_F32) return a.vec ? launch_v<uint16_t, float, 8>(a, s) : launch_v<uint16_t, float, 1>(a, s);
-    return a.vec ? launch_v<uint16_t, uint16_t, 8>(a, s) : launch_v<uint16_t, uint16_t, 1>(a, s);
+    if (dt == CONV2D_F32) return a.group < 4 ? launch_v<float, float, 1>(a, s) : launch_v<float, float, 4>(a, s);
+    if (rdt == CONV2D_F32) return a.group < 8 ? launch_v<uint16_t, float, 1>(a, s) : launch_v<uint16_t, float, 8>(a, s);
+    return a.group < 8 ? launch_v<uint16_t, uint16_t, 1>(a, s) : launch_v<uint16_t, uint16_t, 8>(a, s);
 }
 
 }  // namespace cv

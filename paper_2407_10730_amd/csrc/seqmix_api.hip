@@ -334,7 +334,6 @@ int seqmix_conv_fwd(const seqmix_conv_desc* d, const void* x, const void* w, con
     a.channels = (int32_t)p.channels;
     a.width = p.width;
     a.silu = p.act == SEQMIX_ACT_SILU;
-    a.vec = p.channels >= 16 / esize(p.dtype);
     a.past = p.tokens * p.channels * esize(p.dtype) >= kPastBytes;
     return launch_token_conv(a, p.dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
@@ -404,7 +403,6 @@ int seqmix_norm_fwd(const seqmix_norm_desc* d, const void* u, const float* post_
     a.scale = p.scale;
     a.post_eps = p.post_eps;
     a.pre_eps = p.pre_eps;
-    a.vec = p.group >= 16 / esize(p.dtype);
     a.past = p.rows * p.width * ((y ? esize(p.res_dtype) : 0) + (pre ? esize(p.dtype) : 0)) >= kPastBytes;
     return launch_norm(a, p.dtype, p.res_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK
                                                                                                : CONV2D_E_HIP;

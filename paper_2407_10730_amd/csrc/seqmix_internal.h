@@ -75,7 +75,6 @@ struct ConvArgs {
     void* y;
     int64_t x_row, y_row;
     int32_t channels, width, silu;
-    int32_t vec;          // 16-byte accesses of x, y and the windows are aligned
     int32_t past;         // y is written past the caches
 };
 hipError_t launch_token_conv(const ConvArgs& a, int dt, hipStream_t s);
@@ -93,7 +92,7 @@ struct NormArgs {
     int64_t u_row, gate_row, res_row, y_row, h_row;
     int32_t post, gate_act, gate_first, pre;
     float scale, post_eps, pre_eps;
-    int32_t vec, past;
+    int32_t past;
 };
 hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s);
 
