@@ -483,6 +483,13 @@ def test_token_conv(kw, carry):
     assert torch.equal(out[other], pool[other] if carry == "in place" else torch.full_like(pool[other], 3.0))
 
 
+@pytest.mark.parametrize("kw", [_case(lens=[t], channels=c, width=4, dtype=d)
+                                for t in (1, 45) for c in (5, 9, 2049, 2055) for d in ("bf16", "f32")])
+@pytest.mark.parametrize("carry", ["in place", "zero"])
+def test_token_conv_odd_channels(kw, carry):
+    test_token_conv(kw, carry)
+
+
 def test_token_conv_keeps_sequences_apart():
     """Infinities and NaN in one sequence and in skipped places reach no other sequence and no earlier token."""
     lens, c = [40, 40, 40], 64
@@ -615,6 +622,56 @@ def test_norm(kw):
         passed = passed + t1 * np.sqrt((size ** 2).mean(-1, keepdims=True)) * r * size2
         bound = (passed + t1 * size2) * (1 + R) + (R * np.abs(want) if dtype == "bf16" else 0)
         _near(_host(h), want, bound, 1.0, "h")
+
+
+NORM_MANY = [
+    # enough groups for two accesses per thread; ends inside an access; both types, also in place
+    *[_case(rows=r, width=g * n, group=g, gate="silu") for g, r, n in ((9, 300, 7), (131, 150, 16), (250, 150, 16), (600, 260, 8),
+                                                                      (1003, 260, 8), (2065, 257, 8), (4103, 257, 8))],
+    *[_case(rows=r, width=g * n, group=g, gate="silu", dtype="f32", post="layer")
+      for g, r, n in ((5, 300, 7), (67, 40, 16), (127, 40, 16), (258, 40, 8), (511, 40, 8), (1025, 40, 8), (2051, 40, 8))],
+    *[_case(rows=300, width=d, dtype=t, residual=True, pre="layer", post="layer", gate="sigmoid", gate_run=7, alias=a, pad=1)
+      for d in (13, 130, 515, 1537) for t, a in (("bf16", True), ("f32", False))],
+]
+
+
+@pytest.mark.parametrize("kw", NORM_MANY)
+def test_norm_of_many_groups(kw):
+    test_norm(kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [3, 9, 129, 1027])
+def test_rows_between_nan(dtype, width):
+    """What lies beside the rows of a convolution and of a norm is no operand and stays as it is."""
+    n, td = 70, TD[dtype]
+
+    def home(value):
+        return torch.full(((n + 2) * (width + 3),), value, dtype=td, device="cuda")
+
+    def rows(flat):
+        return flat[1:].as_strided((n, width), (width + 3, 1))
+
+    x, y, h = home(float("nan")), home(5.0), home(5.0)
+    dense = torch.randn(n, width, device="cuda").to(td)
+    rows(x).copy_(dense)
+    strides = {f"{k}_row": width + 3 for k in ("u", "res", "y", "h")}
+    w = torch.rand(width, device="cuda")
+    want, want_h = torch.empty_like(dense), torch.empty_like(dense)
+    kw = dict(rows=n, width=width, dtype=dtype, residual=True, pre="rms")
+    M.GateNorm(**kw, **strides).run(rows(x), w, residual=rows(x), pre_w=w, y=rows(y), h=rows(h))
+    M.GateNorm(**kw).run(dense, w, residual=dense, pre_w=w, y=want, h=want_h)
+    assert torch.equal(rows(y), want) and torch.equal(rows(h), want_h) and bool(torch.isfinite(want).all())
+    taps = torch.randn(width, 4, device="cuda").to(td)
+    win, left = torch.randn(1, 3, width, device="cuda").to(td), torch.full((2, 3, width), 5.0, device="cuda").to(td)
+    kw = dict(tokens=n, seqs=1, channels=width, width=4, dtype=dtype, bias=False)
+    out = home(5.0)
+    M.TokenConv(**kw, x_row=width + 3, y_row=width + 3).run(rows(x), taps, None, win, left[:1], rows(out))
+    M.TokenConv(**kw).run(dense, taps, None, win, win, want)  # in place
+    assert torch.equal(rows(out), want) and torch.equal(left[:1], win) and bool((left[1] == 5.0).all())
+    for flat in (y, h, out):
+        rows(flat).fill_(5.0)
+        assert bool((flat == 5.0).all())
 
 
 def test_norm_rows_stay_apart():
