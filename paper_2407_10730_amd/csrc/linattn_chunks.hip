@@ -16,10 +16,10 @@
 // as three bf16 planes, which hold all 24 bits, so states keep fp32 accuracy over any length.
 //
 // Bound, at 65536 tokens of 8 heads of 128 x 128 in segments of 1024: the full pass by memory (q, k, v and o, 537 MB, in
-// 124 us warm, 4.3 TB/s; without its loads and stores it takes 98 us, without any one of its products the same 124); its
-// matrix unit is busy 0.34 of the cycles, its vector unit 0.48, LDS 0.42.  The state pass by memory as well
-// (268 MB in 67 us).  At 8192 tokens of 16 heads, one workgroup per CU, by the waves' own chains: 38 and 22 us for 134 and
-// 67 MB.
+// 120 us warm, 4.5 TB/s; with neighbouring heads on one XCD 124, then without
+// loads and stores 98, without any one of its products the same 124); its matrix unit is busy 0.34 of the cycles, its vector unit 0.48, LDS 0.42.
+// The state pass by memory as well (268 MB in 66 us).  At 8192 tokens of 16 heads, one workgroup per CU, by the waves'
+// own chains: 38 and 21 us for 134 and 67 MB.
 #include "linattn_device.h"
 
 namespace cv {

@@ -14,9 +14,9 @@ struct AttnPlace {
     int64_t slot, row0, len;
     bool cut, last;  // a segment; the end of its sequence
 };
-// False: nothing (in all threads of the workgroup).  Heads that share q and k, and their column blocks, go to the same XCD,
-// where they share them in its L2; these units go to the XCDs in turn, as ids without work may lie side by side (8 sequences of 200
-// tokens, 16 heads of 128 x 128: 27 us, with neighbouring ids on one XCD 34).
+// False: nothing (in all threads of the workgroup).  Heads that share q and k, and their column blocks, go to the same
+// XCD, where they share them in its L2; these units go to the XCDs in turn, as ids without work may lie side by side (8
+// sequences of 200 tokens, 16 heads of 128 x 128: 27 us, with neighbouring ids on one XCD 34).
 __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, AttnPlace* out) {
     const uint32_t j = blockIdx.x / 8, round = j / (uint32_t)A.unit, u = blockIdx.x % 8 + 8 * round;
     const int id = u / (uint32_t)A.units;

@@ -42,10 +42,10 @@ struct AttnArgs {
     int32_t block, ndvb;  // state columns per workgroup, such blocks per head
     float scale;
     int32_t vec;          // dk and dv are multiples of 16 bytes of q, k and v
-    // Sequences of more than `alone` tokens (more than `segment`) are cut in segments: ids offsets[i] / segment + i + (segment
-    // of sequence i), of which only the first has work where a sequence is not cut.  Only cut ones have a place in the
-    // workspace, ws_mul * offsets[i] / segment + (segment of sequence i): with ws_mul 2 the ranges of two cut sequences are apart, as
-    // 2 len / segment, rounded down, is at least len / segment, rounded up.
+    // Sequences of more than `alone` tokens (more than `segment`) are cut in segments: ids offsets[i] / segment + i +
+    // (segment of sequence i), of which only the first has work where a sequence is not cut.  Only cut ones have a place
+    // in the workspace, ws_mul * offsets[i] / segment + (segment of sequence i): with ws_mul 2 the ranges of two cut
+    // sequences are apart, as 2 len / segment, rounded down, is at least len / segment, rounded up.
     int64_t segment, alone, nseg, nws;
     int32_t ws_mul;
     int32_t places;       // the ids of this pass number places of the workspace
