@@ -120,13 +120,10 @@ int64_t alone(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64
     return left > 0 ? least * 4 * kSeqmixCUs / left : INT64_MAX;
 }
 
-// ... of packed sequences, where a longer one may make the other launches necessary in any case: those of up to a
-// segment and a chunk, and those near the average where that is short or where the sequences fill half of the CUs as
-// they are (8 of 500, 16 heads of 128 x 128: 40 us, all cut in segments of 192: 57).
-int64_t alone_packed(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64_t groups) {
-    const bool even = p.tokens <= 5 * chunk * p.seqs || 2 * groups >= kSeqmixCUs;
-    return std::max(segment + chunk, even ? p.tokens / p.seqs * 9 / 8 : 0);
-}
+// ... of packed sequences, where a longer one may make the other launches necessary in any case.  16 of 62 to 1000 tokens,
+// 8 heads of 64 x 128, segments of 192: 38 us, up to 531 uncut 45; 8 of 500, 16 heads of 128 x 128, whose ends would have met
+// uncut: 57 us, 40; 8 of 200, segments of 128, 27 us, cut 41.
+int64_t alone_packed(int64_t segment, int64_t chunk) { return std::max(segment + chunk, segment * 8 / 5); }
 
 // State columns of a workgroup of the chunk kernels, of which there are `groups` with the wider blocks: 64 also where
 // the last 128 would be half empty (8192 tokens, 16 heads of 128 x 192: 97 us, 100; fp32, 4096 tokens: 130, 148).
@@ -185,7 +182,7 @@ void plan_attn(seqmix_attn_desc* d) {
         d->alone = alone(p, seg, chunk, p.seqs * p.heads * ((p.dv + 63) / 64));
         if (p.tokens > (p.seqs == 1 ? d->alone : alone(p, seg, chunk, 0) + 2 * chunk)) {
             d->plan.segment = seg;
-            d->alone_packed = alone_packed(p, seg, chunk, groups);
+            d->alone_packed = alone_packed(seg, chunk);
             d->plan.workspace_bytes = ws_places(p, seg) * p.heads * ((int64_t)p.dk * p.dv * 4 + 4);
             d->block = chunk_block(p, std::max<int64_t>((p.tokens + seg - 1) / seg, p.seqs) * across);
         }
