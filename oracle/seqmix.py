@@ -28,6 +28,21 @@ def linear_attention(q, k, v, g, lens, state, scale):
     return o, o_abs, left, left_abs
 
 
+def attention_bound(o, o_abs, tokens, dk, dtype, o_dtype, chunks):
+    """How far outputs may be off, point by point, after sequences of up to `tokens` tokens.
+
+    With u = 2^-24 and r = 2^-8 (half a unit in the last of bf16's 8 bits): a term passes through at most two roundings
+    per token (decay and sum), one per chunk or key column summed, and an exponential whose argument is rounded:
+    (2 tokens + dk + 64) u of the sums over absolute values.  Chunks of bf16 tokens multiply scores and states in bf16
+    planes, each holding what the one before left: two planes leave r^2, three (for fp32 outputs) r^3 = u, once for
+    the scores and once for the states.  A bf16 output is rounded once: r |o|."""
+    u, r = 2.0 ** -24, 2.0 ** -8
+    sums = (2 * tokens + dk + 64) * u
+    if chunks and dtype == "bf16":
+        sums += 2 * (u if o_dtype == "f32" else r * r)
+    return sums * o_abs if o_dtype == "f32" else sums * (1 + r) * o_abs + r * np.abs(o)
+
+
 def silu(x):
     return x / (1.0 + np.exp(-x))
 

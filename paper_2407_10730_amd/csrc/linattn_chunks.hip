@@ -11,9 +11,12 @@
 // operand; q is read from LDS in the same order), so S never passes through LDS.  The scores are shared: the waves
 // divide their 16x16 tiles and exchange them through LDS.  Products over tokens read k and v from LDS through the
 // transposing load.
-// Rounding: the scores and, as an operand of q S, the state are rounded to bf16 once (o is bf16 itself, or
-// as exact as bf16 operands make it); the state's own update multiplies exact k by exp(b_C - b_j) v_j
-// as three bf16 planes, which hold all 24 bits, so states keep fp32 accuracy over any length.
+// Rounding: q, k and v are exact; what is computed in fp32 enters a product as bf16 planes, each the rounding of
+// what the ones before left.  The update of the state multiplies k by exp(b_C - b_j) v_j in three planes, which hold all
+// 24 bits, so states keep fp32 accuracy over any length.  The scores and, as an operand of q S, the state take two planes
+// for bf16 results, which leave 2^-16 of each term where the result's own rounding is 2^-8, and three for fp32 results.
+// (8192 tokens, 16 heads of 128 x 128, with one plane, whose roundings are of the result's size: 66 us; with two 71, with three
+// and fp32 results 85.)
 //
 // Bound, at 65536 tokens of 8 heads of 128 x 128 in segments of 1024: the full pass by memory (q, k, v and o, 537 MB, in
 // 120 us warm, 4.5 TB/s; with neighbouring heads on one XCD 124, then without
@@ -75,14 +78,48 @@ __device__ __forceinline__ void lds_write(uint16_t* base, uint32_t off, V v) {
 // waves per SIMD that LDS leaves room for
 constexpr int chunk_occupancy(int dkt, int waves) { return waves == 8 ? (dkt <= 4 ? 4 : 2) : dkt <= 2 ? 4 : dkt <= 4 ? 3 : 1; }
 
-template <int DKT, int WAVES, bool STATE_ONLY, bool VEC>
-__global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_chunks_bf16_kernel(AttnArgs A, int o_f32) {
+// Two fp32 values as PL bf16 planes.  INF: infinities stay so in every plane (the largest float is taken off them);
+// without, the planes after the first are NaN.
+template <bool INF, int PL>
+__device__ __forceinline__ void bf16_planes(float a, float b, uint32_t (&p)[PL]) {
+#pragma unroll
+    for (int x = 0; x < PL; ++x) {
+        p[x] = pack_bf16(a, b);
+        if (x + 1 < PL) {
+            constexpr float kMax = 3.402823466e38f;
+            const float pa = __builtin_bit_cast(float, p[x] << 16), pb = __builtin_bit_cast(float, p[x] & 0xffff0000u);
+            a -= INF ? __builtin_amdgcn_fmed3f(pa, -kMax, kMax) : pa;
+            b -= INF ? __builtin_amdgcn_fmed3f(pb, -kMax, kMax) : pb;
+        }
+    }
+}
+template <int PL>
+__device__ __forceinline__ void bf16_planes8(f32x4 a, f32x4 b, bf16x8 (&p)[PL]) {
+    uint32_t w[4][PL];
+    bf16_planes<true>(a[0], a[1], w[0]);
+    bf16_planes<true>(a[2], a[3], w[1]);
+    bf16_planes<true>(b[0], b[1], w[2]);
+    bf16_planes<true>(b[2], b[3], w[3]);
+#pragma unroll
+    for (int x = 0; x < PL; ++x) p[x] = __builtin_bit_cast(bf16x8, u32x4{w[0][x], w[1][x], w[2][x], w[3][x]});
+}
+
+// Scores in LDS: the six blocks of 16 rows and 32 columns that are read (column half h of rows 16 it: h = 0, and h = 1
+// from it = 2 on), one plane after the other, two blocks side by side in rows of 64.
+__device__ __forceinline__ int score_block(int it, int h, int plane) { return 6 * plane + it + 2 * h; }
+__device__ __forceinline__ uint32_t score_off(uint32_t at, int block) {
+    return (at ^ ((block & 1) << 6)) + (block >> 1) * (32 * kChunk);
+}
+
+// PL: planes of the scores and of the state as an operand; three where results are fp32.
+template <int DKT, int WAVES, bool STATE_ONLY, bool VEC, int PL>
+__global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_chunks_bf16_kernel(AttnArgs A) {
     constexpr int C = kChunk, DKP = 32 * DKT, DVB = 16 * WAVES, NTHR = 64 * WAVES;
     constexpr int MT = 2 * DKT;                            // 16-row tiles of the state
     __shared__ __align__(16) uint16_t sQ[STATE_ONLY ? 1 : C * DKP];
     __shared__ __align__(16) uint16_t sK[C * DKP];
     __shared__ __align__(16) uint16_t sV[C * DVB];
-    __shared__ __align__(16) uint16_t sP[STATE_ONLY ? 1 : C * C];
+    __shared__ __align__(16) uint16_t sP[STATE_ONLY ? 1 : PL * 6 * 16 * 32];
     __shared__ __align__(16) double sB[C];
     __shared__ __align__(16) float sE[C], sD[C];
     __shared__ float sTot;
@@ -189,7 +226,12 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
                     const float f = (float)(bi - (u < 2 ? b01[u] : b23[u - 2]));
                     sc[u] = (on ? sc[u] : 0.0f) * __builtin_amdgcn_exp2f(on ? f : 0.0f);
                 }
-                lds_write(sP, (o_pw ^ (jt << 5)) + it * (32 * C), u32x2{pack_bf16(sc[0], sc[1]), pack_bf16(sc[2], sc[3])});
+                uint32_t p0[PL], p1[PL];
+                bf16_planes<true>(sc[0], sc[1], p0);
+                bf16_planes<true>(sc[2], sc[3], p1);
+#pragma unroll
+                for (int y = 0; y < PL; ++y)
+                    lds_write(sP, score_off(o_pw ^ ((jt & 1) << 5), score_block(it, jt >> 1, y)), u32x2{p0[y], p1[y]});
             }
         }
         if constexpr (!STATE_ONLY) __syncthreads();
@@ -207,12 +249,17 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
             for (int it = 0; it < 4; ++it) O[it] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < DKT; ++k) {
-                const f32x4 a = S[2 * k], b = S[2 * k + 1];
-                const bf16x8 sf = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]),
-                                                                   pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])});
+                // (one step's planes at a time: 8192 tokens, 16 heads of 128 x 128 71 us, with the spills of several 74; three
+                // planes spill more with it)
+                if constexpr (PL == 2) __builtin_amdgcn_sched_barrier(0);
+                bf16x8 sf[PL], qf[4];
+                bf16_planes8(S[2 * k], S[2 * k + 1], sf);
 #pragma unroll
-                for (int it = 0; it < 4; ++it)
-                    O[it] = mfma16(sf, lds_read<bf16x8>(sQ, (o_row ^ (k << 6)) + it * (32 * DKP)), O[it]);
+                for (int it = 0; it < 4; ++it) qf[it] = lds_read<bf16x8>(sQ, (o_row ^ (k << 6)) + it * (32 * DKP));
+#pragma unroll
+                for (int x = PL - 1; x >= 0; --x)
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) O[it] = mfma16(sf[x], qf[it], O[it]);
             }
 #pragma unroll
             for (int it = 0; it < 4; ++it) O[it] *= sD[16 * it + l16];
@@ -228,8 +275,12 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
                     const int i = 16 * it + l16;
+#pragma unroll 1
                     for (int j = 0; j <= i; ++j) {
-                        const float p = to_f32(lds_read<uint16_t>(sP, swz_at<C>(i, j)));
+                        float p = 0.0f;
+#pragma unroll
+                        for (int x = PL - 1; x >= 0; --x)
+                            p += to_f32(lds_read<uint16_t>(sP, score_off(swz_at<C>(l16, j & 31), score_block(it, j >> 5, x))));
                         const uint32_t v = swz_at<DVB>(j, wc + 4 * quad);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) O[it][u] = fmaf(p, to_f32(lds_read<uint16_t>(sV, v + 2 * u)), O[it][u]);
@@ -239,11 +290,13 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int it = 2 * s; it < 4; ++it)
-                        O[it] = mfma16(__builtin_bit_cast(bf16x8, vf[s]),
-                                       lds_read<bf16x8>(sP, (o_pr ^ (s << 6)) + it * (32 * C)), O[it]);
+                    for (int x = PL - 1; x >= 0; --x)
+#pragma unroll
+                        for (int it = 2 * s; it < 4; ++it)
+                            O[it] = mfma16(__builtin_bit_cast(bf16x8, vf[s]),
+                                           lds_read<bf16x8>(sP, score_off(o_pr, score_block(it, s, x))), O[it]);
             }
-            attn_store<4, VEC>(A, o_f32, pl, c, n, c0 + wc + 4 * quad, l16, O);
+            attn_store<4, VEC, PL == 3>(A, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         // the state moves on
         const float tot = sTot;
@@ -257,15 +310,12 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
             const f32x4 e1 = *reinterpret_cast<const f32x4*>(&sE[32 * s + 8 * quad + 4]);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                float lo = __builtin_bit_cast(float, vf[s][w] << 16) * (w < 2 ? e0[2 * w] : e1[2 * w - 4]);
-                float hi = __builtin_bit_cast(float, vf[s][w] & 0xffff0000u) * (w < 2 ? e0[2 * w + 1] : e1[2 * w - 3]);
+                uint32_t p[3];
+                bf16_planes<false>(__builtin_bit_cast(float, vf[s][w] << 16) * (w < 2 ? e0[2 * w] : e1[2 * w - 4]),
+                                   __builtin_bit_cast(float, vf[s][w] & 0xffff0000u) * (w < 2 ? e0[2 * w + 1] : e1[2 * w - 3]),
+                                   p);
 #pragma unroll
-                for (int x = 0; x < 3; ++x) {
-                    const uint32_t p = pack_bf16(lo, hi);
-                    vp[x][w] = p;
-                    lo -= __builtin_bit_cast(float, p << 16);
-                    hi -= __builtin_bit_cast(float, p & 0xffff0000u);
-                }
+                for (int x = 0; x < 3; ++x) vp[x][w] = p[x];
             }
 #pragma unroll
             for (int m = 0; m < MT; m += 2) {  // two tiles side by side: a product does not wait for the one before
@@ -289,23 +339,25 @@ __global__ __launch_bounds__(64 * WAVES, chunk_occupancy(DKT, WAVES)) void attn_
     if (STATE_ONLY && pl.blk == 0 && t == NTHR - 1) A.ws_decay[pl.ws * A.heads + head] = (float)whole;
 }
 
+template <int DKT, int WAVES, bool STATE_ONLY, int PL>
+static void launch_rows(const AttnArgs& a, dim3 grid, hipStream_t s) {
+    if (a.vec)
+        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, STATE_ONLY, true, PL>), grid, dim3(64 * WAVES), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, STATE_ONLY, false, PL>), grid, dim3(64 * WAVES), 0, s, a);
+}
+
 template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.ids * a.units + 7) / 8 * 8 * a.unit;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(64 * WAVES);
-    const int f32 = odt == CONV2D_F32;
-    if (state_only) {
-        if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, true, true>), grid, block, 0, s, a, f32);
-        else
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, true, false>), grid, block, 0, s, a, f32);
-    } else {
-        if (a.vec)
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, false, true>), grid, block, 0, s, a, f32);
-        else
-            hipLaunchKernelGGL((attn_chunks_bf16_kernel<DKT, WAVES, false, false>), grid, block, 0, s, a, f32);
-    }
+    const dim3 grid((unsigned)blocks);
+    if (state_only)
+        launch_rows<DKT, WAVES, true, 2>(a, grid, s);
+    else if (odt == CONV2D_F32)
+        launch_rows<DKT, WAVES, false, 3>(a, grid, s);
+    else
+        launch_rows<DKT, WAVES, false, 2>(a, grid, s);
     return hipGetLastError();
 }
 

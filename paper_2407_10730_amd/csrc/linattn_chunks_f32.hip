@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
                         for (int u = 0; u < 4; ++u) O[it] = mfma_f32(vf[h][u], p[u], O[it]);
                     }
             }
-            attn_store<2, VEC>(A, 1, pl, c, n, c0 + wc + 4 * quad, l16, O);
+            attn_store<2, VEC, true>(A, pl, c, n, c0 + wc + 4 * quad, l16, O);
         }
         const float tot = sTot;
 #pragma unroll

@@ -163,13 +163,13 @@ __device__ __forceinline__ void store_state(const AttnArgs& A, float* p, int c, 
 
 // Results of a chunk of n tokens that starts at token c of the segment, scaled and rounded: tile it holds tokens 16 it + l16,
 // columns col .. col + 3 (those at or past dv are none).
-template <int IT, bool VEC>
-__device__ __forceinline__ void attn_store(const AttnArgs& A, int o_f32, const AttnPlace& pl, int64_t c, int n, int col,
-                                           int l16, const f32x4 (&O)[IT]) {
+template <int IT, bool VEC, bool F32>
+__device__ __forceinline__ void attn_store(const AttnArgs& A, const AttnPlace& pl, int64_t c, int n, int col, int l16,
+                                           const f32x4 (&O)[IT]) {
     const int64_t first = (pl.row0 + c) * A.o_row + pl.head * A.o_head;
     const uint32_t row = (uint32_t)A.o_row, at = (uint32_t)l16 * row + col;
     const int live = A.dv - col;
-    if (o_f32) {
+    if constexpr (F32) {
         const __amdgpu_buffer_rsrc_t r = chunk_rsrc(static_cast<float*>(A.o) + first, n, row, A.dv);
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
