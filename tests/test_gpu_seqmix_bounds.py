@@ -75,3 +75,49 @@ def test_attention_takes_infinite_states(lens, o_dtype, value):
     got = _host(a.o)
     assert (got[:, :, 5] == value).all()
     assert np.isfinite(np.delete(got, 5, 2)).all()
+
+
+def _set(a, first, start, v):
+    """Log2 decays of `first` over the first segment and almost none after it; start states and values of size 2^start, 2^v."""
+    seg = a.op.plan().segment
+    assert a.op.plan().kernel == M.SEQMIX_KERNEL_CHUNKS and 0 < seg < a.lens[0] and abs(first) / seg * 64 < 100
+    a.g.fill_(-0.001)
+    a.g[:seg] = first / seg * float(np.log(2))
+    a.state.mul_(2.0 ** start)
+    a.v.mul_(2.0 ** v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("first,start,v", [(150, -110, -110), (-150, 120, -30), (200, -110, -110), (-200, 120, -80)])
+def test_attention_segments_grow_and_decay(dtype, first, start, v):
+    """A segment's whole decay or growth may lie outside fp32 where what it is of, and what becomes of that, do not."""
+    a = Attn([2000], 16, 16, 64, 64, dtype=dtype)
+    if abs(first) == 200:
+        a = Attn([8000], 16, 16, 64, 64, dtype=dtype)
+    _set(a, first, start, v)
+    left = torch.empty_like(a.state)
+    a.run(a.state, left)
+    _held(a, dtype)
+    _, _, s, s_abs = a.want()
+    _near(_host(left), s, s_abs, (2 * a.n + a.dk + 64) * 2.0 ** -24, "state")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("state", [True, False])
+def test_attention_zeros_stay_zeros_under_growth(dtype, state):
+    """Growth past every float of a state of zeros, for as long as keys and values are zeros."""
+    a = Attn([2000], 16, 16, 64, 64, dtype=dtype, state=state)
+    seg = a.op.plan().segment
+    assert 0 < seg < 1000
+    a.g[:1900] = 1.2 * float(np.log(2))
+    assert 1.2 * seg > 128
+    a.k[:1900] = 0.0
+    a.v[:1900] = 0.0
+    if state:
+        a.state.zero_()
+    left = torch.full((1, 16, 64, 64), 7.0, device="cuda")
+    a.run(a.state, left)
+    _held(a, dtype)
+    assert not a.o[:1900].any()
+    _, _, s, s_abs = a.want()
+    _near(_host(left), s, s_abs, (2 * a.n + a.dk + 64) * 2.0 ** -24, "state")
