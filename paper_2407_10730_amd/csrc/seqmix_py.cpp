@@ -7,6 +7,7 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <exception>
 #include <vector>
 
 namespace {
@@ -37,8 +38,7 @@ bool numbers(PyObject* seq, std::vector<int64_t>* out) {
     return n >= 0 && !PyErr_Occurred();
 }
 
-// make(fn address, descriptor, [(example tensor of the type, sizes, strides), ...])
-PyObject* make(PyObject*, PyObject* args) {
+PyObject* make_call(PyObject* args) {
     unsigned long long fn = 0, desc = 0;
     PyObject* list = nullptr;
     if (!PyArg_ParseTuple(args, "KKO!", &fn, &desc, &PyList_Type, &list)) return nullptr;
@@ -66,7 +66,20 @@ PyObject* make(PyObject*, PyObject* args) {
     return capsule;
 }
 
-bool fits(const at::Tensor& t, const Want& w, int64_t device) {
+// make(fn address, descriptor, [(example tensor of the type, sizes, strides), ...])
+PyObject* make(PyObject*, PyObject* args) {
+    try {
+        return make_call(args);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// The address of t where it is what the call needs.  What stands for a tensor without having memory of its own (in
+// a transform, or a fake one) throws when asked for its strides or address, or has the address zero.
+bool address(const at::Tensor& t, const Want& w, int64_t device, void** out) {
+    if (t.layout() != at::kStrided || t.is_neg()) return false;
     if (static_cast<int64_t>(t.scalar_type()) != w.element || !t.is_cuda() || t.get_device() != device) return false;
     const auto sizes = t.sizes();
     if (sizes.size() != w.sizes.size()) return false;
@@ -77,7 +90,9 @@ bool fits(const at::Tensor& t, const Want& w, int64_t device) {
         empty |= sizes[i] == 0;
         same &= sizes[i] <= 1 || strides[i] == w.strides[i];
     }
-    return same || empty;  // the strides of extents of one and of empty tensors are open
+    if (!same && !empty) return false;  // the strides of extents of one and of empty tensors are open
+    *out = const_cast<void*>(t.const_data_ptr());
+    return *out || empty;
 }
 
 // run(call, device, stream, tensor or None, ...): the C function's status, or 1 + the place of the first tensor that does
@@ -102,9 +117,12 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < tensors; ++i) {
         if (args[i] == Py_None) continue;
         if (!THPVariable_Check(args[i])) return PyLong_FromSsize_t(1 + i);
-        const at::Tensor& t = THPVariable_Unpack(args[i]);
-        if (!fits(t, c->wants[i], device)) return PyLong_FromSsize_t(1 + i);
-        p[i] = const_cast<void*>(t.const_data_ptr());
+        bool fits = false;
+        try {
+            fits = address(THPVariable_Unpack(args[i]), c->wants[i], device, &p[i]);
+        } catch (const std::exception&) {
+        }
+        if (!fits) return PyLong_FromSsize_t(1 + i);
     }
     int st = 0;
     using V = void*;

@@ -183,12 +183,18 @@ class _Operator:
         who = f"{type(self).__name__}: {name}"
         if not isinstance(t, self._torch.Tensor):
             raise TypeError(f"{who} is a tensor or None: got {type(t).__name__}")
-        if t.dtype is not dtype or t.shape != shape:
+        if t.layout is not self._torch.strided:
+            what = f"is {t.layout}: arguments are dense"
+        elif t.dtype is not dtype or t.shape != shape:
             what = f"is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}"
         elif not t.is_cuda or t.get_device() != dev:
             what = f"is on {t.device}: all arguments are on one GPU"
-        else:
+        elif t.is_neg():
+            what = "is a negated view (resolve_neg makes it dense)"
+        elif any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
             what = f"has strides {t.stride()}, not {strides}"
+        else:
+            what = "has no memory of its own (a tensor of a torch transform, or a fake one)"
         raise Conv2dError(B.CONV2D_E_INVALID, f"{who} {what}")
 
     def _launch(self, dev, stream, *tensors):
