@@ -5,6 +5,7 @@
 // once per descriptor (the C function, the descriptor, what each tensor has to be) and runs it with the tensors.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
@@ -16,6 +17,7 @@ constexpr int kMost = 10;  // tensors of a call
 
 struct Want {
     int64_t element;  // bytes and kind: at::ScalarType
+    bool out;         // is written
     std::vector<int64_t> sizes, strides;
 };
 struct Call {
@@ -52,9 +54,10 @@ PyObject* make_call(PyObject* args) {
     bool ok = n <= kMost;
     for (Py_ssize_t i = 0; ok && i < n; ++i) {
         PyObject *like = nullptr, *sizes = nullptr, *strides = nullptr;
-        ok = PyArg_ParseTuple(PyList_GET_ITEM(list, i), "OOO", &like, &sizes, &strides) && THPVariable_Check(like);
+        int written = 0;
+        ok = PyArg_ParseTuple(PyList_GET_ITEM(list, i), "OOOp", &like, &sizes, &strides, &written) && THPVariable_Check(like);
         if (!ok) break;
-        Want w{static_cast<int64_t>(THPVariable_Unpack(like).scalar_type()), {}, {}};
+        Want w{static_cast<int64_t>(THPVariable_Unpack(like).scalar_type()), written != 0, {}, {}};
         ok = numbers(sizes, &w.sizes) && numbers(strides, &w.strides) && w.sizes.size() == w.strides.size();
         c->wants.push_back(std::move(w));
     }
@@ -66,7 +69,7 @@ PyObject* make_call(PyObject* args) {
     return capsule;
 }
 
-// make(fn address, descriptor, [(example tensor of the type, sizes, strides), ...])
+// make(fn address, descriptor, [(example tensor of the type, sizes, strides, is written), ...])
 PyObject* make(PyObject*, PyObject* args) {
     try {
         return make_call(args);
@@ -80,6 +83,7 @@ PyObject* make(PyObject*, PyObject* args) {
 // a transform, or a fake one) throws when asked for its strides or address, or has the address zero.
 bool address(const at::Tensor& t, const Want& w, int64_t device, void** out) {
     if (t.layout() != at::kStrided || t.is_neg()) return false;
+    if (t.requires_grad() && c10::GradMode::is_enabled()) return false;  // there is no backward pass
     if (static_cast<int64_t>(t.scalar_type()) != w.element || !t.is_cuda() || t.get_device() != device) return false;
     const auto sizes = t.sizes();
     if (sizes.size() != w.sizes.size()) return false;
@@ -124,6 +128,11 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
         }
         if (!fits) return PyLong_FromSsize_t(1 + i);
     }
+    for (Py_ssize_t i = 0; i < tensors; ++i)  // graphs that hold an output's former values are to notice
+        if (args[i] != Py_None && c->wants[i].out) {
+            const at::Tensor& t = THPVariable_Unpack(args[i]);
+            if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        }
     int st = 0;
     using V = void*;
     Py_BEGIN_ALLOW_THREADS;

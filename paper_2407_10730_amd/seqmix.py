@@ -3,6 +3,7 @@
 ``seqmix_*`` functions mirror the C ABI (device buffers, streams and errors as in ``binding``).
 ``LinearAttention``, ``TokenConv`` and ``GateNorm`` own a descriptor, check the tensors that they
 are given and launch on torch's current stream.  All arithmetic happens in the HIP library.
+They are forward operators: where gradients are recorded, tensors that require one are refused.
 """
 from __future__ import annotations
 
@@ -160,13 +161,13 @@ class _Operator:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
-    def _expect(self, name, dtype, shape, strides=None):
+    def _expect(self, name, dtype, shape, strides=None, out=False):
         if strides is None:
             strides, n = [], 1
             for d in reversed(shape):
                 strides.insert(0, n)
                 n *= d
-        self._want.append((dtype, tuple(shape), tuple(strides), name))
+        self._want.append((dtype, tuple(shape), tuple(strides), name, out))
 
     def _ready(self):
         """The checks and the C function as one call of the extension module."""
@@ -175,11 +176,19 @@ class _Operator:
             from . import _seqmix as _pycall  # after torch
         fn = ctypes.cast(getattr(load(), f"seqmix_{self.op}_fwd"), ctypes.c_void_p).value
         like = {d: self._torch.empty(0, dtype=d) for d in {w[0] for w in self._want}}
-        self._call = _pycall.make(fn, self.desc, [(like[d], shape, strides) for d, shape, strides, _ in self._want])
+        self._call = _pycall.make(fn, self.desc, [(like[d], shape, strides, out)
+                                             for d, shape, strides, _, out in self._want])
         return self._call
 
+    @staticmethod
+    def _has_memory(t):
+        try:
+            return t.numel() == 0 or t.data_ptr() != 0
+        except RuntimeError:
+            return False
+
     def _refuse(self, t, want, dev):
-        dtype, shape, strides, name = want
+        dtype, shape, strides, name, _ = want
         who = f"{type(self).__name__}: {name}"
         if not isinstance(t, self._torch.Tensor):
             raise TypeError(f"{who} is a tensor or None: got {type(t).__name__}")
@@ -193,8 +202,10 @@ class _Operator:
             what = "is a negated view (resolve_neg makes it dense)"
         elif any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
             what = f"has strides {t.stride()}, not {strides}"
-        else:
+        elif not self._has_memory(t):
             what = "has no memory of its own (a tensor of a torch transform, or a fake one)"
+        else:
+            what = "requires a gradient, and there is none of a forward operator: call it under torch.no_grad(), or with x.detach()"
         raise Conv2dError(B.CONV2D_E_INVALID, f"{who} {what}")
 
     def _launch(self, dev, stream, *tensors):
@@ -258,8 +269,8 @@ class LinearAttention(_Operator):
         self._expect("offsets", torch.int64, (seqs + 1,))
         self._expect("slot_index", torch.int32, (seqs,))
         self._expect("state_in", torch.float32, (slots, heads, dk, dv))
-        self._expect("state_out", torch.float32, (slots, heads, dk, dv))
-        self._expect("o", td[odt], (tokens, heads, dv), (*strides["o"], 1))
+        self._expect("state_out", torch.float32, (slots, heads, dk, dv), out=True)
+        self._expect("o", td[odt], (tokens, heads, dv), (*strides["o"], 1), out=True)
 
     def run(self, q, k, v, decay, state_in, state_out, o, offsets=None, slot_index=None, stream=None):
         self._launch(o.get_device(), stream, q, k, v, decay, offsets, slot_index, state_in, state_out, o)
@@ -295,8 +306,8 @@ class TokenConv(_Operator):
         self._expect("offsets", torch.int64, (seqs + 1,))
         self._expect("slot_index", torch.int32, (seqs,))
         self._expect("window_in", td, (slots, width - 1, channels))
-        self._expect("window_out", td, (slots, width - 1, channels))
-        self._expect("y", td, (tokens, channels), (y_row, 1))
+        self._expect("window_out", td, (slots, width - 1, channels), out=True)
+        self._expect("y", td, (tokens, channels), (y_row, 1), out=True)
 
     def run(self, x, w, bias, window_in, window_out, y, offsets=None, slot_index=None, stream=None):
         self._launch(y.get_device(), stream, x, w, bias, offsets, slot_index, window_in, window_out, y)
@@ -334,8 +345,8 @@ class GateNorm(_Operator):
         self._expect("residual", td[rdt], (rows, width), (row["res_row"], 1))
         for n in ("scale_vec", "pre_w", "pre_b"):
             self._expect(n, torch.float32, (width,))
-        self._expect("y", td[rdt], (rows, width), (row["y_row"], 1))
-        self._expect("h", td[dt], (rows, width), (row["h_row"], 1))
+        self._expect("y", td[rdt], (rows, width), (row["y_row"], 1), out=True)
+        self._expect("h", td[dt], (rows, width), (row["h_row"], 1), out=True)
 
     def run(self, u, post_w=None, post_b=None, gate=None, residual=None, scale_vec=None, pre_w=None, pre_b=None,
             y=None, h=None, stream=None):
