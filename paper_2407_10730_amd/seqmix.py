@@ -208,9 +208,13 @@ class _Operator:
             what = "requires a gradient, and there is none of a forward operator: call it under torch.no_grad(), or with x.detach()"
         raise Conv2dError(B.CONV2D_E_INVALID, f"{who} {what}")
 
-    def _launch(self, dev, stream, *tensors):
-        """Checks the tensors (None: not given) and calls the library with their addresses."""
+    def _launch(self, lead, name, stream, *tensors):
+        """Checks the tensors (None: not given) and calls the library with their addresses, on the GPU of `lead`."""
         cuda = self._torch.cuda
+        try:
+            dev = lead.get_device()
+        except AttributeError:
+            raise TypeError(f"{type(self).__name__}: {name} is a tensor: got {type(lead).__name__}") from None
         call = self._call or self._ready()
         if dev < 0:  # no GPU, no stream: let the checks say which tensor is wrong
             st = _pycall.run(call, dev, 0, *tensors)
@@ -273,7 +277,7 @@ class LinearAttention(_Operator):
         self._expect("o", td[odt], (tokens, heads, dv), (*strides["o"], 1), out=True)
 
     def run(self, q, k, v, decay, state_in, state_out, o, offsets=None, slot_index=None, stream=None):
-        self._launch(o.get_device(), stream, q, k, v, decay, offsets, slot_index, state_in, state_out, o)
+        self._launch(o, "o", stream, q, k, v, decay, offsets, slot_index, state_in, state_out, o)
 
     def plan(self):
         return seqmix_attn_plan_query(self.desc)
@@ -310,7 +314,7 @@ class TokenConv(_Operator):
         self._expect("y", td, (tokens, channels), (y_row, 1), out=True)
 
     def run(self, x, w, bias, window_in, window_out, y, offsets=None, slot_index=None, stream=None):
-        self._launch(y.get_device(), stream, x, w, bias, offsets, slot_index, window_in, window_out, y)
+        self._launch(y, "y", stream, x, w, bias, offsets, slot_index, window_in, window_out, y)
 
 
 class GateNorm(_Operator):
@@ -350,4 +354,4 @@ class GateNorm(_Operator):
 
     def run(self, u, post_w=None, post_b=None, gate=None, residual=None, scale_vec=None, pre_w=None, pre_b=None,
             y=None, h=None, stream=None):
-        self._launch(u.get_device(), stream, u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h)
+        self._launch(u, "u", stream, u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h)

@@ -61,3 +61,13 @@ def test_what_is_told_first(norm):
     _refused(lambda: norm.run(_fake(4, 9), _fake(8), y=_fake(4, 8)), r"u is \(4, 9\)")
     _refused(lambda: norm.run(_fake(8, 4).t(), _fake(8), y=_fake(4, 8)), "u has strides")
     _refused(lambda: norm.run(_fake(4, 8), torch.empty(8), y=_fake(4, 8)), "u has no memory")
+
+
+def test_a_call_without_its_main_tensor(norm):
+    conv = M.TokenConv(tokens=4, seqs=1, channels=8, width=3)
+    attn = M.LinearAttention(tokens=4, seqs=1, heads=1, dk=8, dv=8)
+    for name, call in (("u", lambda: norm.run(None, _fake(8), y=_fake(4, 8))), ("u", lambda: norm.run([1.0])),
+                       ("y", lambda: conv.run(_fake(4, 8), None, None, None, None, None)),
+                       ("o", lambda: attn.run(_fake(4, 1, 8), None, None, None, None, None, None))):
+        with pytest.raises(TypeError, match=f"{name} is a tensor"):
+            call()
