@@ -34,7 +34,12 @@
  *   - seqmix_conv and seqmix_norm descriptors are never written by a call: any number of threads and
  *     streams may use one at a time.  A seqmix_attn descriptor may own a workspace; like a conv2d
  *     descriptor it is used by one host thread at a time, and a call on another stream than the
- *     previous one makes its stream wait for that call.
+ *     previous one makes its stream wait for that call (whose stream must still exist, and must not be
+ *     under capture by then: E_HIP).
+ *   - Under graph capture, calls of one capture wait for each other, on whatever streams of it, and not
+ *     for calls outside it.  The library does not see when a graph is launched: launches of graphs that hold
+ *     calls of one seqmix_attn descriptor, and its other calls, are kept in order by the caller (on one
+ *     stream, or by events) where it owns a workspace.
  */
 #ifndef SEQMIX_H
 #define SEQMIX_H
@@ -95,7 +100,7 @@ int seqmix_attn_desc_create(const seqmix_attn_params* params, seqmix_attn_desc**
 int seqmix_attn_desc_destroy(seqmix_attn_desc* desc);
 int seqmix_attn_plan_query(const seqmix_attn_desc* desc, seqmix_attn_plan_info* out);
 /* Allocate the workspace on the current device now; calls then allocate nothing and can be captured
- * in a graph (all on the stream of the capture).  Without it the first call allocates.  E_NULL, E_ALLOC, E_HIP,
+ * in a graph.  Without it the first call allocates.  E_NULL, E_ALLOC, E_HIP,
  * E_UNSUPPORTED (already on another device). */
 int seqmix_attn_reserve(seqmix_attn_desc* desc);
 /* q, k: [tokens][qk_heads][dk], v: [tokens][heads][dv], o: [tokens][heads][dv] by the strides given;

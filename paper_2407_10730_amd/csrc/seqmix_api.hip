@@ -17,6 +17,9 @@ struct seqmix_attn_desc {
     hipEvent_t done = nullptr;
     hipStream_t last_stream = nullptr;
     bool has_last = false;
+    // the capture that the previous captured call was part of (0: none), and its stream
+    unsigned long long capture = 0;
+    hipStream_t capture_stream = nullptr;
 };
 struct seqmix_conv_desc {
     seqmix_conv_params p;
@@ -91,10 +94,36 @@ int ensure_ws(seqmix_attn_desc* d) {
     }
 }
 
+// Capture that stream s records into, 0: none.
+unsigned long long capture_of(hipStream_t s) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (hipStreamGetCaptureInfo(s, &status, &id) != hipSuccess) {
+        (void)hipGetLastError();
+        return 0;
+    }
+    return status == hipStreamCaptureStatusActive ? id : 0;
+}
+
+int wait_for(seqmix_attn_desc* d, hipStream_t last, hipStream_t s) {
+    if (hipEventRecord(d->done, last) != hipSuccess || hipStreamWaitEvent(s, d->done, 0) != hipSuccess)
+        return CONV2D_E_HIP;
+    return CONV2D_OK;
+}
+
+// A call waits for the previous one's workspace.  Captured calls run when their graph does: they wait for each other
+// within their graph and leave the order of the others' streams as it is.  A stream that is being captured cannot
+// be waited for from outside (its event would draw this call into the capture).
 int order_after_last(seqmix_attn_desc* d, hipStream_t s) {
+    if (const unsigned long long capture = capture_of(s)) {
+        if (d->capture == capture && s != d->capture_stream) SM_TRY(wait_for(d, d->capture_stream, s));
+        d->capture = capture;
+        d->capture_stream = s;
+        return CONV2D_OK;
+    }
     if (d->has_last && s != d->last_stream) {
-        if (hipEventRecord(d->done, d->last_stream) != hipSuccess || hipStreamWaitEvent(s, d->done, 0) != hipSuccess)
-            return CONV2D_E_HIP;
+        if (capture_of(d->last_stream)) return CONV2D_E_HIP;
+        SM_TRY(wait_for(d, d->last_stream, s));
     }
     d->last_stream = s;
     d->has_last = true;
