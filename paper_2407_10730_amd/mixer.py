@@ -13,6 +13,7 @@ requests, and prints the time of each.
 from __future__ import annotations
 
 import argparse
+from collections import OrderedDict
 
 from . import binding as B
 from . import seqmix
@@ -31,18 +32,35 @@ class Projection:
     def run(self, x, y, stream):
         B.conv2d_fwd(self.desc, x, self.w, None, y, B.CONV2D_ALGO_AUTO, stream)
 
+    def close(self):
+        if self.desc:
+            desc, self.desc = self.desc, 0
+            B.conv2d_desc_destroy(desc)
+
     def __del__(self):
         try:
-            B.conv2d_desc_destroy(self.desc)
+            self.close()
         except Exception:
             pass
 
 
+class _Plan:
+    """A call size's descriptors, and by stream the tensors between its operators."""
+
+    def __init__(self, **ops):
+        self.ops, self.between, self.captured = ops, {}, False
+
+
 class MixerLayer:
-    """The layer's weights (random), and the windows and states of up to `slots` requests."""
+    """The layer's weights (random), and the windows and states of up to `slots` requests.
+
+    Descriptors are kept for the `plans` sizes of calls that were used last, and for those that a graph was captured of.
+    What lies between the operators has a place for each stream, as large as the largest call there, so calls of disjoint
+    slots may run on several streams; a captured call has its own.
+    """
 
     def __init__(self, width=1024, heads=8, qk_heads=4, dk=64, dv=128, taps=4, slots=32, scale=0.5, device="cuda:0",
-                 seed=0):
+                 seed=0, plans=32):
         import torch
         self.torch, self.device = torch, torch.device(device)
         self.width, self.heads, self.qk_heads, self.dk, self.dv, self.taps, self.slots = (
@@ -63,52 +81,74 @@ class MixerLayer:
         self.n_next = 1 + randn(width, scale=0.1, dtype=torch.float32)
         self.windows = torch.zeros(slots, taps - 1, self.mixed, device=self.device, dtype=torch.bfloat16)
         self.states = torch.zeros(slots, heads, dk, dv, device=self.device)
-        self._plans = {}
+        self.plans, self._plans, self._places = plans, OrderedDict(), {}
 
-    def _plan(self, tokens, seqs):
-        """Descriptors and buffers of a call's sizes."""
-        plan = self._plans.get((tokens, seqs))
-        if plan is None:
-            torch, cols, bf16 = self.torch, self.columns, self.torch.bfloat16
-            new = lambda n: torch.empty(tokens, n, device=self.device, dtype=bf16)  # noqa: E731
-            p = {"h": new(self.width), "p": new(cols), "c": new(self.mixed), "o": new(self.inner), "g": new(self.inner),
-                 "u": new(self.width)}
-            p["norm"] = seqmix.GateNorm(rows=tokens, width=self.width, post="none", pre="rms")
-            p["in"], p["out"] = Projection(tokens, self.w_in), Projection(tokens, self.w_out)
-            p["conv"] = seqmix.TokenConv(tokens=tokens, seqs=seqs, slots=self.slots, channels=self.mixed, width=self.taps,
-                                         x_row=cols)
-            qk = self.qk_heads * self.dk
-            p["qkv"] = [t.view(tokens, -1, d) for t, d in zip(p["c"].split([qk, qk, self.inner], 1),
-                                                             (self.dk, self.dk, self.dv))]
-            p["attn"] = seqmix.LinearAttention(
-                tokens=tokens, seqs=seqs, slots=self.slots, heads=self.heads, qk_heads=self.qk_heads, dk=self.dk, dv=self.dv,
-                scale=self.dk ** -0.5, **{f"{n}_strides": t.stride()[:2] for n, t in zip("qkv", p["qkv"])})
-            p["gate"] = seqmix.GateNorm(rows=tokens, width=self.inner, group=self.dv, gate="silu", gate_row=cols)
-            p["sum"] = seqmix.GateNorm(rows=tokens, width=self.width, residual=True, scale=self.scale, pre="rms")
-            plan = self._plans[(tokens, seqs)] = p
-        return plan
+    def _plan(self, tokens, seqs, capturing):
+        p = self._plans.get((tokens, seqs))
+        if p is None:
+            cols = self.columns
+            p = self._plans[(tokens, seqs)] = _Plan(
+                norm=seqmix.GateNorm(rows=tokens, width=self.width, post="none", pre="rms"),
+                w_in=Projection(tokens, self.w_in), w_out=Projection(tokens, self.w_out),
+                conv=seqmix.TokenConv(tokens=tokens, seqs=seqs, slots=self.slots, channels=self.mixed, width=self.taps,
+                                      x_row=cols),
+                attn=seqmix.LinearAttention(
+                    tokens=tokens, seqs=seqs, slots=self.slots, heads=self.heads, qk_heads=self.qk_heads, dk=self.dk,
+                    dv=self.dv, scale=self.dk ** -0.5, q_strides=(self.mixed, self.dk), k_strides=(self.mixed, self.dk),
+                    v_strides=(self.mixed, self.dv)),
+                gate=seqmix.GateNorm(rows=tokens, width=self.inner, group=self.dv, gate="silu", gate_row=cols),
+                sum=seqmix.GateNorm(rows=tokens, width=self.width, residual=True, scale=self.scale, pre="rms"))
+            if len(self._plans) > self.plans and not capturing:  # (freeing a workspace is no work for a capture)
+                old = next((k for k, q in self._plans.items() if not q.captured and q is not p), None)
+                if old:
+                    for op in self._plans.pop(old).ops.values():
+                        op.close()
+        self._plans.move_to_end((tokens, seqs))
+        p.captured |= capturing
+        return p
+
+    def _between(self, p, tokens, stream, capturing):
+        """The tensors between the operators, on `stream`."""
+        t = None if capturing else p.between.get(stream)
+        if t is None:
+            torch, qk = self.torch, self.qk_heads * self.dk
+            columns = (self.width, self.columns, self.mixed, self.inner, self.inner, self.width)
+            sizes = [-(-tokens * c // 64) * 64 for c in columns]
+            place = None if capturing else self._places.get(stream)
+            if place is None or place.numel() < sum(sizes):
+                place = torch.empty(sum(sizes), device=self.device, dtype=torch.bfloat16)
+                if not capturing:
+                    self._places[stream] = place
+                    for q in self._plans.values():  # the former place goes
+                        q.between.pop(stream, None)
+            h, proj, mix, o, g, u = (part[:tokens * c].view(tokens, c)
+                                     for part, c in zip(place[:sum(sizes)].split(sizes), columns))
+            q, k, v = (part.view(tokens, -1, d) for part, d in zip(mix.split([qk, qk, self.inner], 1),
+                                                                   (self.dk, self.dk, self.dv)))
+            mixed, z, logits = proj[:, :self.mixed + self.inner + self.heads].split([self.mixed, self.inner, self.heads], 1)
+            t = h, proj, mixed, z, logits, mix, q, k, v, o, o.view(tokens, self.heads, self.dv), g, u
+            if not capturing:
+                p.between[stream] = t
+        return t
 
     def run(self, x, slot_index, offsets=None):
         """x: [tokens, width] bf16, packed; offsets: int64 [requests + 1] (None: equal lengths, so one token each for
         a decoding step); slot_index: int32 [requests].  Windows and states of those slots move on.
         Returns x' and the next layer's normed input."""
-        torch = self.torch
-        p = self._plan(x.shape[0], slot_index.numel())
-        stream = torch.cuda.current_stream(self.device)
-        p["norm"].run(x, pre_w=self.n_in, h=p["h"])
-        p["in"].run(p["h"], p["p"], stream)
-        mixed, z, logits = p["p"][:, :self.mixed], p["p"][:, self.mixed:self.mixed + self.inner], p["p"][
-            :, self.mixed + self.inner:self.mixed + self.inner + self.heads]
+        torch, tokens = self.torch, x.shape[0]
+        capturing, stream = torch.cuda.is_current_stream_capturing(), torch.cuda.current_stream(self.device)
+        p = self._plan(tokens, slot_index.numel(), capturing)
+        h, proj, mixed, z, logits, mix, q, k, v, o, o_heads, g, u = self._between(p, tokens, stream.cuda_stream, capturing)
+        op = p.ops
+        op["norm"].run(x, pre_w=self.n_in, h=h)
+        op["w_in"].run(h, proj, stream)
         decay = torch.nn.functional.logsigmoid(logits.float() + 2) / 8
-        p["conv"].run(mixed, self.w_taps, self.b_taps, self.windows, self.windows, p["c"], offsets=offsets,
-                      slot_index=slot_index)
-        q, k, v = p["qkv"]
-        p["attn"].run(q, k, v, decay, self.states, self.states, p["o"].view(-1, self.heads, self.dv), offsets=offsets,
-                      slot_index=slot_index)
-        p["gate"].run(p["o"], self.n_head, gate=z, y=p["g"])
-        p["out"].run(p["g"], p["u"], stream)
+        op["conv"].run(mixed, self.w_taps, self.b_taps, self.windows, self.windows, mix, offsets=offsets, slot_index=slot_index)
+        op["attn"].run(q, k, v, decay, self.states, self.states, o_heads, offsets=offsets, slot_index=slot_index)
+        op["gate"].run(o, self.n_head, gate=z, y=g)
+        op["w_out"].run(g, u, stream)
         y, h = torch.empty_like(x), torch.empty_like(x)
-        p["sum"].run(p["u"], self.n_out, residual=x, pre_w=self.n_next, y=y, h=h)
+        op["sum"].run(u, self.n_out, residual=x, pre_w=self.n_next, y=y, h=h)
         return y, h
 
     def clear(self, slot_index):
