@@ -134,7 +134,7 @@ class MixerLayer:
     def run(self, x, slot_index, offsets=None):
         """x: [tokens, width] bf16, packed; offsets: int64 [requests + 1] (None: equal lengths, so one token each for
         a decoding step); slot_index: int32 [requests].  Windows and states of those slots move on.
-        Returns x' and the next layer's normed input."""
+        Returns x' and the next layer's normed input; of a request whose slot is outside the pool (an empty place), x' is x."""
         torch, tokens = self.torch, x.shape[0]
         capturing, stream = torch.cuda.is_current_stream_capturing(), torch.cuda.current_stream(self.device)
         p = self._plan(tokens, slot_index.numel(), capturing)
@@ -144,6 +144,7 @@ class MixerLayer:
         op["w_in"].run(h, proj, stream)
         decay = torch.nn.functional.logsigmoid(logits.float() + 2) / 8
         op["conv"].run(mixed, self.w_taps, self.b_taps, self.windows, self.windows, mix, offsets=offsets, slot_index=slot_index)
+        o.zero_()  # rows of empty places stay so
         op["attn"].run(q, k, v, decay, self.states, self.states, o_heads, offsets=offsets, slot_index=slot_index)
         op["gate"].run(o, self.n_head, gate=z, y=g)
         op["w_out"].run(g, u, stream)

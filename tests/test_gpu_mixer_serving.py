@@ -1,8 +1,10 @@
-"""The gated linear-attention layer as a serving program uses it: many sizes, several streams, graphs (needs the GPU)."""
+"""The gated linear-attention layer as a serving program uses it: many sizes, several streams, empty places, graphs (needs the GPU)."""
 import pytest
 import torch
 
+from oracle import seqmix as ref
 from paper_2407_10730_amd.mixer import MixerLayer
+from test_gpu_mixer import TOL, _host, _off
 
 pytestmark = pytest.mark.gpu
 
@@ -62,6 +64,26 @@ def test_streams_with_slots_of_their_own(n):
         for g, w in zip(got, want):
             assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
         assert torch.equal(layer.states, states)
+
+
+@pytest.mark.parametrize("lens", [[1, 1, 1], [40, 3, 25]])
+def test_empty_places_pass_through(lens):
+    """A request without a slot: x' is x, whatever ran before, and nothing of the pool moves."""
+    layer = _layer()
+    n = sum(lens)
+    offsets = None if lens == [1, 1, 1] else torch.tensor([0] + lens, device="cuda").cumsum(0)
+    layer.run(100 * _x(n, 7), _slots(0, 1, 2), offsets)  # another user's rows in memory of these sizes
+    layer.clear(_slots(0, 1, 2))
+    before = layer.states.clone(), layer.windows.clone()
+    x = _x(n)
+    y, h = layer.run(x, _slots(0, -1, 6), offsets)
+    rows = slice(lens[0], n)
+    assert torch.equal(y[rows], x[rows])
+    want, _ = ref.norm(_host(x[rows]), "rms", _host(layer.n_next), None, 1e-6)
+    assert _off(_host(h[rows]), want) <= TOL
+    assert torch.equal(layer.states[1:], before[0][1:]) and torch.equal(layer.windows[1:], before[1][1:])
+    alone, alone_h = (t.clone() for t in layer.run(x[:lens[0]].contiguous(), _slots(3)))
+    assert _off(_host(y[:lens[0]]), _host(alone)) <= TOL and _off(_host(h[:lens[0]]), _host(alone_h)) <= TOL
 
 
 def test_graph_keeps_its_descriptors():
