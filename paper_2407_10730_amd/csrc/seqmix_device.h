@@ -129,7 +129,7 @@ __device__ __forceinline__ SeqPart seq_part(const SeqArgs& a, uint32_t id, uint3
     for (int n = a.seqs; n > 1;) {
         const int step = (n + 63) / 64, i = lane * step;
         const bool at_most = i < n && first_id(lo + i) <= id;
-        const int k = max(__popcll(__ballot(at_most)) - 1, 0);
+        const int k = max((int)__popcll(__ballot(at_most)) - 1, 0);  // (none where offsets lie; the count is unsigned)
         lo += k * step;
         n = min(step, n - k * step);
     }
