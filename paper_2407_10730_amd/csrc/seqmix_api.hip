@@ -154,9 +154,14 @@ int64_t alone(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64
 // uncut: 57 us, 40; 8 of 200, segments of 128, 27 us, cut 41.
 int64_t alone_packed(int64_t segment, int64_t chunk) { return std::max(segment + chunk, segment * 8 / 5); }
 
-// State columns of a workgroup of the chunk kernels, of which there are `groups` with the wider blocks: 64 also where
-// the last 128 would be half empty (8192 tokens, 16 heads of 128 x 192: 97 us, 100; fp32, 4096 tokens: 130, 148).
-int64_t chunk_columns(const seqmix_attn_params& p) { return (p.dv - 1) % 128 < 64 ? 64 : 128; }
+// State columns of a workgroup of the chunk kernels, of which there are `groups` with the wider blocks.  Where the last
+// 128 would be half empty 64 are better in fp32 (4096 tokens, 16 heads of 128 x 192: 129 us, 147) and for keys of up to 64
+// (8192 tokens of 64 x 192 73.6, 74.6; 7 sequences, 3408 tokens of 64 x 189 59.8, 62.6), not for wider bf16 keys, whose
+// scores each block computes (8192 tokens of 128 x 192 110, 103; of 256 x 192 215, 189).
+int64_t chunk_columns(const seqmix_attn_params& p) {
+    const bool narrow = p.dv <= 64 || p.dk <= 64 || p.dtype == CONV2D_F32;
+    return narrow && (p.dv - 1) % 128 < 64 ? 64 : 128;
+}
 int32_t chunk_block(const seqmix_attn_params& p, int64_t groups) {
     return (int32_t)(groups * 2 <= kSeqmixCUs ? 64 : chunk_columns(p));
 }
