@@ -27,10 +27,11 @@
  *     *_in == *_out updates the pool in place; otherwise the two must not overlap.  An empty sequence
  *     carries its entry over unchanged.  Outputs must not overlap any other argument unless said.
  *   - Strides count elements.  Rows may lie apart (columns of a wider tensor); the last dimension is dense.
- *   - Any alignment of an element's size is accepted; 16-byte aligned pointers and strides run
- *     with wide loads.  Results are bitwise reproducible for the same descriptor parameters and the
- *     same alignment (a norm sums in another order where it loads by element).
- *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.
+ *   - Any alignment of an element's size is accepted, at the same speed but for rows below 16 bytes.  Results are
+ *     bitwise reproducible for the same descriptor parameters.
+ *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.  (Attention in bf16
+ *     multiplies what it has computed in fp32, scores and states, as sums of bf16 parts: 2^-16 of each term is
+ *     left out where outputs are bf16, 2^-24 where they are fp32.)
  *   - seqmix_conv and seqmix_norm descriptors are never written by a call: any number of threads and
  *     streams may use one at a time.  A seqmix_attn descriptor may own a workspace; like a conv2d
  *     descriptor it is used by one host thread at a time, and a call on another stream than the
@@ -56,8 +57,9 @@ extern "C" {
  *   S_t = exp(g_t) S_{t-1} + k_t v_t^T      (dk x dv)        o_t = scale * q_t S_t
  *
  * g is the log of the decay.  -infinity clears the state (a document that starts inside a sequence);
- * values above 0 let it grow (by less than 2^100 over any 64 tokens, or results are not finite).  What a token holds never reaches the outputs of tokens before it, also where
- * it is infinite or NaN. */
+ * values above 0 let it grow (by less than 2^100 over any 64 tokens, or results are not finite); decays that come to less
+ * than 2^-126 within 64 tokens may count as 0.  What a token holds never reaches the outputs of tokens before it, also where
+ * it is infinite or NaN; the infinities that follow from it may be NaN. */
 enum {
     SEQMIX_DECAY_NONE = 0,  /* g = 0 */
     SEQMIX_DECAY_HEAD = 1,  /* g[heads], the same for every token */
@@ -80,7 +82,8 @@ typedef struct {
 } seqmix_attn_params;
 
 /* Kernels of an attention call: token by token with the state in registers, or chunks of tokens on the
- * matrix cores (for long sequences in segments that run side by side, their states joined by a scan). */
+ * matrix cores (for long sequences in segments that run side by side, their states joined by a scan).  Chosen by the
+ * sizes here, which of packed sequences are averages: many short ones with a few long ones among them are better called apart. */
 enum { SEQMIX_KERNEL_TOKENS = 0, SEQMIX_KERNEL_CHUNKS = 1 };
 
 typedef struct {
@@ -96,7 +99,8 @@ typedef struct seqmix_attn_desc seqmix_attn_desc;
  * tokens not a multiple of seqs is found at the call), E_UNSUPPORTED (dims over
  * SEQMIX_MAX_HEAD_DIM, unknown types, fp32 q with bf16 o, 2^31 tokens or more). */
 int seqmix_attn_desc_create(const seqmix_attn_params* params, seqmix_attn_desc** out);
-/* Frees the descriptor and its workspace; waits for nothing.  NULL is OK. */
+/* Frees the descriptor and its workspace (which waits for work queued on the device, and is not to be done under
+ * capture; a graph that holds its calls must not be launched afterwards).  NULL is OK. */
 int seqmix_attn_desc_destroy(seqmix_attn_desc* desc);
 int seqmix_attn_plan_query(const seqmix_attn_desc* desc, seqmix_attn_plan_info* out);
 /* Allocate the workspace on the current device now; calls then allocate nothing and can be captured
@@ -158,7 +162,7 @@ enum { SEQMIX_NORM_NONE = 0, SEQMIX_NORM_RMS = 1, SEQMIX_NORM_LAYER = 2 };
 
 typedef struct {
     int64_t rows, width;
-    int64_t group;         /* divides width; with pre or no post norm: width */
+    int64_t group;         /* divides width; with pre: width */
     int64_t gate_run;      /* rows that share a row of the gate: row r reads gate row r / gate_run */
     int32_t dtype;         /* u, gate, h */
     int32_t res_dtype;     /* residual, y: dtype, or CONV2D_F32 */

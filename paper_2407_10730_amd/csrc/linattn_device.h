@@ -16,7 +16,7 @@ struct AttnPlace {
 };
 // False: nothing (in all threads of the workgroup).  Heads that share q and k, and their column blocks, go to the same
 // XCD, where they share them in its L2; these units go to the XCDs in turn, as ids without work may lie side by side (8
-// sequences of 200 tokens, 16 heads of 128 x 128: 27 us, with neighbouring ids on one XCD 34).
+// sequences of 200 tokens, 16 heads of 128 x 128: 29 us, with neighbouring ids on one XCD 39).
 __device__ __forceinline__ bool attn_place(const AttnArgs& A, bool state_only, AttnPlace* out) {
     const uint32_t j = blockIdx.x / 8, round = j / (uint32_t)A.unit, u = blockIdx.x % 8 + 8 * round;
     const int id = u / (uint32_t)A.units;
@@ -101,8 +101,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rsrc(const T* p, int n, 
 // A thread's 16 bytes of a row of `dim` elements, from column `col` on; loads at any address of the element's alignment are
 // whole.  VEC: dim is a multiple of 16 bytes.  Otherwise the last part is read where it ends with the row, and moved down by
 // `shift` bits, which brings in zeros, when it is used (row_part_of); rows below 16 bytes are read by elements.
-// 5664 tokens in 10 sequences, 12 heads of 84 x 100 bf16: 50 us, all by elements 101; 8192 tokens, 16 heads of
-// 127 x 127: 87 us, 168.
+// 5664 tokens in 10 sequences, 12 heads of 84 x 100 bf16: 56 us, all by elements 93; 8192 tokens, 16 heads of
+// 127 x 127: 94 us, 151.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint32_t row_part(uint32_t first, int col, int dim, uint32_t* shift) {
     constexpr int U = 16 / sizeof(T);

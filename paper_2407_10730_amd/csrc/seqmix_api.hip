@@ -137,21 +137,22 @@ bool chunk_rows_near(const seqmix_attn_params& p) {
 }
 
 // Sequences of one length up to this are not cut: the chain of their chunks would be shortened by less than cutting
-// costs, which is 0.6 of the chunks of a segment and 6.5 us.  Chunks take 2.1, 2.9 and 4.5 us for dk up to 64, 128 and
-// 256 (fp32 2.5, 3.9 and 6.9): 256 tokens, 2 heads of 256 x 128: 22.1 us, cut 18.2 (fp32 59, 22); 320, of 64 x 64:
-// 13.6, 12.9.  `groups` workgroups of 64 columns are busy uncut; 1.25 times their share of the CUs is what cutting
-// costs in throughput (16 heads of 128 x 128, 4 sequences: 1000 tokens 51 us, cut 54, and 4000 198, 124; 6 of 700 38,
-// 54; 8 of 2000 107, 128).
+// costs, which is 0.6 of the chunks of a segment and 3 chunks (dk up to 64), 2.75 (128) or 1.5 (256; fp32 2.75, 1.75, 1).
+// Both sides measured: 2 heads, 320 tokens of 64 x 64 15.4 us, cut 13.7; 256 of 256 x 128 24.7, 19.4 (fp32 59.5, 23.0).  At dk
+// 128 the limit is that of 16 heads (300 tokens of 128 x 128 20.1, 19.6); fewer heads gain by cutting from 5 chunks on, and
+// some lengths of theirs stay uncut that need not (8 heads: 256 tokens 16.8, 16.6; 300 20.0, 17.1).  `groups` workgroups
+// of 64 columns are busy uncut; 1.25 times their share of the CUs is what cutting costs in throughput (16 heads of
+// 128 x 128, 4 sequences: 1000 tokens 57 us, cut 56, and 4000 224, 133; 6 of 700 43, 56; 8 of 2000 120, 136).
 int64_t alone(const seqmix_attn_params& p, int64_t segment, int64_t chunk, int64_t groups) {
-    const int quarters[2][3] = {{12, 11, 6}, {11, 7, 4}};  // of a chunk, in 6.5 us and more
+    const int quarters[2][3] = {{12, 11, 6}, {11, 7, 4}};  // of a chunk
     const int64_t least = segment * 8 / 5 + chunk * quarters[p.dtype == CONV2D_F32][p.dk <= 64 ? 0 : p.dk <= 128 ? 1 : 2] / 4;
     const int64_t left = 4 * kSeqmixCUs - 5 * groups;  // of 4 per CU
     return left > 0 ? least * 4 * kSeqmixCUs / left : INT64_MAX;
 }
 
 // ... of packed sequences, where a longer one may make the other launches necessary in any case.  16 of 62 to 1000 tokens,
-// 8 heads of 64 x 128, segments of 192: 38 us, up to 531 uncut 45; 8 of 500, 16 heads of 128 x 128, whose ends would have met
-// uncut: 57 us, 40; 8 of 200, segments of 128, 27 us, cut 41.
+// 8 heads of 64 x 128, segments of 192: 41 us, up to 531 uncut 49; 8 of 500, 16 heads of 128 x 128, whose ends would have met
+// uncut: 58 us, 44; 8 of 200, segments of 128, 29 us, cut 41.
 int64_t alone_packed(int64_t segment, int64_t chunk) { return std::max(segment + chunk, segment * 8 / 5); }
 
 // State columns of a workgroup of the chunk kernels, of which there are `groups` with the wider blocks.  Where the last
@@ -174,25 +175,30 @@ int64_t ws_places(const seqmix_attn_params& p, int64_t segment) {
 // Kernel, state columns per workgroup (block) and where sequences are cut.
 //
 // Up to 2 tokens per sequence (fp32: 4) go token by token.  A chunk costs the same for 1 token as for 64, the token
-// kernel more with each: 8 sequences, 16 heads of 128 x 128 bf16: 6.5, 7.5 and 7.6 us for 1, 2 and 3 tokens, a chunk
-// 8.0; 256 sequences: 113, 118 and 123 us, a chunk 116; fp32, 128 sequences: 58 to 69 us for 1 to 4 tokens, a chunk 78.
-// Its blocks have 32 columns (more workgroups; 64 sequences of 16 heads of 64 x 64: 10.9 us, with 128 columns 11.6)
-// until there are 8 such per CU, then 128 (256 sequences as above: 113 us, with 32 columns 116).  Where dv is no
+// kernel more with each: 8 sequences, 16 heads of 128 x 128 bf16: 4.9, 5.8 and 6.7 us for 1, 2 and 3 tokens, a chunk
+// 8.2; 256 sequences: 105, 113 and 120 us, a chunk 117; fp32, 128 sequences: 55 to 68 us for 1 to 4 tokens, a chunk 74.
+// Its blocks have 32 columns (more workgroups; 64 sequences of 16 heads of 64 x 64: 8.6 us, with 128 columns 8.8)
+// until there are 8 such per CU, then 128 (256 sequences as above: 105 us, with 32 columns 106).  Where dv is no
 // multiple of 32, blocks share cache lines at their ends, and 128 are better from one per CU on (16 heads of 127 x 127,
-// 4, 8 and 64 sequences: 7.9, 12.1 and 43.8 us with 32 columns, 8.4, 9.3 and 24.7 with 128).
+// 4, 8 and 64 sequences: 7.6, 11.7 and 43 us with 32 columns, 8.1, 8.6 and 24 with 128).
 //
 // A workgroup takes its chunks one after the other, about 5 us each (dk = dv = 128) with one workgroup per CU and 8
 // with two. Cutting adds a pass over k and v, two more launches and 16 dk dv bytes per segment and head, so the
 // segments are as long as 256 workgroups allow, or 512 where those still have 8 chunks each: 8192 tokens, 16 heads of
-// 128 x 128 bf16: 71 us in segments of 512, 75 of 256, 78 of 384 (a part of the CUs has two), 110 of 1024; 65536
-// tokens, 8 heads: 227 us in segments of 1024, 237 of 2048, 242 of 512.  In fp32 segments may be one chunk of 32 tokens
-// while they leave half of the CUs empty (512 tokens, 2 heads: 18.2 us, of 64 tokens 21.9; 16 heads: 29.4, 26.7).
+// 128 x 128 bf16: 74 us in segments of 512, 79 of 256, 87 of 384 (a part of the CUs has two), 94 of 1024; 65536
+// tokens, 8 heads: 224 us in segments of 1024, 235 of 2048, 250 of 512.  In fp32 segments may be one chunk of 32 tokens
+// while they leave half of the CUs empty (512 tokens, 2 heads: 18.6 us, of 64 tokens 22.1; 16 heads: 31, 29).
 // Packed sequences, whose lengths the host does not know, take 512 (5664 tokens in 10 sequences, 12 heads of 64 x 128:
-// 41 us in segments of 192, 45 of 256, 50 of 512); the kernels cut the longer ones (alone_packed).  They may be one
-// long prompt among single tokens (1, 570, 3, 1 tokens, 1 head of 191 x 128: 22 us, uncut 61; 64 of 1 and one of 1000,
-// 16 heads of 128 x 128: 57, uncut 78) or of one length, where the other launches are wasted (4 of 150, 4 heads: 17 us,
-// uncut 12.4). Where 128-column blocks leave half of the CUs empty, blocks of 64 (1024 tokens, 8 heads: 19.7 us, 21.4;
-// 300 tokens: 17.3, 21.8).
+// 43 us in segments of 192, 45 of 256, 49 of 512); the kernels cut the longer ones (alone_packed).  They may be one
+// long prompt among single tokens (1, 570, 3, 1 tokens, 1 head of 191 x 128: 23 us, uncut 70; 64 of 1 and one of 1000,
+// 16 heads of 128 x 128: 60, uncut 100) or of one length, where the other launches are wasted (4 of 150, 4 heads: 18 us,
+// uncut 13.6). Where 128-column blocks leave half of the CUs empty, blocks of 64 (8 heads, 1024 tokens: 24.5 us, 25.8;
+// 300 tokens: 20.0, 23.4).
+//
+// The rules look at averages, so packs of many sequences with a long one among them are far from what they could be: with 512
+// workgroups or more and 64 tokens on average nothing is cut (39 of 100 tokens and one of 16384, 16 heads of 128 x 128: 1072 us,
+// of which the long one's bytes are 66), and at 2 tokens on average all go token by token (255 of 1 token and one of 257:
+// 499 us, in chunks 151; 255 empty places and one of 512: 896, 141; but 256 of 2: 114, 138).
 void plan_attn(seqmix_attn_desc* d) {
     const seqmix_attn_params& p = d->p;
     d->plan = seqmix_attn_plan_info{SEQMIX_KERNEL_TOKENS, 0, 0, 0};

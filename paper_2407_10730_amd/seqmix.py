@@ -247,7 +247,8 @@ class LinearAttention(_Operator):
 
     q, k: [tokens, qk_heads, dk], v, o: [tokens, heads, dv], strides as given (elements between rows and
     between heads) or dense; decay: fp32 [tokens, heads] ("token"), [heads] ("head") or None ("none");
-    states: fp32 [slots, heads, dk, dv]; offsets: int64 [seqs + 1]; slot_index: int32 [seqs].
+    states: fp32 [slots, heads, dk, dv]; offsets: int64 [seqs + 1]; slot_index: int32 [seqs].  Of packed sequences the kernels
+    are chosen by the average length: single tokens of many requests and long prompts are better two calls.
     """
 
     op = "attn"
