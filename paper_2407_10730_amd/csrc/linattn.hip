@@ -195,17 +195,23 @@ __device__ __forceinline__ void join_elements(const AttnArgs& A, int seq, int64_
         for (int u = 0; u < AHEAD; ++u)
             if (p + u < parts) {
                 store_pack<float, V>(ws + (p + u) * pitch, S);
-                // exp2(d) in three factors within 2^+-100: together they take every float but zero out of the range, so the
-                // rest of d is not missed, and a state of zeros stays one under any growth
-                float f[3], rest = d[u];
+                if (fabsf(d[u]) <= 100.0f) {
+                    const float f = __builtin_amdgcn_exp2f(d[u]);
 #pragma unroll
-                for (int x = 0; x < 3; ++x) {
-                    const float part = rest > 100.0f ? 100.0f : rest < -100.0f ? -100.0f : rest;
-                    f[x] = __builtin_amdgcn_exp2f(part);
-                    rest -= part;
+                    for (int v = 0; v < V; ++v) S[v] = fmaf(f, S[v], add[u][v]);
+                } else {
+                    // exp2(d) in three factors within 2^+-100: together they take every float but zero out of the range, so the
+                    // rest of d is not missed, and a state of zeros stays one under any growth
+                    float f[3], rest = d[u];
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) {
+                        const float part = rest > 100.0f ? 100.0f : rest < -100.0f ? -100.0f : rest;
+                        f[x] = __builtin_amdgcn_exp2f(part);
+                        rest -= part;
+                    }
+#pragma unroll
+                    for (int v = 0; v < V; ++v) S[v] = fmaf(S[v] * f[0] * f[1], f[2], add[u][v]);
                 }
-#pragma unroll
-                for (int v = 0; v < V; ++v) S[v] = fmaf(S[v] * f[0] * f[1], f[2], add[u][v]);
             }
     }
 }
