@@ -2,8 +2,8 @@
 //
 //   n = post(u) act(gate)   or   post(u act(gate));    y = residual + scale scale_vec n;    h = pre(y)
 //
-// Bound by memory: each tensor is read or written once (8192 x 2048 bf16 by heads of 128 with a gate in 20.5 us, 4.9
-// TB/s; with residual and the next norm in 26.0, 5.1 TB/s; 13 rows of 1537 fp32 in 4.6, a launch and four reductions).
+// Bound by memory: each tensor is read or written once (8192 x 2048 bf16 by heads of 128 with a gate in 20.7 us, 4.9
+// TB/s; with residual and the next norm in 26.0, 5.1 TB/s; 13 rows of 1537 fp32 in 4.5, a launch and four reductions).
 // TPR threads hold one group (a row, or a head of it) in registers between the reductions; statistics, products and y
 // stay in fp32 until they are stored.  The mean of a LAYER norm is taken off before the squares are summed, so a large
 // mean costs no digits.

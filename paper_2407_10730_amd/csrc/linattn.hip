@@ -8,10 +8,10 @@ namespace cv {
 // One workgroup runs one sequence, head and block of DVB columns of the state through all tokens, the state in
 // registers: thread (rg, cg) holds RPT neighbouring rows of 4 columns.  Bound by reading and writing the state (8 dk dv
 // bytes per head against 4 dk dv operations per token), so it is the kernel of one or two tokens: 256 sequences, 16
-// heads of 128 x 128 in 108 us (537 MB of states, 5.0 TB/s); 8 sequences in 4.8, a launch and one chain of loads. All
+// heads of 128 x 128 in 105 us (537 MB of states, 5.1 TB/s); 8 sequences in 4.9, a launch and one chain of loads. All
 // loads are wide at any alignment: a thread whose columns pass the last one moves down to the last four, and owns those
 // from `skip` on only; what it computes of the others is not used (128 sequences, 16 heads of 128 x 189: 101 us, with
-// such rows read by elements 170; of 131 x 130: 90, 262).
+// such rows read by elements 170; of 131 x 130: 86, 262).
 template <typename T, typename TO, int DVB, int RPT>
 __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     constexpr int LR = DVB / 4;  // threads across the columns
@@ -163,7 +163,7 @@ hipError_t launch_attn_tokens(const AttnArgs& a, int dt, int odt, hipStream_t s)
 // Joins the segments of each sequence: ws_state holds the state that each segment but the last adds from
 // zero; afterwards it holds the state that each segment starts from.  One thread owns V neighbouring elements of a state (from
 // e on) and walks along the segments, AHEAD loads ahead of the sum.  Bound by its bytes, 8 dk dv per segment and head (16
-// segments, 16 heads of 128 x 128: 7.7 us, 33 MB from the caches).
+// segments, 16 heads of 128 x 128: 8.1 us, 33 MB from the caches).
 template <int V>
 __device__ __forceinline__ void join_elements(const AttnArgs& A, int seq, int64_t e) {
     constexpr int AHEAD = 8;

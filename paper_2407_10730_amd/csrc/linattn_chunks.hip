@@ -16,13 +16,12 @@
 // 24 bits, so states keep fp32 accuracy over any length.  The scores and, as an operand of q S, the state take two planes
 // for bf16 results, which leave 2^-16 of each term where the result's own rounding is 2^-8, and three for fp32 results.
 // (8192 tokens, 16 heads of 128 x 128, with one plane, whose roundings are of the result's size: 66 us; with two 71, with three
-// and fp32 results 85.)
+// and fp32 results 83.)
 //
-// Bound, at 65536 tokens of 8 heads of 128 x 128 in segments of 1024: the full pass by memory (q, k, v and o, 537 MB, in
-// 120 us warm, 4.5 TB/s; with neighbouring heads on one XCD 124, then without
-// loads and stores 98, without any one of its products the same 124); its matrix unit is busy 0.34 of the cycles, its vector unit 0.48, LDS 0.42.
-// The state pass by memory as well (268 MB in 66 us).  At 8192 tokens of 16 heads, one workgroup per CU, by the waves'
-// own chains: 38 and 21 us for 134 and 67 MB.
+// Bound, at 65536 tokens of 8 heads of 128 x 128 in segments of 1024: the full pass moves q, k, v and o, 537 MB, in 140 us
+// warm (3.8 TB/s; with one plane 120, by memory); its vector unit is busy 0.56 of the cycles, its matrix unit 0.37, LDS 0.39,
+// and two workgroups per CU do not hide all of each other's waits.  The state pass by memory (268 MB in 65 us).  At 8192
+// tokens of 16 heads, one workgroup per CU, by the waves' own chains: 46 and 21 us for 134 and 67 MB.
 #include "linattn_device.h"
 
 namespace cv {

@@ -2,8 +2,8 @@
 //
 // The same four products per chunk and the same division of work as the bf16 kernel (linattn_chunks.hip), on the
 // fp32 matrix instruction: nothing is rounded below fp32.  It multiplies at a sixteenth of the bf16 rate, which makes
-// this kernel bound by it; 32 tokens per chunk halve the products within a chunk.  8192 tokens of 16 heads of 128 x 128: 157 us
-// for all passes; 512 tokens of 2 heads: 18.
+// this kernel bound by it; 32 tokens per chunk halve the products within a chunk.  8192 tokens of 16 heads of 128 x 128: 161 us
+// for all passes; 512 tokens of 2 heads: 19.
 // Operand order: in step (m, u) of a reduction the lanes of quad q multiply index 16 m + 4 q + u, so that a lane's four
 // steps are one 16-byte LDS read, and the state's registers are operands as they are.
 #include "linattn_device.h"
