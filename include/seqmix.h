@@ -8,6 +8,12 @@
  *   seqmix_attn   linear attention with a decay for each head, with a carried state
  *   seqmix_norm   the norms after and before a block, fused with its gate, residual scale and sum
  *
+ * and where some of its layers keep keys and values instead of a state:
+ *
+ *   seqmix_softmax  softmax attention of prompts, of single tokens and of trees of drafted tokens
+ *   seqmix_rotary   rotary positions of q and k, which writes k and v into the cache
+ *   seqmix_pages    which pages of the cache each request has, and where its next tokens go
+ *
  * Forward only, like the 2D convolution.  Prompts, packed prompts of different lengths, prompts
  * that continue and single tokens go through the same entry points.
  *
@@ -32,14 +38,14 @@
  *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.  (Attention in bf16
  *     multiplies what it has computed in fp32, scores and states, as sums of bf16 parts: 2^-16 of each term is
  *     left out where outputs are bf16, 2^-24 where they are fp32.)
- *   - seqmix_conv and seqmix_norm descriptors are never written by a call: any number of threads and
- *     streams may use one at a time.  A seqmix_attn descriptor may own a workspace; like a conv2d
+ *   - seqmix_conv, seqmix_norm, seqmix_rotary and seqmix_pages descriptors are never written by a call: any number of threads
+ *     and streams may use one at a time.  A seqmix_attn or seqmix_softmax descriptor may own a workspace; like a conv2d
  *     descriptor it is used by one host thread at a time, and a call on another stream than the
  *     previous one makes its stream wait for that call (whose stream must still exist, and must not be
  *     under capture by then: E_HIP).
  *   - Under graph capture, calls of one capture wait for each other, on whatever streams of it, and not
  *     for calls outside it.  The library does not see when a graph is launched: launches of graphs that hold
- *     calls of one seqmix_attn descriptor, and its other calls, are kept in order by the caller (on one
+ *     calls of one seqmix_attn or seqmix_softmax descriptor, and its other calls, are kept in order by the caller (on one
  *     stream, or by events) where it owns a workspace.
  */
 #ifndef SEQMIX_H
@@ -189,6 +195,155 @@ int seqmix_norm_desc_destroy(seqmix_norm_desc* desc);
 int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* post_w, const float* post_b,
                     const void* gate, const void* residual, const float* scale_vec, const float* pre_w,
                     const float* pre_b, void* y, void* h, void* stream);
+
+/* ------------------------------------------------------------------ softmax attention
+ * Per row t of sequence i and head h, with the k/v head h / (heads / kv_heads):
+ *
+ *   o_t = sum_j p_tj v_j / sum_j p_tj        p_tj = exp(scale q_t . k_j), over the keys j that t sees
+ *
+ * A sequence of `len` rows has n keys, of which the last `len` are the rows' own (those of its new tokens) and the ones before
+ * them what went before.  A row sees
+ *   SEQMIX_MASK_FULL    all n keys
+ *   SEQMIX_MASK_CAUSAL  keys 0 .. n - len + t
+ *   SEQMIX_MASK_TREE    keys 0 .. n - len - 1, and of the own keys number j < 64 where bit j of tree[t] is set (drafted tokens
+ *                       that continue the text in several ways: the bits of a token, its parent, ...)
+ * Rows that see no key (n = 0, n < len, an empty mask) are zeros.  Keys that a row does not see never reach it, also where
+ * they hold infinities or NaN.  Where it sees values that are not finite, its results there are NaN.  Scores are
+ * compared as they are: one of +infinity makes the row NaN, ones of -infinity count nothing.
+ *
+ * Keys and values lie
+ *   packed (page 0)  in key_tokens rows; sequence i holds rows [key_offsets[i], key_offsets[i+1]); key_offsets NULL: the rows
+ *                    of q (key_tokens = tokens).
+ *   in pages         of `page` tokens (a power of two): key j of the sequence in slot s lies in page
+ *                    table[s][j / page], row j % page, and the slot holds lens[s] keys (the new ones among them).
+ * Lengths and page numbers are clamped to what there is, so bad ones give wrong results but no access out of range.
+ *
+ * Precision: scores and sums are fp32 products and sums of what q, k and v hold; bf16 weights p enter their product with v as
+ * two bf16 parts (2^-16 of each is left out), so results are rounded once. */
+enum { SEQMIX_MASK_FULL = 0, SEQMIX_MASK_CAUSAL = 1, SEQMIX_MASK_TREE = 2 };
+
+#define SEQMIX_MAX_PAGE 65536
+
+typedef struct {
+    int64_t tokens, seqs, slots;
+    int64_t key_tokens;  /* packed: rows of k and v */
+    int64_t pages;       /* in pages: of the cache, */
+    int64_t max_pages;   /* columns of the table, */
+    int32_t page;        /* tokens of a page; 0: packed */
+    int32_t heads;       /* of q and o */
+    int32_t kv_heads;    /* of k and v: divides heads */
+    int32_t dk, dv;      /* 1 .. SEQMIX_MAX_HEAD_DIM */
+    int32_t dtype;       /* q, k, v, o */
+    int32_t mask;        /* SEQMIX_MASK_* */
+    float scale;         /* finite */
+    /* elements from a token to the next, from a head to the next, and from a page to the next (in pages) */
+    int64_t q_row, q_head, o_row, o_head;
+    int64_t k_row, k_head, k_page, v_row, v_head, v_page;
+} seqmix_softmax_params;
+
+/* Kernels of a call: 128 rows of a sequence per workgroup, or 32, whose keys its waves divide. */
+enum { SEQMIX_KERNEL_PROMPT = 0, SEQMIX_KERNEL_STEP = 1 };
+
+typedef struct {
+    int32_t kernel;           /* SEQMIX_KERNEL_* */
+    int32_t pack;             /* heads that share a workgroup */
+    int64_t parts;            /* 0: the keys of a row are not divided among workgroups; else such parts of all rows at most */
+    int64_t workspace_bytes;  /* results of the parts */
+} seqmix_softmax_plan_info;
+
+typedef struct seqmix_softmax_desc seqmix_softmax_desc;
+
+/* E_NULL, E_INVALID (sizes out of range, a stride below the dimension inside it, a page that is no power of two),
+ * E_UNSUPPORTED (dims over SEQMIX_MAX_HEAD_DIM, pages over SEQMIX_MAX_PAGE, unknown types or masks, 2^31 tokens or
+ * cached rows or more).  Workspaces, streams and captures are as those of seqmix_attn. */
+int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softmax_desc** out);
+int seqmix_softmax_desc_destroy(seqmix_softmax_desc* desc);
+int seqmix_softmax_plan_query(const seqmix_softmax_desc* desc, seqmix_softmax_plan_info* out);
+int seqmix_softmax_reserve(seqmix_softmax_desc* desc);
+/* q: [tokens][heads][dk], o: [tokens][heads][dv], k: [key_tokens][kv_heads][dk] or [pages][page][kv_heads][dk], v alike, by the
+ * strides given; key_offsets int64 [seqs + 1] (packed; else ignored); lens int32 [slots], table int32
+ * [slots][max_pages] (in pages; else ignored); tree int64 [tokens] (SEQMIX_MASK_TREE; else ignored).
+ * Rows of skipped sequences, and rows of no sequence, are left as they were.
+ * Errors: E_NULL, E_INVALID (as seqmix_attn_fwd; key_offsets NULL and key_tokens not tokens), E_ALLOC, E_HIP, E_UNSUPPORTED
+ * (workspace on another device). */
+int seqmix_softmax_fwd(seqmix_softmax_desc* desc, const void* q, const void* k, const void* v, const int64_t* offsets,
+                       const int64_t* key_offsets, const int32_t* slot_index, const int32_t* lens, const int32_t* table,
+                       const int64_t* tree, void* o, void* stream);
+
+/* ------------------------------------------------------------------ rotary positions
+ * The first `rot` elements of each head of q and k turn in pairs (a, b) by the angle w = position[t] freqs[i] of pair i:
+ *
+ *   a' = amplitude (a cos w - b sin w)        b' = amplitude (b cos w + a sin w)
+ *
+ * Pair i is elements i and i + rot / 2 (SEQMIX_ROTARY_HALF) or 2 i and 2 i + 1 (SEQMIX_ROTARY_INTERLEAVED); the elements from
+ * rot on are copied.  Angles are computed in 64 bits, whatever the type.  Frequencies that are scaled for long
+ * contexts are other freqs (and amplitude).
+ * With a cache (page > 0), turned k and v as it is go to row place[t] of it: page place[t] / page, row
+ * place[t] % page.  Tokens with a place outside the cache are not stored; no two tokens of a call may have the same place. */
+enum { SEQMIX_ROTARY_HALF = 0, SEQMIX_ROTARY_INTERLEAVED = 1 };
+
+typedef struct {
+    int64_t tokens;
+    int64_t pages;     /* of the cache */
+    int32_t page;      /* tokens of a page, a power of two; 0: no cache */
+    int32_t heads;     /* of q; 0: no q */
+    int32_t kv_heads;  /* of k and v; 0: none */
+    int32_t dk, dv;    /* 1 .. SEQMIX_MAX_HEAD_DIM (dv: with a cache) */
+    int32_t rot;       /* even, 0 .. dk */
+    int32_t layout;    /* SEQMIX_ROTARY_* */
+    int32_t dtype;
+    float amplitude;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
+    int64_t kc_row, kc_head, kc_page, vc_row, vc_head, vc_page;
+} seqmix_rotary_params;
+
+typedef struct seqmix_rotary_desc seqmix_rotary_desc;
+
+/* E_NULL, E_INVALID, E_UNSUPPORTED (as seqmix_softmax_desc_create).  Descriptors are never written by a call. */
+int seqmix_rotary_desc_create(const seqmix_rotary_params* params, seqmix_rotary_desc** out);
+int seqmix_rotary_desc_destroy(seqmix_rotary_desc* desc);
+/* q, q_out: [tokens][heads][dk], k, k_out: [tokens][kv_heads][dk], v: [tokens][kv_heads][dv], by the strides given; position, place:
+ * int32 [tokens]; freqs: float64 [rot / 2], in radians per position.  q_out may be q and k_out k (same strides).  What
+ * is not wanted is NULL: k_out with a cache, or both it and the caches (then k and v are ignored).
+ * Errors: E_NULL, E_HIP. */
+int seqmix_rotary_fwd(const seqmix_rotary_desc* desc, const void* q, const void* k, const void* v, const int32_t* position,
+                      const double* freqs, void* q_out, void* k_out, void* k_cache, void* v_cache, const int32_t* place,
+                      void* stream);
+
+/* ------------------------------------------------------------------ pages of the cache
+ * Moves the requests of a call on to their next tokens.  Slot s of the pool holds a request of lens[s] tokens, in pages
+ * table[s][0 .. ceil(lens[s] / page) - 1].  free_pages holds each page of the cache once; the first *taken of them
+ * are in use (a new pool: free_pages 0, 1, 2, ..., *taken 0, lens 0).  In this order:
+ *
+ *   1. Each sequence goes back to its first kept[i] tokens (at least 0, at most what it has; kept NULL: none goes back: refused
+ *      drafts are taken off so, and requests that have ended, with no new rows).  Pages that it no longer needs
+ *      become the last *taken entries of free_pages that were in use, in the order of the sequences and of
+ *      their pages, and *taken falls.
+ *   2. Its new rows [offsets[i], offsets[i+1]) are added, in pages from free_pages[*taken] on, in the same order; *taken rises.
+ *      A sequence that would need more than max_pages is refused, and so is every one that needs pages from the first on
+ *      that the pool has too few for: it gets none, and keeps its kept[i] tokens.
+ *   3. position[t] and place[t] are the number of each new row in its request and its row of the cache.
+ *      admitted[i] is the sequence's slot, or -1 where it was refused or skipped: the slot_index for the
+ *      operators that follow.  Rows of refused and skipped sequences, and of none, have place -1 and position 0.
+ *
+ * Entries of the table behind a request's pages are left as they were.  One workgroup does 1. and 2. */
+typedef struct {
+    int64_t tokens, seqs, slots;
+    int64_t pages, max_pages;
+    int32_t page;  /* tokens of a page, a power of two */
+} seqmix_pages_params;
+
+typedef struct seqmix_pages_desc seqmix_pages_desc;
+
+/* E_NULL, E_INVALID, E_UNSUPPORTED (as seqmix_softmax_desc_create).  Descriptors are never written by a call. */
+int seqmix_pages_desc_create(const seqmix_pages_params* params, seqmix_pages_desc** out);
+int seqmix_pages_desc_destroy(seqmix_pages_desc* desc);
+/* kept, slot_index, admitted: int32 [seqs]; lens: int32 [slots], table: int32 [slots][max_pages], free_pages: int32 [pages],
+ * taken: int32 [1], all four updated; place, position: int32 [tokens].
+ * Errors: E_NULL, E_INVALID (as seqmix_attn_fwd), E_HIP. */
+int seqmix_pages_fwd(const seqmix_pages_desc* desc, const int32_t* kept, const int64_t* offsets, const int32_t* slot_index,
+                     int32_t* lens, int32_t* table, int32_t* free_pages, int32_t* taken, int32_t* place, int32_t* position,
+                     int32_t* admitted, void* stream);
 
 #ifdef __cplusplus
 }

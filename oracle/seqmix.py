@@ -82,3 +82,105 @@ def norm(x, kind, w, b, eps):
     if b is not None:
         y, size = y + b, size + np.abs(b)
     return y, size
+
+
+def sees(mask, n, keys, tree=None):
+    """[n, keys]: which keys each of a sequence's n rows sees.  tree: the rows' masks as Python numbers of 64 bits."""
+    own = np.arange(keys) - (keys - n)
+    if mask == "full":
+        return np.ones((n, keys), bool)
+    if mask == "causal":
+        return own[None] <= np.arange(n)[:, None]
+    bits = [[i < 0 or (i < 64 and (int(m) >> int(i)) & 1 == 1) for i in own] for m in tree]
+    return np.array(bits, bool).reshape(n, keys)
+
+
+def softmax_attention(q, k, v, on, scale):
+    """One sequence.  q: [n, H, dk], k: [m, Hk, dk], v: [m, Hk, dv], on: [n, m].  Returns o, the same sums over |v|, and for each row
+    and head the largest |scale| sum |q| |k| of the keys that it sees."""
+    n, heads = q.shape[:2]
+    rep = heads // k.shape[1]
+    o, o_abs, most = np.zeros((n, heads, v.shape[2])), np.zeros((n, heads, v.shape[2])), np.zeros((n, heads))
+    for t in range(n):
+        at = np.nonzero(on[t])[0]
+        if not at.size:
+            continue
+        for h in range(heads):
+            kk, vv = k[at, h // rep], v[at, h // rep]
+            with np.errstate(all="ignore"):
+                s = scale * (kk @ q[t, h])
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                o[t, h] = p @ vv
+                o_abs[t, h] = p @ np.abs(vv)
+                most[t, h] = abs(scale) * (np.abs(kk) @ np.abs(q[t, h])).max()
+    return o, o_abs, most
+
+
+def softmax_bound(o, o_abs, most, keys, dk, dtype):
+    """How far outputs may be off, point by point, with u = 2^-24 and r = 2^-8 (half a unit in the last of bf16's 8 bits).
+
+    A score is a sum of dk products, multiplied by the scale (times log2 e, rounded) and lessened by the maximum: off by (dk + 6) u of its
+    sum over absolute values, `most` at most; the exponential of it is off by as much, relatively, and 4 u of its own.  The
+    weights, and their products with v, are summed over `keys` keys, and rescaled when the maximum moves, by two
+    roundings and an exponential (6 u) at most once for 16 keys: (2 keys + 32) u.  The quotient has this error twice.  Weights
+    enter products in bf16 as two parts, which leave r^2.  A bf16 output is rounded once: r |o|."""
+    u, r = 2.0 ** -24, 2.0 ** -8
+    part = 2 * ((dk + 6) * u * most[..., None] + (2 * keys + 32) * u)
+    if dtype == "bf16":
+        return (part + r * r) * (1 + r) * o_abs + r * np.abs(o) + 1e-37
+    return part * o_abs + 1e-37
+
+
+def rotary(x, position, freqs, rot, layout, amplitude):
+    """x: [T, H, d], position: [T], freqs: [rot / 2]."""
+    y = x.copy()
+    w = np.outer(position.astype(np.float64), freqs)[:, None]
+    a = x[..., :rot // 2] if layout == "half" else x[..., 0:rot:2]
+    b = x[..., rot // 2:rot] if layout == "half" else x[..., 1:rot:2]
+    at = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    y[..., at[0]] = amplitude * (a * np.cos(w) - b * np.sin(w))
+    y[..., at[1]] = amplitude * (b * np.cos(w) + a * np.sin(w))
+    return y
+
+
+class Pages:
+    """The pages of a cache's requests, one token at a time."""
+
+    def __init__(self, lens, table, free_pages, taken, page):
+        self.lens, self.table, self.free, self.taken, self.page = list(lens), [list(r) for r in table], list(free_pages), taken, page
+
+    def pages(self, n):
+        return -(-n // self.page)
+
+    def move(self, slots, kept, new):
+        """slots: of each sequence (None: skipped); kept: None or what each goes back to; new: rows that each gets.
+        Returns place, position (of all new rows) and admitted."""
+        gone = []
+        for i, s in enumerate(slots):
+            if s is None:
+                continue
+            keep = self.lens[s] if kept is None else max(0, min(kept[i], self.lens[s]))
+            gone += self.table[s][self.pages(keep):self.pages(self.lens[s])]
+            self.lens[s] = keep
+        self.taken -= len(gone)
+        self.free[self.taken:self.taken + len(gone)] = gone
+        place, position, admitted, full = [], [], [], False
+        for s, n in zip(slots, new):
+            want = 0 if s is None else self.pages(self.lens[s] + n) - self.pages(self.lens[s])
+            room = s is not None and self.pages(self.lens[s] + n) <= len(self.table[s])
+            full |= room and want > 0 and self.taken + want > len(self.free)
+            if not room or (want and full):
+                place += [-1] * n
+                position += [0] * n
+                admitted.append(-1)
+                continue
+            first = self.pages(self.lens[s])
+            self.table[s][first:first + want] = self.free[self.taken:self.taken + want]
+            self.taken += want
+            for t in range(self.lens[s], self.lens[s] + n):
+                place.append(self.table[s][t // self.page] * self.page + t % self.page)
+                position.append(t)
+            self.lens[s] += n
+            admitted.append(s)
+        return place, position, admitted

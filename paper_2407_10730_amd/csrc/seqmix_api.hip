@@ -2,7 +2,7 @@
 #include <algorithm>
 #include <new>
 
-#include "seqmix_internal.h"
+#include "seqmix_workspace.h"
 
 using namespace cv;
 
@@ -11,15 +11,7 @@ struct seqmix_attn_desc {
     seqmix_attn_plan_info plan;
     int32_t block = 0, block_uncut = 0;  // state columns per workgroup; of chunk kernels where no sequence is cut
     int64_t alone = 0, alone_packed = 0;  // sequences of up to this many tokens are not cut: of one length; packed
-    // workspace, on `device`; calls that use it are ordered over streams as in conv2d.h
-    void* ws = nullptr;
-    int device = -1;
-    hipEvent_t done = nullptr;
-    hipStream_t last_stream = nullptr;
-    bool has_last = false;
-    // the capture that the previous captured call was part of (0: none), and its stream
-    unsigned long long capture = 0;
-    hipStream_t capture_stream = nullptr;
+    Workspace ws;  // of plan.workspace_bytes
 };
 struct seqmix_conv_desc {
     seqmix_conv_params p;
@@ -29,106 +21,6 @@ struct seqmix_norm_desc {
 };
 
 namespace {
-
-#define SM_TRY(e)                       \
-    do {                                \
-        const int st_ = (e);            \
-        if (st_ != CONV2D_OK) return st_; \
-    } while (0)
-
-constexpr int64_t kMaxRows = (1LL << 31) - 1;
-
-bool known_dtype(int d) { return d == CONV2D_F32 || d == CONV2D_BF16; }
-int64_t esize(int d) { return d == CONV2D_BF16 ? 2 : 4; }
-
-// Rows, sequences and slots as every sequence operator has them.
-int check_seqs(int64_t tokens, int64_t seqs, int64_t slots) {
-    if (tokens < 0 || seqs < 1 || slots < 1) return CONV2D_E_INVALID;
-    if (tokens > kMaxRows || seqs > kMaxRows || slots > kMaxRows) return CONV2D_E_UNSUPPORTED;
-    return CONV2D_OK;
-}
-
-int seq_args(int64_t tokens, int64_t seqs, int64_t slots, const int64_t* off, const int32_t* slot, SeqArgs* out) {
-    if (!off && tokens % seqs != 0) return CONV2D_E_INVALID;
-    if (!slot && slots < seqs) return CONV2D_E_INVALID;
-    *out = SeqArgs{off, slot, tokens, off ? 0 : tokens / seqs, slots, (int32_t)seqs};
-    return CONV2D_OK;
-}
-
-
-// Rows `row` elements apart, heads `head` elements apart, of `dim` elements each, can hold what they should.
-bool strides_ok(int64_t tokens, int64_t row, int64_t heads, int64_t head, int64_t dim) {
-    if (head < dim && heads > 1) return false;
-    if (head < 0 || row < 0) return false;
-    // either order of rows and heads, without overlap
-    const bool rows_outer = row >= (heads - 1) * head + dim;
-    const bool heads_outer = heads > 1 && row >= dim && head >= (tokens - 1) * row + dim;
-    return tokens <= 1 || rows_outer || heads_outer;
-}
-
-hipError_t alloc_ws(seqmix_attn_desc* d) {
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    if (d->device >= 0) return d->device == dev ? hipSuccess : hipErrorInvalidDevice;
-    e = hipEventCreateWithFlags(&d->done, hipEventDisableTiming);
-    if (e != hipSuccess) return e;
-    e = hipMalloc(&d->ws, (size_t)d->plan.workspace_bytes);
-    if (e != hipSuccess) {
-        (void)hipEventDestroy(d->done);
-        d->done = nullptr;
-        d->ws = nullptr;
-        return e;
-    }
-    d->device = dev;
-    return hipSuccess;
-}
-
-int ensure_ws(seqmix_attn_desc* d) {
-    if (d->plan.workspace_bytes == 0) return CONV2D_OK;
-    switch (alloc_ws(d)) {
-        case hipSuccess: return CONV2D_OK;
-        case hipErrorOutOfMemory: (void)hipGetLastError(); return CONV2D_E_ALLOC;
-        case hipErrorInvalidDevice: return CONV2D_E_UNSUPPORTED;
-        default: return CONV2D_E_HIP;
-    }
-}
-
-// Capture that stream s records into, 0: none.
-unsigned long long capture_of(hipStream_t s) {
-    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    unsigned long long id = 0;
-    if (hipStreamGetCaptureInfo(s, &status, &id) != hipSuccess) {
-        (void)hipGetLastError();
-        return 0;
-    }
-    return status == hipStreamCaptureStatusActive ? id : 0;
-}
-
-int wait_for(seqmix_attn_desc* d, hipStream_t last, hipStream_t s) {
-    if (hipEventRecord(d->done, last) != hipSuccess || hipStreamWaitEvent(s, d->done, 0) != hipSuccess)
-        return CONV2D_E_HIP;
-    return CONV2D_OK;
-}
-
-// A call waits for the previous one's workspace.  Captured calls run when their graph does: they wait for each other
-// within their graph and leave the order of the others' streams as it is.  A stream that is being captured cannot
-// be waited for from outside (its event would draw this call into the capture).
-int order_after_last(seqmix_attn_desc* d, hipStream_t s) {
-    if (const unsigned long long capture = capture_of(s)) {
-        if (d->capture == capture && s != d->capture_stream) SM_TRY(wait_for(d, d->capture_stream, s));
-        d->capture = capture;
-        d->capture_stream = s;
-        return CONV2D_OK;
-    }
-    if (d->has_last && s != d->last_stream) {
-        if (capture_of(d->last_stream)) return CONV2D_E_HIP;
-        SM_TRY(wait_for(d, d->last_stream, s));
-    }
-    d->last_stream = s;
-    d->has_last = true;
-    return CONV2D_OK;
-}
 
 // The chunk kernels address the rows of a chunk by 32-bit byte offsets from its first: rows further apart go
 // token by token.
@@ -259,8 +151,7 @@ int seqmix_attn_desc_create(const seqmix_attn_params* params, seqmix_attn_desc**
 
 int seqmix_attn_desc_destroy(seqmix_attn_desc* d) {
     if (!d) return CONV2D_OK;
-    if (d->ws) (void)hipFree(d->ws);
-    if (d->done) (void)hipEventDestroy(d->done);
+    d->ws.release();
     delete d;
     return CONV2D_OK;
 }
@@ -273,7 +164,7 @@ int seqmix_attn_plan_query(const seqmix_attn_desc* d, seqmix_attn_plan_info* out
 
 int seqmix_attn_reserve(seqmix_attn_desc* d) {
     if (!d) return CONV2D_E_NULL;
-    return ensure_ws(d);
+    return d->ws.ensure(d->plan.workspace_bytes);
 }
 
 int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const void* v, const float* decay,
@@ -319,14 +210,14 @@ int seqmix_attn_fwd(seqmix_attn_desc* d, const void* q, const void* k, const voi
                                       : launch_attn_chunks_f32(a, state_only, s);
     };
     if (!cut) return chunks(false) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
-    SM_TRY(ensure_ws(d));
-    SM_TRY(order_after_last(d, s));
+    SM_TRY(d->ws.ensure(d->plan.workspace_bytes));
+    SM_TRY(d->ws.order_after_last(s));
     a.segment = d->plan.segment;
     a.alone = offsets ? d->alone_packed : a.segment;
     a.nseg = seq_part_ids(a.sq, a.segment);
     a.ws_mul = p.seqs == 1 ? 1 : 2;
     a.nws = ws_places(p, a.segment);
-    a.ws_state = static_cast<float*>(d->ws);
+    a.ws_state = static_cast<float*>(d->ws.data);
     a.ws_decay = a.ws_state + a.nws * p.heads * p.dk * p.dv;
     if (chunks(true) != hipSuccess || launch_attn_join(a, s) != hipSuccess || chunks(false) != hipSuccess)
         return CONV2D_E_HIP;

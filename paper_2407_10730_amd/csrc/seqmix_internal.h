@@ -96,4 +96,54 @@ struct NormArgs {
 };
 hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s);
 
+// A cache of keys or values in pages, or packed rows (shift 0: row j is page j).
+struct CachePlace {
+    int64_t page, row, head;  // elements from one to the next
+};
+
+// Rows of a tile of the softmax kernels are (token, head of `pack` that share it), tokens of one sequence.
+constexpr int kPromptRows = 128, kStepRows = 32;
+
+struct SoftArgs {
+    SeqArgs sq;
+    const void *q, *k, *v;
+    void* o;
+    const int64_t* koff;   // packed: NULL: the rows of q
+    const int32_t *lens, *table;
+    const int64_t* tree;
+    int64_t key_tokens, pages, max_pages;
+    CachePlace kp, vp;
+    int64_t q_row, q_head, o_row, o_head;
+    int32_t paged, shift;  // log2 of the page
+    int32_t heads, rep, pack, blocks;  // rep heads share a k/v head; blocks of `pack` heads
+    int32_t dk, dv, mask;
+    int32_t qsign;         // -1, 0, 1
+    float scale2;          // |scale| log2(e), where the scale is not 0
+    int32_t tile;          // tokens of a tile
+    int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
+};
+hipError_t launch_softmax_bf16(const SoftArgs& a, bool vec, hipStream_t s);
+hipError_t launch_softmax_f32(const SoftArgs& a, bool vec, hipStream_t s);
+
+struct RotaryArgs {
+    const void *q, *k, *v;
+    void *qo, *ko, *kc, *vc;
+    const int32_t *position, *place;
+    const double* freqs;
+    int64_t tokens, rows;  // rows of the cache
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
+    CachePlace kp, vp;
+    int32_t shift, heads, kv_heads, dk, dv, rot;
+    float amplitude;
+};
+hipError_t launch_rotary(const RotaryArgs& a, int dt, int layout, hipStream_t s);
+
+struct PagesArgs {
+    SeqArgs sq;
+    const int32_t* kept;
+    int32_t *lens, *table, *free_pages, *taken, *place, *position, *admitted;
+    int32_t pages, max_pages, shift;
+};
+hipError_t launch_pages(const PagesArgs& a, hipStream_t s);
+
 }  // namespace cv

@@ -1,0 +1,252 @@
+// softmax_api.hip -- C ABI of softmax attention, rotary positions and cache pages: validation, plans, launches.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "seqmix_workspace.h"
+
+using namespace cv;
+
+struct seqmix_softmax_desc {
+    seqmix_softmax_params p;
+    seqmix_softmax_plan_info plan;
+    Workspace ws;  // of plan.workspace_bytes
+};
+struct seqmix_rotary_desc {
+    seqmix_rotary_params p;
+};
+struct seqmix_pages_desc {
+    seqmix_pages_params p;
+};
+
+namespace {
+
+// Heads of one call; more make 32-bit indices of a token's elements overflow.
+constexpr int32_t kMaxHeads = 1 << 20;
+
+int log2_of(int32_t page) { return 31 - __builtin_clz((unsigned)page); }
+
+// A cache of `pages` pages of `page` tokens has less than 2^31 rows.
+int check_pages(int64_t pages, int32_t page) {
+    if (pages < 1 || page < 1 || (page & (page - 1))) return CONV2D_E_INVALID;
+    if (page > SEQMIX_MAX_PAGE || pages > kMaxRows / page) return CONV2D_E_UNSUPPORTED;
+    return CONV2D_OK;
+}
+int check_table(int64_t max_pages, int32_t page) {
+    if (max_pages < 1) return CONV2D_E_INVALID;
+    return max_pages > kMaxRows / page ? CONV2D_E_UNSUPPORTED : CONV2D_OK;
+}
+
+// Rows, heads and pages (one: packed) of a cache of k or v do not overlap.
+bool cache_ok(int64_t rows, int64_t heads, int64_t pages, int64_t row, int64_t head, int64_t page, int64_t dim) {
+    if (!strides_ok(rows, row, heads, head, dim)) return false;
+    return pages <= 1 || page >= (rows - 1) * row + (heads - 1) * head + dim;
+}
+
+// Heads that share a workgroup where sequences are short: as many of those that share a k/v head as fill its rows.
+int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
+    int32_t pack = 1;
+    for (int32_t d = 2; d <= rep; ++d)
+        if (rep % d == 0 && d * length <= rows) pack = d;
+    return pack;
+}
+
+void plan_softmax(seqmix_softmax_desc* d) {
+    const seqmix_softmax_params& p = d->p;
+    const int64_t length = std::max<int64_t>((p.tokens + p.seqs - 1) / p.seqs, 1);
+    d->plan = seqmix_softmax_plan_info{SEQMIX_KERNEL_PROMPT, packed_heads(kPromptRows, length, p.heads / p.kv_heads), 0, 0};
+}
+
+}  // namespace
+
+extern "C" {
+
+// ------------------------------------------------------------------ softmax attention
+int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softmax_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_softmax_params& p = *params;
+    SM_TRY(check_seqs(p.tokens, p.seqs, p.slots));
+    if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads != 0 || p.dk < 1 || p.dv < 1 || !std::isfinite(p.scale))
+        return CONV2D_E_INVALID;
+    if (p.mask < SEQMIX_MASK_FULL || p.mask > SEQMIX_MASK_TREE || !known_dtype(p.dtype) || p.dk > SEQMIX_MAX_HEAD_DIM ||
+        p.dv > SEQMIX_MAX_HEAD_DIM || p.heads > kMaxHeads)
+        return CONV2D_E_UNSUPPORTED;
+    if (p.page) {
+        SM_TRY(check_pages(p.pages, p.page));
+        SM_TRY(check_table(p.max_pages, p.page));
+    } else if (p.key_tokens < 0) {
+        return CONV2D_E_INVALID;
+    } else if (p.key_tokens > kMaxRows) {
+        return CONV2D_E_UNSUPPORTED;
+    }
+    const int64_t rows = p.page ? p.page : p.key_tokens, pages = p.page ? p.pages : 1;
+    if (!strides_ok(p.tokens, p.q_row, p.heads, p.q_head, p.dk) || !strides_ok(p.tokens, p.o_row, p.heads, p.o_head, p.dv) ||
+        !cache_ok(rows, p.kv_heads, pages, p.k_row, p.k_head, p.k_page, p.dk) ||
+        !cache_ok(rows, p.kv_heads, pages, p.v_row, p.v_head, p.v_page, p.dv))
+        return CONV2D_E_INVALID;
+    if ((p.tokens + p.seqs) * p.heads > kMaxRows) return CONV2D_E_UNSUPPORTED;  // workgroups
+    seqmix_softmax_desc* d = new (std::nothrow) seqmix_softmax_desc;
+    if (!d) return CONV2D_E_ALLOC;
+    d->p = p;
+    plan_softmax(d);
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_softmax_desc_destroy(seqmix_softmax_desc* d) {
+    if (!d) return CONV2D_OK;
+    d->ws.release();
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_softmax_plan_query(const seqmix_softmax_desc* d, seqmix_softmax_plan_info* out) {
+    if (!d || !out) return CONV2D_E_NULL;
+    *out = d->plan;
+    return CONV2D_OK;
+}
+
+int seqmix_softmax_reserve(seqmix_softmax_desc* d) {
+    if (!d) return CONV2D_E_NULL;
+    return d->ws.ensure(d->plan.workspace_bytes);
+}
+
+int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, const void* v, const int64_t* offsets,
+                       const int64_t* key_offsets, const int32_t* slot_index, const int32_t* lens, const int32_t* table,
+                       const int64_t* tree, void* o, void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_softmax_params& p = d->p;
+    if (p.tokens > 0 && (!q || !o || (p.mask == SEQMIX_MASK_TREE && !tree))) return CONV2D_E_NULL;
+    if (p.tokens > 0 && (p.page ? !k || !v || !lens || !table : p.key_tokens > 0 && (!k || !v))) return CONV2D_E_NULL;
+    SoftArgs a{};
+    SM_TRY(seq_args(p.tokens, p.seqs, p.slots, offsets, slot_index, &a.sq));
+    if (!p.page && !key_offsets && p.key_tokens != p.tokens) return CONV2D_E_INVALID;
+    if (p.tokens == 0) return CONV2D_OK;
+    a.q = q, a.k = k, a.v = v, a.o = o;
+    a.koff = p.page ? nullptr : key_offsets;
+    a.lens = lens, a.table = table, a.tree = tree;
+    a.key_tokens = p.key_tokens, a.pages = p.pages, a.max_pages = p.max_pages;
+    a.kp = {p.k_page, p.k_row, p.k_head};
+    a.vp = {p.v_page, p.v_row, p.v_head};
+    a.q_row = p.q_row, a.q_head = p.q_head, a.o_row = p.o_row, a.o_head = p.o_head;
+    a.paged = p.page > 0;
+    a.shift = p.page ? log2_of(p.page) : 0;
+    a.heads = p.heads;
+    a.rep = p.heads / p.kv_heads;
+    a.pack = d->plan.pack;
+    a.blocks = p.heads / a.pack;
+    a.dk = p.dk, a.dv = p.dv, a.mask = p.mask;
+    a.scale2 = std::fabs(p.scale) * 1.4426950408889634f;
+    a.qsign = !(a.scale2 > 0.0f) ? 0 : p.scale < 0.0f ? -1 : 1;
+    if (a.qsign == 0) a.scale2 = 1.0f;
+    a.tile = kPromptRows / a.pack;
+    a.ids = seq_part_ids(a.sq, a.tile);
+    const int64_t unit = 16 / esize(p.dtype);
+    const bool vec = p.dk % unit == 0 && p.dv % unit == 0;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = p.dtype == CONV2D_BF16 ? launch_softmax_bf16(a, vec, s) : launch_softmax_f32(a, vec, s);
+    return e == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+}
+
+// ------------------------------------------------------------------ rotary positions
+int seqmix_rotary_desc_create(const seqmix_rotary_params* params, seqmix_rotary_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_rotary_params& p = *params;
+    if (p.tokens < 0 || p.heads < 0 || p.kv_heads < 0 || p.dk < 1 || p.rot < 0 || p.rot % 2 != 0 || p.rot > p.dk)
+        return CONV2D_E_INVALID;
+    if (p.tokens > kMaxRows || p.heads > kMaxHeads || p.kv_heads > kMaxHeads || !known_dtype(p.dtype) ||
+        p.dk > SEQMIX_MAX_HEAD_DIM || (p.layout != SEQMIX_ROTARY_HALF && p.layout != SEQMIX_ROTARY_INTERLEAVED))
+        return CONV2D_E_UNSUPPORTED;
+    if ((p.heads && (!strides_ok(p.tokens, p.q_row, p.heads, p.q_head, p.dk) ||
+                     !strides_ok(p.tokens, p.qo_row, p.heads, p.qo_head, p.dk))) ||
+        (p.kv_heads && (!strides_ok(p.tokens, p.k_row, p.kv_heads, p.k_head, p.dk) ||
+                        !strides_ok(p.tokens, p.ko_row, p.kv_heads, p.ko_head, p.dk))))
+        return CONV2D_E_INVALID;
+    if (p.page) {
+        if (p.kv_heads < 1 || p.dv < 1) return CONV2D_E_INVALID;
+        if (p.dv > SEQMIX_MAX_HEAD_DIM) return CONV2D_E_UNSUPPORTED;
+        SM_TRY(check_pages(p.pages, p.page));
+        if (!strides_ok(p.tokens, p.v_row, p.kv_heads, p.v_head, p.dv) ||
+            !cache_ok(p.page, p.kv_heads, p.pages, p.kc_row, p.kc_head, p.kc_page, p.dk) ||
+            !cache_ok(p.page, p.kv_heads, p.pages, p.vc_row, p.vc_head, p.vc_page, p.dv))
+            return CONV2D_E_INVALID;
+    }
+    seqmix_rotary_desc* d = new (std::nothrow) seqmix_rotary_desc{p};
+    if (!d) return CONV2D_E_ALLOC;
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_rotary_desc_destroy(seqmix_rotary_desc* d) {
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_rotary_fwd(const seqmix_rotary_desc* d, const void* q, const void* k, const void* v, const int32_t* position,
+                      const double* freqs, void* q_out, void* k_out, void* k_cache, void* v_cache, const int32_t* place,
+                      void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_rotary_params& p = d->p;
+    const bool cached = p.page > 0 && (k_cache || v_cache);
+    const bool of_k = p.kv_heads > 0 && (k_out || (cached && k_cache));
+    if (p.tokens > 0 && (!position || (p.rot && !freqs) || (p.heads && (!q || !q_out)) || (of_k && !k) ||
+                         (cached && (!place || !k_cache || !v_cache || !v))))
+        return CONV2D_E_NULL;
+    if (p.tokens == 0) return CONV2D_OK;
+    RotaryArgs a{};
+    a.q = p.heads ? q : nullptr;
+    a.k = of_k ? k : nullptr;
+    a.v = v;
+    a.qo = q_out;
+    a.ko = p.kv_heads ? k_out : nullptr;
+    a.kc = cached ? k_cache : nullptr;
+    a.vc = cached ? v_cache : nullptr;
+    a.position = position;
+    a.place = cached ? place : nullptr;
+    a.freqs = freqs;
+    a.tokens = p.tokens;
+    a.rows = p.page ? p.pages * p.page : 0;
+    a.q_row = p.q_row, a.q_head = p.q_head, a.k_row = p.k_row, a.k_head = p.k_head, a.v_row = p.v_row, a.v_head = p.v_head;
+    a.qo_row = p.qo_row, a.qo_head = p.qo_head, a.ko_row = p.ko_row, a.ko_head = p.ko_head;
+    a.kp = {p.kc_page, p.kc_row, p.kc_head};
+    a.vp = {p.vc_page, p.vc_row, p.vc_head};
+    a.shift = p.page ? log2_of(p.page) : 0;
+    a.heads = p.heads, a.kv_heads = p.kv_heads, a.dk = p.dk, a.dv = p.dv, a.rot = p.rot;
+    a.amplitude = p.amplitude;
+    return launch_rotary(a, p.dtype, p.layout, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+}
+
+// ------------------------------------------------------------------ pages of the cache
+int seqmix_pages_desc_create(const seqmix_pages_params* params, seqmix_pages_desc** out) {
+    if (!params || !out) return CONV2D_E_NULL;
+    const seqmix_pages_params& p = *params;
+    SM_TRY(check_seqs(p.tokens, p.seqs, p.slots));
+    SM_TRY(check_pages(p.pages, p.page));
+    SM_TRY(check_table(p.max_pages, p.page));
+    seqmix_pages_desc* d = new (std::nothrow) seqmix_pages_desc{p};
+    if (!d) return CONV2D_E_ALLOC;
+    *out = d;
+    return CONV2D_OK;
+}
+
+int seqmix_pages_desc_destroy(seqmix_pages_desc* d) {
+    delete d;
+    return CONV2D_OK;
+}
+
+int seqmix_pages_fwd(const seqmix_pages_desc* d, const int32_t* kept, const int64_t* offsets, const int32_t* slot_index,
+                     int32_t* lens, int32_t* table, int32_t* free_pages, int32_t* taken, int32_t* place, int32_t* position,
+                     int32_t* admitted, void* stream) {
+    if (!d) return CONV2D_E_NULL;
+    const seqmix_pages_params& p = d->p;
+    if (!lens || !table || !free_pages || !taken || !admitted || (p.tokens > 0 && (!place || !position))) return CONV2D_E_NULL;
+    PagesArgs a{};
+    SM_TRY(seq_args(p.tokens, p.seqs, p.slots, offsets, slot_index, &a.sq));
+    a.kept = kept;
+    a.lens = lens, a.table = table, a.free_pages = free_pages, a.taken = taken;
+    a.place = place, a.position = position, a.admitted = admitted;
+    a.pages = (int32_t)p.pages, a.max_pages = (int32_t)p.max_pages, a.shift = log2_of(p.page);
+    return launch_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+}
+
+}  // extern "C"

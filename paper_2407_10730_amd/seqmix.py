@@ -1,7 +1,8 @@
 """Token-mixing operators: the ABI of include/seqmix.h, and a device-side helper for each.
 
 ``seqmix_*`` functions mirror the C ABI (device buffers, streams and errors as in ``binding``).
-``LinearAttention``, ``TokenConv`` and ``GateNorm`` own a descriptor, check the tensors that they
+``LinearAttention``, ``TokenConv`` and ``GateNorm``, and for layers with a cache of keys and values ``SoftmaxAttention``,
+``Rotary`` and ``CachePages``, own a descriptor, check the tensors that they
 are given and launch on torch's current stream.  All arithmetic happens in the HIP library.
 They are forward operators: where gradients are recorded, tensors that require one are refused.
 """
@@ -17,11 +18,18 @@ SEQMIX_KERNEL_TOKENS, SEQMIX_KERNEL_CHUNKS = 0, 1
 SEQMIX_ACT_NONE, SEQMIX_ACT_SILU, SEQMIX_ACT_SIGMOID, SEQMIX_ACT_LINEAR = 0, 1, 2, 3
 SEQMIX_NORM_NONE, SEQMIX_NORM_RMS, SEQMIX_NORM_LAYER = 0, 1, 2
 SEQMIX_MAX_HEAD_DIM, SEQMIX_MAX_CONV_WIDTH, SEQMIX_MAX_NORM_WIDTH = 256, 8, 16384
+SEQMIX_MASK_FULL, SEQMIX_MASK_CAUSAL, SEQMIX_MASK_TREE = 0, 1, 2
+SEQMIX_KERNEL_PROMPT, SEQMIX_KERNEL_STEP = 0, 1
+SEQMIX_ROTARY_HALF, SEQMIX_ROTARY_INTERLEAVED = 0, 1
+SEQMIX_MAX_PAGE = 65536
 
 # every function the header declares
 EXPORTS = ("seqmix_attn_desc_create", "seqmix_attn_desc_destroy", "seqmix_attn_plan_query", "seqmix_attn_reserve",
            "seqmix_attn_fwd", "seqmix_conv_desc_create", "seqmix_conv_desc_destroy", "seqmix_conv_fwd",
-           "seqmix_norm_desc_create", "seqmix_norm_desc_destroy", "seqmix_norm_fwd")
+           "seqmix_norm_desc_create", "seqmix_norm_desc_destroy", "seqmix_norm_fwd",
+           "seqmix_softmax_desc_create", "seqmix_softmax_desc_destroy", "seqmix_softmax_plan_query",
+           "seqmix_softmax_reserve", "seqmix_softmax_fwd", "seqmix_rotary_desc_create", "seqmix_rotary_desc_destroy",
+           "seqmix_rotary_fwd", "seqmix_pages_desc_create", "seqmix_pages_desc_destroy", "seqmix_pages_fwd")
 
 
 class seqmix_attn_params(ctypes.Structure):
@@ -53,6 +61,31 @@ class seqmix_norm_params(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("u_row", "gate_row", "res_row", "y_row", "h_row")]
 
 
+class seqmix_softmax_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "seqs", "slots", "key_tokens", "pages", "max_pages")] + [
+        (n, ctypes.c_int32) for n in ("page", "heads", "kv_heads", "dk", "dv", "dtype", "mask")] + [
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "q_row", "q_head", "o_row", "o_head", "k_row", "k_head", "k_page", "v_row", "v_head", "v_page")]
+
+
+class seqmix_softmax_plan_info(ctypes.Structure):
+    _fields_ = [("kernel", ctypes.c_int32), ("pack", ctypes.c_int32), ("parts", ctypes.c_int64),
+                ("workspace_bytes", ctypes.c_int64)]
+
+
+class seqmix_rotary_params(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("pages", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("page", "heads", "kv_heads", "dk", "dv", "rot", "layout", "dtype")] + [
+        ("amplitude", ctypes.c_float)] + [(f"{t}_{d}", ctypes.c_int64) for t in ("q", "k", "v", "qo", "ko")
+                                          for d in ("row", "head")] + [
+        (f"{t}_{d}", ctypes.c_int64) for t in ("kc", "vc") for d in ("row", "head", "page")]
+
+
+class seqmix_pages_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("tokens", "seqs", "slots", "pages", "max_pages")] + [
+        ("page", ctypes.c_int32)]
+
+
 _lib = None
 _pycall = None
 
@@ -65,12 +98,15 @@ def load():
     lib = B.load()
     vp = ctypes.c_void_p
     for op, params, nptr in (("attn", seqmix_attn_params, 10), ("conv", seqmix_conv_params, 9),
-                             ("norm", seqmix_norm_params, 11)):
+                             ("norm", seqmix_norm_params, 11), ("softmax", seqmix_softmax_params, 11),
+                             ("rotary", seqmix_rotary_params, 11), ("pages", seqmix_pages_params, 11)):
         getattr(lib, f"seqmix_{op}_desc_create").argtypes = [ctypes.POINTER(params), ctypes.POINTER(vp)]
         getattr(lib, f"seqmix_{op}_desc_destroy").argtypes = [vp]
         getattr(lib, f"seqmix_{op}_fwd").argtypes = [vp] * (1 + nptr)
     lib.seqmix_attn_plan_query.argtypes = [vp, ctypes.POINTER(seqmix_attn_plan_info)]
     lib.seqmix_attn_reserve.argtypes = [vp]
+    lib.seqmix_softmax_plan_query.argtypes = [vp, ctypes.POINTER(seqmix_softmax_plan_info)]
+    lib.seqmix_softmax_reserve.argtypes = [vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -132,6 +168,56 @@ def seqmix_norm_fwd(desc: int, u, post_w, post_b, gate, residual, scale_vec, pre
     _check(load().seqmix_norm_fwd(desc, _ptr(u), _ptr(post_w), _ptr(post_b), _ptr(gate), _ptr(residual),
                                   _ptr(scale_vec), _ptr(pre_w), _ptr(pre_b), _ptr(y), _ptr(h), _stream(stream)),
            "seqmix_norm_fwd")
+
+
+def seqmix_softmax_desc_create(params: seqmix_softmax_params) -> int:
+    return _create("softmax", params)
+
+
+def seqmix_softmax_desc_destroy(desc: int) -> None:
+    _check(load().seqmix_softmax_desc_destroy(desc), "seqmix_softmax_desc_destroy")
+
+
+def seqmix_softmax_plan_query(desc: int) -> seqmix_softmax_plan_info:
+    out = seqmix_softmax_plan_info()
+    _check(load().seqmix_softmax_plan_query(desc, ctypes.byref(out)), "seqmix_softmax_plan_query")
+    return out
+
+
+def seqmix_softmax_reserve(desc: int) -> None:
+    _check(load().seqmix_softmax_reserve(desc), "seqmix_softmax_reserve")
+
+
+def seqmix_softmax_fwd(desc: int, q, k, v, offsets, key_offsets, slot_index, lens, table, tree, o, stream=None) -> None:
+    _check(load().seqmix_softmax_fwd(desc, *(_ptr(t) for t in (q, k, v, offsets, key_offsets, slot_index, lens, table, tree,
+                                                               o)), _stream(stream)), "seqmix_softmax_fwd")
+
+
+def seqmix_rotary_desc_create(params: seqmix_rotary_params) -> int:
+    return _create("rotary", params)
+
+
+def seqmix_rotary_desc_destroy(desc: int) -> None:
+    _check(load().seqmix_rotary_desc_destroy(desc), "seqmix_rotary_desc_destroy")
+
+
+def seqmix_rotary_fwd(desc: int, q, k, v, position, freqs, q_out, k_out, k_cache, v_cache, place, stream=None) -> None:
+    _check(load().seqmix_rotary_fwd(desc, *(_ptr(t) for t in (q, k, v, position, freqs, q_out, k_out, k_cache, v_cache,
+                                                              place)), _stream(stream)), "seqmix_rotary_fwd")
+
+
+def seqmix_pages_desc_create(params: seqmix_pages_params) -> int:
+    return _create("pages", params)
+
+
+def seqmix_pages_desc_destroy(desc: int) -> None:
+    _check(load().seqmix_pages_desc_destroy(desc), "seqmix_pages_desc_destroy")
+
+
+def seqmix_pages_fwd(desc: int, kept, offsets, slot_index, lens, table, free_pages, taken, place, position, admitted,
+                     stream=None) -> None:
+    _check(load().seqmix_pages_fwd(desc, *(_ptr(t) for t in (kept, offsets, slot_index, lens, table, free_pages, taken, place,
+                                                             position, admitted)), _stream(stream)), "seqmix_pages_fwd")
 
 
 _DTYPES = {"f32": B.CONV2D_F32, "bf16": B.CONV2D_BF16}
@@ -356,3 +442,155 @@ class GateNorm(_Operator):
     def run(self, u, post_w=None, post_b=None, gate=None, residual=None, scale_vec=None, pre_w=None, pre_b=None,
             y=None, h=None, stream=None):
         self._launch(u, "u", stream, u, post_w, post_b, gate, residual, scale_vec, pre_w, pre_b, y, h)
+
+
+def _strides(given, *sizes):
+    """Elements from one to the next of all but the last dimension: as given, or dense."""
+    if given is not None:
+        return tuple(given)
+    dense, n = [], 1
+    for d in reversed(sizes[1:]):
+        n *= d
+        dense.insert(0, n)
+    return tuple(dense)
+
+
+class SoftmaxAttention(_Operator):
+    """seqmix_softmax of `tokens` rows in `seqs` sequences.
+
+    q: [tokens, heads, dk], o: [tokens, heads, dv], strides as given (elements between rows and between heads) or dense;
+    offsets: int64 [seqs + 1]; slot_index: int32 [seqs]; tree (mask "tree"): int64 [tokens].  Keys and values either
+    packed (page 0), k: [key_tokens, kv_heads, dk], v alike, key_offsets: int64 [seqs + 1] (None: the rows of q),
+    or in `pages` pages of `page` tokens, k: [pages, page, kv_heads, dk], v alike (three strides), lens: int32 [slots],
+    table: int32 [slots, max_pages].  The kernels are chosen by the average number of rows of a sequence.
+    """
+
+    op = "softmax"
+
+    def __init__(self, *, tokens, seqs, heads, dk, dv=None, kv_heads=None, slots=None, dtype="bf16", mask="causal", scale=None,
+                 key_tokens=None, page=0, pages=0, max_pages=0, q_strides=None, k_strides=None, v_strides=None,
+                 o_strides=None):
+        kv_heads = heads if kv_heads is None else kv_heads
+        dv = dk if dv is None else dv
+        slots = seqs if slots is None else slots
+        key_tokens = tokens if key_tokens is None else key_tokens
+        dt = _pick(_DTYPES, dtype, "dtype")
+        kind = _pick({"full": SEQMIX_MASK_FULL, "causal": SEQMIX_MASK_CAUSAL, "tree": SEQMIX_MASK_TREE}, mask, "mask")
+        where = (pages, page) if page else (key_tokens,)
+        qs, os_ = _strides(q_strides, tokens, heads, dk), _strides(o_strides, tokens, heads, dv)
+        ks, vs = _strides(k_strides, *where, kv_heads, dk), _strides(v_strides, *where, kv_heads, dv)
+        super().__init__(seqmix_softmax_params(
+            tokens=tokens, seqs=seqs, slots=slots, key_tokens=key_tokens, pages=pages, max_pages=max_pages, page=page,
+            heads=heads, kv_heads=kv_heads, dk=dk, dv=dv, dtype=dt, mask=kind,
+            scale=dk ** -0.5 if scale is None else scale, q_row=qs[0], q_head=qs[1], o_row=os_[0], o_head=os_[1],
+            k_row=ks[-2], k_head=ks[-1], k_page=ks[0] if page else 0, v_row=vs[-2], v_head=vs[-1],
+            v_page=vs[0] if page else 0))
+        td, torch = self._td[dt], self._torch
+        self._expect("q", td, (tokens, heads, dk), (*qs, 1))
+        self._expect("k", td, (*where, kv_heads, dk), (*ks, 1))
+        self._expect("v", td, (*where, kv_heads, dv), (*vs, 1))
+        self._expect("offsets", torch.int64, (seqs + 1,))
+        self._expect("key_offsets", torch.int64, (seqs + 1,))
+        self._expect("slot_index", torch.int32, (seqs,))
+        self._expect("lens", torch.int32, (slots,))
+        self._expect("table", torch.int32, (slots, max_pages))
+        self._expect("tree", torch.int64, (tokens,))
+        self._expect("o", td, (tokens, heads, dv), (*os_, 1), out=True)
+
+    def run(self, q, k, v, o, offsets=None, key_offsets=None, slot_index=None, lens=None, table=None, tree=None, stream=None):
+        self._launch(o, "o", stream, q, k, v, offsets, key_offsets, slot_index, lens, table, tree, o)
+
+    def plan(self):
+        return seqmix_softmax_plan_query(self.desc)
+
+    def reserve(self):
+        """Allocate the workspace now (before a graph capture)."""
+        seqmix_softmax_reserve(self.desc)
+
+
+class Rotary(_Operator):
+    """seqmix_rotary: q, q_out: [tokens, heads, dk], k, k_out: [tokens, kv_heads, dk], v: [tokens, kv_heads, dv], strides as
+    given or dense (q_out may be q, k_out k); position, place: int32 [tokens]; freqs: float64 [rot / 2]
+    (`rotary_frequencies`); caches of `pages` pages of `page` tokens, k_cache: [pages, page, kv_heads, dk], v_cache alike."""
+
+    op = "rotary"
+
+    def __init__(self, *, tokens, heads, kv_heads, dk, dv=None, rot=None, layout="half", dtype="bf16", amplitude=1.0, page=0,
+                 pages=0, q_strides=None, k_strides=None, v_strides=None, q_out_strides=None, k_out_strides=None,
+                 k_cache_strides=None, v_cache_strides=None):
+        dv = dk if dv is None else dv
+        rot = dk if rot is None else rot
+        dt = _pick(_DTYPES, dtype, "dtype")
+        rows = {n: _strides(s, tokens, h, d) for n, s, h, d in (
+            ("q", q_strides, heads, dk), ("k", k_strides, kv_heads, dk), ("v", v_strides, kv_heads, dv),
+            ("qo", q_out_strides, heads, dk), ("ko", k_out_strides, kv_heads, dk))}
+        caches = {n: _strides(s, pages, page, kv_heads, d) for n, s, d in (("kc", k_cache_strides, dk),
+                                                                           ("vc", v_cache_strides, dv))}
+        super().__init__(seqmix_rotary_params(
+            tokens=tokens, pages=pages, page=page, heads=heads, kv_heads=kv_heads, dk=dk, dv=dv, rot=rot,
+            layout=_pick({"half": SEQMIX_ROTARY_HALF, "interleaved": SEQMIX_ROTARY_INTERLEAVED}, layout, "layout"),
+            dtype=dt, amplitude=amplitude,
+            **{f"{n}_{d}": s[i] for n, s in rows.items() for i, d in enumerate(("row", "head"))},
+            **{f"{n}_{d}": s[i] for n, s in caches.items() for i, d in enumerate(("page", "row", "head"))}))
+        td, torch = self._td[dt], self._torch
+        self._expect("q", td, (tokens, heads, dk), (*rows["q"], 1))
+        self._expect("k", td, (tokens, kv_heads, dk), (*rows["k"], 1))
+        self._expect("v", td, (tokens, kv_heads, dv), (*rows["v"], 1))
+        self._expect("position", torch.int32, (tokens,))
+        self._expect("freqs", torch.float64, (rot // 2,))
+        self._expect("q_out", td, (tokens, heads, dk), (*rows["qo"], 1), out=True)
+        self._expect("k_out", td, (tokens, kv_heads, dk), (*rows["ko"], 1), out=True)
+        self._expect("k_cache", td, (pages, page, kv_heads, dk), (*caches["kc"], 1), out=True)
+        self._expect("v_cache", td, (pages, page, kv_heads, dv), (*caches["vc"], 1), out=True)
+        self._expect("place", torch.int32, (tokens,))
+
+    def run(self, q, k, v, position, freqs, q_out, k_out=None, k_cache=None, v_cache=None, place=None, stream=None):
+        self._launch(position, "position", stream, q, k, v, position, freqs, q_out, k_out, k_cache, v_cache, place)
+
+
+def rotary_frequencies(rot, base=10000.0, factor=1.0, trained=None, low=1.0, high=4.0, device="cuda"):
+    """float64 [rot / 2]: base ** (-2 i / rot) radians per position, for texts `factor` times longer than trained on.
+
+    Without `trained` all are divided by the factor.  With it (the positions trained on), those that turn less than `low` times
+    over them are, those that turn more than `high` times stay as they are, and between them the share grows evenly with the turns."""
+    import math
+
+    import torch
+    if not low < high:
+        raise ValueError(f"low < high: got {low} and {high}")
+    f = base ** -(torch.arange(rot // 2, dtype=torch.float64, device=device) * 2 / max(rot, 1))
+    if trained is None:
+        return f / factor
+    keep = ((trained * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+    return f * keep + f / factor * (1 - keep)
+
+
+class CachePages(_Operator):
+    """seqmix_pages of `tokens` new rows in `seqs` sequences: kept, slot_index, admitted: int32 [seqs]; offsets: int64
+    [seqs + 1]; lens: int32 [slots], table: int32 [slots, max_pages], free_pages: int32 [pages], taken: int32 [1] (all updated);
+    place, position: int32 [tokens].  `empty` makes the four of a pool without requests."""
+
+    op = "pages"
+
+    def __init__(self, *, tokens, seqs, page, pages, max_pages, slots=None):
+        slots = seqs if slots is None else slots
+        super().__init__(seqmix_pages_params(tokens=tokens, seqs=seqs, slots=slots, pages=pages, max_pages=max_pages,
+                                             page=page))
+        i32 = self._torch.int32
+        self._expect("kept", i32, (seqs,))
+        self._expect("offsets", self._torch.int64, (seqs + 1,))
+        self._expect("slot_index", i32, (seqs,))
+        for n, shape in (("lens", (slots,)), ("table", (slots, max_pages)), ("free_pages", (pages,)), ("taken", (1,)),
+                         ("place", (tokens,)), ("position", (tokens,)), ("admitted", (seqs,))):
+            self._expect(n, i32, shape, out=True)
+
+    @staticmethod
+    def empty(slots, pages, max_pages, device="cuda"):
+        """lens, table, free_pages, taken."""
+        import torch
+        return (torch.zeros(slots, dtype=torch.int32, device=device),
+                torch.full((slots, max_pages), -1, dtype=torch.int32, device=device),
+                torch.arange(pages, dtype=torch.int32, device=device), torch.zeros(1, dtype=torch.int32, device=device))
+
+    def run(self, kept, lens, table, free_pages, taken, place, position, admitted, offsets=None, slot_index=None, stream=None):
+        self._launch(lens, "lens", stream, kept, offsets, slot_index, lens, table, free_pages, taken, place, position, admitted)
