@@ -125,7 +125,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.q = q, a.k = k, a.v = v, a.o = o;
     a.koff = p.page ? nullptr : key_offsets;
     a.lens = lens, a.table = table, a.tree = tree;
-    a.key_tokens = p.key_tokens, a.pages = p.pages, a.max_pages = p.max_pages;
+    a.key_tokens = p.key_tokens, a.pages = p.page ? p.pages : 1, a.max_pages = p.max_pages;
     a.kp = {p.k_page, p.k_row, p.k_head};
     a.vp = {p.v_page, p.v_row, p.v_head};
     a.q_row = p.q_row, a.q_head = p.q_head, a.o_row = p.o_row, a.o_head = p.o_head;
@@ -142,7 +142,10 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.tile = kPromptRows / a.pack;
     a.ids = seq_part_ids(a.sq, a.tile);
     const int64_t unit = 16 / esize(p.dtype);
-    const bool vec = p.dk % unit == 0 && p.dv % unit == 0;
+    // rows of k and v in 16-byte units, enough of them in a page, none that a 32-bit offset does not reach
+    const bool units = p.dk % unit == 0 && p.dv % unit == 0 && !(((uintptr_t)k | (uintptr_t)v) & 15) &&
+                       !((p.k_row | p.k_head | p.k_page | p.v_row | p.v_head | p.v_page) % unit);
+    const bool vec = units && (!p.page || p.page >= 8) && std::max(p.k_row, p.v_row) < (1LL << 24);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = p.dtype == CONV2D_BF16 ? launch_softmax_bf16(a, vec, s) : launch_softmax_f32(a, vec, s);
     return e == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;

@@ -145,6 +145,8 @@ __device__ __forceinline__ RowMask row_mask(const SoftArgs& A, const SoftPlace& 
     return m;
 }
 
+constexpr float kSlack = 8.0f;  // weights are below 2^8 then
+
 // The state of 32 rows of a wave.
 template <typename T, int DKP, int DVP>
 struct SoftRows {
@@ -275,19 +277,22 @@ struct SoftRows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
         mx = fmaxf(mx, other_half(mx)) * scale2;
-        const float now = fmaxf(m, mx);
-        const float fade = __builtin_amdgcn_exp2f(m - now);
-        m = now;
-        l *= fade;
+        // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
+        if (__any(mx > m + kSlack)) {
+            const float now = fmaxf(m, mx);
+            const float fade = __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= fade;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[mt][i] *= fade;
+                for (int i = 0; i < 16; ++i) o[mt][i] *= fade;
+        }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -now));
+                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -m));
                 l += s[b][i];
             }
             add<CAREFUL>(sV, 32 * b, s[b], seen[b]);
@@ -319,11 +324,69 @@ __device__ __forceinline__ void store4(T* p, int live, f32x4 v) {
     }
 }
 
+// A wave's 64 units of 16 bytes go from memory to LDS, from `to` on, without passing registers.  The compiler does not count
+// these loads: loads_done() waits for them.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, const u32x4* to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                     __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to)),
+                 "v"(off), "s"(r)
+                 : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Loads the rows of tiles of keys (or values) into LDS, RI rows per instruction of a wave.  What lies past the last key or past a
+// row's end reads as zero by the buffer's range.  In pages, at least RI rows of a page follow each other, and the
+// pages of a tile are looked up (next) one tile before it is loaded.
+template <typename T, int UNITS, int KT, bool OF_K>
+struct DirectLoad {
+    static constexpr int E = 16 / sizeof(T), RI = 64 / UNITS, N = KT / RI / 4;
+    static constexpr int KINDS = RI == 1 ? 2 : 1;  // an instruction's rows are in LDS in one of these orders
+    const T* base;
+    uint32_t off[KINDS];  // of this lane, in bytes
+    int page;             // lane i < N: of instruction i
+    uint32_t row_bytes, last;  // last: bytes of a row that count
+
+    __device__ __forceinline__ DirectLoad(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane / UNITS, at = lane % UNITS;
+        base = static_cast<const T*>(p) + pl.kv_head * c.head + (A.paged ? 0 : pl.key0 * c.row);
+        row_bytes = (uint32_t)c.row * sizeof(T);
+        last = dim * sizeof(T);
+        page = 0;
+#pragma unroll
+        for (int i = 0; i < KINDS; ++i) {
+            const int row = first_row(i, wave) + r;
+            const int u = (OF_K ? k_unit<UNITS>(row, at) : v_unit<UNITS>(row, at)) - row * UNITS;
+            off[i] = u * E < dim ? r * row_bytes + u * 16 : OOB_OFF;
+        }
+    }
+    static __device__ __forceinline__ int first_row(int i, int wave) { return (4 * i + wave) * RI; }
+    __device__ __forceinline__ void next(const SoftArgs& A, const SoftPlace& pl, int key0) {
+        if (!A.paged) return;
+        const int key = key0 + first_row(threadIdx.x & 63, threadIdx.x >> 6);
+        page = (threadIdx.x & 63) < N && key < pl.keys ? A.table[pl.slot * A.max_pages + (key >> A.shift)] : 0;
+    }
+    __device__ __forceinline__ void tile(const SoftArgs& A, const SoftPlace& pl, const CachePlace& c, int key0, const u32x4* to) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int in_page = A.paged ? (1 << A.shift) - 1 : -1;  // (packed: all in page 0)
+        int at[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] = min(max(__builtin_amdgcn_readlane(page, i), 0), (int)A.pages - 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = first_row(i, wave), key = key0 + row;
+            const int left = pl.keys - key;
+            const T* p = base + at[i] * c.page + (int64_t)(key & in_page) * c.row;
+            load_to_lds(make_rsrc(p, left > 0 ? (uint32_t)(min(left, RI) - 1) * row_bytes + last : 0u), off[i % KINDS],
+                        to + row * UNITS);
+        }
+    }
+};
+
 template <typename T, int DKP, int DVP, int KT, bool VEC>
-__global__ __launch_bounds__(256) void softmax_prompt_kernel(SoftArgs A) {
+__global__ __launch_bounds__(256, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_kernel(SoftArgs A) {
     using R = SoftRows<T, DKP, DVP>;
     constexpr int KU = R::KU, VU = R::VU;
-    __shared__ u32x4 sK[KT * KU], sV[KT * VU];
+    __shared__ u32x4 sK[(VEC ? 2 : 1) * KT * KU], sV[(VEC ? 2 : 1) * KT * VU];
     const int tid = threadIdx.x, wave = tid >> 6, n = tid & 31, h = tid >> 5 & 1;
     const uint32_t at = blockIdx.x / (uint32_t)A.blocks;
     SoftPlace pl;
@@ -350,26 +413,48 @@ __global__ __launch_bounds__(256) void softmax_prompt_kernel(SoftArgs A) {
         if (live) rows.q[c] = SoftMath<T>::sign(load_unit<T, VEC>(q, 2 * c + h, A.dk), A.qsign);
     }
 
-    auto load = [&](int key0) {
-        for (int x = tid; x < KT * KU; x += 256) {
-            const int r = x / KU, u = x % KU;
-            const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
-            sK[k_unit<KU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
-        }
-        for (int x = tid; x < KT * VU; x += 256) {
-            const int r = x / VU, u = x % VU;
-            const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
-            sV[v_unit<VU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
-        }
-    };
     auto pass = [&](auto careful) {
-        rows.clear();
-        for (int key0 = 0; key0 < end; key0 += KT) {
-            __syncthreads();
-            load(key0);
-            __syncthreads();
+        auto step = [&](const u32x4* k, const u32x4* v, int key0) {
             if (key0 < wave_end)
-                rows.template step<KT, decltype(careful)::value>(sK, sV, key0, key0 + KT > wave_full, mask, A.scale2);
+                rows.template step<KT, decltype(careful)::value>(k, v, key0, key0 + KT > wave_full, mask, A.scale2);
+        };
+        rows.clear();
+        if constexpr (VEC) {
+            DirectLoad<T, KU, KT, true> load_k(A, pl, A.k, A.kp, A.dk);
+            DirectLoad<T, VU, KT, false> load_v(A, pl, A.v, A.vp, A.dv);
+            auto load = [&](int key0, int b) {  // ... and the pages of the tile after it
+                load_k.tile(A, pl, A.kp, key0, sK + b * KT * KU);
+                load_v.tile(A, pl, A.vp, key0, sV + b * KT * VU);
+                load_k.next(A, pl, key0 + KT);
+                load_v.next(A, pl, key0 + KT);
+            };
+            load_k.next(A, pl, 0);
+            load_v.next(A, pl, 0);
+            int b = 0;
+            if (end > 0) load(0, 0);
+            for (int key0 = 0; key0 < end; key0 += KT, b ^= 1) {
+                loads_done();
+                __syncthreads();  // this tile is there, and the one before has been used
+                if (key0 + KT < end) load(key0 + KT, b ^ 1);
+                step(sK + b * KT * KU, sV + b * KT * VU, key0);
+            }
+            __syncthreads();
+        } else {
+            for (int key0 = 0; key0 < end; key0 += KT) {
+                __syncthreads();
+                for (int x = tid; x < KT * KU; x += 256) {
+                    const int r = x / KU, u = x % KU;
+                    const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
+                    sK[k_unit<KU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
+                }
+                for (int x = tid; x < KT * VU; x += 256) {
+                    const int r = x / VU, u = x % VU;
+                    const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
+                    sV[v_unit<VU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
+                }
+                __syncthreads();
+                step(sK, sV, key0);
+            }
         }
     };
     pass(std::false_type{});
