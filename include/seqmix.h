@@ -37,7 +37,7 @@
  *     bitwise reproducible for the same descriptor parameters.
  *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.  (Attention in bf16
  *     multiplies what it has computed in fp32, scores and states, as sums of bf16 parts: 2^-16 of each term is
- *     left out where outputs are bf16, 2^-24 where they are fp32.)
+ *     left out where outputs are bf16, 2^-24 where they are fp32.  seqmix_softmax says for itself.)
  *   - seqmix_conv, seqmix_norm, seqmix_rotary and seqmix_pages descriptors are never written by a call: any number of threads
  *     and streams may use one at a time.  A seqmix_attn or seqmix_softmax descriptor may own a workspace; like a conv2d
  *     descriptor it is used by one host thread at a time, and a call on another stream than the
@@ -218,8 +218,9 @@ int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* po
  *                    table[s][j / page], row j % page, and the slot holds lens[s] keys (the new ones among them).
  * Lengths and page numbers are clamped to what there is, so bad ones give wrong results but no access out of range.
  *
- * Precision: scores and sums are fp32 products and sums of what q, k and v hold; bf16 weights p enter their product with v as
- * two bf16 parts (2^-16 of each is left out), so results are rounded once. */
+ * Precision: scores and sums are fp32 products and sums of what q, k and v hold.  bf16: the step kernel multiplies v by weights
+ * in two bf16 parts (2^-16 of each is left out), so results are rounded once; the prompt kernel by weights rounded to
+ * bf16 (2^-8 of each at most, about the result's own rounding), which halves its longest products. */
 enum { SEQMIX_MASK_FULL = 0, SEQMIX_MASK_CAUSAL = 1, SEQMIX_MASK_TREE = 2 };
 
 #define SEQMIX_MAX_PAGE 65536
@@ -241,14 +242,15 @@ typedef struct {
     int64_t k_row, k_head, k_page, v_row, v_head, v_page;
 } seqmix_softmax_params;
 
-/* Kernels of a call: 128 rows of a sequence per workgroup, or 32, whose keys its waves divide. */
+/* Kernels of a call: 128 rows of a sequence per workgroup, or 32, whose keys its waves divide; chosen by the average number of
+ * rows of a sequence (times the heads that share a k/v head). */
 enum { SEQMIX_KERNEL_PROMPT = 0, SEQMIX_KERNEL_STEP = 1 };
 
 typedef struct {
     int32_t kernel;           /* SEQMIX_KERNEL_* */
     int32_t pack;             /* heads that share a workgroup */
-    int64_t parts;            /* 0: the keys of a row are not divided among workgroups; else such parts of all rows at most */
-    int64_t workspace_bytes;  /* results of the parts */
+    int64_t shares;           /* 0: a workgroup takes all keys of its rows; else the keys of all rows are divided in so many shares */
+    int64_t workspace_bytes;  /* results of rows whose keys are in several shares */
 } seqmix_softmax_plan_info;
 
 typedef struct seqmix_softmax_desc seqmix_softmax_desc;

@@ -117,18 +117,19 @@ def softmax_attention(q, k, v, on, scale):
     return o, o_abs, most
 
 
-def softmax_bound(o, o_abs, most, keys, dk, dtype):
+def softmax_bound(o, o_abs, most, keys, dk, dtype, parts=1):
     """How far outputs may be off, point by point, with u = 2^-24 and r = 2^-8 (half a unit in the last of bf16's 8 bits).
 
     A score is a sum of dk products, multiplied by the scale (times log2 e, rounded) and lessened by the maximum: off by (dk + 6) u of its
     sum over absolute values, `most` at most; the exponential of it is off by as much, relatively, and 4 u of its own.  The
     weights, and their products with v, are summed over `keys` keys, and rescaled when the maximum moves, by two
     roundings and an exponential (6 u) at most once for 16 keys: (2 keys + 32) u.  The quotient has this error twice.  Weights
-    enter products in bf16 as two parts, which leave r^2.  A bf16 output is rounded once: r |o|."""
+    enter products in bf16 as `parts` parts, each the rounding of what the ones before left: r^parts is left out.  A bf16
+    output is rounded once: r |o|."""
     u, r = 2.0 ** -24, 2.0 ** -8
     part = 2 * ((dk + 6) * u * most[..., None] + (2 * keys + 32) * u)
     if dtype == "bf16":
-        return (part + r * r) * (1 + r) * o_abs + r * np.abs(o) + 1e-37
+        return (part + r ** parts) * (1 + r) * o_abs + r * np.abs(o) + 1e-37
     return part * o_abs + 1e-37
 
 

@@ -14,7 +14,8 @@ PYCALL = os.path.join(HERE, "_seqmix.so")
 SOURCES = ["conv2d_api.hip", "gemm_mfma.hip", "pack_kernels.hip", "direct_kernels.hip", "slice_conv.hip",
            "probes.hip", "winograd.hip", "patch_conv.hip", "seqmix_api.hip", "linattn.hip",
            "linattn_chunks.hip", "linattn_chunks_f32.hip", "token_conv.hip", "gate_norm.hip",
-           "softmax_api.hip", "softmax_bf16.hip", "softmax_f32.hip", "rotary.hip", "cache_pages.hip"]
+           "softmax_api.hip", "softmax_prompt_bf16.hip", "softmax_prompt_f32.hip", "softmax_step_bf16.hip",
+           "softmax_step_f32.hip", "rotary.hip", "cache_pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -114,16 +114,26 @@ struct SoftArgs {
     int64_t key_tokens, pages, max_pages;
     CachePlace kp, vp;
     int64_t q_row, q_head, o_row, o_head;
-    int32_t paged, shift;  // log2 of the page
+    int32_t shift;         // log2 of a page's rows; packed (table NULL): of rows that a 32-bit offset reaches
     int32_t heads, rep, pack, blocks;  // rep heads share a k/v head; blocks of `pack` heads
     int32_t dk, dv, mask;
     int32_t qsign;         // -1, 0, 1
     float scale2;          // |scale| log2(e), where the scale is not 0
     int32_t tile;          // tokens of a tile
     int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
+    int32_t shares;        // 0: a workgroup takes a tile; else that many take the same number of quanta of all tiles' keys
+    int32_t quantum;       // log2 of its keys
+    int32_t grow;          // quanta that a tile has more than the one before it where the mask is causal; 0: not counted on
+    int32_t least, whole;  // quanta: of a share at least; units of up to so many are not divided
+    int32_t most;          // quanta of a block of heads at most
+    void* ws;              // [shares][2] results of parts
+    void* marks;           // [shares] of up to kMarkBytes each: parts that are done, zero between calls; or what is to be joined
 };
-hipError_t launch_softmax_bf16(const SoftArgs& a, bool vec, hipStream_t s);
-hipError_t launch_softmax_f32(const SoftArgs& a, bool vec, hipStream_t s);
+constexpr int kMarkBytes = 128;
+hipError_t launch_softmax_prompt_bf16(const SoftArgs& a, bool vec, hipStream_t s);
+hipError_t launch_softmax_prompt_f32(const SoftArgs& a, bool vec, hipStream_t s);
+hipError_t launch_softmax_step_bf16(const SoftArgs& a, bool vec, hipStream_t s);
+hipError_t launch_softmax_step_f32(const SoftArgs& a, bool vec, hipStream_t s);
 
 struct RotaryArgs {
     const void *q, *k, *v;

@@ -58,10 +58,10 @@ struct Workspace {
         done = nullptr;
     }
 
-    // `bytes` on the current device, once.
-    int ensure(int64_t bytes) {
+    // `bytes` on the current device, once; `cleared`: zeros.
+    int ensure(int64_t bytes, bool cleared = false) {
         if (bytes == 0) return CONV2D_OK;
-        switch (alloc(bytes)) {
+        switch (alloc(bytes, cleared)) {
             case hipSuccess: return CONV2D_OK;
             case hipErrorOutOfMemory: (void)hipGetLastError(); return CONV2D_E_ALLOC;
             case hipErrorInvalidDevice: return CONV2D_E_UNSUPPORTED;
@@ -89,7 +89,7 @@ struct Workspace {
     }
 
 private:
-    hipError_t alloc(int64_t bytes) {
+    hipError_t alloc(int64_t bytes, bool cleared) {
         int dev = -1;
         hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
@@ -97,6 +97,11 @@ private:
         e = hipEventCreateWithFlags(&done, hipEventDisableTiming);
         if (e != hipSuccess) return e;
         e = hipMalloc(&data, (size_t)bytes);
+        if (e == hipSuccess && cleared) {
+            e = hipMemset(data, 0, (size_t)bytes);  // waits for nothing that is queued; later calls wait for it
+            if (e == hipSuccess) e = hipDeviceSynchronize();
+            if (e != hipSuccess) (void)hipFree(data);
+        }
         if (e != hipSuccess) {
             (void)hipEventDestroy(done);
             done = nullptr;

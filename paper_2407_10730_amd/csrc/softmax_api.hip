@@ -10,7 +10,8 @@ using namespace cv;
 struct seqmix_softmax_desc {
     seqmix_softmax_params p;
     seqmix_softmax_plan_info plan;
-    Workspace ws;  // of plan.workspace_bytes
+    int quantum = 0;  // of shares: log2 of keys
+    Workspace ws;     // of plan.workspace_bytes
 };
 struct seqmix_rotary_desc {
     seqmix_rotary_params p;
@@ -23,6 +24,7 @@ namespace {
 
 // Heads of one call; more make 32-bit indices of a token's elements overflow.
 constexpr int32_t kMaxHeads = 1 << 20;
+constexpr int kPackedShift = 10;
 
 int log2_of(int32_t page) { return 31 - __builtin_clz((unsigned)page); }
 
@@ -51,10 +53,37 @@ int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
     return pack;
 }
 
+// Where the tiles of rows are fewer than this, their keys are divided in shares, one for each workgroup that the card holds.
+// 128 rows per tile: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles): 217 us, by tiles
+// 400; 10 packed ones, 12 heads of 64 x 128 (648 tiles): 80 us, by tiles 70.  32 rows: 64 single tokens over up to 8000
+// keys, 4 k/v heads (288): 115 us, by tiles 131; 2 over 65536 (8): 68 us, 700.
+constexpr int64_t kFullPrompt = 2 * kSeqmixCUs, kFullStep = 4 * kSeqmixCUs;
+// ... and sequences are at most this many, as each wave looks at all of them.
+constexpr int64_t kShareSeqs = 1024;
+// Shares of the prompt kernel: two workgroups per CU (the prompts above 217 us, with one 320), of fp32, whose matrix
+// instructions take 8 times as long, one (3 prompts of 31 to 1300 tokens, 6 heads of 80 x 112: 98 us, with two 119).  Of
+// the step kernel, whose tiles fill LDS, one (2 tokens as above 68 us, with two 80).
+int64_t shares_of(bool step, int dtype) { return step || dtype == CONV2D_F32 ? kSeqmixCUs : 2 * kSeqmixCUs; }
+// Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: joining parts costs some.
+constexpr int32_t kLeast = 4, kWhole = 6;
+
+int64_t part_bytes(const seqmix_softmax_params& p, int64_t rows) { return rows * ((p.dv + 3) / 4 * 16 + 16); }
+
 void plan_softmax(seqmix_softmax_desc* d) {
     const seqmix_softmax_params& p = d->p;
     const int64_t length = std::max<int64_t>((p.tokens + p.seqs - 1) / p.seqs, 1);
-    d->plan = seqmix_softmax_plan_info{SEQMIX_KERNEL_PROMPT, packed_heads(kPromptRows, length, p.heads / p.kv_heads), 0, 0};
+    const int32_t rep = p.heads / p.kv_heads;
+    const bool step = packed_heads(kStepRows, length, rep) == rep && length * rep <= kStepRows;
+    const int32_t rows = step ? kStepRows : kPromptRows, pack = packed_heads(rows, length, rep);
+    d->plan = seqmix_softmax_plan_info{step ? SEQMIX_KERNEL_STEP : SEQMIX_KERNEL_PROMPT, pack, 0, 0};
+    const int64_t blocks = p.heads / pack, tiles = p.tokens / (rows / pack) + p.seqs;
+    if (tiles * blocks < (step ? kFullStep : kFullPrompt) && p.seqs <= kShareSeqs) {
+        d->plan.shares = shares_of(step, p.dtype);
+        // quanta of all rows are counted in 32 bits
+        const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
+        for (d->quantum = step ? 7 : 6; tiles * blocks * ((keys >> d->quantum) + 2) >= 1LL << 31;) ++d->quantum;
+        d->plan.workspace_bytes = d->plan.shares * (2 * part_bytes(p, rows / pack * pack) + kMarkBytes);
+    }
 }
 
 }  // namespace
@@ -108,7 +137,7 @@ int seqmix_softmax_plan_query(const seqmix_softmax_desc* d, seqmix_softmax_plan_
 
 int seqmix_softmax_reserve(seqmix_softmax_desc* d) {
     if (!d) return CONV2D_E_NULL;
-    return d->ws.ensure(d->plan.workspace_bytes);
+    return d->ws.ensure(d->plan.workspace_bytes, true);
 }
 
 int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, const void* v, const int64_t* offsets,
@@ -124,13 +153,13 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     if (p.tokens == 0) return CONV2D_OK;
     a.q = q, a.k = k, a.v = v, a.o = o;
     a.koff = p.page ? nullptr : key_offsets;
-    a.lens = lens, a.table = table, a.tree = tree;
+    a.lens = lens, a.table = p.page ? table : nullptr, a.tree = tree;
     a.key_tokens = p.key_tokens, a.pages = p.page ? p.pages : 1, a.max_pages = p.max_pages;
     a.kp = {p.k_page, p.k_row, p.k_head};
     a.vp = {p.v_page, p.v_row, p.v_head};
     a.q_row = p.q_row, a.q_head = p.q_head, a.o_row = p.o_row, a.o_head = p.o_head;
-    a.paged = p.page > 0;
-    a.shift = p.page ? log2_of(p.page) : 0;
+    a.shift = p.page ? log2_of(p.page) : kPackedShift;
+    if (!p.page) a.kp.page = p.k_row << kPackedShift, a.vp.page = p.v_row << kPackedShift;
     a.heads = p.heads;
     a.rep = p.heads / p.kv_heads;
     a.pack = d->plan.pack;
@@ -139,16 +168,32 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.scale2 = std::fabs(p.scale) * 1.4426950408889634f;
     a.qsign = !(a.scale2 > 0.0f) ? 0 : p.scale < 0.0f ? -1 : 1;
     if (a.qsign == 0) a.scale2 = 1.0f;
-    a.tile = kPromptRows / a.pack;
-    a.ids = seq_part_ids(a.sq, a.tile);
+    const bool step = d->plan.kernel == SEQMIX_KERNEL_STEP;
     const int64_t unit = 16 / esize(p.dtype);
     // rows of k and v in 16-byte units, enough of them in a page, none that a 32-bit offset does not reach
     const bool units = p.dk % unit == 0 && p.dv % unit == 0 && !(((uintptr_t)k | (uintptr_t)v) & 15) &&
                        !((p.k_row | p.k_head | p.k_page | p.v_row | p.v_head | p.v_page) % unit);
-    const bool vec = units && (!p.page || p.page >= 8) && std::max(p.k_row, p.v_row) < (1LL << 24);
+    const bool vec = units && (!p.page || p.page >= 8) && std::max(a.kp.page, a.vp.page) < (1LL << 28) &&
+                     std::max(p.k_row, p.v_row) < (1LL << 22);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t e = p.dtype == CONV2D_BF16 ? launch_softmax_bf16(a, vec, s) : launch_softmax_f32(a, vec, s);
-    return e == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
+    a.tile = (step ? kStepRows : kPromptRows) / a.pack;
+    a.ids = seq_part_ids(a.sq, a.tile);
+    if (d->plan.shares) {
+        SM_TRY(d->ws.ensure(d->plan.workspace_bytes, true));
+        SM_TRY(d->ws.order_after_last(s));
+        a.shares = (int32_t)d->plan.shares;
+        a.quantum = d->quantum;
+        a.grow = p.mask == SEQMIX_MASK_CAUSAL && a.tile % (1 << a.quantum) == 0 ? a.tile >> a.quantum : 0;
+        a.least = kLeast;
+        a.whole = kWhole;
+        a.most = (int32_t)((1LL << 31) / a.blocks - 1);
+        a.ws = d->ws.data;
+        a.marks = static_cast<char*>(d->ws.data) +
+                                               2 * d->plan.shares * part_bytes(p, (int64_t)a.tile * a.pack);
+    }
+    auto launch = p.dtype == CONV2D_BF16 ? (step ? launch_softmax_step_bf16 : launch_softmax_prompt_bf16)
+                                         : (step ? launch_softmax_step_f32 : launch_softmax_prompt_f32);
+    return launch(a, vec, s) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
 
 // ------------------------------------------------------------------ rotary positions

@@ -7,22 +7,38 @@
 #pragma once
 
 #include <cfloat>
+#include <type_traits>
 
 #include "seqmix_device.h"
 
 namespace cv {
 
-// What a workgroup works on: rows [t0, t0 + tile) of a sequence for the heads from `head` on, keys [0, keys).
+// What a workgroup works on: a unit is rows [t0, t0 + tile) of a sequence for the heads from `head` on; a part of it is its keys
+// [first, last).
 struct SoftPlace {
-    int seq, head, kv_head;
+    int head, kv_head;
     int t0, len, keys;
+    int first, last;
     int64_t row0, slot;
-    int64_t key0;  // packed: first row of the sequence's keys
+    int64_t key0;           // packed: first row of the sequence's keys
+    uint32_t part, parts;   // of the unit; part p is that of share `share` + p
+    uint32_t share;
+
+    // All of it in scalar registers (it is the same for all threads, which the compiler does not see everywhere).
+    __device__ __forceinline__ void uniform() {
+        auto one = [](auto& v) { v = __builtin_amdgcn_readfirstlane(v); };
+        auto two = [](int64_t& v) {
+            v = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                          (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+        };
+        one(head), one(kv_head), one(t0), one(len), one(keys), one(first), one(last), one(part), one(parts), one(share);
+        two(row0), two(slot), two(key0);
+    }
 };
 
 __device__ __forceinline__ int seq_keys(const SoftArgs& A, int seq, int64_t slot, const SeqRange& r, int64_t* first) {
     *first = 0;
-    if (A.paged) {
+    if (A.table) {
         const int64_t most = A.max_pages << A.shift;
         return (int)min<int64_t>(max(A.lens[slot], 0), most);
     }
@@ -35,27 +51,204 @@ __device__ __forceinline__ int seq_keys(const SoftArgs& A, int seq, int64_t slot
     return e > b ? (int)(e - b) : 0;
 }
 
-// False: nothing to do (in all threads).
-__device__ __forceinline__ bool soft_place(const SoftArgs& A, uint32_t id, int block, SoftPlace* out) {
+__device__ __forceinline__ void soft_heads(const SoftArgs& A, int block, SoftPlace* out) {
+    out->head = block * A.pack;
+    out->kv_head = out->head / A.rep;
+}
+
+// Unit `id` of a block of heads, all of its keys.  False: there is none (in all threads).
+__device__ __forceinline__ bool soft_unit(const SoftArgs& A, uint32_t id, int block, SoftPlace* out) {
     const SeqPart sp = seq_part(A.sq, id, (uint32_t)A.tile);
     if (sp.seq >= A.sq.seqs || sp.part < 0) return false;
     const SeqRange r = seq_range(A.sq, sp.seq);
     const int64_t t0 = (int64_t)sp.part * A.tile;
     out->slot = seq_slot(A.sq, sp.seq);
     if (t0 >= r.len || out->slot < 0) return false;
-    out->seq = sp.seq;
+    soft_heads(A, block, out);
     out->t0 = (int)t0;
     out->len = (int)r.len;
     out->row0 = r.first;
-    out->head = block * A.pack;
-    out->kv_head = out->head / A.rep;
     out->keys = seq_keys(A, sp.seq, out->slot, r, &out->key0);
+    out->first = 0;
+    out->last = out->keys;
+    out->part = out->share = 0;
+    out->parts = 1;
     return true;
 }
 
+// n / d and what is left, for quotients below 2^22 (r: of d, in single precision).
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t* left) {
+    uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
+    int32_t m = (int32_t)(n - q * d);
+    if (m < 0) --q, m += d;
+    if (m >= (int32_t)d) ++q, m -= d;
+    *left = (uint32_t)m;
+    return q;
+}
+// Sums over the lanes up to this one, and over all.
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t v) {
+#define SCAN_STEP(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false);
+    SCAN_STEP(0x111, 0xf)
+    SCAN_STEP(0x112, 0xf)
+    SCAN_STEP(0x114, 0xf)
+    SCAN_STEP(0x118, 0xf)
+    SCAN_STEP(0x142, 0xa)
+    SCAN_STEP(0x143, 0xc)
+#undef SCAN_STEP
+    return v;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+
+// Shares.  Where units alone would not fill the card evenly, what there is to do is put in a row: the keys of a unit in
+// quanta, unit after unit, sequence after sequence, block of heads after block of heads.  Each workgroup takes a share of the
+// same number of quanta, which may begin and end inside units; parts of a unit are joined by the one that is done last.
+// Every wave finds its share from the lengths of all sequences (a lane each), so nothing needs to be known on the host.  Where no
+// unit has more than A.whole quanta, units are not divided: a share is a unit.
+struct SoftSeq {
+    uint32_t row0, len, keys, key0;
+    int slot;
+    uint32_t tiles, first, grow;  // tile t has first + grow t quanta
+    __device__ __forceinline__ uint32_t quanta(uint32_t n) const { return n * first + grow * (n * (n - 1) / 2); }  // of n tiles
+    __device__ __forceinline__ uint32_t longest() const { return tiles ? first + grow * (tiles - 1) : 0; }
+};
+__device__ __forceinline__ SoftSeq soft_seq(const SoftArgs& A, int i) {
+    SoftSeq s{0, 0, 0, 0, -1, 0, 0, 0};
+    if (i >= A.sq.seqs) return s;
+    const SeqRange r = seq_range(A.sq, i);
+    s.slot = (int)seq_slot(A.sq, i);
+    if (s.slot < 0) return s;
+    int64_t key0;
+    s.row0 = (uint32_t)r.first;
+    s.len = (uint32_t)r.len;
+    s.keys = (uint32_t)seq_keys(A, i, s.slot, r, &key0);
+    s.key0 = (uint32_t)key0;
+    uint32_t left;
+    s.tiles = quotient(s.len + A.tile - 1, A.tile, &left);
+    const uint32_t round = (1u << A.quantum) - 1;
+    s.first = max((s.keys + round) >> A.quantum, 1u);
+    if (A.grow && s.tiles > 1 && s.keys >= s.len) {  // the triangle of a causal mask
+        s.first = (s.keys - s.len + A.tile + round) >> A.quantum;
+        s.grow = A.grow;
+    }
+    return s;
+}
+
+// Neighbouring shares go to one XCD, where they find keys and values in its L2.
+__device__ __forceinline__ uint32_t share_of_block(const SoftArgs& A) {
+    return A.shares ? (uint32_t)xcd_remap(blockIdx.x, A.shares) : blockIdx.x;
+}
+
+struct SoftShares {
+    uint32_t each;       // quanta (or units) of a block of heads
+    uint32_t size;       // of a share
+    bool whole;          // units are not divided
+    uint32_t at, stop;   // this workgroup's
+    bool none;           // it has nothing to do
+    SoftSeq seq;         // of this lane (up to 64 sequences)
+
+    __device__ __forceinline__ uint32_t weight(const SoftSeq& s) const { return whole ? s.tiles : s.quanta(s.tiles); }
+
+    // Without shares workgroup n has one unit, the last ones (the longest of a prompt) first.
+    __device__ __forceinline__ SoftShares(const SoftArgs& A, uint32_t n) {
+        at = n;
+        stop = n + 1;
+        none = false;
+        if (!A.shares) return;
+        const int lane = threadIdx.x & 63;
+        seq = soft_seq(A, lane);
+        whole = false;
+        uint32_t work = weight(seq), units = seq.tiles, most = seq.longest();
+#pragma unroll 1
+        for (int c = 64; c < A.sq.seqs; c += 64) {
+            const SoftSeq x = soft_seq(A, c + lane);
+            work += weight(x);
+            units += x.tiles;
+            most = max(most, x.longest());
+        }
+        units = last_lane(scan_lanes(units));
+        each = last_lane(scan_lanes(work));
+        whole = __ballot(most > (uint32_t)A.whole) == 0 && units * A.blocks <= (uint32_t)A.shares;
+        // (offsets that lie may make it more than the host counted on)
+        if (!(lanes_sum<64>((float)work) <= (float)A.most) || units > (uint32_t)A.most) each = units = 0;
+        if (whole) {
+            each = units;
+            size = 1;
+        } else {
+            uint32_t left;
+            size = max(quotient(each * A.blocks + A.shares - 1, A.shares, &left), (uint32_t)A.least);
+        }
+        const uint32_t all = each * A.blocks;
+        at = min(n * size, all);
+        stop = min(at + size, all);
+        none = at >= stop;
+    }
+
+    // The part that begins at `at`, which moves to its end.
+    __device__ __forceinline__ bool next(const SoftArgs& A, SoftPlace* out) {
+        if (at >= stop) return false;
+        uint32_t y;
+        if (!A.shares) {
+            const uint32_t id = quotient(at++, A.blocks, &y);
+            return soft_unit(A, (uint32_t)A.ids - 1 - id, (int)y, out);
+        }
+        soft_heads(A, (int)quotient(at, each, &y), out);
+        uint32_t before = 0;
+#pragma unroll 1
+        for (int c = 0; c < A.sq.seqs; c += 64) {
+            const SoftSeq s = A.sq.seqs > 64 ? soft_seq(A, c + (threadIdx.x & 63)) : seq;
+            const uint32_t mine = weight(s), up = before + scan_lanes(mine), start = up - mine;
+            const uint64_t hit = __ballot(y >= start && y - start < mine);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                auto get = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+                SoftSeq u;
+                u.len = get(s.len), u.keys = get(s.keys), u.first = get(s.first), u.grow = get(s.grow), u.tiles = get(s.tiles);
+                const uint32_t in = y - get(start);
+                out->slot = (int)get((uint32_t)s.slot);
+                out->row0 = get(s.row0);
+                out->key0 = get(s.key0);
+                out->len = (int)u.len;
+                out->keys = (int)u.keys;
+                if (whole) {
+                    out->t0 = (int)(in * A.tile);
+                    out->first = 0;
+                    out->last = (int)u.keys;
+                    out->part = out->share = 0;
+                    out->parts = 1;
+                    ++at;
+                    return true;
+                }
+                uint32_t tile, left;
+                if (u.grow == 0) {
+                    tile = quotient(in, u.first, &left);
+                } else {  // the last whose tiles before it have `in` quanta at most: near the root of a quadratic
+                    const float a = (float)u.first / (float)u.grow - 0.5f;
+                    tile = (uint32_t)__builtin_amdgcn_readfirstlane(
+                        (int)fminf(fmaxf(__builtin_amdgcn_sqrtf(a * a + 2.0f * (float)in / (float)u.grow) - a, 0.0f),
+                                   (float)(u.tiles - 1)));
+                    while (tile && u.quanta(tile) > in) --tile;
+                    while (tile + 1 < u.tiles && u.quanta(tile + 1) <= in) ++tile;
+                }
+                const uint32_t unit = at - in + u.quanta(tile);  // where the unit begins
+                const uint32_t behind = unit + u.first + u.grow * tile, end = min(stop, behind);
+                out->t0 = (int)tile * A.tile;
+                out->first = (int)min((at - unit) << A.quantum, u.keys);
+                out->last = (int)min((end - unit) << A.quantum, u.keys);
+                out->share = quotient(unit, size, &left);
+                out->part = quotient(at, size, &left) - out->share;
+                out->parts = quotient(behind - 1, size, &left) - out->share + 1;
+                at = end;
+                return true;
+            }
+            before = last_lane(up);
+        }
+        return false;
+    }
+};
+
 // Element offset of a key's row, in k or v.
 __device__ __forceinline__ int64_t key_row(const SoftArgs& A, const SoftPlace& pl, const CachePlace& c, int key) {
-    if (!A.paged) return (pl.key0 + key) * c.row + pl.kv_head * c.head;
+    if (!A.table) return (pl.key0 + key) * c.row + pl.kv_head * c.head;
     const int page = A.table[pl.slot * A.max_pages + (key >> A.shift)];
     const int64_t p = min<int64_t>(max(page, 0), A.pages - 1);
     return p * c.page + (key & ((1 << A.shift) - 1)) * c.row + pl.kv_head * c.head;
@@ -78,18 +271,44 @@ __device__ __forceinline__ u32x4 load_unit(const T* row, int u, int dim) {
     return v;
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// v of lane l and of lane l ^ 32, in either order.
+__device__ __forceinline__ u32x2 both_halves(float v) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return u32x2{r[0], r[1]};
+}
+__device__ __forceinline__ float max_of_halves(float v) {
+    const f32x2 w = __builtin_bit_cast(f32x2, both_halves(v));
+    return fmaxf(w[0], w[1]);
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+    const f32x2 w = __builtin_bit_cast(f32x2, both_halves(v));
+    return w[0] + w[1];
+}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Where LDS holds unit u (16 bytes) of a row of k or v, in units.
+// Where LDS holds unit u (16 bytes) of a row of k or v, in units.  An instruction that loads past registers fills 64 units in a
+// row (RI rows); which rows and units those are, and where the next 64 begin, is free.  It is chosen such that what
+// one access takes lies in distinct banks: 16 rows of one unit of k, four rows of four or eight rows of two units of v
+// (8192 tokens, 16 heads of 128: a third of the LDS cycles were conflicts where 16 rows shared 8 places).
 template <int UNITS>
-__device__ __forceinline__ int k_unit(int row, int u) { return row * UNITS + (u ^ (row & 7)); }
+struct KeyTile {
+    static constexpr int RI = 64 / UNITS, TURN = RI >= 4 ? 3 : RI - 1, PAD = RI >= 4 ? 4 : RI;
+    static constexpr int GROUP = 64 + PAD;  // units from RI rows to the next
+    static __host__ __device__ constexpr int turn(int row) { return RI == 8 ? row >> 1 & 3 : row & TURN; }
+    static __host__ __device__ constexpr int at(int row, int u) { return row / RI * GROUP + row % RI * UNITS + (u ^ turn(row)); }
+    static constexpr int units(int rows) { return rows / RI * GROUP; }
+};
 template <int UNITS>
-__device__ __forceinline__ int v_unit(int row, int u) {
-    const int f = UNITS >= 16 ? 4 * (row & 3) ^ 2 * (row >> 2 & 1) : 4 * (row >> 1 & 1) ^ 2 * (row >> 2 & 1);
-    return row * UNITS + (u ^ f);
-}
+struct ValueTile {
+    static constexpr int RI = 64 / UNITS, GROUP = 64;
+    static __host__ __device__ constexpr int turn(int row) {
+        return UNITS >= 16 ? 4 * (row & 3) ^ 2 * (row >> 2 & 1) : 4 * (row >> 1 & 1) ^ 2 * (row >> 2 & 1);
+    }
+    static __host__ __device__ constexpr int at(int row, int u) { return row * UNITS + (u ^ turn(row)); }
+    static constexpr int units(int rows) { return rows * UNITS; }
+};
 
 template <typename T>
 struct SoftMath;
@@ -127,14 +346,17 @@ struct RowMask {
     int limit;      // keys below this (TREE: of those before the sequence's own) are seen
     int own0;       // TREE: number of the first own key
     uint64_t own;   // TREE: own keys that are seen
-    __device__ __forceinline__ bool sees(int key) const {
-        const int i = key - own0;
-        return key < limit || ((uint32_t)i < 64u && (own >> (i & 63) & 1));
+    // Bit i: whether key key0 + i is seen.
+    __device__ __forceinline__ uint64_t bits(int key0) const {
+        const int n = limit - key0, d = own0 - key0;
+        const uint64_t before = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull;
+        const uint64_t mine = d >= 64 || d <= -64 ? 0ull : d >= 0 ? own << d : own >> -d;
+        return before | mine;
     }
 };
 // ... of row t (t < 0: of none).  end: behind the last key that it sees; full: it sees all before this.
 __device__ __forceinline__ RowMask row_mask(const SoftArgs& A, const SoftPlace& pl, int t) {
-    RowMask m{pl.keys, 0x7fffffff, 0};
+    RowMask m{pl.keys, 0, 0};
     if (t < 0) m.limit = 0;
     else if (A.mask == SEQMIX_MASK_CAUSAL) m.limit = min(max(pl.keys - pl.len + t + 1, 0), pl.keys);
     else if (A.mask == SEQMIX_MASK_TREE) {
@@ -145,6 +367,8 @@ __device__ __forceinline__ RowMask row_mask(const SoftArgs& A, const SoftPlace& 
     return m;
 }
 
+constexpr int kMfma = 0x8, kDsRead = 0x100, kValu = 0x2, kTrans = 0x400;  // kinds of instructions, for sched_group_barrier
+constexpr int PLANES = 2;  // bf16 parts of a weight, where rows are few
 constexpr float kSlack = 8.0f;  // weights are below 2^8 then
 
 // The state of 32 rows of a wave.
@@ -154,6 +378,7 @@ struct SoftRows {
     u32x4 q[KU / 2];
     f32x16 o[MT];
     float m, l;
+    uint32_t odd[MT / 2];  // of o: results that are NaN
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -164,139 +389,295 @@ struct SoftRows {
         l = 0.0f;
     }
 
-    // Scores of 32 keys, from row `row` of the tile in LDS on.
-    __device__ __forceinline__ f32x16 scores(const u32x4* sK, int row) const {
-        const int n = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
-        f32x16 s;
+    // Where this lane's operands lie in a tile of k and of v, in bytes.  The units of a row are permuted by an exclusive or with
+    // a number of the row below 16 (k: 4), which is the same for all of the lane's rows (of bf16, and of k), so four (two)
+    // addresses and constant distances are enough.
+    using KT_ = KeyTile<KU>;
+    using VT_ = ValueTile<VU>;
+    uint32_t at_k[2], at_v[4];
+    __device__ __forceinline__ void place() {
+        const int l64 = threadIdx.x & 63, n = l64 & 31, h = l64 >> 5;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < KU / 2; ++c) s = SoftMath<T>::score(sK[k_unit<KU>(row + n, 2 * c + h)], q[c], s);
-        return s;
+        for (int x = 0; x < 4; ++x) {
+            if (x < 2) at_k[x] = KT_::at(n, 2 * x + h) * 16;
+            if constexpr (sizeof(T) == 2) {  // column 32 x, rows 4 h + 0 .. 3 by the lane's place among 16
+                const int col = (32 * x + 16 * (l64 >> 4 & 1) + 4 * (l64 & 3)) % DVP;
+                at_v[x] = VT_::at(4 * h + (l64 & 15) / 4, col / 8) * 16 + (col & 4) * 2;
+            } else {  // row 4 h + x, less x rows
+                at_v[x] = (VT_::at(4 * h + x, n / 4) - x * VU) * 16 + (n & 3) * 4;
+            }
+        }
+    }
+    template <typename V>
+    static __device__ __forceinline__ V read(uint32_t at) {
+        return *(const __attribute__((address_space(3))) V*)(uintptr_t)at;
     }
 
-    // Adds 32 keys with weights p (as scores() leaves them).  CAREFUL: values that are not finite count only for rows that see
-    // them (`seen`, a bit for each of p), and make them NaN.
-    template <bool CAREFUL>
-    __device__ __forceinline__ void add(const u32x4* sV, int row, const f32x16& p, uint32_t seen) {
-        const int l64 = threadIdx.x & 63, h = l64 >> 5;
+    // Scores of 32 NB keys.
+    template <int NB>
+    __device__ __forceinline__ void scores(uint32_t tile, f32x16 (&s)[NB]) const {
+        constexpr int C = KU / 2, X = NB * C, D = 4;  // operands are read D products ahead
+        uint32_t at[2] = {tile + at_k[0], tile + at_k[1]};
+        asm volatile("" : "+v"(at[0]), "+v"(at[1]));  // (or each address is computed anew, where a constant offset does)
+        auto operand = [&](int x) {
+            return read<u32x4>(at[x % C & 1] + ((x % C >> 1) * 64 + x / C * (KT_::units(32) * 16)));
+        };
+        u32x4 k[D];
+#pragma unroll
+        for (int x = 0; x < D; ++x) k[x] = operand(x);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            s[x / C] = SoftMath<T>::score(k[x % D], q[x % C], s[x / C]);
+            if (x + D < X) k[x % D] = operand(x + D);
+        }
+        constexpr int PER = sizeof(T) == 2 ? 1 : 4;  // matrix instructions of a product
+        __builtin_amdgcn_sched_group_barrier(kDsRead, D, 0);
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, PER, 0);
+            if (x + D < X) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
+    }
+
+    // v as an operand: of bf16 the 16 keys from `row` on, columns 32 mt ..; of fp32 the keys that weight i of p belongs to.
+    struct ValuePlaces {
+        uint32_t at[4];
+    };
+    __device__ __forceinline__ ValuePlaces places(uint32_t tile) const {
+        ValuePlaces p;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            p.at[x] = tile + at_v[x];
+            asm volatile("" : "+v"(p.at[x]));
+        }
+        return p;
+    }
+    static __device__ __forceinline__ u32x4 values(const ValuePlaces& p, int row, int mt) {
+        u32x4 v;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t at = p.at[mt & 3] + ((mt >> 2) * 256 + (row + 8 * x) * (VU * 16));
+            const u32x2 w = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
+            v[2 * x] = w[0];
+            v[2 * x + 1] = w[1];
+        }
+        return v;
+    }
+    __device__ __forceinline__ float value(uint32_t tile, int i, int mt) const {
+        // (column 32 mt is 8 mt units on, of which the row's number may turn bit 3)
+        return read<float>(tile + ((at_v[i & 3]) ^ ((mt & 1) * 128)) + (mt >> 1) * 256 + (32 * (i / 16) + 8 * (i % 16 / 4) + i % 4) * (VU * 16));
+    }
+
+    // Adds 32 NB keys with weights p (as scores() leaves them).
+    template <int NB>
+    __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB]) {
         if constexpr (sizeof(T) == 2) {
+            constexpr int X = 2 * NB * MT, D = 2;
+            const ValuePlaces at = places(tile);
+            u32x4 v[D];
+            bf16x8 part[PLANES];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                bf16x8 hi, lo, on;
+            for (int x = 0; x < D; ++x) v[x] = values(at, 16 * (x / MT), x % MT);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    hi[j] = (__bf16)p[8 * c + j];
-                    lo[j] = (__bf16)(p[8 * c + j] - (float)hi[j]);
-                    if constexpr (CAREFUL) on[j] = (__bf16)((seen >> (8 * c + j)) & 1 ? 1.0f : 0.0f);
-                }
-                const int r0 = row + 16 * c + 4 * h + (l64 & 15) / 4, col = 16 * (l64 >> 4 & 1) + 4 * (l64 & 3);
+            for (int x = 0; x < X; ++x) {
+                const int c = x / MT, mt = x % MT;
+                if (mt == 0) planes(p[c / 2], 8 * (c % 2), part);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    u32x4 v;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int r = r0 + 8 * x;
-                        const char* at = reinterpret_cast<const char*>(sV) + v_unit<VU>(r, (32 * mt + col) / 8) * 16 + (col & 4) * 2;
-                        const u32x2 w = __builtin_bit_cast(
-                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
-                        v[2 * x] = w[0];
-                        v[2 * x + 1] = w[1];
-                    }
-                    if constexpr (CAREFUL) {
-                        u32x4 odd;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const bool a = (v[i] & 0x7f80u) == 0x7f80u, b = (v[i] & 0x7f800000u) == 0x7f800000u;
-                            odd[i] = (a ? 0x3f80u : 0u) | (b ? 0x3f800000u : 0u);
-                            v[i] &= (a ? 0u : 0xffffu) | (b ? 0u : 0xffff0000u);
-                        }
-                        f32x16 count;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) count[i] = 0.0f;
-                        count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, odd), on, count, 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[mt][i] = count[i] > 0.0f ? NAN : o[mt][i];
-                    }
-                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), hi, o[mt], 0, 0, 0);
-                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), lo, o[mt], 0, 0, 0);
-                }
+                for (int i = 0; i < PLANES; ++i)
+                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[x % D]), part[i], o[mt], 0, 0, 0);
+                if (x + D < X) v[x % D] = values(at, 16 * ((x + D) / MT), (x + D) % MT);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = row + 8 * (i / 4) + 4 * h + i % 4;
+            for (int i = 0; i < 16 * NB; ++i)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const int col = 32 * mt + (l64 & 31);
-                    float v = reinterpret_cast<const float*>(sV + v_unit<VU>(r, col / 4))[col & 3];
-                    if constexpr (CAREFUL) {
-                        const bool odd = !(__builtin_fabsf(v) <= FLT_MAX);
-                        f32x16 count;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) count[j] = 0.0f;
-                        count = __builtin_amdgcn_mfma_f32_32x32x2f32(odd ? 1.0f : 0.0f, seen >> i & 1 ? 1.0f : 0.0f, count, 0, 0, 0);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) o[mt][j] = count[j] > 0.0f ? NAN : o[mt][j];
-                        v = odd ? 0.0f : v;
-                    }
-                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[mt], 0, 0, 0);
-                }
-            }
+                for (int mt = 0; mt < MT; ++mt)
+                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tile, i, mt), p[i / 16][i % 16], o[mt], 0, 0, 0);
         }
     }
 
+    // 8 weights, from number `first` of p on, as bf16 parts, each the rounding of what the ones before left.
+    static __device__ __forceinline__ void planes(const f32x16& p, int first, bf16x8 (&part)[PLANES]) {
+        u32x4 w[PLANES];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float a = p[first + 2 * j], b = p[first + 2 * j + 1];
+#pragma unroll
+            for (int i = 0; i < PLANES; ++i) {
+                const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+                w[i][j] = both;
+                a -= __builtin_bit_cast(float, both << 16);
+                b -= __builtin_bit_cast(float, both & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i) part[i] = __builtin_bit_cast(bf16x8, w[i]);
+    }
+
+    __device__ __forceinline__ void rescale(float mx) {
+        const float now = fmaxf(m, mx);
+        const float fade = __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= fade;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[mt][i] *= fade;
+    }
+
     // One tile of KT keys, of which lane i of s[b] is key key0 + 32 b + 8 (i / 4) + 4 h + i % 4.
-    template <int KT, bool CAREFUL>
-    __device__ __forceinline__ void step(const u32x4* sK, const u32x4* sV, int key0, bool masked, const RowMask& mask,
-                                         float scale2) {
+    template <int KT>
+    __device__ __forceinline__ void step(uint32_t tile_k, uint32_t tile_v, int key0, bool masked, bool counting,
+                                         const RowMask& mask, float scale2) {
         constexpr int NB = KT / 32;
         const int h = threadIdx.x >> 5 & 1;
         f32x16 s[NB];
-        uint32_t seen[NB];
-        float mx = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            s[b] = scores(sK, 32 * b);
-            seen[b] = 0xffff;
-        }
+        scores(tile_k, s);
+        uint64_t seen = ~0ull;
+        auto sees = [&](int b, int i) { return (uint32_t)(seen >> (32 * b)) >> (8 * (i / 4) + i % 4) & 1; };
         if (masked) {
+            seen = mask.bits(key0) >> (4 * h);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                seen[b] = 0;
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool on = mask.sees(key0 + 32 * b + 8 * (i / 4) + 4 * h + i % 4);
-                    s[b][i] = on ? s[b][i] : -INFINITY;
-                    seen[b] |= on ? 1u << i : 0u;
-                }
-            }
+                for (int i = 0; i < 16; ++i) s[b][i] = sees(b, i) ? s[b][i] : -INFINITY;
         }
+        float mx = -INFINITY;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-        mx = fmaxf(mx, other_half(mx)) * scale2;
+        mx = max_of_halves(mx) * scale2;
         // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
-        if (__any(mx > m + kSlack)) {
-            const float now = fmaxf(m, mx);
-            const float fade = __builtin_amdgcn_exp2f(m - now);
-            m = now;
-            l *= fade;
+        if (__any(mx > m + kSlack)) rescale(mx);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[mt][i] *= fade;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -m));
                 l += s[b][i];
             }
-            add<CAREFUL>(sV, 32 * b, s[b], seen[b]);
+        if (counting) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[b][i] = sees(b, i) ? 1.0f : 0.0f;
         }
+        add(tile_v, s);
+    }
+
+    // After a pass that counted: which results see a value that is not finite.
+    __device__ __forceinline__ void counted() {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) odd[mt / 2] |= o[mt][i] > 0.0f ? 1u << (mt % 2 * 16 + i) : 0u;
+    }
+    __device__ __forceinline__ void mark() {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[mt][i] = odd[mt / 2] >> (mt % 2 * 16 + i) & 1 ? NAN : o[mt][i];
+    }
+
+    // The same in two steps, for blocks of 32 keys of bf16, so that each has matrix instructions of one block beside vector
+    // instructions of another: `lead` adds the weights w of the block before and finds the maximum of this one's scores s (and
+    // rescales), `follow` turns them into weights and computes the scores of the next one.  The compiler puts the two kinds
+    // one after the other (8192 tokens, 16 heads of 128: 322 us, 315), so each matrix instruction is fenced off
+    // with what is to run beside it.  Each step begins with operands that the one before has read (AHEAD).
+    static constexpr int AHEAD = 4;
+    struct KeyPlaces {
+        uint32_t at[2];
+    };
+    __device__ __forceinline__ KeyPlaces key_places(uint32_t tile) const {
+        KeyPlaces p{{tile + at_k[0], tile + at_k[1]}};
+        asm volatile("" : "+v"(p.at[0]), "+v"(p.at[1]));  // (or each address is computed anew, where a constant offset does)
+        return p;
+    }
+    static __device__ __forceinline__ u32x4 keys(const KeyPlaces& p, int x) { return read<u32x4>(p.at[x & 1] + (x >> 1) * 64); }
+    static __device__ __forceinline__ u32x4 values_of(const ValuePlaces& p, int x) { return values(p, 16 * (x / MT), x % MT); }
+    static __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+    __device__ __forceinline__ void lead(const ValuePlaces& at, u32x4 (&v)[AHEAD], const u32x4 (&w)[2], f32x16& s, bool masked,
+                                         uint32_t seen, float scale2, const KeyPlaces& then, u32x4 (&k)[AHEAD]) {
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = seen >> (8 * (i / 4) + i % 4) & 1 ? s[i] : -INFINITY;
+        }
+        constexpr int X = 2 * MT;
+        float mx = -INFINITY;
+        __builtin_amdgcn_s_setprio(1);  // the other wave has vector instructions: 318 us, 313
+        fence();
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            o[x % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[x % AHEAD]),
+                                                                __builtin_bit_cast(bf16x8, w[x / MT]), o[x % MT], 0, 0, 0);
+            if (x + AHEAD < X) v[x % AHEAD] = values_of(at, x + AHEAD);
+            else k[x + AHEAD - X] = keys(then, x + AHEAD - X);
+#pragma unroll
+            for (int i = 16 * x / X; i < 16 * (x + 1) / X; ++i) mx = fmaxf(mx, s[i]);
+            fence();
+        }
+        __builtin_amdgcn_s_setprio(0);
+        mx = max_of_halves(mx) * scale2;
+        if (__any(mx > m + kSlack)) rescale(mx);
+    }
+    template <bool MORE>  // the next step's first values can be read
+    __device__ __forceinline__ void follow(const KeyPlaces& at, u32x4 (&k)[AHEAD], const f32x16& s, float scale2, f32x16& next,
+                                           u32x4 (&w)[2], const ValuePlaces& then, u32x4 (&v)[AHEAD]) {
+        constexpr int X = KU / 2;
+        float p[16], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[i] = 0.0f;
+        fence();
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            next = SoftMath<T>::score(k[x % AHEAD], q[x], next);
+            if (x + AHEAD < X) k[x % AHEAD] = keys(at, x + AHEAD);
+            else if (MORE) v[x + AHEAD - X] = values_of(then, x + AHEAD - X);
+#pragma unroll
+            for (int i = 16 * x / X; i < 16 * (x + 1) / X; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale2, -m));
+                if (i & 1) {
+                    w[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[i - 1], p[i]}, bf16x2));
+                    asm volatile("" : "+v"(w[i / 8][i % 8 / 2]));
+                    sum[i / 2 & 1] += p[i - 1] + p[i];
+                }
+            }
+            fence();
+        }
+        l += sum[0] + sum[1];
+    }
+    __device__ __forceinline__ void first_scores(uint32_t tile_k, f32x16& s) const {
+        f32x16 x[1];
+        scores(tile_k, x);
+        s = x[0];
+    }
+    __device__ __forceinline__ void last_product(uint32_t tile_v, const u32x4 (&w)[2]) {
+        const ValuePlaces at = places(tile_v);
+#pragma unroll
+        for (int x = 0; x < 2 * MT; ++x)
+            o[x % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(at, 16 * (x / MT), x % MT)),
+                                                                __builtin_bit_cast(bf16x8, w[x / MT]), o[x % MT], 0, 0, 0);
+    }
+    // (A pass that counts has ones for what is seen in place of weights.)
+    __device__ __forceinline__ void seen_weights(uint32_t seen, u32x4 (&w)[2]) const {
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const uint32_t b = seen >> (8 * (i / 4) + i % 4) & 3;
+            w[i / 8][i % 8 / 2] = (b & 1 ? 0x3f80u : 0u) | (b & 2 ? 0x3f800000u : 0u);
+        }
+    }
+
+    __device__ __forceinline__ void turn_q(int sign) {
+#pragma unroll
+        for (int c = 0; c < KU / 2; ++c) q[c] = SoftMath<T>::sign(q[c], sign);
     }
 
     // Whether a value that is not finite came up (in any lane): what rows that do not see it hold has to be computed again.
@@ -324,74 +705,203 @@ __device__ __forceinline__ void store4(T* p, int live, f32x4 v) {
     }
 }
 
-// A wave's 64 units of 16 bytes go from memory to LDS, from `to` on, without passing registers.  The compiler does not count
-// these loads: loads_done() waits for them.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, const u32x4* to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
-                     __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)to)),
-                 "v"(off), "s"(r)
-                 : "memory");
-}
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-// Loads the rows of tiles of keys (or values) into LDS, RI rows per instruction of a wave.  What lies past the last key or past a
-// row's end reads as zero by the buffer's range.  In pages, at least RI rows of a page follow each other, and the
-// pages of a tile are looked up (next) one tile before it is loaded.
-template <typename T, int UNITS, int KT, bool OF_K>
-struct DirectLoad {
-    static constexpr int E = 16 / sizeof(T), RI = 64 / UNITS, N = KT / RI / 4;
-    static constexpr int KINDS = RI == 1 ? 2 : 1;  // an instruction's rows are in LDS in one of these orders
-    const T* base;
-    uint32_t off[KINDS];  // of this lane, in bytes
-    int page;             // lane i < N: of instruction i
-    uint32_t row_bytes, last;  // last: bytes of a row that count
-
-    __device__ __forceinline__ DirectLoad(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane / UNITS, at = lane % UNITS;
-        base = static_cast<const T*>(p) + pl.kv_head * c.head + (A.paged ? 0 : pl.key0 * c.row);
-        row_bytes = (uint32_t)c.row * sizeof(T);
-        last = dim * sizeof(T);
-        page = 0;
-#pragma unroll
-        for (int i = 0; i < KINDS; ++i) {
-            const int row = first_row(i, wave) + r;
-            const int u = (OF_K ? k_unit<UNITS>(row, at) : v_unit<UNITS>(row, at)) - row * UNITS;
-            off[i] = u * E < dim ? r * row_bytes + u * 16 : OOB_OFF;
-        }
+// What a part leaves in the workspace: for each row of its tile the maximum and the sum of the weights, and the sums over v.
+// Parts of a row may run on different XCDs, whose L2 caches are not coherent: where the same launch joins them
+// (SAME), everything is stored and loaded past the caches (device scope).
+template <bool SAME>
+struct PartRows {
+    static constexpr int kDevice = SAME ? 1 << 4 : 0;  // cache policy bit of buffer accesses
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t row_bytes;
+    // A share has places for two parts: of a unit that began before it, and of one that begins in it (part 0).
+    __device__ __forceinline__ PartRows(const SoftArgs& A, const SoftPlace& pl, uint32_t part) {
+        const uint32_t rows = (uint32_t)A.tile * A.pack;
+        row_bytes = ((uint32_t)A.dv + 3) / 4 * 16 + 16;
+        r = make_rsrc(static_cast<char*>(A.ws) + (int64_t)(2 * (pl.share + part) + (part == 0)) * (rows * row_bytes),
+                      rows * row_bytes);
     }
-    static __device__ __forceinline__ int first_row(int i, int wave) { return (4 * i + wave) * RI; }
-    __device__ __forceinline__ void next(const SoftArgs& A, const SoftPlace& pl, int key0) {
-        if (!A.paged) return;
-        const int key = key0 + first_row(threadIdx.x & 63, threadIdx.x >> 6);
-        page = (threadIdx.x & 63) < N && key < pl.keys ? A.table[pl.slot * A.max_pages + (key >> A.shift)] : 0;
+    __device__ __forceinline__ void put_sums(int row, f32x2 v) const {
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, row * row_bytes, 0, kDevice);
     }
-    __device__ __forceinline__ void tile(const SoftArgs& A, const SoftPlace& pl, const CachePlace& c, int key0, const u32x4* to) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int in_page = A.paged ? (1 << A.shift) - 1 : -1;  // (packed: all in page 0)
-        int at[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) at[i] = min(max(__builtin_amdgcn_readlane(page, i), 0), (int)A.pages - 1);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int row = first_row(i, wave), key = key0 + row;
-            const int left = pl.keys - key;
-            const T* p = base + at[i] * c.page + (int64_t)(key & in_page) * c.row;
-            load_to_lds(make_rsrc(p, left > 0 ? (uint32_t)(min(left, RI) - 1) * row_bytes + last : 0u), off[i % KINDS],
-                        to + row * UNITS);
-        }
+    __device__ __forceinline__ void put(int row, int c, f32x4 v) const {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, row * row_bytes + 16 + c * 4, 0, kDevice);
+    }
+    __device__ __forceinline__ f32x2 sums(int row) const {
+        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, row * row_bytes, 0, kDevice));
+    }
+    __device__ __forceinline__ f32x4 get(int row, int c) const {
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, row * row_bytes + 16 + c * 4, 0, kDevice));
     }
 };
 
-template <typename T, int DKP, int DVP, int KT, bool VEC>
-__global__ __launch_bounds__(256, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_kernel(SoftArgs A) {
-    using R = SoftRows<T, DKP, DVP>;
-    constexpr int KU = R::KU, VU = R::VU;
-    __shared__ u32x4 sK[(VEC ? 2 : 1) * KT * KU], sV[(VEC ? 2 : 1) * KT * VU];
-    const int tid = threadIdx.x, wave = tid >> 6, n = tid & 31, h = tid >> 5 & 1;
-    const uint32_t at = blockIdx.x / (uint32_t)A.blocks;
-    SoftPlace pl;
-    if (!soft_place(A, (uint32_t)A.ids - 1 - at, (int)(blockIdx.x - at * A.blocks), &pl)) return;
+// Joins the parts of a unit, in their order: rows [first, first + rows) of its tile.
+template <typename T, bool VEC, bool SAME>
+__device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl, int first, int rows, int threads) {
+    const int groups = (A.dv + 3) / 4;
+#pragma unroll 1
+    for (int x = threadIdx.x; x < rows * groups; x += threads) {
+        const int at = x / groups, row = first + at, c = 4 * (x - at * groups);
+        f32x4 o{0, 0, 0, 0};
+        float m = -FLT_MAX, l = 0.0f;
+        constexpr int AHEAD = SAME ? 4 : 8;
+#pragma unroll 1
+        for (uint32_t p = 0; p < pl.parts; p += AHEAD) {
+            f32x2 s[AHEAD];
+            f32x4 v[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const PartRows<SAME> part(A, pl, min(p + i, pl.parts - 1));
+                s[i] = part.sums(row);
+                v[i] = part.get(row, c);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (p + i < pl.parts) {
+                    const float now = fmaxf(m, s[i][0]);
+                    const float a = __builtin_amdgcn_exp2f(m - now), b = __builtin_amdgcn_exp2f(s[i][0] - now);
+                    m = now;
+                    l = l * a + s[i][1] * b;
+                    o = o * a + v[i] * b;
+                }
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int t = pl.t0 + row / A.pack, head = pl.head + row % A.pack;
+        store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head + c, A.dv - c, o * inv);
+    }
+}
 
+// Few rows are joined by the workgroup whose part is done last, which clears their count for the next call.  The others return
+// at once.
+template <typename T, bool VEC>
+__device__ __forceinline__ void join_last(const SoftArgs& A, const SoftPlace& pl, int threads) {
+    __shared__ int s_last;
+    uint32_t* const count = static_cast<uint32_t*>(A.marks) + pl.share;  // only one unit begins in a share and goes on behind it
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's results are where all XCDs see them
+    __syncthreads();
+    if (threadIdx.x == 0)
+        s_last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pl.parts - 1;
+    __syncthreads();
+    if (!s_last) return;
+    join_rows<T, VEC, true>(A, pl, 0, min(A.tile, pl.len - pl.t0) * A.pack, threads);
+    if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Values that are not finite would reach rows that do not see them, as a product with zero.  Where a pass over the keys comes
+// upon one (in the result, at no cost while there is none), two more passes follow: one counts, for each result, the
+// values of that kind that its row sees, and one leaves them out.  For them the values in LDS are replaced: 16 bytes by
+// ones where they are not finite and zeros else (COUNT), or by themselves with zeros there.
+enum { PLAIN = 0, COUNT = 1, CLEAN = 2 };
+template <typename T>
+__device__ __forceinline__ u32x4 only_finite(u32x4 v, bool count) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            const bool a = (v[i] & 0x7f80u) == 0x7f80u, b = (v[i] & 0x7f800000u) == 0x7f800000u;
+            v[i] = count ? (a ? 0x3f80u : 0u) | (b ? 0x3f800000u : 0u) : v[i] & ((a ? 0u : 0xffffu) | (b ? 0u : 0xffff0000u));
+        } else {
+            const bool a = (v[i] & 0x7f800000u) == 0x7f800000u;
+            v[i] = count ? (a ? 0x3f800000u : 0u) : a ? 0u : v[i];
+        }
+    }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void clean_tile(u32x4* v, int units, int from, int step, int mode) {
+#pragma unroll 1
+    for (int x = from; x < units; x += step) v[x] = only_finite<T>(v[x], mode == COUNT);
+}
+
+// A wave's 64 units of 16 bytes go from memory to LDS, from byte `to` + MORE on, without passing registers.  The compiler does not count
+// these loads: loads_done() waits for them.
+// WAIT: wait states; five where a part of r comes straight from a lane.
+template <int WAIT, int MORE>
+__device__ __forceinline__ void load_to_lds(u32x4 r, uint32_t off, uint32_t to) {
+    asm volatile("s_add_i32 m0, %0, %4\n\ts_nop %3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r), "n"(WAIT - 1),
+                 "n"(MORE)
+                 : "memory", "scc");
+}
+template <int N, typename F>
+__device__ __forceinline__ void each_of(F f) {  // f(0) .. f(N - 1), as constants
+    if constexpr (N > 0) {
+        each_of<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+// ... 64 elements of 4 bytes.
+__device__ __forceinline__ void load_words_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r) : "memory");
+}
+typedef __attribute__((address_space(3))) const void* lds_address;
+template <int LEFT = 0>  // all but the last LEFT
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT < 63 ? LEFT : 63) : "memory"); }
+
+// Loads the rows of tiles of keys (or values) into LDS, RI rows per instruction of a wave.  What lies past the last key or past a
+// row's end reads as zero by the buffer's range.  Where a page (of packed rows: some rows that a 32-bit offset
+// reaches) begins, and how much of it counts, is worked out for all instructions of a tile at once, a lane each.
+template <typename T, int UNITS, int KT, int WAVES, typename LDS>
+struct DirectLoad {
+    static constexpr int E = 16 / sizeof(T), RI = 64 / UNITS, N = KT / RI / WAVES;
+    static constexpr int KINDS = RI * WAVES < 8 ? 8 / (RI * WAVES) : 1;  // rows of instructions i and i + KINDS have one order
+    uint64_t base;
+    uint32_t off[KINDS];  // of this lane, in bytes
+    uint32_t page_bytes, row_bytes, last;  // last: bytes of a row that count
+    int wave;             // (0: each wave loads its own tiles)
+
+    __device__ __forceinline__ DirectLoad(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim) {
+        const int lane = threadIdx.x & 63, r = lane / UNITS, at = lane % UNITS;
+        base = reinterpret_cast<uint64_t>(static_cast<const T*>(p) + pl.kv_head * c.head + pl.key0 * c.row);
+        page_bytes = (uint32_t)c.page * sizeof(T);
+        row_bytes = (uint32_t)c.row * sizeof(T);
+        last = dim * sizeof(T);
+        wave = WAVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+#pragma unroll
+        for (int i = 0; i < KINDS; ++i) {
+            const int row = first_row(i) + r;
+            const int u = at ^ LDS::turn(row);
+            off[i] = u * E < dim ? r * row_bytes + u * 16 : OOB_OFF;
+        }
+    }
+    // WAVES waves load a tile together, or each its own (1).
+    __device__ __forceinline__ int first_row(int i) const { return (WAVES * i + wave) * RI; }
+    // `page` of lane i: of instruction i's rows.  What an instruction's buffer is comes from its lane, or from lane 0 for
+    // all where the tile lies in one page (tiles begin at multiples of KT).
+    __device__ __forceinline__ void tile(const SoftArgs& A, const SoftPlace& pl, int key0, int page, uint32_t to) const {
+        constexpr int LINE = LDS::GROUP * 16;
+        auto get = [&](uint32_t v, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)v, i); };
+        to += wave * LINE;
+        if ((1 << A.shift) >= KT) {
+            const uint32_t key = (uint32_t)(key0 + wave * RI), at = A.table ? get((uint32_t)page, 0) : key >> A.shift;
+            const uint64_t p = base + (uint64_t)at * page_bytes + (uint64_t)(key & ((1u << A.shift) - 1)) * row_bytes;
+            const int left = pl.keys - (int)key;
+            const uint32_t rows = left < KT ? left : KT, each = WAVES * RI * row_bytes;
+            const uint32_t bytes = left > 0 ? (rows - 1) * row_bytes + last : 0u;
+            const u32x4 r{(uint32_t)p, (uint32_t)(p >> 32), bytes, RSRC_WORD3};
+            each_of<N>([&](auto i) { load_to_lds<1, i * WAVES * LINE>(r, off[i % KINDS] + i * each, to); });
+        } else {
+            const int key = key0 + first_row(threadIdx.x & 63);
+            const uint64_t p = base + (uint64_t)(uint32_t)page * page_bytes +
+                               (uint64_t)(uint32_t)(key & ((1 << A.shift) - 1)) * row_bytes;
+            const int rows = min(max(pl.keys - key, 0), RI);
+            const uint32_t bytes = rows ? (rows - 1) * row_bytes + last : 0u;
+            each_of<N>([&](auto i) {
+                load_to_lds<5, i * WAVES * LINE>(u32x4{get((uint32_t)p, i), get((uint32_t)(p >> 32), i), get(bytes, i), RSRC_WORD3},
+                                                 off[i % KINDS], to);
+            });
+        }
+    }
+};
+// The page that holds the rows of lane i's instruction.
+__device__ __forceinline__ int clamp_page(const SoftArgs& A, int page) { return min(max(page, 0), (int)A.pages - 1); }
+
+constexpr int kPromptWaves = kPromptRows / 32;
+
+// One part of a unit.
+template <typename T, int DKP, int DVP, int KT, bool VEC>
+__device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& pl, u32x4* lds) {
+    using R = SoftRows<T, DKP, DVP>;
+    constexpr int KU = R::KU, VU = R::VU, KEYS = KeyTile<KU>::units(KT);
+    u32x4 *const sK = lds, *const sV = lds + (VEC ? 2 : 1) * KEYS;
+    const int tid = threadIdx.x, wave = tid >> 6, n = tid & 31, h = tid >> 5 & 1;
     // this lane's row, and the rows of its wave and of the workgroup
     const int row = 32 * wave + n;
     const int t = pl.t0 + row / A.pack, head = pl.head + row % A.pack;
@@ -400,111 +910,449 @@ __global__ __launch_bounds__(256, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_
     const bool causal = A.mask == SEQMIX_MASK_CAUSAL, tree = A.mask == SEQMIX_MASK_TREE;
     const int back = pl.keys - pl.len;
     auto behind = [&](int tt) { return causal ? min(max(back + min(tt, pl.len - 1) + 1, 0), pl.keys) : pl.keys; };
-    const int end = behind(pl.t0 + A.tile - 1);
+    const int end = min(behind(pl.t0 + A.tile - 1), pl.last);
     const int w0 = pl.t0 + 32 * wave / A.pack;
     const int wave_end = w0 < pl.len ? behind(pl.t0 + (32 * wave + 31) / A.pack) : 0;
     const int wave_full = tree ? max(back, 0) : behind(w0);
 
     R rows;
+#pragma unroll
+    for (int i = 0; i < R::MT / 2; ++i) rows.odd[i] = 0;
+    rows.place();
     const T* q = static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head;
 #pragma unroll
     for (int c = 0; c < KU / 2; ++c) {
         rows.q[c] = u32x4{0, 0, 0, 0};
-        if (live) rows.q[c] = SoftMath<T>::sign(load_unit<T, VEC>(q, 2 * c + h, A.dk), A.qsign);
+        if (live) rows.q[c] = load_unit<T, VEC>(q, 2 * c + h, A.dk);
     }
+    if (A.qsign != 1) rows.turn_q(A.qsign);
 
-    auto pass = [&](auto careful) {
-        auto step = [&](const u32x4* k, const u32x4* v, int key0) {
+    const uint32_t at_k = (uint32_t)(uintptr_t)(lds_address)sK, at_v = (uint32_t)(uintptr_t)(lds_address)sV;
+#pragma unroll 1
+    for (int mode = PLAIN;; ++mode) {
+        auto step = [&](int b, int key0) {
+            if (mode) {
+                clean_tile<T>(sV + b * KT * VU, KT * VU, tid, 64 * kPromptWaves, mode);
+                __syncthreads();
+            }
             if (key0 < wave_end)
-                rows.template step<KT, decltype(careful)::value>(k, v, key0, key0 + KT > wave_full, mask, A.scale2);
+                rows.template step<KT>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, key0 + KT > wave_full,
+                                       mode == COUNT, mask, A.scale2);
         };
         rows.clear();
         if constexpr (VEC) {
-            DirectLoad<T, KU, KT, true> load_k(A, pl, A.k, A.kp, A.dk);
-            DirectLoad<T, VU, KT, false> load_v(A, pl, A.v, A.vp, A.dv);
-            auto load = [&](int key0, int b) {  // ... and the pages of the tile after it
-                load_k.tile(A, pl, A.kp, key0, sK + b * KT * KU);
-                load_v.tile(A, pl, A.vp, key0, sV + b * KT * VU);
-                load_k.next(A, pl, key0 + KT);
-                load_v.next(A, pl, key0 + KT);
+            constexpr bool PIPED = sizeof(T) == 2;
+            DirectLoad<T, KU, KT, kPromptWaves, KeyTile<KU>> load_k(A, pl, A.k, A.kp, A.dk);
+            DirectLoad<T, VU, KT, kPromptWaves, ValueTile<VU>> load_v(A, pl, A.v, A.vp, A.dv);
+            auto look = [&](const auto& load, int j) {  // the pages of tile j
+                const int lane = tid & 63, key = pl.first + j * KT + load.first_row(lane);
+                return A.table && lane < load.N && key < pl.keys ? A.table[pl.slot * A.max_pages + (key >> A.shift)] : 0;
             };
-            load_k.next(A, pl, 0);
-            load_v.next(A, pl, 0);
-            int b = 0;
-            if (end > 0) load(0, 0);
-            for (int key0 = 0; key0 < end; key0 += KT, b ^= 1) {
+            if constexpr (PIPED) {
+                // Scores run a block ahead, products with v a block behind.  After the first block of tile j the values of tile
+                // j - 1 have been used (and the keys of j - 1 long since), and after the last the keys of j + 1 are
+                // needed: between the two, k of j + 1 and v of j have to be there, and the loads of k of j + 2 and of v of
+                // j + 1 start, with the time of a whole tile to arrive.
+                const int tiles = (end - pl.first + KT - 1) / KT;
+                constexpr int NB = KT / 32;
+                f32x16 s[2];
+                u32x4 w[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
+                auto clean = [&](int j) {
+                    if (mode) {
+                        clean_tile<T>(sV + (j & 1) * KT * VU, KT * VU, tid, 64 * kPromptWaves, mode);
+                        __syncthreads();
+                    }
+                };
+                u32x4 first_k[R::AHEAD], first_v[R::AHEAD];
+                auto keys_at = [&](int j, int b) { return rows.key_places(at_k + (j & 1) * (KEYS * 16) + b * (KEYS / NB * 16)); };
+                auto values_at = [&](int j, int b) { return rows.places(at_v + (j & 1) * (KT * VU * 16) + b * (32 * VU * 16)); };
+                auto read_values = [&](const typename R::ValuePlaces& p) {
+#pragma unroll
+                    for (int x = 0; x < R::AHEAD; ++x) first_v[x] = R::values_of(p, x);
+                };
+                auto seen_of = [&](int key0) { return (uint32_t)(mask.bits(key0) >> (4 * h)); };
+                auto load_keys = [&](int j, int page) {
+                    if (j < tiles) load_k.tile(A, pl, pl.first + j * KT, clamp_page(A, page), at_k + (j & 1) * (KEYS * 16));
+                };
+                auto load_values = [&](int j, int page) {
+                    if (j < tiles) load_v.tile(A, pl, pl.first + j * KT, clamp_page(A, page), at_v + (j & 1) * (KT * VU * 16));
+                };
+                if (tiles > 0) {
+                    int page_k = 0, page_v = 0;
+                    if (A.table) {
+                        const int page_0 = look(load_k, 0), page_1 = look(load_k, 1), page = look(load_v, 0);
+                        page_k = look(load_k, 2), page_v = look(load_v, 1);
+                        load_keys(0, page_0);
+                        load_values(0, page);
+                        load_keys(1, page_1);
+                    } else {
+                        load_keys(0, 0);
+                        load_values(0, 0);
+                        load_keys(1, 0);
+                    }
+                    loads_done();
+                    __syncthreads();
+                    clean(0);
+                    rows.first_scores(at_k, s[0]);
+                    typename R::ValuePlaces vp = values_at(0, 0);  // (at first some values with weights of zero)
+                    read_values(vp);
+#pragma unroll 1
+                    for (int j = 0; j < tiles; ++j) {
+                        const int key0 = pl.first + j * KT;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) {
+                            const bool masked = key0 + 32 * b + 32 > wave_full;
+                            const uint32_t seen = masked || mode == COUNT ? seen_of(key0 + 32 * b) : 0;
+                            // (at last some scores that are not used)
+                            const auto kp = b + 1 < NB ? keys_at(j, b + 1) : keys_at(j + 1, 0);
+                            rows.lead(vp, first_v, w, s[b & 1], masked, seen, A.scale2, kp, first_k);
+                            if (b == 0) {
+                                rows.template follow<false>(kp, first_k, s[0], A.scale2, s[1], w, vp, first_v);
+                            } else {
+                                vp = values_at(j, b);
+                                rows.template follow<true>(kp, first_k, s[b & 1], A.scale2, s[b + 1 & 1], w, vp, first_v);
+                            }
+                            if (mode == COUNT) rows.seen_weights(seen, w);
+                            if (b == 0) {
+                                loads_done();
+                                __syncthreads();
+                                if (j) clean(j);
+                                vp = values_at(j, 0);
+                                read_values(vp);
+                                load_keys(j + 2, page_k);
+                                load_values(j + 1, page_v);
+                                if (A.table) page_k = look(load_k, j + 3), page_v = look(load_v, j + 2);
+                            }
+                        }
+                    }
+                    rows.last_product(at_v + ((tiles - 1) & 1) * (KT * VU * 16) + (KT - 32) * VU * 16, w);
+                }
                 loads_done();
-                __syncthreads();  // this tile is there, and the one before has been used
-                if (key0 + KT < end) load(key0 + KT, b ^ 1);
-                step(sK + b * KT * KU, sV + b * KT * VU, key0);
+            } else {
+                auto load = [&](int j) {
+                    load_k.tile(A, pl, pl.first + j * KT, clamp_page(A, look(load_k, j)), at_k + (j & 1) * (KEYS * 16));
+                    load_v.tile(A, pl, pl.first + j * KT, clamp_page(A, look(load_v, j)), at_v + (j & 1) * (KT * VU * 16));
+                };
+                if (pl.first < end) load(0);
+                                for (int j = 0, key0 = pl.first; key0 < end; ++j, key0 += KT) {
+                    loads_done();
+                    __syncthreads();  // this tile is there, and the one before has been used
+                    if (key0 + KT < end) load(j + 1);
+                    step(j & 1, key0);
+                }
             }
             __syncthreads();
         } else {
-            for (int key0 = 0; key0 < end; key0 += KT) {
+                        for (int key0 = pl.first; key0 < end; key0 += KT) {
                 __syncthreads();
-                for (int x = tid; x < KT * KU; x += 256) {
+                for (int x = tid; x < KT * KU; x += 64 * kPromptWaves) {
                     const int r = x / KU, u = x % KU;
                     const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
-                    sK[k_unit<KU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
+                    sK[KeyTile<KU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
                 }
-                for (int x = tid; x < KT * VU; x += 256) {
+                for (int x = tid; x < KT * VU; x += 64 * kPromptWaves) {
                     const int r = x / VU, u = x % VU;
                     const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
-                    sV[v_unit<VU>(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
+                    sV[ValueTile<VU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
                 }
                 __syncthreads();
-                step(sK, sV, key0);
+                step(0, key0);
             }
         }
-    };
-    pass(std::false_type{});
-    __shared__ int s_again;
-    if (tid == 0) s_again = 0;
-    __syncthreads();
-    if (rows.spoilt()) s_again = 1;
-    __syncthreads();
-    if (s_again) pass(std::true_type{});
-
-    const float l = rows.l + other_half(rows.l);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (!live) return;
-    T* o = static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head;
-#pragma unroll
-    for (int mt = 0; mt < R::MT; ++mt)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int c = 32 * mt + 8 * b + 4 * h;
-            const f32x4 v{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]};
-            store4<T, VEC>(o + c, A.dv - c, v * inv);
+        if (mode == COUNT) rows.counted();
+        if (mode == CLEAN) {
+            rows.mark();
+            break;
         }
+        if (mode == PLAIN) {
+            __shared__ int s_again;
+            if (tid == 0) s_again = 0;
+            __syncthreads();
+            if (rows.spoilt()) s_again = 1;
+            __syncthreads();
+            if (!s_again) break;
+        }
+    }
+
+    const float l = sum_of_halves(rows.l);
+    if (pl.parts == 1) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        if (!live) return;
+        T* o = static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head;
+#pragma unroll
+        for (int mt = 0; mt < R::MT; ++mt)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int c = 32 * mt + 8 * b + 4 * h;
+                const f32x4 v{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]};
+                store4<T, VEC>(o + c, A.dv - c, v * inv);
+            }
+        return;
+    }
+    const PartRows<false> part(A, pl, pl.part);
+    if (live) {
+        part.put_sums(row, f32x2{rows.m, l});
+#pragma unroll
+        for (int mt = 0; mt < R::MT; ++mt)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int c = 32 * mt + 8 * b + 4 * h;
+                if (c < A.dv)
+                    part.put(row, c, f32x4{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]});
+            }
+    }
 }
 
 template <typename T, int DKP, int DVP, int KT, bool VEC>
-hipError_t launch_softmax_prompt(const SoftArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((softmax_prompt_kernel<T, DKP, DVP, KT, VEC>), dim3((unsigned)(a.ids * a.blocks)), dim3(256), 0, s, a);
+__global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_kernel(SoftArgs A) {
+    using R = SoftRows<T, DKP, DVP>;
+    __shared__ u32x4 lds[(VEC ? 2 : 1) * (KeyTile<R::KU>::units(KT) + KT * R::VU)];
+    SoftPlace pl;
+    SoftShares shares(A, share_of_block(A));
+    while (shares.next(A, &pl)) {
+        pl.uniform();
+        prompt_part<T, DKP, DVP, KT, VEC>(A, pl, lds);
+        __syncthreads();
+    }
+    // for the launch that joins: the unit that begins in this share and goes on behind it
+    if (A.shares && threadIdx.x == 0) {
+        if (shares.none || pl.part != 0) pl.parts = 1;
+        static_cast<SoftPlace*>(A.marks)[share_of_block(A)] = pl;
+    }
+}
+
+// Many rows are joined by a launch of their own: blockIdx.x is a share, in which one unit at most begins and goes on behind it;
+// each blockIdx.y takes kJoinRows of its rows.
+constexpr int kJoinRows = 8;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void softmax_join_kernel(SoftArgs A) {
+    SoftPlace pl = static_cast<const SoftPlace*>(A.marks)[blockIdx.x];
+    pl.uniform();
+    if (pl.parts == 1) return;
+    const int rows = min(A.tile, pl.len - pl.t0) * A.pack, first = blockIdx.y * kJoinRows;
+    if (first < rows) join_rows<T, VEC, false>(A, pl, first, min(kJoinRows, rows - first), 256);
+}
+
+// Few rows: each wave takes every WAVES-th 32 keys of the unit's, for the same rows, through LDS of its own, so that
+// waves do not wait for each other until the end.
+template <int BYTES>  // of 32 keys and values
+constexpr int step_waves() { return BYTES <= 16384 ? 4 : BYTES <= 32768 ? 2 : 1; }
+
+template <typename T, int DKP, int DVP>
+struct StepTiles {
+    static constexpr int KT = 32, E = 16 / sizeof(T), KEYS = KeyTile<DKP / E>::units(KT), TILE = KEYS + KT * DVP / E;
+    static constexpr int WAVES = step_waves<KT * (DKP + DVP) * sizeof(T)>();
+    static constexpr int LDS = WAVES * 2 * TILE;
+};
+
+template <typename T, int DKP, int DVP, bool VEC>
+__device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl, u32x4* lds, f32x2 (*s_sums)[32],
+                                          int (*s_pages)[2][64]) {
+    using R = SoftRows<T, DKP, DVP>;
+    using S = StepTiles<T, DKP, DVP>;
+    constexpr int KU = R::KU, VU = R::VU, KT = S::KT, KEYS = S::KEYS, TILE = S::TILE, WAVES = S::WAVES;
+    constexpr int PITCH = DVP + 4;  // of a row of results in LDS, in floats
+    static_assert(WAVES * 32 * PITCH * 4 <= WAVES * 2 * TILE * 16, "results fit in the tiles' place");
+    const int tid = threadIdx.x, n = tid & 31, h = tid >> 5 & 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t = pl.t0 + n / A.pack, head = pl.head + n % A.pack;
+    const bool live = n < A.tile * A.pack && t < pl.len;
+    const RowMask mask = row_mask(A, pl, live ? t : -1);
+    const bool causal = A.mask == SEQMIX_MASK_CAUSAL, tree = A.mask == SEQMIX_MASK_TREE;
+    const int back = pl.keys - pl.len;
+    auto behind = [&](int tt) { return causal ? min(max(back + min(tt, pl.len - 1) + 1, 0), pl.keys) : pl.keys; };
+    const int end = min(behind(pl.t0 + A.tile - 1), pl.last);
+    const int full = tree ? max(back, 0) : behind(pl.t0);
+
+    u32x4* const mine = lds + wave * 2 * TILE;
+    const uint32_t to = (uint32_t)(uintptr_t)(lds_address)lds + wave * (2 * TILE * 16);
+    const int first = pl.first + wave * KT;
+    constexpr int STRIDE = WAVES * KT, EARLY = 2 * STRIDE;
+    // The pages of a tile's rows go through LDS too: a load to a register would be waited for together with all before it.
+    const __amdgpu_buffer_rsrc_t table =
+        make_rsrc(A.table ? A.table + pl.slot * A.max_pages : nullptr, A.table ? (uint32_t)A.max_pages * 4 : 0u);
+    const int lane = tid & 63;
+    const uint32_t to_pages = (uint32_t)(uintptr_t)(lds_address)&s_pages[wave][0][0];
+    auto look = [&](int key0, int b) {
+        if (A.table) load_words_to_lds(table, (uint32_t)((key0 + lane) >> A.shift) * 4u, to_pages + b * 256);
+    };
+    if constexpr (VEC) {
+        look(first, 0);
+        look(first + STRIDE, 1);
+    }
+    R rows;
+#pragma unroll
+    for (int i = 0; i < R::MT / 2; ++i) rows.odd[i] = 0;
+    rows.place();
+    const T* q = static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head;
+#pragma unroll
+    for (int c = 0; c < KU / 2; ++c) {
+        rows.q[c] = u32x4{0, 0, 0, 0};
+        if (live) rows.q[c] = load_unit<T, VEC>(q, 2 * c + h, A.dk);
+    }
+    if (A.qsign != 1) rows.turn_q(A.qsign);
+#pragma unroll 1
+    for (int mode = PLAIN;; ++mode) {
+        auto step = [&](int b, int key0) {
+            if (mode) {
+                clean_tile<T>(mine + b * TILE + KEYS, KT * VU, tid & 63, 64, mode);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+            rows.template step<KT>(to + b * (TILE * 16), to + b * (TILE * 16) + KEYS * 16, key0, key0 + KT > full, mode == COUNT,
+                                   mask, A.scale2);
+        };
+        rows.clear();
+        if constexpr (VEC) {
+            DirectLoad<T, KU, KT, 1, KeyTile<KU>> load_k(A, pl, A.k, A.kp, A.dk);
+            DirectLoad<T, VU, KT, 1, ValueTile<VU>> load_v(A, pl, A.v, A.vp, A.dv);
+            constexpr int LOADS = decltype(load_k)::N + decltype(load_v)::N;
+            auto load = [&](int key0, int b) {
+                const int k = load_k.first_row(lane), v = load_v.first_row(lane);
+                int page_k = 0, page_v = 0;
+                if (A.table) {
+                    page_k = clamp_page(A, s_pages[wave][b][k & 63]);
+                    page_v = KU == VU ? page_k : clamp_page(A, s_pages[wave][b][v & 63]);
+                }
+                load_k.tile(A, pl, key0, page_k, to + b * (TILE * 16));
+                load_v.tile(A, pl, key0, page_v, to + b * (TILE * 16) + KEYS * 16);
+            };
+            // two tiles are under way (the first two times round there is only a load); the pages of the one after them are
+            // looked up before the second
+            if (mode) {
+                look(first, 0);
+                look(first + STRIDE, 1);
+            }
+            loads_done();
+            int b = 0;
+            for (int key0 = first - EARLY; key0 < end; key0 += STRIDE, b ^= 1) {
+                if (key0 >= first) {
+                    if (key0 + STRIDE < end) loads_done<LOADS>();
+                    else loads_done();
+                    step(b, key0);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile, and the pages of the next one, have been read
+                if (key0 + EARLY < end) {
+                    if (key0 > first - EARLY) look(key0 + EARLY + STRIDE, b ^ 1);
+                    load(key0 + EARLY, b);
+                }
+            }
+            loads_done();
+        } else {
+            for (int key0 = first; key0 < end; key0 += WAVES * KT) {
+                for (int x = tid & 63; x < KT * KU; x += 64) {
+                    const int r = x / KU, u = x % KU;
+                    const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
+                    mine[KeyTile<KU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
+                }
+                for (int x = tid & 63; x < KT * VU; x += 64) {
+                    const int r = x / VU, u = x % VU;
+                    const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
+                    mine[KEYS + ValueTile<VU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                step(0, key0);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+        }
+        if (mode == COUNT) rows.counted();
+        if (mode == CLEAN) {
+            rows.mark();
+            break;
+        }
+        if (mode == PLAIN && !rows.spoilt()) break;
+    }
+
+    // the waves' results, in their order
+    __syncthreads();
+    float* const sO = reinterpret_cast<float*>(lds);
+    const float l = sum_of_halves(rows.l);
+    if (h == 0) s_sums[wave][n] = f32x2{rows.m, l};
+#pragma unroll
+    for (int mt = 0; mt < R::MT; ++mt)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            *reinterpret_cast<f32x4*>(&sO[(wave * 32 + n) * PITCH + 32 * mt + 8 * b + 4 * h]) =
+                f32x4{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]};
+    __syncthreads();
+    const PartRows<true> part(A, pl, pl.part);
+    const int groups = (A.dv + 3) / 4, count = min(A.tile, pl.len - pl.t0) * A.pack;
+#pragma unroll 1
+    for (int x = tid; x < count * groups; x += 64 * WAVES) {
+        const int row = x / groups, c = 4 * (x - row * groups);
+        float m = -FLT_MAX, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_sums[w][row][0]);
+        f32x4 o{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const f32x2 s = s_sums[w][row];
+            const float f = __builtin_amdgcn_exp2f(s[0] - m);
+            sum += s[1] * f;
+            o += *reinterpret_cast<const f32x4*>(&sO[(w * 32 + row) * PITCH + c]) * f;
+        }
+        if (pl.parts > 1) {
+            part.put(row, c, o);
+            if (c == 0) part.put_sums(row, f32x2{m, sum});
+        } else {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const int tt = pl.t0 + row / A.pack, hh = pl.head + row % A.pack;
+            store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + tt) * A.o_row + (int64_t)hh * A.o_head + c, A.dv - c, o * inv);
+        }
+    }
+    if (pl.parts > 1) join_last<T, VEC>(A, pl, 64 * WAVES);
+}
+
+template <typename T, int DKP, int DVP, bool VEC>
+__global__ __launch_bounds__(64 * step_waves<32 * (DKP + DVP) * sizeof(T)>())
+__attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step_kernel(SoftArgs A) {
+    __shared__ u32x4 lds[StepTiles<T, DKP, DVP>::LDS];
+    __shared__ f32x2 sums[StepTiles<T, DKP, DVP>::WAVES][32];
+    __shared__ int pages[StepTiles<T, DKP, DVP>::WAVES][2][64];
+    SoftPlace pl;
+    SoftShares shares(A, share_of_block(A));
+    while (shares.next(A, &pl)) {
+        pl.uniform();
+        step_part<T, DKP, DVP, VEC>(A, pl, lds, sums, pages);
+        __syncthreads();
+    }
+}
+
+template <typename T, bool STEP, int DKP, int DVP, bool VEC>
+hipError_t launch_softmax_one(const SoftArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.shares ? a.shares : a.ids * a.blocks));
+    if constexpr (STEP) {
+        hipLaunchKernelGGL((softmax_step_kernel<T, DKP, DVP, VEC>), grid,
+                           dim3(64 * step_waves<32 * (DKP + DVP) * sizeof(T)>()), 0, s, a);
+    } else {
+        constexpr int KT = sizeof(T) == 4 && DKP + DVP > 128 ? 32 : 64;
+        hipLaunchKernelGGL((softmax_prompt_kernel<T, DKP, DVP, KT, VEC>), grid, dim3(64 * kPromptWaves), 0, s, a);
+        if (a.shares)
+            hipLaunchKernelGGL((softmax_join_kernel<T, VEC>),
+                               dim3((unsigned)a.shares, (unsigned)((a.tile * a.pack + kJoinRows - 1) / kJoinRows)), dim3(256), 0, s, a);
+    }
     return hipGetLastError();
 }
 
 // Kernels for heads of up to 64, 128 and 256 elements; of dims that fill no 16 bytes, by the larger of the two.
-template <typename T, int WIDE>
+template <typename T, bool STEP>
 hipError_t launch_softmax(const SoftArgs& a, bool vec, hipStream_t s) {
     const int k = a.dk <= 64 ? 64 : a.dk <= 128 ? 128 : 256, v = a.dv <= 64 ? 64 : a.dv <= 128 ? 128 : 256;
     if (!vec) {
         const int d = k > v ? k : v;
-        if (d == 64) return launch_softmax_prompt<T, 64, 64, 64, false>(a, s);
-        if (d == 128) return launch_softmax_prompt<T, 128, 128, 64, false>(a, s);
-        return launch_softmax_prompt<T, 256, 256, WIDE, false>(a, s);
+        if (d == 64) return launch_softmax_one<T, STEP, 64, 64, false>(a, s);
+        if (d == 128) return launch_softmax_one<T, STEP, 128, 128, false>(a, s);
+        return launch_softmax_one<T, STEP, 256, 256, false>(a, s);
     }
     switch (1000 * k + v) {
-        case 64064: return launch_softmax_prompt<T, 64, 64, 64, true>(a, s);
-        case 64128: return launch_softmax_prompt<T, 64, 128, 64, true>(a, s);
-        case 64256: return launch_softmax_prompt<T, 64, 256, WIDE, true>(a, s);
-        case 128064: return launch_softmax_prompt<T, 128, 64, 64, true>(a, s);
-        case 128128: return launch_softmax_prompt<T, 128, 128, 64, true>(a, s);
-        case 128256: return launch_softmax_prompt<T, 128, 256, WIDE, true>(a, s);
-        case 256064: return launch_softmax_prompt<T, 256, 64, WIDE, true>(a, s);
-        case 256128: return launch_softmax_prompt<T, 256, 128, WIDE, true>(a, s);
-        default: return launch_softmax_prompt<T, 256, 256, WIDE, true>(a, s);
+        case 64064: return launch_softmax_one<T, STEP, 64, 64, true>(a, s);
+        case 64128: return launch_softmax_one<T, STEP, 64, 128, true>(a, s);
+        case 64256: return launch_softmax_one<T, STEP, 64, 256, true>(a, s);
+        case 128064: return launch_softmax_one<T, STEP, 128, 64, true>(a, s);
+        case 128128: return launch_softmax_one<T, STEP, 128, 128, true>(a, s);
+        case 128256: return launch_softmax_one<T, STEP, 128, 256, true>(a, s);
+        case 256064: return launch_softmax_one<T, STEP, 256, 64, true>(a, s);
+        case 256128: return launch_softmax_one<T, STEP, 256, 128, true>(a, s);
+        default: return launch_softmax_one<T, STEP, 256, 256, true>(a, s);
     }
 }
 

@@ -69,7 +69,7 @@ class seqmix_softmax_params(ctypes.Structure):
 
 
 class seqmix_softmax_plan_info(ctypes.Structure):
-    _fields_ = [("kernel", ctypes.c_int32), ("pack", ctypes.c_int32), ("parts", ctypes.c_int64),
+    _fields_ = [("kernel", ctypes.c_int32), ("pack", ctypes.c_int32), ("shares", ctypes.c_int64),
                 ("workspace_bytes", ctypes.c_int64)]
 
 

@@ -119,6 +119,10 @@ class Soft:
                     table=self.table, tree=self.tree, **kw)
         return self
 
+    def parts(self):
+        """bf16 parts of a weight."""
+        return 2 if self.op.plan().kernel == M.SEQMIX_KERNEL_STEP else 1
+
     def held(self, i):
         """Keys and values of sequence i."""
         if self.page:
@@ -140,7 +144,7 @@ class Soft:
             k, v = self.held(i)
             on = ref.sees(self.mask, n, self.keys[i], None if self.tree_host is None else self.tree_host[rows])
             o, o_abs, most = ref.softmax_attention(q[rows], k, v, on, self.scale)
-            bound = ref.softmax_bound(o, o_abs, most, self.keys[i], self.dk, self.dtype)
+            bound = ref.softmax_bound(o, o_abs, most, self.keys[i], self.dk, self.dtype, self.parts())
             _near(got[rows], o, bound, f"sequence {i}")
             assert (got[rows][~on.any(1)] == 0).all(), "rows that see nothing"
         return self
@@ -242,7 +246,7 @@ def test_what_is_not_seen_does_not_matter(dtype, mask, page):
         fine = np.isfinite(o)
         assert np.array_equal(np.isfinite(rows), fine)
         assert np.isnan(rows[~fine]).all()
-        bound = ref.softmax_bound(o, o_abs, most, p.keys[i], p.dk, dtype)
+        bound = ref.softmax_bound(o, o_abs, most, p.keys[i], p.dk, dtype, p.parts())
         assert (np.abs(rows - o)[fine] <= bound[fine]).all()
 
 
