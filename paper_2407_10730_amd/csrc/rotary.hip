@@ -36,14 +36,14 @@ __device__ __forceinline__ void copy_unit(const T* from, T* to, T* too, int n, i
 }
 
 template <typename T, int N>
-__device__ __forceinline__ void store_both(T* to, T* too, int c, const float (&v)[N]) {
-    if (to) store_pack<T, N>(to + c, v);
-    if (too) store_pack<T, N>(too + c, v);
+__device__ __forceinline__ void store_both(T* to, T* too, int c, const float (&v)[N], bool past) {
+    if (to) store_result<T, N>(to + c, v, past);
+    if (too) store_result<T, N>(too + c, v, past);
 }
 
 // Unit u of a head: from -> to and too (NULL: not), f the factors of the token's pairs.
 template <typename T, int V, bool HALF>
-__device__ __forceinline__ void turn_unit(const T* from, T* to, T* too, const f32x2* f, int dk, int rot, int u) {
+__device__ __forceinline__ void turn_unit(const T* from, T* to, T* too, const f32x2* f, int dk, int rot, int u, bool past) {
     using U = HeadUnits<V, HALF>;
     const int np = U::pairs(rot), nt = U::turned(rot);
     if (u >= nt) {
@@ -61,8 +61,8 @@ __device__ __forceinline__ void turn_unit(const T* from, T* to, T* too, const f3
                 x[i] = a[i] * w[0] - b[i] * w[1];
                 y[i] = b[i] * w[0] + a[i] * w[1];
             }
-            store_both<T, N>(to, too, c, x);
-            store_both<T, N>(to, too, half + c, y);
+            store_both<T, N>(to, too, c, x, past);
+            store_both<T, N>(to, too, half + c, y, past);
         };
         if (u < np) turn(std::integral_constant<int, V>{}, u * V);
         else turn(std::integral_constant<int, 1>{}, np * V + (u - np));
@@ -77,7 +77,7 @@ __device__ __forceinline__ void turn_unit(const T* from, T* to, T* too, const f3
                 x[i] = a[i] * w[0] - a[i + 1] * w[1];
                 x[i + 1] = a[i + 1] * w[0] + a[i] * w[1];
             }
-            store_both<T, N>(to, too, c, x);
+            store_both<T, N>(to, too, c, x, past);
         };
         if (u < np) turn(std::integral_constant<int, V>{}, u * V);
         else turn(std::integral_constant<int, 2>{}, np * V + 2 * (u - np));
@@ -121,14 +121,14 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs A, in
             const f32x2* f = s_factor + t * half;
             if (of_q) {
                 turn_unit<T, V, HALF>(static_cast<const T*>(A.q) + row * A.q_row + h * A.q_head,
-                                      static_cast<T*>(A.qo) + row * A.qo_row + h * A.qo_head, nullptr, f, A.dk, A.rot, u);
+                                      static_cast<T*>(A.qo) + row * A.qo_row + h * A.qo_head, nullptr, f, A.dk, A.rot, u, A.past);
             } else {
                 h -= heads;
                 T* const to = A.ko ? static_cast<T*>(A.ko) + row * A.ko_row + h * A.ko_head : nullptr;
                 T* const too = A.kc && page >= 0
                                    ? static_cast<T*>(A.kc) + page * A.kp.page + at * A.kp.row + h * A.kp.head : nullptr;
                 if (to || too)
-                    turn_unit<T, V, HALF>(static_cast<const T*>(A.k) + row * A.k_row + h * A.k_head, to, too, f, A.dk, A.rot, u);
+                    turn_unit<T, V, HALF>(static_cast<const T*>(A.k) + row * A.k_row + h * A.k_head, to, too, f, A.dk, A.rot, u, A.past);
             }
         } else if (page >= 0) {
             u -= turned;

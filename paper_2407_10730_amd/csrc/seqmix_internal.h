@@ -144,6 +144,7 @@ struct RotaryArgs {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
     CachePlace kp, vp;
     int32_t shift, heads, kv_heads, dk, dv, rot;
+    int32_t past;  // turned q and k are written past the caches
     float amplitude;
 };
 hipError_t launch_rotary(const RotaryArgs& a, int dt, int layout, hipStream_t s);
@@ -153,6 +154,7 @@ struct PagesArgs {
     const int32_t* kept;
     int32_t *lens, *table, *free_pages, *taken, *place, *position, *admitted;
     int32_t pages, max_pages, shift;
+    FastDiv by_len;  // rows of a sequence, where all have as many
 };
 hipError_t launch_pages(const PagesArgs& a, hipStream_t s);
 

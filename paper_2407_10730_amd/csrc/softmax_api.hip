@@ -261,6 +261,7 @@ int seqmix_rotary_fwd(const seqmix_rotary_desc* d, const void* q, const void* k,
     a.shift = p.page ? log2_of(p.page) : 0;
     a.heads = p.heads, a.kv_heads = p.kv_heads, a.dk = p.dk, a.dv = p.dv, a.rot = p.rot;
     a.amplitude = p.amplitude;
+    a.past = p.tokens * (p.heads + (of_k ? p.kv_heads : 0)) * p.dk * esize(p.dtype) >= kPastBytes;
     return launch_rotary(a, p.dtype, p.layout, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
 
@@ -294,6 +295,7 @@ int seqmix_pages_fwd(const seqmix_pages_desc* d, const int32_t* kept, const int6
     a.lens = lens, a.table = table, a.free_pages = free_pages, a.taken = taken;
     a.place = place, a.position = position, a.admitted = admitted;
     a.pages = (int32_t)p.pages, a.max_pages = (int32_t)p.max_pages, a.shift = log2_of(p.page);
+    a.by_len = make_fastdiv((uint32_t)std::max<int64_t>(a.sq.seq_len, 1));
     return launch_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? CONV2D_OK : CONV2D_E_HIP;
 }
 
