@@ -120,6 +120,7 @@ struct SoftArgs {
     int32_t qsign;         // -1, 0, 1
     float scale2;          // |scale| log2(e), where the scale is not 0
     int32_t tile;          // tokens of a tile
+    FastDiv by_pack, by_groups;  // heads of a tile, groups of 4 columns of o
     int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
     int32_t shares;        // 0: a workgroup takes a tile; else that many take the same number of quanta of all tiles' keys
     int32_t quantum;       // log2 of its keys

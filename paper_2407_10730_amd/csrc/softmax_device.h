@@ -555,13 +555,15 @@ struct SoftRows {
         mx = max_of_halves(mx) * scale2;
         // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
         if (__any(mx > m + kSlack)) rescale(mx);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -m));
-                l += s[b][i];
+                sum[i & 3] += s[b][i];
             }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         if (counting) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -682,12 +684,12 @@ struct SoftRows {
 
     // Whether a value that is not finite came up (in any lane): what rows that do not see it hold has to be computed again.
     __device__ __forceinline__ bool spoilt() const {
-        float bad = l * 0.0f;
+        float bad[4] = {l * 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) bad += o[mt][i] * 0.0f;
-        return __any(!(bad == 0.0f));
+            for (int i = 0; i < 16; ++i) bad[i & 3] = __builtin_fmaf(o[mt][i], 0.0f, bad[i & 3]);
+        return __any(!((bad[0] + bad[1]) + (bad[2] + bad[3]) == 0.0f));
     }
 };
 
@@ -740,7 +742,7 @@ __device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl
     const int groups = (A.dv + 3) / 4;
 #pragma unroll 1
     for (int x = threadIdx.x; x < rows * groups; x += threads) {
-        const int at = x / groups, row = first + at, c = 4 * (x - at * groups);
+        const int at = (int)fdiv(x, A.by_groups), row = first + at, c = 4 * (x - at * groups);
         f32x4 o{0, 0, 0, 0};
         float m = -FLT_MAX, l = 0.0f;
         constexpr int AHEAD = SAME ? 4 : 8;
@@ -765,7 +767,7 @@ __device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl
                 }
         }
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int t = pl.t0 + row / A.pack, head = pl.head + row % A.pack;
+        const int t = pl.t0 + (int)fdiv(row, A.by_pack), head = pl.head + row - (int)fdiv(row, A.by_pack) * A.pack;
         store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head + c, A.dv - c, o * inv);
     }
 }
@@ -904,15 +906,15 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
     const int tid = threadIdx.x, wave = tid >> 6, n = tid & 31, h = tid >> 5 & 1;
     // this lane's row, and the rows of its wave and of the workgroup
     const int row = 32 * wave + n;
-    const int t = pl.t0 + row / A.pack, head = pl.head + row % A.pack;
+    const int t = pl.t0 + (int)fdiv(row, A.by_pack), head = pl.head + row - (int)fdiv(row, A.by_pack) * A.pack;
     const bool live = row < A.tile * A.pack && t < pl.len;
     const RowMask mask = row_mask(A, pl, live ? t : -1);
     const bool causal = A.mask == SEQMIX_MASK_CAUSAL, tree = A.mask == SEQMIX_MASK_TREE;
     const int back = pl.keys - pl.len;
     auto behind = [&](int tt) { return causal ? min(max(back + min(tt, pl.len - 1) + 1, 0), pl.keys) : pl.keys; };
     const int end = min(behind(pl.t0 + A.tile - 1), pl.last);
-    const int w0 = pl.t0 + 32 * wave / A.pack;
-    const int wave_end = w0 < pl.len ? behind(pl.t0 + (32 * wave + 31) / A.pack) : 0;
+    const int w0 = pl.t0 + (int)fdiv(32 * wave, A.by_pack);
+    const int wave_end = w0 < pl.len ? behind(pl.t0 + (int)fdiv(32 * wave + 31, A.by_pack)) : 0;
     const int wave_full = tree ? max(back, 0) : behind(w0);
 
     R rows;
@@ -1134,28 +1136,29 @@ __global__ __launch_bounds__(256) void softmax_join_kernel(SoftArgs A) {
 }
 
 // Few rows: each wave takes every WAVES-th 32 keys of the unit's, for the same rows, through LDS of its own, so that
-// waves do not wait for each other until the end.
+// waves do not wait for each other until the end.  Two waves on a SIMD with a tile each: while one works the other's
+// comes (WAVES_US).
 template <int BYTES>  // of 32 keys and values
-constexpr int step_waves() { return BYTES <= 16384 ? 4 : BYTES <= 32768 ? 2 : 1; }
+constexpr int step_waves() { return BYTES <= 16384 ? 8 : BYTES <= 32768 ? 4 : 2; }
 
 template <typename T, int DKP, int DVP>
 struct StepTiles {
     static constexpr int KT = 32, E = 16 / sizeof(T), KEYS = KeyTile<DKP / E>::units(KT), TILE = KEYS + KT * DVP / E;
     static constexpr int WAVES = step_waves<KT * (DKP + DVP) * sizeof(T)>();
-    static constexpr int LDS = WAVES * 2 * TILE;
+    static constexpr int PITCH = DVP + 4;  // of a row of results in LDS, in floats
+    static constexpr int LDS = WAVES * (TILE > 8 * PITCH ? TILE : 8 * PITCH);
 };
 
 template <typename T, int DKP, int DVP, bool VEC>
 __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl, u32x4* lds, f32x2 (*s_sums)[32],
-                                          int (*s_pages)[2][64]) {
+                                          int (*s_pages)[64]) {
     using R = SoftRows<T, DKP, DVP>;
     using S = StepTiles<T, DKP, DVP>;
     constexpr int KU = R::KU, VU = R::VU, KT = S::KT, KEYS = S::KEYS, TILE = S::TILE, WAVES = S::WAVES;
-    constexpr int PITCH = DVP + 4;  // of a row of results in LDS, in floats
-    static_assert(WAVES * 32 * PITCH * 4 <= WAVES * 2 * TILE * 16, "results fit in the tiles' place");
+    constexpr int PITCH = S::PITCH;
     const int tid = threadIdx.x, n = tid & 31, h = tid >> 5 & 1;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int t = pl.t0 + n / A.pack, head = pl.head + n % A.pack;
+    const int t = pl.t0 + (int)fdiv(n, A.by_pack), head = pl.head + n - (int)fdiv(n, A.by_pack) * A.pack;
     const bool live = n < A.tile * A.pack && t < pl.len;
     const RowMask mask = row_mask(A, pl, live ? t : -1);
     const bool causal = A.mask == SEQMIX_MASK_CAUSAL, tree = A.mask == SEQMIX_MASK_TREE;
@@ -1164,22 +1167,19 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
     const int end = min(behind(pl.t0 + A.tile - 1), pl.last);
     const int full = tree ? max(back, 0) : behind(pl.t0);
 
-    u32x4* const mine = lds + wave * 2 * TILE;
-    const uint32_t to = (uint32_t)(uintptr_t)(lds_address)lds + wave * (2 * TILE * 16);
+    u32x4* const mine = lds + wave * TILE;
+    const uint32_t to = (uint32_t)(uintptr_t)(lds_address)lds + wave * (TILE * 16);
     const int first = pl.first + wave * KT;
-    constexpr int STRIDE = WAVES * KT, EARLY = 2 * STRIDE;
+    constexpr int STRIDE = WAVES * KT;
     // The pages of a tile's rows go through LDS too: a load to a register would be waited for together with all before it.
     const __amdgpu_buffer_rsrc_t table =
         make_rsrc(A.table ? A.table + pl.slot * A.max_pages : nullptr, A.table ? (uint32_t)A.max_pages * 4 : 0u);
     const int lane = tid & 63;
-    const uint32_t to_pages = (uint32_t)(uintptr_t)(lds_address)&s_pages[wave][0][0];
-    auto look = [&](int key0, int b) {
-        if (A.table) load_words_to_lds(table, (uint32_t)((key0 + lane) >> A.shift) * 4u, to_pages + b * 256);
+    const uint32_t to_pages = (uint32_t)(uintptr_t)(lds_address)&s_pages[wave][0];
+    auto look = [&](int key0) {
+        if (A.table) load_words_to_lds(table, (uint32_t)((key0 + lane) >> A.shift) * 4u, to_pages);
     };
-    if constexpr (VEC) {
-        look(first, 0);
-        look(first + STRIDE, 1);
-    }
+    if constexpr (VEC) look(first);
     R rows;
 #pragma unroll
     for (int i = 0; i < R::MT / 2; ++i) rows.odd[i] = 0;
@@ -1193,48 +1193,38 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
     if (A.qsign != 1) rows.turn_q(A.qsign);
 #pragma unroll 1
     for (int mode = PLAIN;; ++mode) {
-        auto step = [&](int b, int key0) {
+        auto step = [&](int key0) {
             if (mode) {
-                clean_tile<T>(mine + b * TILE + KEYS, KT * VU, tid & 63, 64, mode);
+                clean_tile<T>(mine + KEYS, KT * VU, tid & 63, 64, mode);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            rows.template step<KT>(to + b * (TILE * 16), to + b * (TILE * 16) + KEYS * 16, key0, key0 + KT > full, mode == COUNT,
-                                   mask, A.scale2);
+            rows.template step<KT>(to, to + KEYS * 16, key0, key0 + KT > full, mode == COUNT, mask, A.scale2);
         };
         rows.clear();
         if constexpr (VEC) {
             DirectLoad<T, KU, KT, 1, KeyTile<KU>> load_k(A, pl, A.k, A.kp, A.dk);
             DirectLoad<T, VU, KT, 1, ValueTile<VU>> load_v(A, pl, A.v, A.vp, A.dv);
-            constexpr int LOADS = decltype(load_k)::N + decltype(load_v)::N;
-            auto load = [&](int key0, int b) {
+            auto load = [&](int key0) {
                 const int k = load_k.first_row(lane), v = load_v.first_row(lane);
                 int page_k = 0, page_v = 0;
                 if (A.table) {
-                    page_k = clamp_page(A, s_pages[wave][b][k & 63]);
-                    page_v = KU == VU ? page_k : clamp_page(A, s_pages[wave][b][v & 63]);
+                    page_k = clamp_page(A, s_pages[wave][k & 63]);
+                    page_v = KU == VU ? page_k : clamp_page(A, s_pages[wave][v & 63]);
+                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(page_k), "+v"(page_v)::"memory");  // read before the next ones come
                 }
-                load_k.tile(A, pl, key0, page_k, to + b * (TILE * 16));
-                load_v.tile(A, pl, key0, page_v, to + b * (TILE * 16) + KEYS * 16);
+                load_k.tile(A, pl, key0, page_k, to);
+                load_v.tile(A, pl, key0, page_v, to + KEYS * 16);
+                look(key0 + STRIDE);
             };
-            // two tiles are under way (the first two times round there is only a load); the pages of the one after them are
-            // looked up before the second
-            if (mode) {
-                look(first, 0);
-                look(first + STRIDE, 1);
-            }
+            // a wave's tile comes while the other waves work; with it the pages of its next one
+            if (mode) look(first);
             loads_done();
-            int b = 0;
-            for (int key0 = first - EARLY; key0 < end; key0 += STRIDE, b ^= 1) {
-                if (key0 >= first) {
-                    if (key0 + STRIDE < end) loads_done<LOADS>();
-                    else loads_done();
-                    step(b, key0);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile, and the pages of the next one, have been read
-                if (key0 + EARLY < end) {
-                    if (key0 > first - EARLY) look(key0 + EARLY + STRIDE, b ^ 1);
-                    load(key0 + EARLY, b);
-                }
+            if (first < end) load(first);
+            for (int key0 = first; key0 < end; key0 += STRIDE) {
+                loads_done();
+                step(key0);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
+                if (key0 + STRIDE < end) load(key0 + STRIDE);
             }
             loads_done();
         } else {
@@ -1250,7 +1240,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
                     mine[KEYS + ValueTile<VU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                step(0, key0);
+                step(key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
         }
@@ -1278,7 +1268,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
     const int groups = (A.dv + 3) / 4, count = min(A.tile, pl.len - pl.t0) * A.pack;
 #pragma unroll 1
     for (int x = tid; x < count * groups; x += 64 * WAVES) {
-        const int row = x / groups, c = 4 * (x - row * groups);
+        const int row = (int)fdiv(x, A.by_groups), c = 4 * (x - row * groups);
         float m = -FLT_MAX, sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_sums[w][row][0]);
@@ -1295,7 +1285,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             if (c == 0) part.put_sums(row, f32x2{m, sum});
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const int tt = pl.t0 + row / A.pack, hh = pl.head + row % A.pack;
+            const int tt = pl.t0 + (int)fdiv(row, A.by_pack), hh = pl.head + row - (int)fdiv(row, A.by_pack) * A.pack;
             store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + tt) * A.o_row + (int64_t)hh * A.o_head + c, A.dv - c, o * inv);
         }
     }
@@ -1307,7 +1297,7 @@ __global__ __launch_bounds__(64 * step_waves<32 * (DKP + DVP) * sizeof(T)>())
 __attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step_kernel(SoftArgs A) {
     __shared__ u32x4 lds[StepTiles<T, DKP, DVP>::LDS];
     __shared__ f32x2 sums[StepTiles<T, DKP, DVP>::WAVES][32];
-    __shared__ int pages[StepTiles<T, DKP, DVP>::WAVES][2][64];
+    __shared__ int pages[StepTiles<T, DKP, DVP>::WAVES][64];
     SoftPlace pl;
     SoftShares shares(A, share_of_block(A));
     while (shares.next(A, &pl)) {
