@@ -254,14 +254,26 @@ __device__ __forceinline__ int64_t key_row(const SoftArgs& A, const SoftPlace& p
     return p * c.page + (key & ((1 << A.shift) - 1)) * c.row + pl.kv_head * c.head;
 }
 
-// 16 bytes of a row of `dim` elements from unit u (of 16 bytes) on, zeros past its end.
+// 16 bytes of a row of `dim` elements from unit u (of 16 bytes) on, zeros past its end.  Not VEC (dim is no multiple of 16 bytes):
+// at any address of the element's alignment; the last part is read where it ends with the row, and moved down; rows below
+// 16 bytes are read by elements.
 template <typename T, bool VEC>
 __device__ __forceinline__ u32x4 load_unit(const T* row, int u, int dim) {
     constexpr int E = 16 / sizeof(T);
     const int c = u * E;
     u32x4 v{0, 0, 0, 0};
-    if constexpr (VEC) {
-        if (c < dim) v = *reinterpret_cast<const u32x4_any*>(row + c);
+    if (VEC || dim >= E) {
+        const int over = VEC ? 0 : max(c + E - dim, 0);  // elements
+        if (c < dim) {
+            v = *reinterpret_cast<const u32x4_any*>(row + c - over);
+            if (!VEC && over) {
+                uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+                const int bits = over * 8 * (int)sizeof(T);
+                if (bits >= 64) lo = hi >> (bits - 64), hi = 0;
+                else lo = lo >> bits | hi << (64 - bits), hi >>= bits;
+                v = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+            }
+        }
     } else {
         T e[E];
 #pragma unroll
@@ -892,6 +904,40 @@ struct DirectLoad {
         }
     }
 };
+// ... rows that lie otherwise: through registers, N units of each thread at a time.
+template <typename T, int UNITS, int N, int THREADS, typename LDS>
+struct RegisterLoad {
+    u32x4 v[N];
+    __device__ __forceinline__ void fetch(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim, int key0,
+                                          int x0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = x0 + i * THREADS, r = x / UNITS, u = x % UNITS;
+            const int64_t from = key_row(A, pl, c, min(key0 + r, pl.keys - 1));
+            v[i] = load_unit<T, false>(static_cast<const T*>(p) + from, u, dim);
+        }
+    }
+    __device__ __forceinline__ void store(u32x4* to, int x0) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = x0 + i * THREADS;
+            to[LDS::at(x / UNITS, x % UNITS)] = v[i];
+        }
+    }
+};
+// A whole tile of ROWS rows so: as many units in flight as divide it, four at most.
+template <typename T, int UNITS, int ROWS, int THREADS, typename LDS>
+__device__ __forceinline__ void copy_rows(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim, int key0,
+                                          u32x4* to, int thread) {
+    constexpr int EACH = ROWS * UNITS / THREADS, N = EACH % 4 == 0 ? 4 : EACH % 3 == 0 ? 3 : EACH % 2 == 0 ? 2 : 1;
+    static_assert(EACH * THREADS == ROWS * UNITS);
+#pragma unroll 1
+    for (int x = thread; x < ROWS * UNITS; x += N * THREADS) {
+        RegisterLoad<T, UNITS, N, THREADS, LDS> l;
+        l.fetch(A, pl, p, c, dim, key0, x);
+        l.store(to, x);
+    }
+}
 // The page that holds the rows of lane i's instruction.
 __device__ __forceinline__ int clamp_page(const SoftArgs& A, int page) { return min(max(page, 0), (int)A.pages - 1); }
 
@@ -1045,20 +1091,34 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
             }
             __syncthreads();
         } else {
-                        for (int key0 = pl.first; key0 < end; key0 += KT) {
-                __syncthreads();
-                for (int x = tid; x < KT * KU; x += 64 * kPromptWaves) {
-                    const int r = x / KU, u = x % KU;
-                    const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
-                    sK[KeyTile<KU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
+            constexpr int THREADS = 64 * kPromptWaves;
+            if constexpr (sizeof(T) == 2 && DKP + DVP <= 256) {
+                // the next tile's while this one is used (2048 tokens, 16 heads of 127: 167 -> 152 us; wider rows and fp32 have no
+                // registers for it: 335 -> 416 us at 231 + 128)
+                RegisterLoad<T, KU, KT * KU / THREADS, THREADS, KeyTile<KU>> k;
+                static_assert(KT * KU % THREADS == 0 && KT * VU % THREADS == 0);
+                RegisterLoad<T, VU, KT * VU / THREADS, THREADS, ValueTile<VU>> v;
+                auto fetch = [&](int key0) {
+                    k.fetch(A, pl, A.k, A.kp, A.dk, key0, tid);
+                    v.fetch(A, pl, A.v, A.vp, A.dv, key0, tid);
+                };
+                if (pl.first < end) fetch(pl.first);
+                for (int key0 = pl.first; key0 < end; key0 += KT) {
+                    __syncthreads();
+                    k.store(sK, tid);
+                    v.store(sV, tid);
+                    __syncthreads();
+                    if (key0 + KT < end) fetch(key0 + KT);
+                    step(0, key0);
                 }
-                for (int x = tid; x < KT * VU; x += 64 * kPromptWaves) {
-                    const int r = x / VU, u = x % VU;
-                    const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
-                    sV[ValueTile<VU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
+            } else {
+                for (int key0 = pl.first; key0 < end; key0 += KT) {
+                    __syncthreads();
+                    copy_rows<T, KU, KT, THREADS, KeyTile<KU>>(A, pl, A.k, A.kp, A.dk, key0, sK, tid);
+                    copy_rows<T, VU, KT, THREADS, ValueTile<VU>>(A, pl, A.v, A.vp, A.dv, key0, sV, tid);
+                    __syncthreads();
+                    step(0, key0);
                 }
-                __syncthreads();
-                step(0, key0);
             }
         }
         if (mode == COUNT) rows.counted();
@@ -1228,17 +1288,9 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             }
             loads_done();
         } else {
-            for (int key0 = first; key0 < end; key0 += WAVES * KT) {
-                for (int x = tid & 63; x < KT * KU; x += 64) {
-                    const int r = x / KU, u = x % KU;
-                    const int64_t from = key_row(A, pl, A.kp, min(key0 + r, pl.keys - 1));
-                    mine[KeyTile<KU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.k) + from, u, A.dk);
-                }
-                for (int x = tid & 63; x < KT * VU; x += 64) {
-                    const int r = x / VU, u = x % VU;
-                    const int64_t from = key_row(A, pl, A.vp, min(key0 + r, pl.keys - 1));
-                    mine[KEYS + ValueTile<VU>::at(r, u)] = load_unit<T, VEC>(static_cast<const T*>(A.v) + from, u, A.dv);
-                }
+            for (int key0 = first; key0 < end; key0 += STRIDE) {
+                copy_rows<T, KU, KT, 64, KeyTile<KU>>(A, pl, A.k, A.kp, A.dk, key0, mine, lane);
+                copy_rows<T, VU, KT, 64, ValueTile<VU>>(A, pl, A.v, A.vp, A.dv, key0, mine + KEYS, lane);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 step(key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
