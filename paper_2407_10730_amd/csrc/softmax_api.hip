@@ -67,7 +67,9 @@ int64_t shares_of(bool step, int dtype) { return step || dtype == CONV2D_F32 ? k
 // Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: joining parts costs some.
 constexpr int32_t kLeast = 4, kWhole = 6;
 
-int64_t part_bytes(const seqmix_softmax_params& p, int64_t rows) { return rows * ((p.dv + 3) / 4 * 16 + 16); }
+int64_t part_bytes(const seqmix_softmax_params& p, bool step, int64_t rows) {
+    return step ? rows * ((p.dv + 3) / 4 * 16 + 16) : (rows + 31) / 32 * ((p.dv + 7) / 8 * 1024 + 256);
+}
 
 void plan_softmax(seqmix_softmax_desc* d) {
     const seqmix_softmax_params& p = d->p;
@@ -82,7 +84,7 @@ void plan_softmax(seqmix_softmax_desc* d) {
         // quanta of all rows are counted in 32 bits
         const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
         for (d->quantum = step ? 7 : 6; tiles * blocks * ((keys >> d->quantum) + 2) >= 1LL << 31;) ++d->quantum;
-        d->plan.workspace_bytes = d->plan.shares * (2 * part_bytes(p, rows / pack * pack) + kMarkBytes);
+        d->plan.workspace_bytes = d->plan.shares * (2 * part_bytes(p, step, rows / pack * pack) + kMarkBytes);
     }
 }
 
@@ -191,7 +193,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
         a.most = (int32_t)((1LL << 31) / a.blocks - 1);
         a.ws = d->ws.data;
         a.marks = static_cast<char*>(d->ws.data) +
-                                               2 * d->plan.shares * part_bytes(p, (int64_t)a.tile * a.pack);
+                                               2 * d->plan.shares * part_bytes(p, step, (int64_t)a.tile * a.pack);
     }
     auto launch = p.dtype == CONV2D_BF16 ? (step ? launch_softmax_step_bf16 : launch_softmax_prompt_bf16)
                                          : (step ? launch_softmax_step_f32 : launch_softmax_prompt_f32);

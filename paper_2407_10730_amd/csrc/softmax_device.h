@@ -13,6 +13,15 @@
 
 namespace cv {
 
+// The arguments of the running kernel, its only parameter, to be read where they are used: held from the start on they fill the
+// scalar registers and are kept in lanes of vector registers, which cost a thousand instructions (16 requests of 24
+// drafts over up to 5000 keys 58 -> 54 us).
+__device__ __forceinline__ const SoftArgs& args_here() {
+    auto p = (const __attribute__((address_space(4))) SoftArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const SoftArgs*)p;
+}
+
 // What a workgroup works on: a unit is rows [t0, t0 + tile) of a sequence for the heads from `head` on; a part of it is its keys
 // [first, last).
 struct SoftPlace {
@@ -113,15 +122,30 @@ struct SoftSeq {
 };
 __device__ __forceinline__ SoftSeq soft_seq(const SoftArgs& A, int i) {
     SoftSeq s{0, 0, 0, 0, -1, 0, 0, 0};
-    if (i >= A.sq.seqs) return s;
-    const SeqRange r = seq_range(A.sq, i);
-    s.slot = (int)seq_slot(A.sq, i);
-    if (s.slot < 0) return s;
-    int64_t key0;
-    s.row0 = (uint32_t)r.first;
-    s.len = (uint32_t)r.len;
-    s.keys = (uint32_t)seq_keys(A, i, s.slot, r, &key0);
-    s.key0 = (uint32_t)key0;
+    // what is at hand is asked for at once: one after the other finding a workgroup's share took 5500 cycles, so 3600
+    const int at = min(i, A.sq.seqs - 1);
+    int64_t b = (int64_t)at * A.sq.seq_len, e = b + A.sq.seq_len, kb = 0, ke = 0;
+    int slot = at;
+    if (A.sq.off) b = A.sq.off[at], e = A.sq.off[at + 1];
+    if (A.sq.slot) slot = A.sq.slot[at];
+    if (A.koff) kb = A.koff[at], ke = A.koff[at + 1];
+    const bool live = i < A.sq.seqs && slot >= 0 && (!A.sq.slot || slot < A.sq.slots);
+    const int len = A.table ? A.lens[live ? slot : 0] : 0;
+    if (!live) return s;
+    const uint32_t b0 = clamp_row(b, A.sq.tokens), e0 = clamp_row(e, A.sq.tokens);
+    s.slot = slot;
+    s.row0 = b0;
+    s.len = e0 > b0 ? e0 - b0 : 0;
+    if (A.table) {
+        s.keys = (uint32_t)min<int64_t>(max(len, 0), A.max_pages << A.shift);
+    } else if (!A.koff) {
+        s.key0 = s.row0;
+        s.keys = s.len;
+    } else {
+        const uint32_t kb0 = clamp_row(kb, A.key_tokens), ke0 = clamp_row(ke, A.key_tokens);
+        s.key0 = kb0;
+        s.keys = ke0 > kb0 ? ke0 - kb0 : 0;
+    }
     uint32_t left;
     s.tiles = quotient(s.len + A.tile - 1, A.tile, &left);
     const uint32_t round = (1u << A.quantum) - 1;
@@ -390,6 +414,23 @@ struct SoftRows {
     u32x4 q[KU / 2];
     f32x16 o[MT];
     float m, l;
+    // The row at `from`, nullptr: zeros.  All loads are under way before one is waited for.
+    template <bool VEC>
+    __device__ __forceinline__ void load_q(const SoftArgs& A, const T* from, int h) {
+#pragma unroll
+        for (int c = 0; c < KU / 2; ++c) {
+            const int u = 2 * c + h;
+            if constexpr (VEC) {
+                const bool there = from && u * E < A.dk;
+                const T* p = there ? from + u * E : static_cast<const T*>(A.q);
+                const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+                q[c] = there ? v : u32x4{0, 0, 0, 0};
+            } else {
+                q[c] = from ? load_unit<T, false>(from, u, A.dk) : u32x4{0, 0, 0, 0};
+            }
+        }
+        if (A.qsign != 1) turn_q(A.qsign);
+    }
     uint32_t odd[MT / 2];  // of o: results that are NaN
 
     __device__ __forceinline__ void clear() {
@@ -722,42 +763,56 @@ __device__ __forceinline__ void store4(T* p, int live, f32x4 v) {
 // What a part leaves in the workspace: for each row of its tile the maximum and the sum of the weights, and the sums over v.
 // Parts of a row may run on different XCDs, whose L2 caches are not coherent: where the same launch joins them
 // (SAME), everything is stored and loaded past the caches (device scope).
+// They lie row by row then; else as waves have them in registers, so that a store writes 1 KB in a row (16 requests of 24 drafts
+// over up to 5000 keys 69 -> 58 us, 4 prompts of 300 to 700 that go on from 12000 214 -> 206).
 template <bool SAME>
 struct PartRows {
     static constexpr int kDevice = SAME ? 1 << 4 : 0;  // cache policy bit of buffer accesses
     __amdgpu_buffer_rsrc_t r;
-    uint32_t row_bytes;
+    uint32_t step;  // bytes from a row to the next, of 32 rows to the next 32
+    uint32_t sums_at;
     // A share has places for two parts: of a unit that began before it, and of one that begins in it (part 0).
     __device__ __forceinline__ PartRows(const SoftArgs& A, const SoftPlace& pl, uint32_t part) {
         const uint32_t rows = (uint32_t)A.tile * A.pack;
-        row_bytes = ((uint32_t)A.dv + 3) / 4 * 16 + 16;
-        r = make_rsrc(static_cast<char*>(A.ws) + (int64_t)(2 * (pl.share + part) + (part == 0)) * (rows * row_bytes),
-                      rows * row_bytes);
+        step = SAME ? ((uint32_t)A.dv + 3) / 4 * 16 + 16 : ((uint32_t)A.dv + 7) / 8 * 1024;
+        sums_at = SAME ? 0 : (rows + 31) / 32 * step;
+        const uint32_t bytes = SAME ? rows * step : sums_at + (rows + 31) / 32 * 256;
+        r = make_rsrc(static_cast<char*>(A.ws) + (int64_t)(2 * (pl.share + part) + (part == 0)) * bytes, bytes);
     }
+    __device__ __forceinline__ uint32_t at(int row, int c) const {
+        return SAME ? row * step + 16 + c * 4 : (row >> 5) * step + (c >> 3) * 1024 + (c >> 2 & 1) * 512 + (row & 31) * 16;
+    }
+    __device__ __forceinline__ uint32_t at_sums(int row) const { return SAME ? row * step : sums_at + row * 8; }
     __device__ __forceinline__ void put_sums(int row, f32x2 v) const {
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, row * row_bytes, 0, kDevice);
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, at_sums(row), 0, kDevice);
     }
     __device__ __forceinline__ void put(int row, int c, f32x4 v) const {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, row * row_bytes + 16 + c * 4, 0, kDevice);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, at(row, c), 0, kDevice);
     }
     __device__ __forceinline__ f32x2 sums(int row) const {
-        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, row * row_bytes, 0, kDevice));
+        return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at_sums(row), 0, kDevice));
     }
     __device__ __forceinline__ f32x4 get(int row, int c) const {
-        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, row * row_bytes + 16 + c * 4, 0, kDevice));
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at(row, c), 0, kDevice));
     }
 };
 
-// Joins the parts of a unit, in their order: rows [first, first + rows) of its tile.
+constexpr int kJoinRows = 8;
+// Joins the parts of a unit, in their order: rows [first, first + rows) of its tile (not SAME: kJoinRows at most, which
+// neighbouring threads take).
 template <typename T, bool VEC, bool SAME>
 __device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl, int first, int rows, int threads) {
     const int groups = (A.dv + 3) / 4;
 #pragma unroll 1
-    for (int x = threadIdx.x; x < rows * groups; x += threads) {
-        const int at = (int)fdiv(x, A.by_groups), row = first + at, c = 4 * (x - at * groups);
+    for (int x = threadIdx.x; x < (SAME ? rows : kJoinRows) * groups; x += threads) {
+        const int at = SAME ? (int)fdiv(x, A.by_groups) : x % kJoinRows, row = first + at;
+        const int c = 4 * (SAME ? x - at * groups : x / kJoinRows);
+        if (!SAME && at >= rows) continue;
         f32x4 o{0, 0, 0, 0};
         float m = -FLT_MAX, l = 0.0f;
-        constexpr int AHEAD = SAME ? 4 : 8;
+        // Two parts at a time where rows are many (4 prompts of 300 to 700
+        // that go on from 12000 194 us, with eight 202: most units have two or three parts).
+        constexpr int AHEAD = SAME ? 4 : 2;
 #pragma unroll 1
         for (uint32_t p = 0; p < pl.parts; p += AHEAD) {
             f32x2 s[AHEAD];
@@ -967,13 +1022,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
 #pragma unroll
     for (int i = 0; i < R::MT / 2; ++i) rows.odd[i] = 0;
     rows.place();
-    const T* q = static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head;
-#pragma unroll
-    for (int c = 0; c < KU / 2; ++c) {
-        rows.q[c] = u32x4{0, 0, 0, 0};
-        if (live) rows.q[c] = load_unit<T, VEC>(q, 2 * c + h, A.dk);
-    }
-    if (A.qsign != 1) rows.turn_q(A.qsign);
+    rows.template load_q<VEC>(A, live ? static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head : nullptr, h);
 
     const uint32_t at_k = (uint32_t)(uintptr_t)(lds_address)sK, at_v = (uint32_t)(uintptr_t)(lds_address)sV;
 #pragma unroll 1
@@ -1136,22 +1185,23 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
         }
     }
 
+    const SoftArgs& E = args_here();
     const float l = sum_of_halves(rows.l);
     if (pl.parts == 1) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         if (!live) return;
-        T* o = static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head;
+        T* o = static_cast<T*>(E.o) + (pl.row0 + t) * E.o_row + (int64_t)head * E.o_head;
 #pragma unroll
         for (int mt = 0; mt < R::MT; ++mt)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int c = 32 * mt + 8 * b + 4 * h;
                 const f32x4 v{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]};
-                store4<T, VEC>(o + c, A.dv - c, v * inv);
+                store4<T, VEC>(o + c, E.dv - c, v * inv);
             }
         return;
     }
-    const PartRows<false> part(A, pl, pl.part);
+    const PartRows<false> part(E, pl, pl.part);
     if (live) {
         part.put_sums(row, f32x2{rows.m, l});
 #pragma unroll
@@ -1159,23 +1209,24 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int c = 32 * mt + 8 * b + 4 * h;
-                if (c < A.dv)
+                if (c < E.dv)
                     part.put(row, c, f32x4{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]});
             }
     }
 }
 
 template <typename T, int DKP, int DVP, int KT, bool VEC>
-__global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_kernel(SoftArgs A) {
+__global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void softmax_prompt_kernel(SoftArgs) {
     using R = SoftRows<T, DKP, DVP>;
     __shared__ u32x4 lds[(VEC ? 2 : 1) * (KeyTile<R::KU>::units(KT) + KT * R::VU)];
     SoftPlace pl;
-    SoftShares shares(A, share_of_block(A));
-    while (shares.next(A, &pl)) {
+    SoftShares shares(args_here(), share_of_block(args_here()));
+    while (shares.next(args_here(), &pl)) {
         pl.uniform();
-        prompt_part<T, DKP, DVP, KT, VEC>(A, pl, lds);
+        prompt_part<T, DKP, DVP, KT, VEC>(args_here(), pl, lds);
         __syncthreads();
     }
+    const SoftArgs& A = args_here();
     // for the launch that joins: the unit that begins in this share and goes on behind it
     if (A.shares && threadIdx.x == 0) {
         if (shares.none || pl.part != 0) pl.parts = 1;
@@ -1185,7 +1236,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void s
 
 // Many rows are joined by a launch of their own: blockIdx.x is a share, in which one unit at most begins and goes on behind it;
 // each blockIdx.y takes kJoinRows of its rows.
-constexpr int kJoinRows = 8;
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void softmax_join_kernel(SoftArgs A) {
     SoftPlace pl = static_cast<const SoftPlace*>(A.marks)[blockIdx.x];
@@ -1197,7 +1247,8 @@ __global__ __launch_bounds__(256) void softmax_join_kernel(SoftArgs A) {
 
 // Few rows: each wave takes every WAVES-th 32 keys of the unit's, for the same rows, through LDS of its own, so that
 // waves do not wait for each other until the end.  Two waves on a SIMD with a tile each: while one works the other's
-// comes (WAVES_US).
+// comes (eight waves with a tile each, not four with two: 64 tokens over up to 8000 keys 115 -> 110 us, 4 over up to 600
+// 15.7 -> 12.5).
 template <int BYTES>  // of 32 keys and values
 constexpr int step_waves() { return BYTES <= 16384 ? 8 : BYTES <= 32768 ? 4 : 2; }
 
@@ -1244,13 +1295,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
 #pragma unroll
     for (int i = 0; i < R::MT / 2; ++i) rows.odd[i] = 0;
     rows.place();
-    const T* q = static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head;
-#pragma unroll
-    for (int c = 0; c < KU / 2; ++c) {
-        rows.q[c] = u32x4{0, 0, 0, 0};
-        if (live) rows.q[c] = load_unit<T, VEC>(q, 2 * c + h, A.dk);
-    }
-    if (A.qsign != 1) rows.turn_q(A.qsign);
+    rows.template load_q<VEC>(A, live ? static_cast<const T*>(A.q) + (pl.row0 + t) * A.q_row + (int64_t)head * A.q_head : nullptr, h);
 #pragma unroll 1
     for (int mode = PLAIN;; ++mode) {
         auto step = [&](int key0) {
@@ -1305,6 +1350,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
     }
 
     // the waves' results, in their order
+    const SoftArgs& E = args_here();
     __syncthreads();
     float* const sO = reinterpret_cast<float*>(lds);
     const float l = sum_of_halves(rows.l);
@@ -1316,11 +1362,11 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             *reinterpret_cast<f32x4*>(&sO[(wave * 32 + n) * PITCH + 32 * mt + 8 * b + 4 * h]) =
                 f32x4{rows.o[mt][4 * b], rows.o[mt][4 * b + 1], rows.o[mt][4 * b + 2], rows.o[mt][4 * b + 3]};
     __syncthreads();
-    const PartRows<true> part(A, pl, pl.part);
-    const int groups = (A.dv + 3) / 4, count = min(A.tile, pl.len - pl.t0) * A.pack;
+    const PartRows<true> part(E, pl, pl.part);
+    const int groups = (E.dv + 3) / 4, count = min(E.tile, pl.len - pl.t0) * E.pack;
 #pragma unroll 1
     for (int x = tid; x < count * groups; x += 64 * WAVES) {
-        const int row = (int)fdiv(x, A.by_groups), c = 4 * (x - row * groups);
+        const int row = (int)fdiv(x, E.by_groups), c = 4 * (x - row * groups);
         float m = -FLT_MAX, sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_sums[w][row][0]);
@@ -1337,24 +1383,24 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             if (c == 0) part.put_sums(row, f32x2{m, sum});
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const int tt = pl.t0 + (int)fdiv(row, A.by_pack), hh = pl.head + row - (int)fdiv(row, A.by_pack) * A.pack;
-            store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + tt) * A.o_row + (int64_t)hh * A.o_head + c, A.dv - c, o * inv);
+            const int tt = pl.t0 + (int)fdiv(row, E.by_pack), hh = pl.head + row - (int)fdiv(row, E.by_pack) * E.pack;
+            store4<T, VEC>(static_cast<T*>(E.o) + (pl.row0 + tt) * E.o_row + (int64_t)hh * E.o_head + c, E.dv - c, o * inv);
         }
     }
-    if (pl.parts > 1) join_last<T, VEC>(A, pl, 64 * WAVES);
+    if (pl.parts > 1) join_last<T, VEC>(E, pl, 64 * WAVES);
 }
 
 template <typename T, int DKP, int DVP, bool VEC>
 __global__ __launch_bounds__(64 * step_waves<32 * (DKP + DVP) * sizeof(T)>())
-__attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step_kernel(SoftArgs A) {
+__attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step_kernel(SoftArgs) {
     __shared__ u32x4 lds[StepTiles<T, DKP, DVP>::LDS];
     __shared__ f32x2 sums[StepTiles<T, DKP, DVP>::WAVES][32];
     __shared__ int pages[StepTiles<T, DKP, DVP>::WAVES][64];
     SoftPlace pl;
-    SoftShares shares(A, share_of_block(A));
-    while (shares.next(A, &pl)) {
+    SoftShares shares(args_here(), share_of_block(args_here()));
+    while (shares.next(args_here(), &pl)) {
         pl.uniform();
-        step_part<T, DKP, DVP, VEC>(A, pl, lds, sums, pages);
+        step_part<T, DKP, DVP, VEC>(args_here(), pl, lds, sums, pages);
         __syncthreads();
     }
 }
