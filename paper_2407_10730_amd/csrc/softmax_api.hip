@@ -54,10 +54,15 @@ int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
 }
 
 // Where the tiles of rows are fewer than this, their keys are divided in shares, one for each workgroup that the card holds.
-// 128 rows per tile: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles): 217 us, by tiles
-// 400; 10 packed ones, 12 heads of 64 x 128 (648 tiles): 80 us, by tiles 70.  32 rows: 64 single tokens over up to 8000
-// keys, 4 k/v heads (288): 115 us, by tiles 131; 2 over 65536 (8): 68 us, 700.
-constexpr int64_t kFullPrompt = 2 * kSeqmixCUs, kFullStep = 4 * kSeqmixCUs;
+// 128 rows per tile, keys in a cache: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles):
+// 194 us, by tiles 400; about as many keys as tokens, where tiles see half of them on average and the card overlaps short
+// and long ones: 3 of 1000 tokens (384): 54 us, by tiles 42; one of 2200 (288): 61 and 62; 10 packed ones, 12 heads of 64 x 128
+// (648): 71, by tiles 64; fp32 holds one workgroup per CU (3 of 1300, 12 heads of 80 x 112: 269 us, by tiles 387).
+// 32 rows: 64 single tokens over up to 8000 keys, 4 k/v heads (288): 111 us, by tiles 131; 2 over 65536 (8): 67 us, 700.
+int64_t full_card(const seqmix_softmax_params& p, bool step) {
+    if (step) return 4 * kSeqmixCUs;
+    return p.dtype == CONV2D_BF16 && !p.page && p.key_tokens <= 2 * p.tokens ? kSeqmixCUs : 2 * kSeqmixCUs;
+}
 // ... and sequences are at most this many, as each wave looks at all of them.
 constexpr int64_t kShareSeqs = 1024;
 // Shares of the prompt kernel: two workgroups per CU (the prompts above 217 us, with one 320), of fp32, whose matrix
@@ -79,7 +84,7 @@ void plan_softmax(seqmix_softmax_desc* d) {
     const int32_t rows = step ? kStepRows : kPromptRows, pack = packed_heads(rows, length, rep);
     d->plan = seqmix_softmax_plan_info{step ? SEQMIX_KERNEL_STEP : SEQMIX_KERNEL_PROMPT, pack, 0, 0};
     const int64_t blocks = p.heads / pack, tiles = p.tokens / (rows / pack) + p.seqs;
-    if (tiles * blocks < (step ? kFullStep : kFullPrompt) && p.seqs <= kShareSeqs) {
+    if (tiles * blocks < full_card(p, step) && p.seqs <= kShareSeqs) {
         d->plan.shares = shares_of(step, p.dtype);
         // quanta of all rows are counted in 32 bits
         const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
