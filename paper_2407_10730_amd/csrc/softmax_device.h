@@ -1141,6 +1141,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
             __syncthreads();
         } else {
             constexpr int THREADS = 64 * kPromptWaves;
+            const SoftArgs L = A;  // (what the loops need, read once)
             if constexpr (sizeof(T) == 2 && DKP + DVP <= 256) {
                 // the next tile's while this one is used (2048 tokens, 16 heads of 127: 167 -> 152 us; wider rows and fp32 have no
                 // registers for it: 335 -> 416 us at 231 + 128)
@@ -1148,8 +1149,8 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
                 static_assert(KT * KU % THREADS == 0 && KT * VU % THREADS == 0);
                 RegisterLoad<T, VU, KT * VU / THREADS, THREADS, ValueTile<VU>> v;
                 auto fetch = [&](int key0) {
-                    k.fetch(A, pl, A.k, A.kp, A.dk, key0, tid);
-                    v.fetch(A, pl, A.v, A.vp, A.dv, key0, tid);
+                    k.fetch(L, pl, L.k, L.kp, L.dk, key0, tid);
+                    v.fetch(L, pl, L.v, L.vp, L.dv, key0, tid);
                 };
                 if (pl.first < end) fetch(pl.first);
                 for (int key0 = pl.first; key0 < end; key0 += KT) {
@@ -1163,8 +1164,8 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
             } else {
                 for (int key0 = pl.first; key0 < end; key0 += KT) {
                     __syncthreads();
-                    copy_rows<T, KU, KT, THREADS, KeyTile<KU>>(A, pl, A.k, A.kp, A.dk, key0, sK, tid);
-                    copy_rows<T, VU, KT, THREADS, ValueTile<VU>>(A, pl, A.v, A.vp, A.dv, key0, sV, tid);
+                    copy_rows<T, KU, KT, THREADS, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, sK, tid);
+                    copy_rows<T, VU, KT, THREADS, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, sV, tid);
                     __syncthreads();
                     step(0, key0);
                 }
@@ -1333,9 +1334,10 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             }
             loads_done();
         } else {
+            const SoftArgs L = A;  // (what the loop needs, read once)
             for (int key0 = first; key0 < end; key0 += STRIDE) {
-                copy_rows<T, KU, KT, 64, KeyTile<KU>>(A, pl, A.k, A.kp, A.dk, key0, mine, lane);
-                copy_rows<T, VU, KT, 64, ValueTile<VU>>(A, pl, A.v, A.vp, A.dv, key0, mine + KEYS, lane);
+                copy_rows<T, KU, KT, 64, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, mine, lane);
+                copy_rows<T, VU, KT, 64, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, mine + KEYS, lane);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 step(key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
