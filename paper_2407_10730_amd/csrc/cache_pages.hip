@@ -12,18 +12,6 @@ namespace cv {
 
 constexpr int64_t kOneLaunch = 4096;
 
-// Sums over the lanes up to this one.
-__device__ __forceinline__ uint32_t scan_wave(uint32_t v) {
-#define SCAN_STEP(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false);
-    SCAN_STEP(0x111, 0xf)
-    SCAN_STEP(0x112, 0xf)
-    SCAN_STEP(0x114, 0xf)
-    SCAN_STEP(0x118, 0xf)
-    SCAN_STEP(0x142, 0xa)
-    SCAN_STEP(0x143, 0xc)
-#undef SCAN_STEP
-    return v;
-}
 // Of two values each, sums over the threads before this one, and over all.
 struct Two {
     uint32_t a, b;
@@ -32,7 +20,7 @@ template <int THREADS>
 __device__ __forceinline__ Two scan_before(Two v, Two* sums, Two* total) {
     constexpr int WAVES = THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Two up{scan_wave(v.a), scan_wave(v.b)};
+    const Two up{scan_lanes(v.a), scan_lanes(v.b)};
     Two before{0, 0}, all{0, 0};
     if constexpr (WAVES == 1) {
         all = {(uint32_t)__builtin_amdgcn_readlane((int)up.a, 63), (uint32_t)__builtin_amdgcn_readlane((int)up.b, 63)};

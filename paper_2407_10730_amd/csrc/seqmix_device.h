@@ -159,6 +159,19 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return (row(0) + row(16)) + (row(32) + row(48));
 }
 
+// Sums over the lanes up to this one.
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t v) {
+#define SCAN_STEP(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false);
+    SCAN_STEP(0x111, 0xf)
+    SCAN_STEP(0x112, 0xf)
+    SCAN_STEP(0x114, 0xf)
+    SCAN_STEP(0x118, 0xf)
+    SCAN_STEP(0x142, 0xa)
+    SCAN_STEP(0x143, 0xc)
+#undef SCAN_STEP
+    return v;
+}
+
 // 1 / (1 + exp(-x)) on the hardware's exponential and reciprocal (each within 1 ulp of fp32).
 __device__ __forceinline__ float sigmoid(float x) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));

@@ -115,12 +115,12 @@ struct SoftArgs {
     CachePlace kp, vp;
     int64_t q_row, q_head, o_row, o_head;
     int32_t shift;         // log2 of a page's rows; packed (table NULL): of rows that a 32-bit offset reaches
-    int32_t heads, rep, pack, blocks;  // rep heads share a k/v head; blocks of `pack` heads
+    int32_t pack, blocks;  // blocks of `pack` heads
     int32_t dk, dv, mask;
     int32_t qsign;         // -1, 0, 1
     float scale2;          // |scale| log2(e), where the scale is not 0
     int32_t tile;          // tokens of a tile
-    FastDiv by_pack, by_groups;  // heads of a tile, groups of 4 columns of o
+    FastDiv by_pack, by_groups, by_rep;  // heads of a tile, groups of 4 columns of o, heads that share a k/v head
     int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
     int32_t shares;        // 0: a workgroup takes a tile; else that many take the same number of quanta of all tiles' keys
     int32_t quantum;       // log2 of its keys

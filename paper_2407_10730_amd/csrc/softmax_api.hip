@@ -71,8 +71,18 @@ constexpr int64_t kShareSeqs = 1024;
 // instructions take 8 times as long, one (3 prompts of 31 to 1300 tokens, 6 heads of 80 x 112: 98 us, with two 119).  Of
 // the step kernel, whose tiles fill LDS, one (2 tokens as above 68 us, with two 80).
 int64_t shares_of(bool step, int dtype) { return step || dtype == CONV2D_F32 ? kSeqmixCUs : 2 * kSeqmixCUs; }
-// Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: joining parts costs some.
-constexpr int32_t kLeast = 4, kWhole = 6;
+// Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: beginning and joining parts
+// costs some.  bf16 prompts (16 heads of 128): 400 tokens whole 16 us, divided 31, 1000 (16 quanta) 33 and 35, 4 x 24 drafts over
+// 2000 keys (32 quanta) 70 and 35, with shares of 8 at least 41.  Single tokens: 4 over up to 1500 keys whole 17 us,
+// divided 21 (shares of 2 at least: 18); 2 over 5000 with shares of 4 at least 17, of 2 15.  fp32, whose quanta take
+// longer than all that: 300 tokens, 6 heads of 80 x 112, shares of 4 quanta at least 66 us, of 2 40, of 1 28.
+struct Division {
+    int32_t least, whole;
+};
+Division division_of(bool step, int dtype) {
+    if (dtype == CONV2D_F32) return {1, 1};
+    return step ? Division{2, 12} : Division{4, 16};
+}
 
 int64_t part_bytes(const seqmix_softmax_params& p, bool step, int64_t rows) {
     return step ? rows * ((p.dv + 3) / 4 * 16 + 16) : (rows + 31) / 32 * ((p.dv + 7) / 8 * 1024 + 256);
@@ -86,11 +96,12 @@ void plan_softmax(seqmix_softmax_desc* d) {
     const int32_t rows = step ? kStepRows : kPromptRows, pack = packed_heads(rows, length, rep);
     d->plan = seqmix_softmax_plan_info{step ? SEQMIX_KERNEL_STEP : SEQMIX_KERNEL_PROMPT, pack, 0, 0};
     const int64_t blocks = p.heads / pack, tiles = p.tokens / (rows / pack) + p.seqs;
-    if (tiles * blocks < full_card(p, step) && p.seqs <= kShareSeqs) {
+    const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
+    d->quantum = step ? 7 : 6;
+    if (tiles * blocks < full_card(p, step) && p.seqs <= kShareSeqs && keys > (int64_t)division_of(step, p.dtype).whole << d->quantum) {
         d->plan.shares = shares_of(step, p.dtype);
         // quanta of all rows are counted in 32 bits
-        const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
-        for (d->quantum = step ? 7 : 6; tiles * blocks * ((keys >> d->quantum) + 2) >= 1LL << 31;) ++d->quantum;
+        for (; tiles * blocks * ((keys >> d->quantum) + 2) >= 1LL << 31;) ++d->quantum;
         d->plan.workspace_bytes = d->plan.shares * (2 * part_bytes(p, step, rows / pack * pack) + kMarkBytes);
     }
 }
@@ -169,10 +180,9 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.q_row = p.q_row, a.q_head = p.q_head, a.o_row = p.o_row, a.o_head = p.o_head;
     a.shift = p.page ? log2_of(p.page) : kPackedShift;
     if (!p.page) a.kp.page = p.k_row << kPackedShift, a.vp.page = p.v_row << kPackedShift;
-    a.heads = p.heads;
-    a.rep = p.heads / p.kv_heads;
     a.pack = d->plan.pack;
     a.blocks = p.heads / a.pack;
+    a.by_rep = make_fastdiv((uint32_t)(p.heads / p.kv_heads));
     a.by_pack = make_fastdiv((uint32_t)a.pack);
     a.by_groups = make_fastdiv((uint32_t)((p.dv + 3) / 4));
     a.dk = p.dk, a.dv = p.dv, a.mask = p.mask;
@@ -195,8 +205,8 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
         a.shares = (int32_t)d->plan.shares;
         a.quantum = d->quantum;
         a.grow = p.mask == SEQMIX_MASK_CAUSAL && a.tile % (1 << a.quantum) == 0 ? a.tile >> a.quantum : 0;
-        a.least = kLeast;
-        a.whole = kWhole;
+        a.least = division_of(step, p.dtype).least;
+        a.whole = division_of(step, p.dtype).whole;
         a.most = (int32_t)((1LL << 31) / a.blocks - 1);
         a.ws = d->ws.data;
         a.marks = static_cast<char*>(d->ws.data) +

@@ -62,7 +62,7 @@ __device__ __forceinline__ int seq_keys(const SoftArgs& A, int seq, int64_t slot
 
 __device__ __forceinline__ void soft_heads(const SoftArgs& A, int block, SoftPlace* out) {
     out->head = block * A.pack;
-    out->kv_head = out->head / A.rep;
+    out->kv_head = (int)fdiv(out->head, A.by_rep);
 }
 
 // Unit `id` of a block of heads, all of its keys.  False: there is none (in all threads).
@@ -94,18 +94,7 @@ __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t* l
     *left = (uint32_t)m;
     return q;
 }
-// Sums over the lanes up to this one, and over all.
-__device__ __forceinline__ uint32_t scan_lanes(uint32_t v) {
-#define SCAN_STEP(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false);
-    SCAN_STEP(0x111, 0xf)
-    SCAN_STEP(0x112, 0xf)
-    SCAN_STEP(0x114, 0xf)
-    SCAN_STEP(0x118, 0xf)
-    SCAN_STEP(0x142, 0xa)
-    SCAN_STEP(0x143, 0xc)
-#undef SCAN_STEP
-    return v;
-}
+// ... of the last lane.
 __device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
 
 // Shares.  Where units alone would not fill the card evenly, what there is to do is put in a row: the keys of a unit in
@@ -423,7 +412,7 @@ struct SoftRows {
             if constexpr (VEC) {
                 const bool there = from && u * E < A.dk;
                 const T* p = there ? from + u * E : static_cast<const T*>(A.q);
-                const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+                const u32x4 v = *reinterpret_cast<const u32x4_any*>(p);
                 q[c] = there ? v : u32x4{0, 0, 0, 0};
             } else {
                 q[c] = from ? load_unit<T, false>(from, u, A.dk) : u32x4{0, 0, 0, 0};
@@ -797,24 +786,21 @@ struct PartRows {
     }
 };
 
-constexpr int kJoinRows = 8;
-// Joins the parts of a unit, in their order: rows [first, first + rows) of its tile (not SAME: kJoinRows at most, which
-// neighbouring threads take).
-template <typename T, bool VEC, bool SAME>
-__device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl, int first, int rows, int threads) {
-    const int groups = (A.dv + 3) / 4;
+// 4 columns of a row over some of its parts, in their order.
+struct Joined {
+    f32x4 o{0, 0, 0, 0};
+    float m = -FLT_MAX, l = 0.0f;
+    __device__ __forceinline__ void add(f32x4 v, f32x2 s) {
+        const float now = fmaxf(m, s[0]), a = __builtin_amdgcn_exp2f(m - now), b = __builtin_amdgcn_exp2f(s[0] - now);
+        m = now;
+        l = l * a + s[1] * b;
+        o = o * a + v * b;
+    }
+    // Parts [p, end), AHEAD of them at a time.
+    template <int AHEAD, bool SAME>
+    __device__ __forceinline__ void parts(const SoftArgs& A, const SoftPlace& pl, int row, int c, uint32_t p, uint32_t end) {
 #pragma unroll 1
-    for (int x = threadIdx.x; x < (SAME ? rows : kJoinRows) * groups; x += threads) {
-        const int at = SAME ? (int)fdiv(x, A.by_groups) : x % kJoinRows, row = first + at;
-        const int c = 4 * (SAME ? x - at * groups : x / kJoinRows);
-        if (!SAME && at >= rows) continue;
-        f32x4 o{0, 0, 0, 0};
-        float m = -FLT_MAX, l = 0.0f;
-        // Two parts at a time where rows are many (4 prompts of 300 to 700
-        // that go on from 12000 194 us, with eight 202: most units have two or three parts).
-        constexpr int AHEAD = SAME ? 4 : 2;
-#pragma unroll 1
-        for (uint32_t p = 0; p < pl.parts; p += AHEAD) {
+        for (; p < end; p += AHEAD) {
             f32x2 s[AHEAD];
             f32x4 v[AHEAD];
 #pragma unroll
@@ -825,24 +811,22 @@ __device__ __forceinline__ void join_rows(const SoftArgs& A, const SoftPlace& pl
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i)
-                if (p + i < pl.parts) {
-                    const float now = fmaxf(m, s[i][0]);
-                    const float a = __builtin_amdgcn_exp2f(m - now), b = __builtin_amdgcn_exp2f(s[i][0] - now);
-                    m = now;
-                    l = l * a + s[i][1] * b;
-                    o = o * a + v[i] * b;
-                }
+                if (p + i < end) add(v[i], s[i]);
         }
+    }
+    template <typename T, bool VEC>
+    __device__ __forceinline__ void store(const SoftArgs& A, const SoftPlace& pl, int row, int c) const {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const int t = pl.t0 + (int)fdiv(row, A.by_pack), head = pl.head + row - (int)fdiv(row, A.by_pack) * A.pack;
         store4<T, VEC>(static_cast<T*>(A.o) + (pl.row0 + t) * A.o_row + (int64_t)head * A.o_head + c, A.dv - c, o * inv);
     }
-}
+};
 
 // Few rows are joined by the workgroup whose part is done last, which clears their count for the next call.  The others return
-// at once.
+// at once.  Threads that rows leave idle take some of the parts, and what they have is joined in order through `lds` (2 tokens over
+// 65536 keys, 32 parts each: 67 -> 62 us).
 template <typename T, bool VEC>
-__device__ __forceinline__ void join_last(const SoftArgs& A, const SoftPlace& pl, int threads) {
+__device__ __forceinline__ void join_last(const SoftArgs& A, const SoftPlace& pl, int threads, u32x4* lds) {
     __shared__ int s_last;
     uint32_t* const count = static_cast<uint32_t*>(A.marks) + pl.share;  // only one unit begins in a share and goes on behind it
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's results are where all XCDs see them
@@ -851,7 +835,35 @@ __device__ __forceinline__ void join_last(const SoftArgs& A, const SoftPlace& pl
         s_last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pl.parts - 1;
     __syncthreads();
     if (!s_last) return;
-    join_rows<T, VEC, true>(A, pl, 0, min(A.tile, pl.len - pl.t0) * A.pack, threads);
+    const uint32_t groups = (A.dv + 3) / 4, all = min(A.tile, pl.len - pl.t0) * A.pack * groups;
+    uint32_t slices = 1;
+    while (2 * slices * all <= (uint32_t)threads && 8 * slices < pl.parts) slices *= 2;
+    const uint32_t each = (pl.parts + slices - 1) / slices;
+    auto* const s_o = reinterpret_cast<f32x4*>(lds);
+    auto* const s_sums = reinterpret_cast<f32x2*>(lds + threads);
+#pragma unroll 1
+    for (uint32_t x = threadIdx.x; x < slices * all; x += threads) {
+        uint32_t at = x;
+        const uint32_t slice = slices == 1 ? 0 : quotient(x, all, &at);
+        const int row = (int)fdiv(at, A.by_groups), c = 4 * (at - row * groups);
+        Joined of;
+        of.parts<8, true>(A, pl, row, c, slice * each, min((slice + 1) * each, pl.parts));
+        if (slices == 1) {
+            of.store<T, VEC>(A, pl, row, c);
+        } else {
+            s_o[x] = of.o;
+            s_sums[x] = f32x2{of.m, of.l};
+        }
+    }
+    if (slices > 1) {
+        __syncthreads();
+        if (threadIdx.x < all) {
+            const int row = (int)fdiv(threadIdx.x, A.by_groups), c = 4 * (threadIdx.x - row * groups);
+            Joined of;
+            for (uint32_t i = threadIdx.x; i < slices * all; i += all) of.add(s_o[i], s_sums[i]);
+            of.store<T, VEC>(A, pl, row, c);
+        }
+    }
     if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -1236,14 +1248,23 @@ __global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void s
 }
 
 // Many rows are joined by a launch of their own: blockIdx.x is a share, in which one unit at most begins and goes on behind it;
-// each blockIdx.y takes kJoinRows of its rows.
+// each blockIdx.y takes kJoinRows of its rows, neighbouring threads neighbouring ones.  Two parts at a time (4 prompts of 300 to
+// 700 that go on from 12000 194 us, with eight 202: most units have two or three parts).
+constexpr int kJoinRows = 8;
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void softmax_join_kernel(SoftArgs A) {
     SoftPlace pl = static_cast<const SoftPlace*>(A.marks)[blockIdx.x];
     pl.uniform();
     if (pl.parts == 1) return;
-    const int rows = min(A.tile, pl.len - pl.t0) * A.pack, first = blockIdx.y * kJoinRows;
-    if (first < rows) join_rows<T, VEC, false>(A, pl, first, min(kJoinRows, rows - first), 256);
+    const int rows = min(A.tile, pl.len - pl.t0) * A.pack;
+#pragma unroll 1
+    for (int x = threadIdx.x; x < kJoinRows * ((A.dv + 3) / 4); x += 256) {
+        const int row = blockIdx.y * kJoinRows + x % kJoinRows, c = 4 * (x / kJoinRows);
+        if (row >= rows) return;
+        Joined of;
+        of.parts<2, false>(A, pl, row, c, 0, pl.parts);
+        of.store<T, VEC>(A, pl, row, c);
+    }
 }
 
 // Few rows: each wave takes every WAVES-th 32 keys of the unit's, for the same rows, through LDS of its own, so that
@@ -1389,7 +1410,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             store4<T, VEC>(static_cast<T*>(E.o) + (pl.row0 + tt) * E.o_row + (int64_t)hh * E.o_head + c, E.dv - c, o * inv);
         }
     }
-    if (pl.parts > 1) join_last<T, VEC>(E, pl, 64 * WAVES);
+    if (pl.parts > 1) join_last<T, VEC>(E, pl, 64 * WAVES, lds);
 }
 
 template <typename T, int DKP, int DVP, bool VEC>

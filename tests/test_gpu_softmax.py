@@ -250,6 +250,58 @@ def test_what_is_not_seen_does_not_matter(dtype, mask, page):
         assert (np.abs(rows - o)[fine] <= bound[fine]).all()
 
 
+# Few tiles over many keys: bf16 rows over more than 1024 keys (single tokens 1536), fp32 rows over more than 64, are divided and joined.
+DIVIDED = [
+    _case(new=[300, 7], keys=[2000, 900], heads=4, kv_heads=2, dk=128, dv=128, page=16),
+    _case(new=[130], keys=[5000], mask="full", heads=2, kv_heads=1, dk=64, dv=256),
+    _case(new=[40, 3, 0], keys=[2500, 64, 30], mask="full", heads=8, kv_heads=1, dk=128, dv=128),
+    _case(new=[130, 40], keys=[4500, 40], heads=3, kv_heads=3, dk=99, dv=37, page=16),
+    _case(new=[1500], heads=1, kv_heads=1, dk=80, dv=112),
+    _case(new=[1500, 2], heads=2, kv_heads=1, dk=64, dv=64, dtype="f32"),
+    _case(new=[200, 1], keys=[1300, 700], heads=3, kv_heads=1, dk=33, dv=70, dtype="f32", page=8),
+    *[_case(new=[24] * 3, keys=[3000, 24, 1900], mask="tree", heads=8, kv_heads=2, dk=d, dv=d, page=32) for d in (64, 128, 192)],
+    *[_case(new=[t] * 2, keys=[6000, 1600], heads=8, kv_heads=2, dk=128, dv=128, page=16, dtype=d) for t in (1, 3, 8) for d in ("bf16", "f32")],
+    _case(new=[1] * 2, keys=[40000, 1], heads=4, kv_heads=4, dk=64, dv=64, page=64),   # 512 shares' worth of parts for one row
+    _case(new=[1] * 2, keys=[4000, 2000], heads=5, kv_heads=1, dk=127, dv=63, page=16),
+    _case(new=[1] * 70, keys=[3000 if i % 9 == 0 else i for i in range(70)], heads=2, kv_heads=2, dk=64, dv=64, page=16),
+    _case(new=[2] * 70, keys=[1700 if i == 66 else 2 for i in range(70)], heads=2, kv_heads=1, dk=64, dv=64, page=16, skip=(65, 67)),
+    _case(new=[66] * 3 + [0, 140], keys=[66, 1500, 4000, 9, 200], heads=4, kv_heads=1, dk=128, dv=64, page=64, skip=(1,)),
+]
+
+
+@pytest.mark.parametrize("kw", DIVIDED)
+def test_divided(kw):
+    p = Soft(**kw)
+    assert p.op.plan().shares > 0
+    p.run().check()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("n,heads", ((3, 4), (40, 2), (150, 2)))
+def test_divided_rows_and_values_that_are_not_finite(dtype, n, heads):
+    """One value early and one late of many keys: the rows that see them are NaN there, whichever part holds them, and no others."""
+    keys = 5000
+    p = Soft([n], keys=[keys], heads=heads, kv_heads=heads // 2, dk=64, dv=64, dtype=dtype, page=16)
+    where = p.where[0][1]
+
+    def at(t, j):
+        return t[int(where[j // 16]), j % 16]
+
+    at(p.v, 100)[0, 5] = float("inf")            # seen by all rows
+    at(p.v, keys - 1)[heads // 2 - 1, 9] = float("nan")  # by the last row only
+    at(p.v, keys - 2)[0, 11] = float("-inf")     # by the last two
+    assert p.op.plan().shares > 0
+    p.run()
+    got, q = _host(p.o), _host(p.q)
+    k, v = p.held(0)
+    on = ref.sees("causal", n, keys)
+    o, o_abs, most = ref.softmax_attention(q, k, v, on, p.scale)
+    fine = np.isfinite(o)
+    assert not fine.all() and np.array_equal(np.isfinite(got), fine) and np.isnan(got[~fine]).all()
+    bound = ref.softmax_bound(o, o_abs, most, keys, p.dk, dtype, p.parts())
+    assert (np.abs(got - o)[fine] <= bound[fine]).all()
+
+
 def test_query_that_is_not_finite_stays_with_its_row():
     p = Soft([50, 30], heads=2, kv_heads=1)
     p.q[7, 1, 3] = float("nan")
