@@ -57,9 +57,10 @@ int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
 // 128 rows per tile, keys in a cache: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles):
 // 194 us, by tiles 400; about as many keys as tokens, where tiles see half of them on average and the card overlaps short
 // and long ones: 3 of 1000 tokens (384): 54 us, by tiles 42; one of 2200 (288): 61 and 62; 10 packed ones, 12 heads of 64 x 128
-// (648): 71, by tiles 64; fp32 holds one workgroup per CU (3 of 1300, 12 heads of 80 x 112: 269 us, by tiles 387), and rows
-// that are no multiple of 16 bytes come slowly (2048 tokens, 16 heads of 127, 272 tiles: 152, by tiles 184).
-// 32 rows: 64 single tokens over up to 8000 keys, 4 k/v heads (288): 111 us, by tiles 131; 2 over 65536 (8): 67 us, 700.
+// (648): 71, by tiles 64; fp32 is
+// slower by tiles (3 of 1300, 12 heads of 80 x 112: 222 us, by tiles 387), and so are rows
+// that are no multiple of 16 bytes (2048 tokens, 16 heads of 127, 272 tiles: 152, by tiles 184).
+// 32 rows: 64 single tokens over up to 8000 keys, 4 k/v heads (288): 111 us, by tiles 131; 2 over 65536 (8): 61 us, 700.
 int64_t full_card(const seqmix_softmax_params& p, bool step) {
     if (step) return 4 * kSeqmixCUs;
     const bool quick = p.dtype == CONV2D_BF16 && p.dk % 8 == 0 && p.dv % 8 == 0;
@@ -67,10 +68,13 @@ int64_t full_card(const seqmix_softmax_params& p, bool step) {
 }
 // ... and sequences are at most this many, as each wave looks at all of them.
 constexpr int64_t kShareSeqs = 1024;
-// Shares of the prompt kernel: two workgroups per CU (the prompts above 217 us, with one 320), of fp32, whose matrix
-// instructions take 8 times as long, one (3 prompts of 31 to 1300 tokens, 6 heads of 80 x 112: 98 us, with two 119).  Of
-// the step kernel, whose tiles fill LDS, one (2 tokens as above 68 us, with two 80).
-int64_t shares_of(bool step, int dtype) { return step || dtype == CONV2D_F32 ? kSeqmixCUs : 2 * kSeqmixCUs; }
+// Shares of the prompt kernel: as many workgroups as its registers allow, two per CU or, of dims padded to more than 256 together,
+// one (the prompts above with heads of 256 428 us, with two 450; fp32, 3 of 1300 tokens, 12 heads of 80 x 112 222 with two, 269
+// with one).  Of the step kernel, whose tiles fill LDS, one (2 tokens as above 68 us, with two 80).
+int64_t shares_of(const seqmix_softmax_params& p, bool step) {
+    auto padded = [](int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; };
+    return step || padded(p.dk) + padded(p.dv) > 256 ? kSeqmixCUs : 2 * kSeqmixCUs;
+}
 // Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: beginning and joining parts
 // costs some.  bf16 prompts (16 heads of 128): 400 tokens whole 16 us, divided 31, 1000 (16 quanta) 33 and 35, 4 x 24 drafts over
 // 2000 keys (32 quanta) 70 and 35, with shares of 8 at least 41.  Single tokens: 4 over up to 1500 keys whole 17 us,
@@ -99,7 +103,7 @@ void plan_softmax(seqmix_softmax_desc* d) {
     const int64_t keys = p.page ? p.max_pages * p.page : p.key_tokens;
     d->quantum = step ? 7 : 6;
     if (tiles * blocks < full_card(p, step) && p.seqs <= kShareSeqs && keys > (int64_t)division_of(step, p.dtype).whole << d->quantum) {
-        d->plan.shares = shares_of(step, p.dtype);
+        d->plan.shares = shares_of(p, step);
         // quanta of all rows are counted in 32 bits
         for (; tiles * blocks * ((keys >> d->quantum) + 2) >= 1LL << 31;) ++d->quantum;
         d->plan.workspace_bytes = d->plan.shares * (2 * part_bytes(p, step, rows / pack * pack) + kMarkBytes);
