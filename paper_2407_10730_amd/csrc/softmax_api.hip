@@ -57,9 +57,8 @@ int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
 // 128 rows per tile, keys in a cache: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles):
 // 194 us, by tiles 400; about as many keys as tokens, where tiles see half of them on average and the card overlaps short
 // and long ones: 3 of 1000 tokens (384): 54 us, by tiles 42; one of 2200 (288): 61 and 62; 10 packed ones, 12 heads of 64 x 128
-// (648): 71, by tiles 64; fp32 is
-// slower by tiles (3 of 1300, 12 heads of 80 x 112: 222 us, by tiles 387), and so are rows
-// that are no multiple of 16 bytes (2048 tokens, 16 heads of 127, 272 tiles: 152, by tiles 184).
+// (648): 71, by tiles 64; fp32 is slower by tiles (3 of 1300, 12 heads of 80 x 112: 222 us, by tiles 387), and so are rows that
+// are no multiple of 16 bytes (2048 tokens, 16 heads of 127, 272 tiles: 152, by tiles 184).
 // 32 rows: 64 single tokens over up to 8000 keys, 4 k/v heads (288): 111 us, by tiles 131; 2 over 65536 (8): 61 us, 700.
 int64_t full_card(const seqmix_softmax_params& p, bool step) {
     if (step) return 4 * kSeqmixCUs;
@@ -76,16 +75,16 @@ int64_t shares_of(const seqmix_softmax_params& p, bool step) {
     return step || padded(p.dk) + padded(p.dv) > 256 ? kSeqmixCUs : 2 * kSeqmixCUs;
 }
 // Quanta (64 keys, 128 in the step kernel) of a share at least, and of units that are not divided: beginning and joining parts
-// costs some.  bf16 prompts (16 heads of 128): 400 tokens whole 16 us, divided 31, 1000 (16 quanta) 33 and 35, 4 x 24 drafts over
-// 2000 keys (32 quanta) 70 and 35, with shares of 8 at least 41.  Single tokens: 4 over up to 1500 keys whole 17 us,
-// divided 21 (shares of 2 at least: 18); 2 over 5000 with shares of 4 at least 17, of 2 15.  fp32, whose quanta take
-// longer than all that: 300 tokens, 6 heads of 80 x 112, shares of 4 quanta at least 66 us, of 2 40, of 1 28.
+// costs some.  bf16 prompts (16 heads of 128): 600 tokens (10 quanta) whole 22 us, divided 27, 1000 (16) 33 and 31, 100 after 800
+// (15) 32 and 26; shares of 3 at least: 1000 tokens 37, 100 after 800 21.  Single tokens: 4 over up to 1500 keys whole 17 us, in
+// shares of 1 at least 12; 2 over 5000 in shares of 1, 2, 3 at least 16, 14, 18.  fp32, whose quanta take longer than all
+// that: 300 tokens, 6 heads of 80 x 112, shares of 4 at least 66 us, of 2 40, of 1 28.
 struct Division {
     int32_t least, whole;
 };
 Division division_of(bool step, int dtype) {
     if (dtype == CONV2D_F32) return {1, 1};
-    return step ? Division{2, 12} : Division{4, 16};
+    return step ? Division{1, 6} : Division{4, 10};
 }
 
 int64_t part_bytes(const seqmix_softmax_params& p, bool step, int64_t rows) {
