@@ -122,6 +122,7 @@ struct SoftArgs {
     int32_t tile;          // tokens of a tile
     FastDiv by_pack, by_groups, by_rep;  // heads of a tile, groups of 4 columns of o, heads that share a k/v head
     int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
+    int32_t near;          // rows of k and v: 16 bytes at least, 8 or more in a page, all that a tile reads within 32-bit offsets
     int32_t shares;        // 0: a workgroup takes a tile; else that many take the same number of quanta of all tiles' keys
     int32_t quantum;       // log2 of its keys
     int32_t grow;          // quanta that a tile has more than the one before it where the mask is causal; 0: not counted on

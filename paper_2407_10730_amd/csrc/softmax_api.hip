@@ -194,11 +194,12 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     if (a.qsign == 0) a.scale2 = 1.0f;
     const bool step = d->plan.kernel == SEQMIX_KERNEL_STEP;
     const int64_t unit = 16 / esize(p.dtype);
-    // rows of k and v in 16-byte units, enough of them in a page, none that a 32-bit offset does not reach
+    // rows of k and v in 16-byte units
     const bool units = p.dk % unit == 0 && p.dv % unit == 0 && !(((uintptr_t)k | (uintptr_t)v) & 15) &&
                        !((p.k_row | p.k_head | p.k_page | p.v_row | p.v_head | p.v_page) % unit);
-    const bool vec = units && (!p.page || p.page >= 8) && std::max(a.kp.page, a.vp.page) < (1LL << 28) &&
-                     std::max(p.k_row, p.v_row) < (1LL << 22);
+    a.near = p.dk >= unit && p.dv >= unit && (!p.page || p.page >= 8) && std::max(a.kp.page, a.vp.page) < (1LL << 28) &&
+             std::max(p.k_row, p.v_row) < (1LL << 22);
+    const bool vec = units && a.near;
     hipStream_t s = static_cast<hipStream_t>(stream);
     a.tile = (step ? kStepRows : kPromptRows) / a.pack;
     a.ids = seq_part_ids(a.sq, a.tile);

@@ -915,6 +915,9 @@ typedef __attribute__((address_space(3))) const void* lds_address;
 template <int LEFT = 0>  // all but the last LEFT
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT < 63 ? LEFT : 63) : "memory"); }
 
+// The page that holds the rows of lane i's instruction.
+__device__ __forceinline__ int clamp_page(const SoftArgs& A, int page) { return min(max(page, 0), (int)A.pages - 1); }
+
 // Loads the rows of tiles of keys (or values) into LDS, RI rows per instruction of a wave.  What lies past the last key or past a
 // row's end reads as zero by the buffer's range.  Where a page (of packed rows: some rows that a 32-bit offset
 // reaches) begins, and how much of it counts, is worked out for all instructions of a tile at once, a lane each.
@@ -926,6 +929,7 @@ struct DirectLoad {
     uint32_t off[KINDS];  // of this lane, in bytes
     uint32_t page_bytes, row_bytes, last;  // last: bytes of a row that count
     int wave;             // (0: each wave loads its own tiles)
+    uint32_t ends;        // bit i: off[i] is a row's last 16 bytes, of a row that is no multiple of them
 
     __device__ __forceinline__ DirectLoad(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim) {
         const int lane = threadIdx.x & 63, r = lane / UNITS, at = lane % UNITS;
@@ -933,12 +937,14 @@ struct DirectLoad {
         page_bytes = (uint32_t)c.page * sizeof(T);
         row_bytes = (uint32_t)c.row * sizeof(T);
         last = dim * sizeof(T);
+        ends = 0;
         wave = WAVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
 #pragma unroll
         for (int i = 0; i < KINDS; ++i) {
             const int row = first_row(i) + r;
             const int u = at ^ LDS::turn(row);
-            off[i] = u * E < dim ? r * row_bytes + u * 16 : OOB_OFF;
+            off[i] = u * E < dim ? r * row_bytes + min(u * 16u, last - 16) : OOB_OFF;
+            ends |= (u * E < dim && u * 16u > last - 16 ? 1u : 0u) << i;
         }
     }
     // WAVES waves load a tile together, or each its own (1).
@@ -968,6 +974,56 @@ struct DirectLoad {
                                                  off[i % KINDS], to);
             });
         }
+    }
+    // Rows of any alignment and size (16 bytes at least): into registers, with the scalar work of `tile` and no more (each
+    // address by itself, in 64 bits, and pages by lanes: 64 single tokens of 127 over up to 8000 keys 323 us, so 198;
+    // 2048 tokens 152 and 127),
+    __device__ __forceinline__ void fetch(const SoftArgs& A, const SoftPlace& pl, int key0, int page, u32x4 (&v)[N]) const {
+        auto get = [&](uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)x, i); };
+        auto load = [&](uint64_t p, uint32_t bytes, uint32_t o) {
+            return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc((const void*)p, bytes), o, 0, 0));
+        };
+        if ((1 << A.shift) >= KT) {
+            const uint32_t key = (uint32_t)(key0 + wave * RI), at = A.table ? get((uint32_t)page, 0) : key >> A.shift;
+            const uint64_t p = base + (uint64_t)at * page_bytes + (uint64_t)(key & ((1u << A.shift) - 1)) * row_bytes;
+            const int left = pl.keys - (int)key;
+            const uint32_t rows = left < KT ? left : KT, each = WAVES * RI * row_bytes;
+            const uint32_t bytes = left > 0 ? (rows - 1) * row_bytes + last : 0u;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = load(p, bytes, off[i % KINDS] + i * each);
+        } else {
+            const int key = key0 + first_row(threadIdx.x & 63);
+            const uint64_t p = base + (uint64_t)(uint32_t)page * page_bytes +
+                               (uint64_t)(uint32_t)(key & ((1 << A.shift) - 1)) * row_bytes;
+            const int rows = min(max(pl.keys - key, 0), RI);
+            const uint32_t bytes = rows ? (rows - 1) * row_bytes + last : 0u;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = load((uint64_t)get((uint32_t)(p >> 32), i) << 32 | get((uint32_t)p, i), get(bytes, i), off[i % KINDS]);
+        }
+    }
+    // ... and on to LDS, with the last part of a row, which was read where it ends with the row, moved down.
+    __device__ __forceinline__ void store(const u32x4 (&v)[N], u32x4* to) const {
+        const uint32_t cut = (16 - (last & 15)) * 8 & 127;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            u32x4 w = v[i];
+            if (cut) {
+                u32x4 x = w;
+                if (cut & 64) x = u32x4{x[2], x[3], 0, 0};
+                if (cut & 32) x = u32x4{x[1], x[2], x[3], 0};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    x[c] = (uint32_t)(((uint64_t)(c < 3 ? x[c + 1] : 0u) << 32 | x[c]) >> (cut & 31));
+                w = ends >> (i % KINDS) & 1 ? x : w;
+            }
+            to[(i * WAVES + wave) * LDS::GROUP + (threadIdx.x & 63)] = w;
+        }
+    }
+    // The page of instruction `lane`'s rows of the tile from key0 on.
+    __device__ __forceinline__ int look(const SoftArgs& A, const SoftPlace& pl, int key0) const {
+        const int lane = threadIdx.x & 63, key = key0 + first_row(lane);
+        return A.table && lane < N && key < pl.keys ? A.table[pl.slot * A.max_pages + (key >> A.shift)] : 0;
     }
 };
 // ... rows that lie otherwise: through registers, N units of each thread at a time.
@@ -1004,9 +1060,6 @@ __device__ __forceinline__ void copy_rows(const SoftArgs& A, const SoftPlace& pl
         l.store(to, x);
     }
 }
-// The page that holds the rows of lane i's instruction.
-__device__ __forceinline__ int clamp_page(const SoftArgs& A, int page) { return min(max(page, 0), (int)A.pages - 1); }
-
 constexpr int kPromptWaves = kPromptRows / 32;
 
 // One part of a unit.
@@ -1153,30 +1206,45 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
         } else {
             constexpr int THREADS = 64 * kPromptWaves;
             const SoftArgs L = A;  // (what the loops need, read once)
-            if constexpr (sizeof(T) == 2 && DKP + DVP <= 256) {
-                // the next tile's while this one is used (2048 tokens, 16 heads of 127: 167 -> 152 us; wider rows and fp32 have no
-                // registers for it: 335 -> 416 us at 231 + 128)
-                RegisterLoad<T, KU, KT * KU / THREADS, THREADS, KeyTile<KU>> k;
-                static_assert(KT * KU % THREADS == 0 && KT * VU % THREADS == 0);
-                RegisterLoad<T, VU, KT * VU / THREADS, THREADS, ValueTile<VU>> v;
+            const DirectLoad<T, KU, KT, kPromptWaves, KeyTile<KU>> load_k(L, pl, L.k, L.kp, L.dk);
+            const DirectLoad<T, VU, KT, kPromptWaves, ValueTile<VU>> load_v(L, pl, L.v, L.vp, L.dv);
+            u32x4 k[load_k.N], v[load_v.N];
+            int page_k = 0, page_v = 0;
+            auto look = [&](int key0) { page_k = load_k.look(L, pl, key0), page_v = load_v.look(L, pl, key0); };
+            if (!L.near) {
+                for (int key0 = pl.first; key0 < end; key0 += KT) {
+                    __syncthreads();
+                    copy_rows<T, KU, KT, THREADS, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, sK, tid);
+                    copy_rows<T, VU, KT, THREADS, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, sV, tid);
+                    __syncthreads();
+                    step(0, key0);
+                }
+            } else if constexpr (sizeof(T) == 2 && DKP + DVP <= 256) {
+                // the next tile's while this one is used (wider rows and fp32 have no registers for it)
                 auto fetch = [&](int key0) {
-                    k.fetch(L, pl, L.k, L.kp, L.dk, key0, tid);
-                    v.fetch(L, pl, L.v, L.vp, L.dv, key0, tid);
+                    load_k.fetch(L, pl, key0, clamp_page(L, page_k), k);
+                    load_v.fetch(L, pl, key0, clamp_page(L, page_v), v);
+                    look(key0 + KT);
                 };
+                look(pl.first);
                 if (pl.first < end) fetch(pl.first);
                 for (int key0 = pl.first; key0 < end; key0 += KT) {
                     __syncthreads();
-                    k.store(sK, tid);
-                    v.store(sV, tid);
+                    load_k.store(k, sK);
+                    load_v.store(v, sV);
                     __syncthreads();
                     if (key0 + KT < end) fetch(key0 + KT);
                     step(0, key0);
                 }
             } else {
+                look(pl.first);
                 for (int key0 = pl.first; key0 < end; key0 += KT) {
+                    load_k.fetch(L, pl, key0, clamp_page(L, page_k), k);
                     __syncthreads();
-                    copy_rows<T, KU, KT, THREADS, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, sK, tid);
-                    copy_rows<T, VU, KT, THREADS, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, sV, tid);
+                    load_k.store(k, sK);
+                    load_v.fetch(L, pl, key0, clamp_page(L, page_v), v);
+                    look(key0 + KT);
+                    load_v.store(v, sV);
                     __syncthreads();
                     step(0, key0);
                 }
@@ -1354,10 +1422,25 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             }
             loads_done();
         } else {
-            const SoftArgs L = A;  // (what the loop needs, read once)
+            const SoftArgs L = A;  // (what the loops need, read once)
+            const DirectLoad<T, KU, KT, 1, KeyTile<KU>> load_k(L, pl, L.k, L.kp, L.dk);
+            const DirectLoad<T, VU, KT, 1, ValueTile<VU>> load_v(L, pl, L.v, L.vp, L.dv);
+            u32x4 k[load_k.N], v[load_v.N];
+            int page_k = 0, page_v = 0;
+            auto look = [&](int key0) { page_k = load_k.look(L, pl, key0), page_v = load_v.look(L, pl, key0); };
+            look(first);
             for (int key0 = first; key0 < end; key0 += STRIDE) {
-                copy_rows<T, KU, KT, 64, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, mine, lane);
-                copy_rows<T, VU, KT, 64, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, mine + KEYS, lane);
+                if (!L.near) {
+                    copy_rows<T, KU, KT, 64, KeyTile<KU>>(L, pl, L.k, L.kp, L.dk, key0, mine, lane);
+                    copy_rows<T, VU, KT, 64, ValueTile<VU>>(L, pl, L.v, L.vp, L.dv, key0, mine + KEYS, lane);
+                } else {
+                    load_k.fetch(L, pl, key0, clamp_page(L, page_k), k);
+                    if (load_k.N > 8) load_k.store(k, mine);
+                    load_v.fetch(L, pl, key0, clamp_page(L, page_v), v);
+                    look(key0 + STRIDE);
+                    if (load_k.N <= 8) load_k.store(k, mine);
+                    load_v.store(v, mine + KEYS);
+                }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 step(key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1443,27 +1526,25 @@ hipError_t launch_softmax_one(const SoftArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Kernels for heads of up to 64, 128 and 256 elements; of dims that fill no 16 bytes, by the larger of the two.
+// Kernels for heads of up to 64, 128 and 256 elements.
+template <typename T, bool STEP, bool VEC>
+hipError_t launch_softmax_dims(const SoftArgs& a, hipStream_t s) {
+    const int k = a.dk <= 64 ? 64 : a.dk <= 128 ? 128 : 256, v = a.dv <= 64 ? 64 : a.dv <= 128 ? 128 : 256;
+    switch (1000 * k + v) {
+        case 64064: return launch_softmax_one<T, STEP, 64, 64, VEC>(a, s);
+        case 64128: return launch_softmax_one<T, STEP, 64, 128, VEC>(a, s);
+        case 64256: return launch_softmax_one<T, STEP, 64, 256, VEC>(a, s);
+        case 128064: return launch_softmax_one<T, STEP, 128, 64, VEC>(a, s);
+        case 128128: return launch_softmax_one<T, STEP, 128, 128, VEC>(a, s);
+        case 128256: return launch_softmax_one<T, STEP, 128, 256, VEC>(a, s);
+        case 256064: return launch_softmax_one<T, STEP, 256, 64, VEC>(a, s);
+        case 256128: return launch_softmax_one<T, STEP, 256, 128, VEC>(a, s);
+        default: return launch_softmax_one<T, STEP, 256, 256, VEC>(a, s);
+    }
+}
 template <typename T, bool STEP>
 hipError_t launch_softmax(const SoftArgs& a, bool vec, hipStream_t s) {
-    const int k = a.dk <= 64 ? 64 : a.dk <= 128 ? 128 : 256, v = a.dv <= 64 ? 64 : a.dv <= 128 ? 128 : 256;
-    if (!vec) {
-        const int d = k > v ? k : v;
-        if (d == 64) return launch_softmax_one<T, STEP, 64, 64, false>(a, s);
-        if (d == 128) return launch_softmax_one<T, STEP, 128, 128, false>(a, s);
-        return launch_softmax_one<T, STEP, 256, 256, false>(a, s);
-    }
-    switch (1000 * k + v) {
-        case 64064: return launch_softmax_one<T, STEP, 64, 64, true>(a, s);
-        case 64128: return launch_softmax_one<T, STEP, 64, 128, true>(a, s);
-        case 64256: return launch_softmax_one<T, STEP, 64, 256, true>(a, s);
-        case 128064: return launch_softmax_one<T, STEP, 128, 64, true>(a, s);
-        case 128128: return launch_softmax_one<T, STEP, 128, 128, true>(a, s);
-        case 128256: return launch_softmax_one<T, STEP, 128, 256, true>(a, s);
-        case 256064: return launch_softmax_one<T, STEP, 256, 64, true>(a, s);
-        case 256128: return launch_softmax_one<T, STEP, 256, 128, true>(a, s);
-        default: return launch_softmax_one<T, STEP, 256, 256, true>(a, s);
-    }
+    return vec ? launch_softmax_dims<T, STEP, true>(a, s) : launch_softmax_dims<T, STEP, false>(a, s);
 }
 
 }  // namespace cv

@@ -269,6 +269,26 @@ DIVIDED = [
 ]
 
 
+# Rows that are no multiple of 16 bytes, of each pair of kernels' sizes: in one page a tile or several, packed, a few or many rows.
+ODD = [_case(new=new, keys=keys, heads=4, kv_heads=2, dk=dk, dv=dv, dtype=d, page=page, shift=shift)
+       for (dk, dv), (new, keys, page, shift) in zip(
+           ((33, 57), (33, 100), (35, 131), (99, 61), (127, 127), (101, 255), (131, 64), (203, 99), (231, 233), (9, 5), (64, 66), (82, 112)) * 3,
+           (([70, 9], [170, 300], 16, 0), ([1, 1, 1], [500, 1, 67], 64, 1), ([130], None, 0, 0), ([3, 1], [90, 700], 8, 0),
+            ([40, 90], [333, 90], 128, 1)) * 8)
+       for d in ("bf16", "f32")]
+
+
+@pytest.mark.parametrize("kw", ODD)
+def test_odd_rows(kw):
+    p = Soft(**kw)
+    if p.page:  # what lies behind the ends is never read
+        for i, (_, pages) in enumerate(p.where):
+            if p.keys[i] % p.page:
+                for t in (p.k, p.v):
+                    t[int(pages[-1]), p.keys[i] % p.page:] = float("nan")
+    p.run().check()
+
+
 @pytest.mark.parametrize("kw", DIVIDED)
 def test_divided(kw):
     p = Soft(**kw)
