@@ -266,26 +266,26 @@ __device__ __forceinline__ int64_t key_row(const SoftArgs& A, const SoftPlace& p
     return p * c.page + (key & ((1 << A.shift) - 1)) * c.row + pl.kv_head * c.head;
 }
 
-// 16 bytes of a row of `dim` elements from unit u (of 16 bytes) on, zeros past its end.  Not VEC (dim is no multiple of 16 bytes):
-// at any address of the element's alignment; the last part is read where it ends with the row, and moved down; rows below
-// 16 bytes are read by elements.
-template <typename T, bool VEC>
+// 16 bytes, moved down by `bits` (below 128), zeros behind them.
+__device__ __forceinline__ u32x4 moved_down(u32x4 v, uint32_t bits) {
+    if (bits & 64) v = u32x4{v[2], v[3], 0, 0};
+    if (bits & 32) v = u32x4{v[1], v[2], v[3], 0};
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)(((uint64_t)(i < 3 ? v[i + 1] : 0u) << 32 | v[i]) >> (bits & 31));
+    return w;
+}
+
+// 16 bytes of a row of `dim` elements from unit u (of 16 bytes) on, zeros past its end, at any address of the element's
+// alignment: the last part is read where it ends with the row, and moved down; rows below 16 bytes are read by elements.
+template <typename T>
 __device__ __forceinline__ u32x4 load_unit(const T* row, int u, int dim) {
     constexpr int E = 16 / sizeof(T);
     const int c = u * E;
     u32x4 v{0, 0, 0, 0};
-    if (VEC || dim >= E) {
-        const int over = VEC ? 0 : max(c + E - dim, 0);  // elements
-        if (c < dim) {
-            v = *reinterpret_cast<const u32x4_any*>(row + c - over);
-            if (!VEC && over) {
-                uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
-                const int bits = over * 8 * (int)sizeof(T);
-                if (bits >= 64) lo = hi >> (bits - 64), hi = 0;
-                else lo = lo >> bits | hi << (64 - bits), hi >>= bits;
-                v = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-            }
-        }
+    if (dim >= E) {
+        const int over = max(c + E - dim, 0);  // elements
+        if (c < dim) v = moved_down(*reinterpret_cast<const u32x4_any*>(row + c - over), over * 8 * sizeof(T));
     } else {
         T e[E];
 #pragma unroll
@@ -402,20 +402,32 @@ struct SoftRows {
     u32x4 q[KU / 2];
     f32x16 o[MT];
     float m, l;
-    // The row at `from`, nullptr: zeros.  All loads are under way before one is waited for.
+    // The row at `from`, nullptr: zeros.  All loads are under way before one is waited for, and only the unit that is a row's
+    // last is moved down (code that runs once costs most by its length).
     template <bool VEC>
     __device__ __forceinline__ void load_q(const SoftArgs& A, const T* from, int h) {
+        if (VEC || A.dk >= E) {
 #pragma unroll
-        for (int c = 0; c < KU / 2; ++c) {
-            const int u = 2 * c + h;
-            if constexpr (VEC) {
-                const bool there = from && u * E < A.dk;
-                const T* p = there ? from + u * E : static_cast<const T*>(A.q);
+            for (int c = 0; c < KU / 2; ++c) {
+                const int at = (2 * c + h) * E;
+                const bool there = from && at < A.dk;
+                const T* p = there ? from + (VEC ? at : min(at, A.dk - E)) : static_cast<const T*>(A.q);
                 const u32x4 v = *reinterpret_cast<const u32x4_any*>(p);
                 q[c] = there ? v : u32x4{0, 0, 0, 0};
-            } else {
-                q[c] = from ? load_unit<T, false>(from, u, A.dk) : u32x4{0, 0, 0, 0};
             }
+            const int past = A.dk % E;
+            if (!VEC && past) {
+                u32x4 v{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < KU / 2; ++c) v = 2 * c + h == A.dk / E ? q[c] : v;
+                v = moved_down(v, (E - past) * 8 * sizeof(T));
+#pragma unroll
+                for (int c = 0; c < KU / 2; ++c) q[c] = 2 * c + h == A.dk / E ? v : q[c];
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < KU / 2; ++c) q[c] = u32x4{0, 0, 0, 0};
+            if (from) q[0] = load_unit<T>(from, h, A.dk);
         }
         if (A.qsign != 1) turn_q(A.qsign);
     }
@@ -514,9 +526,9 @@ struct SoftRows {
         return read<float>(tile + ((at_v[i & 3]) ^ ((mt & 1) * 128)) + (mt >> 1) * 256 + (32 * (i / 16) + 8 * (i % 16 / 4) + i % 4) * (VU * 16));
     }
 
-    // Adds 32 NB keys with weights p (as scores() leaves them).
+    // Adds 32 NB keys, of which the first `left` count, with weights p (as scores() leaves them).
     template <int NB>
-    __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB]) {
+    __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB], int left) {
         if constexpr (sizeof(T) == 2) {
             constexpr int X = 2 * NB * MT, D = 2;
             const ValuePlaces at = places(tile);
@@ -538,7 +550,8 @@ struct SoftRows {
             for (int i = 0; i < 16 * NB; ++i)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
-                    o[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tile, i, mt), p[i / 16][i % 16], o[mt], 0, 0, 0);
+                    if (i < 4 || 8 * (i / 4) < left)  // (products take long: 8 keys at a time)
+                        o[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tile, i, mt), p[i / 16][i % 16], o[mt], 0, 0, 0);
         }
     }
 
@@ -573,7 +586,7 @@ struct SoftRows {
 
     // One tile of KT keys, of which lane i of s[b] is key key0 + 32 b + 8 (i / 4) + 4 h + i % 4.
     template <int KT>
-    __device__ __forceinline__ void step(uint32_t tile_k, uint32_t tile_v, int key0, bool masked, bool counting,
+    __device__ __forceinline__ void step(uint32_t tile_k, uint32_t tile_v, int key0, int left, bool masked, bool counting,
                                          const RowMask& mask, float scale2) {
         constexpr int NB = KT / 32;
         const int h = threadIdx.x >> 5 & 1;
@@ -612,7 +625,7 @@ struct SoftRows {
                 for (int i = 0; i < 16; ++i)
                     s[b][i] = sees(b, i) ? 1.0f : 0.0f;
         }
-        add(tile_v, s);
+        add(tile_v, s, left);
     }
 
     // After a pass that counted: which results see a value that is not finite.
@@ -929,7 +942,6 @@ struct DirectLoad {
     uint32_t off[KINDS];  // of this lane, in bytes
     uint32_t page_bytes, row_bytes, last;  // last: bytes of a row that count
     int wave;             // (0: each wave loads its own tiles)
-    uint32_t ends;        // bit i: off[i] is a row's last 16 bytes, of a row that is no multiple of them
 
     __device__ __forceinline__ DirectLoad(const SoftArgs& A, const SoftPlace& pl, const void* p, const CachePlace& c, int dim) {
         const int lane = threadIdx.x & 63, r = lane / UNITS, at = lane % UNITS;
@@ -937,14 +949,12 @@ struct DirectLoad {
         page_bytes = (uint32_t)c.page * sizeof(T);
         row_bytes = (uint32_t)c.row * sizeof(T);
         last = dim * sizeof(T);
-        ends = 0;
         wave = WAVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
 #pragma unroll
         for (int i = 0; i < KINDS; ++i) {
             const int row = first_row(i) + r;
             const int u = at ^ LDS::turn(row);
             off[i] = u * E < dim ? r * row_bytes + min(u * 16u, last - 16) : OOB_OFF;
-            ends |= (u * E < dim && u * 16u > last - 16 ? 1u : 0u) << i;
         }
     }
     // WAVES waves load a tile together, or each its own (1).
@@ -1002,22 +1012,17 @@ struct DirectLoad {
                 v[i] = load((uint64_t)get((uint32_t)(p >> 32), i) << 32 | get((uint32_t)p, i), get(bytes, i), off[i % KINDS]);
         }
     }
-    // ... and on to LDS, with the last part of a row, which was read where it ends with the row, moved down.
+    // ... and on to LDS, where the last part of a row, which was read where it ends with the row, is moved down.
     __device__ __forceinline__ void store(const u32x4 (&v)[N], u32x4* to) const {
-        const uint32_t cut = (16 - (last & 15)) * 8 & 127;
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            u32x4 w = v[i];
-            if (cut) {
-                u32x4 x = w;
-                if (cut & 64) x = u32x4{x[2], x[3], 0, 0};
-                if (cut & 32) x = u32x4{x[1], x[2], x[3], 0};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    x[c] = (uint32_t)(((uint64_t)(c < 3 ? x[c + 1] : 0u) << 32 | x[c]) >> (cut & 31));
-                w = ends >> (i % KINDS) & 1 ? x : w;
+        for (int i = 0; i < N; ++i) to[(i * WAVES + wave) * LDS::GROUP + lane] = v[i];
+        if (last & 15) {
+            static_assert(RI * N <= 64);
+            if (lane < RI * N) {
+                u32x4& end = to[LDS::at(first_row(lane / RI) + lane % RI, (int)(last / 16))];
+                end = moved_down(end, (16 - (last & 15)) * 8);
             }
-            to[(i * WAVES + wave) * LDS::GROUP + (threadIdx.x & 63)] = w;
         }
     }
     // The page of instruction `lane`'s rows of the tile from key0 on.
@@ -1036,7 +1041,7 @@ struct RegisterLoad {
         for (int i = 0; i < N; ++i) {
             const int x = x0 + i * THREADS, r = x / UNITS, u = x % UNITS;
             const int64_t from = key_row(A, pl, c, min(key0 + r, pl.keys - 1));
-            v[i] = load_unit<T, false>(static_cast<const T*>(p) + from, u, dim);
+            v[i] = load_unit<T>(static_cast<const T*>(p) + from, u, dim);
         }
     }
     __device__ __forceinline__ void store(u32x4* to, int x0) const {
@@ -1097,7 +1102,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
                 __syncthreads();
             }
             if (key0 < wave_end)
-                rows.template step<KT>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, key0 + KT > wave_full,
+                rows.template step<KT>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, end - key0, key0 + KT > wave_full,
                                        mode == COUNT, mask, A.scale2);
         };
         rows.clear();
@@ -1392,7 +1397,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
                 clean_tile<T>(mine + KEYS, KT * VU, tid & 63, 64, mode);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            rows.template step<KT>(to, to + KEYS * 16, key0, key0 + KT > full, mode == COUNT, mask, A.scale2);
+            rows.template step<KT>(to, to + KEYS * 16, key0, end - key0, key0 + KT > full, mode == COUNT, mask, A.scale2);
         };
         rows.clear();
         if constexpr (VEC) {
