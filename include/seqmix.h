@@ -33,8 +33,9 @@
  *     *_in == *_out updates the pool in place; otherwise the two must not overlap.  An empty sequence
  *     carries its entry over unchanged.  Outputs must not overlap any other argument unless said.
  *   - Strides count elements.  Rows may lie apart (columns of a wider tensor); the last dimension is dense.
- *   - Any alignment of an element's size is accepted, at the same speed but for rows below 16 bytes.  Results are
- *     bitwise reproducible for the same descriptor parameters.
+ *   - Any alignment of an element's size is accepted, at the same speed but for rows below 16 bytes (softmax attention: up
+ *     to twice the time where k and v are not in whole 16 bytes).  Results are bitwise reproducible for the same
+ *     descriptor parameters.
  *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.  (Attention in bf16
  *     multiplies what it has computed in fp32, scores and states, as sums of bf16 parts: 2^-16 of each term is
  *     left out where outputs are bf16, 2^-24 where they are fp32.  seqmix_softmax says for itself.)

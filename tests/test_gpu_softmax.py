@@ -339,6 +339,59 @@ def test_far_pages():
     p.run().check()
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("stride", ((1 << 18) + 8, (1 << 22) + 1))
+def test_far_rows(stride, dtype):
+    """Packed keys and values whose rows lie further apart than 32-bit offsets of a tile reach."""
+    p = Soft([5, 40], keys=[20, 70], heads=2, kv_heads=1, dk=64, dv=64, dtype=dtype)
+    for name in ("k", "v"):
+        old = getattr(p, name)
+        flat = torch.empty(89 * stride + 64, dtype=old.dtype, device="cuda")
+        new = flat.as_strided((90, 1, 64), (stride, 64, 1))
+        setattr(p, name, new.copy_(old))
+    p.op = M.SoftmaxAttention(tokens=45, seqs=2, heads=2, kv_heads=1, dk=64, dv=64, dtype=dtype, scale=p.scale, key_tokens=90,
+                              q_strides=p.q.stride()[:2], o_strides=p.o.stride()[:2], k_strides=(stride, 64), v_strides=(stride, 64))
+    p.run().check()
+
+
+@pytest.mark.parametrize("kw", [dict(new=[1] * 1100, page=16, heads=2, kv_heads=1), dict(new=[40] + [2] * 1030 + [0, 90], heads=1, kv_heads=1),
+                                dict(new=[3] * 1050, page=8, heads=2, kv_heads=2, mask="tree", dtype="f32")])
+def test_many_sequences(kw):
+    """More sequences than a wave looks over for shares."""
+    more = kw.get("page") and dict(keys=[n + (i * 37) % 90 for i, n in enumerate(kw["new"])])
+    p = Soft(dk=64, dv=64, **kw, **(more or {}))
+    assert p.op.plan().shares == 0
+    p.run().check()
+
+
+def test_two_graphs_of_one_descriptor():
+    """Graphs that share a workspace, replayed one after the other with an eager call between them."""
+    p = Soft([1] * 2, keys=[9000, 3000], heads=8, kv_heads=2, dk=128, dv=128, page=16)
+    p.op.reserve()
+    p.run()
+    outs, graphs = [torch.empty_like(p.o) for _ in range(2)], []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for o in outs:
+        p.o = o
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+            p.run()
+        graphs.append(g)
+    p.o = torch.empty_like(outs[0])
+    for seed in range(3):
+        p.q.copy_(torch.randn(p.q.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(seed)))
+        for o in outs:
+            o.zero_()
+        graphs[0].replay()
+        p.run()
+        graphs[1].replay()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], p.o) and torch.equal(outs[1], p.o)
+    p.check()
+
+
 @pytest.mark.parametrize("kw", [dict(new=[7, 300, 0, 20]), dict(new=[1, 1, 1], keys=[700, 20, 3000], page=16),
                                 dict(new=[9, 9], keys=[2000, 9], mask="tree", page=16)])
 def test_bad_lengths_and_pages_stay_inside(kw):
