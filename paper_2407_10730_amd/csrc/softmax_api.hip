@@ -213,8 +213,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
         a.whole = division_of(step, p.dtype).whole;
         a.most = (int32_t)((1LL << 31) / a.blocks - 1);
         a.ws = d->ws.data;
-        a.marks = static_cast<char*>(d->ws.data) +
-                                               2 * d->plan.shares * part_bytes(p, step, (int64_t)a.tile * a.pack);
+        a.marks = static_cast<char*>(d->ws.data) + 2 * d->plan.shares * part_bytes(p, step, (int64_t)a.tile * a.pack);
     }
     auto launch = p.dtype == CONV2D_BF16 ? (step ? launch_softmax_step_bf16 : launch_softmax_prompt_bf16)
                                          : (step ? launch_softmax_step_f32 : launch_softmax_prompt_f32);

@@ -14,7 +14,7 @@
 namespace cv {
 
 // The arguments of the running kernel, its only parameter, to be read where they are used: held from the start on they fill the
-// scalar registers and are kept in lanes of vector registers, which cost a thousand instructions (16 requests of 24
+// scalar registers and are kept in lanes of vector registers, which cost two thousand instructions (16 requests of 24
 // drafts over up to 5000 keys 58 -> 54 us).
 __device__ __forceinline__ const SoftArgs& args_here() {
     auto p = (const __attribute__((address_space(4))) SoftArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -523,7 +523,8 @@ struct SoftRows {
     }
     __device__ __forceinline__ float value(uint32_t tile, int i, int mt) const {
         // (column 32 mt is 8 mt units on, of which the row's number may turn bit 3)
-        return read<float>(tile + ((at_v[i & 3]) ^ ((mt & 1) * 128)) + (mt >> 1) * 256 + (32 * (i / 16) + 8 * (i % 16 / 4) + i % 4) * (VU * 16));
+        const uint32_t row = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
+        return read<float>(tile + ((at_v[i & 3]) ^ ((mt & 1) * 128)) + (mt >> 1) * 256 + row * (VU * 16));
     }
 
     // Adds 32 NB keys, of which the first `left` count, with weights p (as scores() leaves them).
@@ -1200,7 +1201,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
                     load_v.tile(A, pl, pl.first + j * KT, clamp_page(A, look(load_v, j)), at_v + (j & 1) * (KT * VU * 16));
                 };
                 if (pl.first < end) load(0);
-                                for (int j = 0, key0 = pl.first; key0 < end; ++j, key0 += KT) {
+                for (int j = 0, key0 = pl.first; key0 < end; ++j, key0 += KT) {
                     loads_done();
                     __syncthreads();  // this tile is there, and the one before has been used
                     if (key0 + KT < end) load(j + 1);
