@@ -466,10 +466,10 @@ struct SoftRows {
         return *(const __attribute__((address_space(3))) V*)(uintptr_t)at;
     }
 
-    // Scores of 32 NB keys.
-    template <int NB>
-    __device__ __forceinline__ void scores(uint32_t tile, f32x16 (&s)[NB]) const {
-        constexpr int C = KU / 2, X = NB * C, D = 4;  // operands are read D products ahead
+    // Scores of 32 NB keys, over the first 2 C units of a row.
+    template <int C, int NB>
+    __device__ __forceinline__ void scores_over(uint32_t tile, f32x16 (&s)[NB]) const {
+        constexpr int X = NB * C, D = 4;  // operands are read D products ahead
         uint32_t at[2] = {tile + at_k[0], tile + at_k[1]};
         asm volatile("" : "+v"(at[0]), "+v"(at[1]));  // (or each address is computed anew, where a constant offset does)
         auto operand = [&](int x) {
@@ -494,6 +494,13 @@ struct SoftRows {
             __builtin_amdgcn_sched_group_barrier(kMfma, PER, 0);
             if (x + D < X) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
+    }
+    // fp32 products take long: a last quarter that is only padding is left out, of k here and of v below, where rows are few (32
+    // single tokens of 80 over up to 8000 keys 161 -> 140 us; the prompt kernel has no registers for two ways: 82 -> 106).
+    template <int NB>
+    __device__ __forceinline__ void scores(uint32_t tile, f32x16 (&s)[NB], int dk) const {
+        if (sizeof(T) == 4 && dk <= 3 * DKP / 4) scores_over<3 * KU / 8>(tile, s);
+        else scores_over<KU / 2>(tile, s);
     }
 
     // v as an operand: of bf16 the 16 keys from `row` on, columns 32 mt ..; of fp32 the keys that weight i of p belongs to.
@@ -529,7 +536,7 @@ struct SoftRows {
 
     // Adds 32 NB keys, of which the first `left` count, with weights p (as scores() leaves them).
     template <int NB>
-    __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB], int left) {
+    __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB], int left, int dv) {
         if constexpr (sizeof(T) == 2) {
             constexpr int X = 2 * NB * MT, D = 2;
             const ValuePlaces at = places(tile);
@@ -547,11 +554,18 @@ struct SoftRows {
                 if (x + D < X) v[x % D] = values(at, 16 * ((x + D) / MT), (x + D) % MT);
             }
         } else {
+            if (MT % 4 == 0 && dv <= 24 * MT) add_over<MT % 4 == 0 ? 3 * MT / 4 : MT>(tile, p, left);
+            else add_over<MT>(tile, p, left);
+        }
+    }
+    template <int LIVE, int NB>
+    __device__ __forceinline__ void add_over(uint32_t tile, const f32x16 (&p)[NB], int left) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < 16 * NB; ++i)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    if (i < 4 || 8 * (i / 4) < left)  // (products take long: 8 keys at a time)
+                for (int mt = 0; mt < LIVE; ++mt)
+                    if (i < 4 || 8 * (i / 4) < left)  // (8 keys at a time)
                         o[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tile, i, mt), p[i / 16][i % 16], o[mt], 0, 0, 0);
         }
     }
@@ -588,11 +602,11 @@ struct SoftRows {
     // One tile of KT keys, of which lane i of s[b] is key key0 + 32 b + 8 (i / 4) + 4 h + i % 4.
     template <int KT>
     __device__ __forceinline__ void step(uint32_t tile_k, uint32_t tile_v, int key0, int left, bool masked, bool counting,
-                                         const RowMask& mask, float scale2) {
+                                         const RowMask& mask, float scale2, int dk, int dv) {
         constexpr int NB = KT / 32;
         const int h = threadIdx.x >> 5 & 1;
         f32x16 s[NB];
-        scores(tile_k, s);
+        scores(tile_k, s, dk);
         uint64_t seen = ~0ull;
         auto sees = [&](int b, int i) { return (uint32_t)(seen >> (32 * b)) >> (8 * (i / 4) + i % 4) & 1; };
         if (masked) {
@@ -626,7 +640,7 @@ struct SoftRows {
                 for (int i = 0; i < 16; ++i)
                     s[b][i] = sees(b, i) ? 1.0f : 0.0f;
         }
-        add(tile_v, s, left);
+        add(tile_v, s, left, dv);
     }
 
     // After a pass that counted: which results see a value that is not finite.
@@ -713,7 +727,7 @@ struct SoftRows {
     }
     __device__ __forceinline__ void first_scores(uint32_t tile_k, f32x16& s) const {
         f32x16 x[1];
-        scores(tile_k, x);
+        scores(tile_k, x, DKP);
         s = x[0];
     }
     __device__ __forceinline__ void last_product(uint32_t tile_v, const u32x4 (&w)[2]) {
@@ -1104,7 +1118,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
             }
             if (key0 < wave_end)
                 rows.template step<KT>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, end - key0, key0 + KT > wave_full,
-                                       mode == COUNT, mask, A.scale2);
+                                       mode == COUNT, mask, A.scale2, DKP, DVP);
         };
         rows.clear();
         if constexpr (VEC) {
@@ -1398,7 +1412,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
                 clean_tile<T>(mine + KEYS, KT * VU, tid & 63, 64, mode);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            rows.template step<KT>(to, to + KEYS * 16, key0, end - key0, key0 + KT > full, mode == COUNT, mask, A.scale2);
+            rows.template step<KT>(to, to + KEYS * 16, key0, end - key0, key0 + KT > full, mode == COUNT, mask, A.scale2, A.dk, A.dv);
         };
         rows.clear();
         if constexpr (VEC) {

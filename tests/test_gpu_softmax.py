@@ -278,6 +278,11 @@ ODD = [_case(new=new, keys=keys, heads=4, kv_heads=2, dk=dk, dv=dv, dtype=d, pag
        for d in ("bf16", "f32")]
 
 
+# Dims around three quarters of the kernels' sizes, few rows, keys that end inside 8.
+ODD += [_case(new=[1, 3], keys=[301, 41], heads=4, kv_heads=2, dk=dk, dv=dv, dtype="f32", page=16, shift=0)
+        for dk, dv in ((48, 48), (80, 80), (96, 96), (97, 97), (96, 128), (128, 96), (192, 192), (193, 192), (192, 193), (256, 100))]
+
+
 @pytest.mark.parametrize("kw", ODD)
 def test_odd_rows(kw):
     p = Soft(**kw)
