@@ -588,11 +588,13 @@ struct SoftRows {
         for (int i = 0; i < PLANES; ++i) part[i] = __builtin_bit_cast(bf16x8, w[i]);
     }
 
-    __device__ __forceinline__ void rescale(float mx) {
+    // (o of a pass that counts holds numbers of values, which no maximum makes fewer.)
+    __device__ __forceinline__ void rescale(float mx, bool counting) {
         const float now = fmaxf(m, mx);
         const float fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= fade;
+        if (counting) return;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -623,7 +625,7 @@ struct SoftRows {
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
         mx = max_of_halves(mx) * scale2;
         // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
-        if (__any(mx > m + kSlack)) rescale(mx);
+        if (__any(mx > m + kSlack)) rescale(mx, counting);
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -676,7 +678,7 @@ struct SoftRows {
     static __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
     __device__ __forceinline__ void lead(const ValuePlaces& at, u32x4 (&v)[AHEAD], const u32x4 (&w)[2], f32x16& s, bool masked,
-                                         uint32_t seen, float scale2, const KeyPlaces& then, u32x4 (&k)[AHEAD]) {
+                                         bool counting, uint32_t seen, float scale2, const KeyPlaces& then, u32x4 (&k)[AHEAD]) {
         if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = seen >> (8 * (i / 4) + i % 4) & 1 ? s[i] : -INFINITY;
@@ -697,7 +699,7 @@ struct SoftRows {
         }
         __builtin_amdgcn_s_setprio(0);
         mx = max_of_halves(mx) * scale2;
-        if (__any(mx > m + kSlack)) rescale(mx);
+        if (__any(mx > m + kSlack)) rescale(mx, counting);
     }
     template <bool MORE>  // the next step's first values can be read
     __device__ __forceinline__ void follow(const KeyPlaces& at, u32x4 (&k)[AHEAD], const f32x16& s, float scale2, f32x16& next,
@@ -1186,7 +1188,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
                             const uint32_t seen = masked || mode == COUNT ? seen_of(key0 + 32 * b) : 0;
                             // (at last some scores that are not used)
                             const auto kp = b + 1 < NB ? keys_at(j, b + 1) : keys_at(j + 1, 0);
-                            rows.lead(vp, first_v, w, s[b & 1], masked, seen, A.scale2, kp, first_k);
+                            rows.lead(vp, first_v, w, s[b & 1], masked, mode == COUNT, seen, A.scale2, kp, first_k);
                             if (b == 0) {
                                 rows.template follow<false>(kp, first_k, s[0], A.scale2, s[1], w, vp, first_v);
                             } else {
