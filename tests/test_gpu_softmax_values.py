@@ -1,7 +1,7 @@
 """Softmax attention over values that are infinite or NaN, where the rows' maxima move far (needs the GPU)."""
-
 import numpy as np
 import pytest
+import torch
 
 from oracle import seqmix as ref
 from paper_2407_10730_amd import seqmix as M
