@@ -922,13 +922,12 @@ __device__ __forceinline__ void clean_tile(u32x4* v, int units, int from, int st
 }
 
 // A wave's 64 units of 16 bytes go from memory to LDS, from byte `to` + MORE on, without passing registers.  The compiler does not count
-// these loads: loads_done() waits for them.
-// WAIT: wait states; five where a part of r comes straight from a lane.
-template <int WAIT, int MORE>
+// these loads: loads_done() waits for them.  Nor does it see that they read r and m0: a vector instruction that writes a part
+// of r (a lane's value read, also by the compiler where it kept r in lanes) has to be 5 wait states before, a scalar one that writes m0 1.
+template <int MORE>
 __device__ __forceinline__ void load_to_lds(u32x4 r, uint32_t off, uint32_t to) {
-    asm volatile("s_add_i32 m0, %0, %4\n\ts_nop %3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r), "n"(WAIT - 1),
-                 "n"(MORE)
-                 : "memory", "scc");
+    asm volatile("s_add_i32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r), "n"(MORE)
+                 : "memory", "scc", "m0");
 }
 template <int N, typename F>
 __device__ __forceinline__ void each_of(F f) {  // f(0) .. f(N - 1), as constants
@@ -939,7 +938,7 @@ __device__ __forceinline__ void each_of(F f) {  // f(0) .. f(N - 1), as constant
 }
 // ... 64 elements of 4 bytes.
 __device__ __forceinline__ void load_words_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r) : "memory", "m0");
 }
 typedef __attribute__((address_space(3))) const void* lds_address;
 template <int LEFT = 0>  // all but the last LEFT
@@ -989,7 +988,7 @@ struct DirectLoad {
             const uint32_t rows = left < KT ? left : KT, each = WAVES * RI * row_bytes;
             const uint32_t bytes = left > 0 ? (rows - 1) * row_bytes + last : 0u;
             const u32x4 r{(uint32_t)p, (uint32_t)(p >> 32), bytes, RSRC_WORD3};
-            each_of<N>([&](auto i) { load_to_lds<1, i * WAVES * LINE>(r, off[i % KINDS] + i * each, to); });
+            each_of<N>([&](auto i) { load_to_lds<i * WAVES * LINE>(r, off[i % KINDS] + i * each, to); });
         } else {
             const int key = key0 + first_row(threadIdx.x & 63);
             const uint64_t p = base + (uint64_t)(uint32_t)page * page_bytes +
@@ -997,7 +996,7 @@ struct DirectLoad {
             const int rows = min(max(pl.keys - key, 0), RI);
             const uint32_t bytes = rows ? (rows - 1) * row_bytes + last : 0u;
             each_of<N>([&](auto i) {
-                load_to_lds<5, i * WAVES * LINE>(u32x4{get((uint32_t)p, i), get((uint32_t)(p >> 32), i), get(bytes, i), RSRC_WORD3},
+                load_to_lds<i * WAVES * LINE>(u32x4{get((uint32_t)p, i), get((uint32_t)(p >> 32), i), get(bytes, i), RSRC_WORD3},
                                                  off[i % KINDS], to);
             });
         }
