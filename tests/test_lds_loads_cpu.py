@@ -16,7 +16,7 @@ from paper_2407_10730_amd import build
 
 OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 VECTOR_STATES, M0_STATES = 5, 1
-KERNELS = ("softmax_prompt_kernel", "softmax_step_kernel")
+KERNELS = {"softmax_prompt_kernel": 500, "softmax_step_kernel": 1000, "slice_conv_kernel": 50}  # loads that there are at least
 
 _LOAD = re.compile(r"buffer_load_\w+ (.*) lds$")
 # (of these the second operand is written too)
@@ -103,7 +103,7 @@ def test_loads_wait_for_what_they_read(functions, kernel):
         if kernel in name:
             loads += sum(bool(_LOAD.match(x)) for x in lines)
             assert not list(hazards(lines)), name
-    assert loads > 100
+    assert loads >= KERNELS[kernel]
 
 
 @pytest.mark.parametrize("before,bad", [
