@@ -753,14 +753,15 @@ struct SoftRows {
         for (int c = 0; c < KU / 2; ++c) q[c] = SoftMath<T>::sign(q[c], sign);
     }
 
-    // Whether a value that is not finite came up (in any lane): what rows that do not see it hold has to be computed again.
-    __device__ __forceinline__ bool spoilt() const {
+    // Whether a value that is not finite came up (in any lane that has a row): what rows that do not see it hold has to be
+    // computed again.  Lanes without one multiply zeros with every key, so an infinite one alone would spoil them.
+    __device__ __forceinline__ bool spoilt(bool live) const {
         float bad[4] = {l * 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) bad[i & 3] = __builtin_fmaf(o[mt][i], 0.0f, bad[i & 3]);
-        return __any(!((bad[0] + bad[1]) + (bad[2] + bad[3]) == 0.0f));
+        return __any(live && !((bad[0] + bad[1]) + (bad[2] + bad[3]) == 0.0f));
     }
 };
 
@@ -1280,7 +1281,7 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
             __shared__ int s_again;
             if (tid == 0) s_again = 0;
             __syncthreads();
-            if (rows.spoilt()) s_again = 1;
+            if (rows.spoilt(live)) s_again = 1;
             __syncthreads();
             if (!s_again) break;
         }
@@ -1472,7 +1473,7 @@ __device__ __forceinline__ void step_part(const SoftArgs& A, const SoftPlace& pl
             rows.mark();
             break;
         }
-        if (mode == PLAIN && !rows.spoilt()) break;
+        if (mode == PLAIN && !rows.spoilt(live)) break;
     }
 
     // the waves' results, in their order

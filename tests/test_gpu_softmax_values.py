@@ -57,3 +57,30 @@ def test_values_before_far_higher_scores(kernel, new, keys, heads, kv_heads, dk,
     assert np.array_equal(np.isnan(got), want) and np.isfinite(got[fine]).all()
     bound = ref.softmax_bound(o, o_abs, most, keys, dk, dtype, p.parts())
     assert (np.abs(got - o)[fine] <= bound[fine]).all()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("new,heads,kv_heads,keys", [([70] * 2, 4, 4, 6000), ([1] * 16, 8, 8, 3000)])
+def test_places_without_a_row_cost_nothing(new, heads, kv_heads, keys, dtype):
+    """Keys of -infinity that every row gives a weight of zero: no pass over the keys is done again for the places of a tile
+    that no row has (their scores are not numbers)."""
+    p = Soft(new, keys=[keys] * len(new), heads=heads, kv_heads=kv_heads, dk=128, dv=128, dtype=dtype)
+    p.q[..., 0] = 1
+
+    def timed(value):
+        p.k[5::100, :, 0] = value
+        best = []
+        for _ in range(6):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(20):
+                p.run()
+            b.record()
+            b.synchronize()
+            best.append(a.elapsed_time(b))
+        return min(best), p.o.clone()
+
+    (t0, o0), (t1, o1) = timed(-1e30), timed(float("-inf"))
+    assert torch.isfinite(o0).all() and torch.equal(o0, o1)
+    print(f"  {t0 / 20 * 1e3:.1f} us, {t1 / 20 * 1e3:.1f} us", flush=True)
+    assert t1 < 1.5 * t0  # (three passes are done where one does not do)
