@@ -392,7 +392,7 @@ __device__ __forceinline__ RowMask row_mask(const SoftArgs& A, const SoftPlace& 
 }
 
 constexpr int kMfma = 0x8, kDsRead = 0x100, kValu = 0x2, kTrans = 0x400;  // kinds of instructions, for sched_group_barrier
-constexpr int PLANES = 2;  // bf16 parts of a weight, where rows are few
+constexpr int PLANES = 2;  // bf16 parts of a weight, where rows are few (of prompts one)
 constexpr float kSlack = 8.0f;  // weights are below 2^8 then
 
 // The state of 32 rows of a wave.
@@ -534,14 +534,14 @@ struct SoftRows {
         return read<float>(tile + ((at_v[i & 3]) ^ ((mt & 1) * 128)) + (mt >> 1) * 256 + row * (VU * 16));
     }
 
-    // Adds 32 NB keys, of which the first `left` count, with weights p (as scores() leaves them).
-    template <int NB>
+    // Adds 32 NB keys, of which the first `left` count, with weights p (as scores() leaves them) in P parts.
+    template <int P, int NB>
     __device__ __forceinline__ void add(uint32_t tile, const f32x16 (&p)[NB], int left, int dv) {
         if constexpr (sizeof(T) == 2) {
-            constexpr int X = 2 * NB * MT, D = 2;
+            constexpr int X = 2 * NB * MT, D = P > 1 ? 2 : 4;  // operands are read D ahead
             const ValuePlaces at = places(tile);
             u32x4 v[D];
-            bf16x8 part[PLANES];
+            bf16x8 part[P];
 #pragma unroll
             for (int x = 0; x < D; ++x) v[x] = values(at, 16 * (x / MT), x % MT);
 #pragma unroll
@@ -549,7 +549,7 @@ struct SoftRows {
                 const int c = x / MT, mt = x % MT;
                 if (mt == 0) planes(p[c / 2], 8 * (c % 2), part);
 #pragma unroll
-                for (int i = 0; i < PLANES; ++i)
+                for (int i = 0; i < P; ++i)
                     o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[x % D]), part[i], o[mt], 0, 0, 0);
                 if (x + D < X) v[x % D] = values(at, 16 * ((x + D) / MT), (x + D) % MT);
             }
@@ -571,13 +571,14 @@ struct SoftRows {
     }
 
     // 8 weights, from number `first` of p on, as bf16 parts, each the rounding of what the ones before left.
-    static __device__ __forceinline__ void planes(const f32x16& p, int first, bf16x8 (&part)[PLANES]) {
-        u32x4 w[PLANES];
+    template <int P>
+    static __device__ __forceinline__ void planes(const f32x16& p, int first, bf16x8 (&part)[P]) {
+        u32x4 w[P];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a = p[first + 2 * j], b = p[first + 2 * j + 1];
 #pragma unroll
-            for (int i = 0; i < PLANES; ++i) {
+            for (int i = 0; i < P; ++i) {
                 const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
                 w[i][j] = both;
                 a -= __builtin_bit_cast(float, both << 16);
@@ -585,7 +586,7 @@ struct SoftRows {
             }
         }
 #pragma unroll
-        for (int i = 0; i < PLANES; ++i) part[i] = __builtin_bit_cast(bf16x8, w[i]);
+        for (int i = 0; i < P; ++i) part[i] = __builtin_bit_cast(bf16x8, w[i]);
     }
 
     // (o of a pass that counts holds numbers of values, which no maximum makes fewer.)
@@ -601,11 +602,13 @@ struct SoftRows {
             for (int i = 0; i < 16; ++i) o[mt][i] *= fade;
     }
 
-    // One tile of KT keys, of which lane i of s[b] is key key0 + 32 b + 8 (i / 4) + 4 h + i % 4.
-    template <int KT>
+    // One tile of KT keys, of which lane i of s[b] is key key0 + 32 b + 8 (i / 4) + 4 h + i % 4, with weights in P parts.  One part (prompts
+    // in bf16) goes by blocks of 32 keys, each with a maximum of its own and sums in follow()'s order, so that a row has the same
+    // numbers here and in the two steps below.
+    template <int KT, int P = PLANES>
     __device__ __forceinline__ void step(uint32_t tile_k, uint32_t tile_v, int key0, int left, bool masked, bool counting,
                                          const RowMask& mask, float scale2, int dk, int dv) {
-        constexpr int NB = KT / 32;
+        constexpr int NB = KT / 32, G = P > 1 ? NB : 1;
         const int h = threadIdx.x >> 5 & 1;
         f32x16 s[NB];
         scores(tile_k, s, dk);
@@ -618,31 +621,35 @@ struct SoftRows {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] = sees(b, i) ? s[b][i] : -INFINITY;
         }
-        float mx = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int g = 0; g < NB; g += G) {
+            float mx = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-        mx = max_of_halves(mx) * scale2;
-        // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
-        if (__any(mx > m + kSlack)) rescale(mx, counting);
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int b = g; b < g + G; ++b)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+            mx = max_of_halves(mx) * scale2;
+            // sums are relative to a maximum that may be up to kSlack behind: most tiles leave them as they are
+            if (__any(mx > m + kSlack)) rescale(mx, counting);
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            f32x16 w[G];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale2, -m));
-                sum[i & 3] += s[b][i];
+            for (int b = 0; b < G; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    w[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g + b][i], scale2, -m));
+                    if constexpr (P > 1) sum[i & 3] += w[b][i];
+                    else if (i & 1) sum[i / 2 & 1] += w[b][i - 1] + w[b][i];
+                }
+            l += P > 1 ? (sum[0] + sum[1]) + (sum[2] + sum[3]) : sum[0] + sum[1];
+            if (counting) {
+#pragma unroll
+                for (int b = 0; b < G; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[b][i] = sees(g + b, i) ? 1.0f : 0.0f;
             }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (counting) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[b][i] = sees(b, i) ? 1.0f : 0.0f;
+            add<P>(tile_v + g * (32 * VU * 16), w, left - 32 * g, dv);
         }
-        add(tile_v, s, left, dv);
     }
 
     // After a pass that counted: which results see a value that is not finite.
@@ -1119,8 +1126,8 @@ __device__ __forceinline__ void prompt_part(const SoftArgs& A, const SoftPlace& 
                 __syncthreads();
             }
             if (key0 < wave_end)
-                rows.template step<KT>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, end - key0, key0 + KT > wave_full,
-                                       mode == COUNT, mask, A.scale2, DKP, DVP);
+                rows.template step<KT, sizeof(T) == 2 ? 1 : PLANES>(at_k + b * (KEYS * 16), at_v + b * (KT * VU * 16), key0, end - key0,
+                                                                    key0 + KT > wave_full, mode == COUNT, mask, A.scale2, DKP, DVP);
         };
         rows.clear();
         if constexpr (VEC) {

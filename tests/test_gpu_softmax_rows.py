@@ -1,5 +1,6 @@
 """Softmax attention of few rows over keys of every kernel's head sizes, as they lie in memory (needs the GPU)."""
 import pytest
+import torch
 
 from paper_2407_10730_amd import seqmix as M
 from test_gpu_softmax import Soft, _gpu  # noqa: F401
@@ -32,3 +33,41 @@ def test_few_rows_of_every_head_size(dk, dv, dtype, page):
         assert not page or (p.k.data_ptr() | p.v.data_ptr()) % 16 == 0
         _behind(p, float("nan"))
         p.run().check()
+
+
+def _moved(t, by):
+    """A copy of t with its strides, `by` elements further on from an address of 16 bytes."""
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    flat = torch.zeros(last + 1 + by + 16, dtype=t.dtype, device=t.device)
+    assert flat.data_ptr() % 16 == 0
+    return flat.as_strided(t.shape, t.stride(), by).copy_(t)
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("kw", [
+    dict(new=[300]), dict(new=[1000, 90, 0, 3], heads=16, kv_heads=4), dict(new=[300, 7], keys=[2000, 900], page=16),
+    dict(new=[130, 40], keys=[5000, 77], page=64, dk=128, dv=128), dict(new=[70, 150], keys=[333, 4000], mask="full", dk=256, dv=64),
+    dict(new=[200], keys=[1300], dk=256, dv=256), dict(new=[24] * 3, keys=[3000, 24, 1900], mask="tree", heads=8, page=32),
+    dict(new=[1] * 3, keys=[5000, 70, 900], page=16, heads=8), dict(new=[3, 1], keys=[90, 700], dk=96, dv=72),
+    dict(new=[90], dk=72, dv=104, qscale=20.0), dict(new=[40] * 600, heads=2, kv_heads=1),
+])
+def test_results_do_not_depend_on_addresses(kw, dtype):
+    """The same descriptor and numbers at addresses of 16 bytes and of one element give the same bits, also where values are not
+    finite."""
+    p = Soft(**dict(dict(heads=4, kv_heads=2, dk=64, dv=64, dtype=dtype), **kw))
+    for bad in (False, True):
+        if bad:
+            p.v.view(-1, *p.v.shape[-2:])[9, 0, 5] = float("inf")
+            p.k.view(-1, *p.k.shape[-2:])[20, -1, 3] = float("-inf")
+        at = {n: getattr(p, n) for n in ("q", "k", "v")}
+        outs = []
+        for by in (0, 1, 3):
+            for n, t in at.items():
+                setattr(p, n, _moved(t, by))
+            p.o = _moved(torch.full_like(at["q"][..., :1], 7).expand(p.o.shape).contiguous(), by)
+            outs.append(p.run().o.clone())
+        for n, t in at.items():
+            setattr(p, n, t)
+        for o in outs[1:]:
+            same = (o == outs[0]) | (torch.isnan(o) & torch.isnan(outs[0]))
+            assert same.all(), f"{int((~same).sum())} of {same.numel()} results differ"
