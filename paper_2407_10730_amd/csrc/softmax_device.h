@@ -930,11 +930,14 @@ __device__ __forceinline__ void clean_tile(u32x4* v, int units, int from, int st
 }
 
 // A wave's 64 units of 16 bytes go from memory to LDS, from byte `to` + MORE on, without passing registers.  The compiler does not count
-// these loads: loads_done() waits for them.  Nor does it see that they read r and m0: a vector instruction that writes a part
-// of r (a lane's value read, also by the compiler where it kept r in lanes) has to be 5 wait states before, a scalar one that writes m0 1.
-template <int MORE>
+// these loads: loads_done() waits for them.  Nor does it see that they read r and m0: a scalar instruction that writes m0 has to
+// be 1 wait state before, a vector one that writes a part of r (a lane's value read, also by the compiler where it kept r in lanes) 5.
+// FIRST: of those with this r.  The others follow the first at once, and a test holds the built code to it (waiting 5 states at each
+// takes 2 % of prompts' time).
+template <bool FIRST, int MORE>
 __device__ __forceinline__ void load_to_lds(u32x4 r, uint32_t off, uint32_t to) {
-    asm volatile("s_add_i32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r), "n"(MORE)
+    asm volatile("s_add_i32 m0, %0, %3\n\ts_nop %4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r), "n"(MORE),
+                 "n"(FIRST ? 3 : 0)
                  : "memory", "scc", "m0");
 }
 template <int N, typename F>
@@ -996,7 +999,7 @@ struct DirectLoad {
             const uint32_t rows = left < KT ? left : KT, each = WAVES * RI * row_bytes;
             const uint32_t bytes = left > 0 ? (rows - 1) * row_bytes + last : 0u;
             const u32x4 r{(uint32_t)p, (uint32_t)(p >> 32), bytes, RSRC_WORD3};
-            each_of<N>([&](auto i) { load_to_lds<i * WAVES * LINE>(r, off[i % KINDS] + i * each, to); });
+            each_of<N>([&](auto i) { load_to_lds<i == 0, i * WAVES * LINE>(r, off[i % KINDS] + i * each, to); });
         } else {
             const int key = key0 + first_row(threadIdx.x & 63);
             const uint64_t p = base + (uint64_t)(uint32_t)page * page_bytes +
@@ -1004,8 +1007,8 @@ struct DirectLoad {
             const int rows = min(max(pl.keys - key, 0), RI);
             const uint32_t bytes = rows ? (rows - 1) * row_bytes + last : 0u;
             each_of<N>([&](auto i) {
-                load_to_lds<i * WAVES * LINE>(u32x4{get((uint32_t)p, i), get((uint32_t)(p >> 32), i), get(bytes, i), RSRC_WORD3},
-                                                 off[i % KINDS], to);
+                load_to_lds<true, i * WAVES * LINE>(u32x4{get((uint32_t)p, i), get((uint32_t)(p >> 32), i), get(bytes, i), RSRC_WORD3},
+                                                    off[i % KINDS], to);
             });
         }
     }
