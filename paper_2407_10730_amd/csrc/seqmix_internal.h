@@ -121,7 +121,9 @@ struct SoftArgs {
     float scale2;          // |scale| log2(e), where the scale is not 0
     int32_t tile;          // tokens of a tile
     FastDiv by_pack, by_groups, by_rep;  // heads of a tile, groups of 4 columns of o, heads that share a k/v head
+    FastDiv by_blocks;
     int64_t ids;           // tiles, numbered as the parts of sequences (seq_part)
+    int32_t first;         // of the blocks of tiles that a launch of several takes
     int32_t near;          // rows of k and v: 16 bytes at least, 8 or more in a page, all that a tile reads within 32-bit offsets
     int32_t shares;        // 0: a workgroup takes a tile; else that many take the same number of quanta of all tiles' keys
     int32_t quantum;       // log2 of its keys

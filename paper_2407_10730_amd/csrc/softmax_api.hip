@@ -187,6 +187,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.blocks = p.heads / a.pack;
     a.by_rep = make_fastdiv((uint32_t)(p.heads / p.kv_heads));
     a.by_pack = make_fastdiv((uint32_t)a.pack);
+    a.by_blocks = make_fastdiv((uint32_t)a.blocks);
     a.by_groups = make_fastdiv((uint32_t)((p.dv + 3) / 4));
     a.dk = p.dk, a.dv = p.dv, a.mask = p.mask;
     a.scale2 = std::fabs(p.scale) * 1.4426950408889634f;

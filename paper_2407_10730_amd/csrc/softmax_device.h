@@ -6,6 +6,7 @@
 // of the result that lane half h holds are keys 8 b + 4 h + i (b, i < 4), and v is read in that order.
 #pragma once
 
+#include <algorithm>
 #include <cfloat>
 #include <type_traits>
 
@@ -85,7 +86,8 @@ __device__ __forceinline__ bool soft_unit(const SoftArgs& A, uint32_t id, int bl
     return true;
 }
 
-// n / d and what is left, for quotients below 2^22 (r: of d, in single precision).
+// n / d and what is left, for quotients below 2^22 (the product in single precision is off by 2^-22 of them, less than 1), and for n
+// up to 2^31 where d is a power of two of 256 or more.
 __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t* left) {
     uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
     int32_t m = (int32_t)(n - q * d);
@@ -160,7 +162,7 @@ struct SoftShares {
 
     // Without shares workgroup n has one unit, the last ones (the longest of a prompt) first.
     __device__ __forceinline__ explicit SoftShares(const SoftArgs& A) {
-        at = share = blockIdx.x;
+        at = share = (uint32_t)A.first + blockIdx.x;
         stop = at + 1;
         none = false;
         if (!A.shares) return;
@@ -200,7 +202,8 @@ struct SoftShares {
         if (at >= stop) return false;
         uint32_t y;
         if (!A.shares) {
-            const uint32_t id = quotient(at++, A.blocks, &y);
+            const uint32_t id = fdiv(at, A.by_blocks);
+            y = at++ - id * A.blocks;
             return soft_unit(A, (uint32_t)A.ids - 1 - id, (int)y, out);
         }
         soft_heads(A, (int)quotient(at, each, &y), out);
@@ -1544,18 +1547,26 @@ __attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step
 
 template <typename T, bool STEP, int DKP, int DVP, bool VEC>
 hipError_t launch_softmax_one(const SoftArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.shares ? a.shares : a.ids * a.blocks));
-    if constexpr (STEP) {
-        hipLaunchKernelGGL((softmax_step_kernel<T, DKP, DVP, VEC>), grid,
-                           dim3(64 * step_waves<32 * (DKP + DVP) * sizeof(T)>()), 0, s, a);
-    } else {
-        constexpr int KT = sizeof(T) == 4 && DKP + DVP > 128 ? 32 : 64;
-        hipLaunchKernelGGL((softmax_prompt_kernel<T, DKP, DVP, KT, VEC>), grid, dim3(64 * kPromptWaves), 0, s, a);
-        if (a.shares)
-            hipLaunchKernelGGL((softmax_join_kernel<T, VEC>),
-                               dim3((unsigned)a.shares, (unsigned)((a.tile * a.pack + kJoinRows - 1) / kJoinRows)), dim3(256), 0, s, a);
+    constexpr int THREADS = 64 * (STEP ? step_waves<32 * (DKP + DVP) * sizeof(T)>() : kPromptWaves);
+    constexpr int64_t MOST = ((1LL << 32) - 1) / THREADS;  // workgroups: a launch has less than 2^32 threads
+    const int64_t all = a.shares ? a.shares : a.ids * a.blocks;
+    SoftArgs b = a;
+    for (int64_t first = 0; first < all; first += MOST) {
+        b.first = (int32_t)first;
+        const dim3 grid((unsigned)std::min(MOST, all - first));
+        if constexpr (STEP) {
+            hipLaunchKernelGGL((softmax_step_kernel<T, DKP, DVP, VEC>), grid, dim3(THREADS), 0, s, b);
+        } else {
+            constexpr int KT = sizeof(T) == 4 && DKP + DVP > 128 ? 32 : 64;
+            hipLaunchKernelGGL((softmax_prompt_kernel<T, DKP, DVP, KT, VEC>), grid, dim3(THREADS), 0, s, b);
+            if (a.shares)
+                hipLaunchKernelGGL((softmax_join_kernel<T, VEC>),
+                                   dim3((unsigned)a.shares, (unsigned)((a.tile * a.pack + kJoinRows - 1) / kJoinRows)), dim3(256), 0, s, b);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 // Kernels for heads of up to 64, 128 and 256 elements.

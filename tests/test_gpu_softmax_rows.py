@@ -71,3 +71,16 @@ def test_results_do_not_depend_on_addresses(kw, dtype):
         for o in outs[1:]:
             same = (o == outs[0]) | (torch.isnan(o) & torch.isnan(outs[0]))
             assert same.all(), f"{int((~same).sum())} of {same.numel()} results differ"
+
+
+@pytest.mark.parametrize("heads", (1, 3))
+def test_more_workgroups_than_a_launch_holds(heads):
+    """Single tokens that each see one key: as many workgroups, of 512 threads, as sequences times heads, past 2^32 threads (and, with 3
+    heads, past 2^25 workgroups).  A row that sees one key is its value, bit by bit."""
+    n = (1 << 23) + 1003 if heads == 1 else (1 << 25) // 3 + 1003
+    q, k, v = (torch.randn(n, heads, 8, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    o = torch.full_like(v, 7)
+    op = M.SoftmaxAttention(tokens=n, seqs=n, heads=heads, dk=8)
+    assert op.plan().kernel == M.SEQMIX_KERNEL_STEP and op.plan().shares == 0
+    op.run(q, k, v, o)
+    assert torch.equal(o, v)
