@@ -149,11 +149,28 @@ static hipError_t launch(const RotaryArgs& a, hipStream_t s) {
     const int units = heads * per_head + (a.vc ? a.kv_heads * per_value : 0);
     if (a.tokens == 0 || units == 0) return hipSuccess;
     const int each = a.tokens >= 1024 ? 4 : 1;
-    const int64_t blocks = (a.tokens + each - 1) / each;
-    hipLaunchKernelGGL((rotary_kernel<T, V, HALF>), dim3((unsigned)blocks), dim3(kRotaryThreads),
-                       (size_t)each * (a.rot / 2) * sizeof(f32x2), s, a, each, make_fastdiv((uint32_t)units),
-                       make_fastdiv((uint32_t)per_head), make_fastdiv((uint32_t)std::max(per_value, 1)));
-    return hipGetLastError();
+    constexpr int64_t MOST = 1 << 25;  // tokens of a launch, which has less than 2^32 threads
+    RotaryArgs b = a;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += MOST) {
+        b.tokens = std::min(MOST, a.tokens - t0);
+        const int64_t blocks = (b.tokens + each - 1) / each;
+        hipLaunchKernelGGL((rotary_kernel<T, V, HALF>), dim3((unsigned)blocks), dim3(kRotaryThreads),
+                           (size_t)each * (a.rot / 2) * sizeof(f32x2), s, b, each, make_fastdiv((uint32_t)units),
+                           make_fastdiv((uint32_t)per_head), make_fastdiv((uint32_t)std::max(per_value, 1)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        auto on = [](auto& p, int64_t row) {  // to the next launch's first row
+            if (p) p = static_cast<const T*>(p) + MOST * row;
+        };
+        auto on_out = [](void*& p, int64_t row) {
+            if (p) p = static_cast<T*>(p) + MOST * row;
+        };
+        on(b.q, a.q_row), on(b.k, a.k_row), on(b.v, a.v_row);
+        on_out(b.qo, a.qo_row), on_out(b.ko, a.ko_row);
+        b.position += MOST;
+        if (b.place) b.place += MOST;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_rotary(const RotaryArgs& a, int dt, int layout, hipStream_t s) {

@@ -84,3 +84,35 @@ def test_more_workgroups_than_a_launch_holds(heads):
     assert op.plan().kernel == M.SEQMIX_KERNEL_STEP and op.plan().shares == 0
     op.run(q, k, v, o)
     assert torch.equal(o, v)
+
+
+def test_rotary_positions_of_more_tokens_than_a_launch_holds():
+    """2^26 tokens and more, four to a workgroup of 256 threads: each launch's last and first tokens as calls of their own turn them."""
+    n, part = (1 << 26) + 5003, 4096
+    gen = torch.Generator("cuda").manual_seed(0)
+    q, k, v = (torch.randn(n, 1, d, device="cuda", generator=gen).bfloat16() for d in (2, 4, 3))
+    position = torch.arange(n, device="cuda", dtype=torch.int32) // 64
+    place = torch.arange(n - 1, -1, -1, device="cuda", dtype=torch.int32)
+    freqs = M.rotary_frequencies(2)
+    pages = -(-n // 16)
+
+    def call(at, qo, ko, kc, vc):
+        m = q[at].shape[0]
+        M.Rotary(tokens=m, heads=1, kv_heads=1, dk=2, dv=3, page=16, pages=pages, k_strides=(4, 2)).run(
+            q[at], k[at][..., :2], v[at], position[at], freqs, qo, ko, kc, vc, place[at])
+
+    def new(m):
+        return torch.full((m, 1, 2), 7.0, device="cuda", dtype=q.dtype), torch.full((m, 1, 2), 7.0, device="cuda", dtype=q.dtype), \
+            *(torch.full((pages, 16, 1, d), 7.0, device="cuda", dtype=q.dtype) for d in (2, 3))
+
+    whole = new(n)
+    call(slice(None), *whole)
+    for first in (0, (1 << 25) - part // 2, (1 << 26) - part // 2, n - part):
+        at = slice(first, first + part)
+        want = new(part)
+        call(at, *want)
+        assert torch.equal(whole[0][at], want[0]) and torch.equal(whole[1][at], want[1])
+        rows = place[at].long()
+        for got, one in zip(whole[2:], want[2:]):
+            assert torch.equal(got.flatten(0, 1)[rows], one.flatten(0, 1)[rows])
+    assert not (whole[0] == 7).all(-1).any()
