@@ -111,7 +111,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gate_norm_kernel(NormAr
     constexpr int NT = TPR < 256 ? 256 : TPR;
     __shared__ float red[NT / 64];
     const int t = threadIdx.x % TPR;
-    int64_t id = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    int64_t id = (A.first + blockIdx.x) * (NT / TPR) + threadIdx.x / TPR;
     const bool live = id < A.rows;  // TPR > 64 has one group per block: all its threads agree
     id = live ? id : A.rows - 1;
     // (64-bit divisions take longer than a small group's sums: 8105 x 4096 bf16 by groups of 128 53.2 us, 49.9; 64 x 200
@@ -188,14 +188,21 @@ template <typename T, typename TR, int TPR, int V, int ITEMS>
 static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
     constexpr int NT = TPR < 256 ? 256 : TPR;
     const int64_t blocks = (a.rows + NT / TPR - 1) / (NT / TPR);
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    constexpr int64_t MOST = ((1LL << 32) - 1) / NT;  // a launch has less than 2^32 threads
     // With fewer than two blocks per CU the time is one block's chain of loads: weights early take one wait out of it (13 rows of
     // 1537 fp32 6.5 -> 5.1 us).  With many, their registers cost waves (8192 x 2048 bf16 by heads of 128: 26 us, late 23.5).
-    if (ITEMS * V <= 8 && blocks < 2 * kSeqmixCUs)
+    if (ITEMS * V <= 8 && blocks < 2 * kSeqmixCUs) {
         hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS, (ITEMS * V <= 8)>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
-    else
-        hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS, false>), dim3((unsigned)blocks), dim3(NT), 0, s, a);
-    return hipGetLastError();
+        return hipGetLastError();
+    }
+    NormArgs b = a;
+    for (b.first = 0; b.first < blocks; b.first += MOST) {
+        hipLaunchKernelGGL((gate_norm_kernel<T, TR, TPR, V, ITEMS, false>), dim3((unsigned)std::min(MOST, blocks - b.first)), dim3(NT), 0,
+                           s, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // V values per access: 16 bytes, or 1 in groups below that.  Groups up to 16 accesses: 16 lanes each; up to 64: a wave;

@@ -87,6 +87,7 @@ struct NormArgs {
     const float *scale_vec, *pre_w, *pre_b;
     void *y, *h;
     int64_t rows;         // rows * groups of the call
+    int64_t first;        // workgroup of a launch that is not the call's first
     int32_t group, ngroups;
     FastDiv by_groups, by_run;  // rows below 2^31
     int64_t u_row, gate_row, res_row, y_row, h_row;
