@@ -188,7 +188,7 @@ template <typename T, typename TR, int TPR, int V, int ITEMS>
 static hipError_t launch_one(const NormArgs& a, hipStream_t s) {
     constexpr int NT = TPR < 256 ? 256 : TPR;
     const int64_t blocks = (a.rows + NT / TPR - 1) / (NT / TPR);
-    constexpr int64_t MOST = ((1LL << 32) - 1) / NT;  // a launch has less than 2^32 threads
+    constexpr int64_t MOST = kMostThreads / NT;
     // With fewer than two blocks per CU the time is one block's chain of loads: weights early take one wait out of it (13 rows of
     // 1537 fp32 6.5 -> 5.1 us).  With many, their registers cost waves (8192 x 2048 bf16 by heads of 128: 26 us, late 23.5).
     if (ITEMS * V <= 8 && blocks < 2 * kSeqmixCUs) {

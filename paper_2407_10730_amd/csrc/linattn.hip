@@ -17,8 +17,8 @@ __global__ __launch_bounds__(256) void attn_tokens_kernel(AttnArgs A) {
     constexpr int LR = DVB / 4;  // threads across the columns
     __shared__ float red[2][4][DVB];
     const int t = threadIdx.x, cg = t % LR, rg = t / LR;
-    const uint32_t bh = blockIdx.x / (uint32_t)A.ndvb;
-    const int blk = (int)(blockIdx.x - bh * A.ndvb);
+    const uint32_t block = (uint32_t)A.first + blockIdx.x, bh = block / (uint32_t)A.ndvb;
+    const int blk = (int)(block - bh * A.ndvb);
     const int seq = (int)(bh / (uint32_t)A.heads), head = (int)(bh - (uint32_t)seq * A.heads);
     const SeqRange r = seq_range(A.sq, seq);
     const int r0 = rg * RPT, nc = min(4, A.dv - blk * DVB - cg * 4);  // owned columns (none: below 1)
@@ -137,16 +137,22 @@ template <typename T, typename TO, int DVB>
 static hipError_t launch_tokens_b(const AttnArgs& a, hipStream_t s) {
     const int64_t blocks = (int64_t)a.sq.seqs * a.heads * a.ndvb;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
-    if (a.dk <= 32)
-        launch_tokens_r<T, TO, DVB, 32>(a, grid, s);
-    else if (a.dk <= 64)
-        launch_tokens_r<T, TO, DVB, 64>(a, grid, s);
-    else if (a.dk <= 128)
-        launch_tokens_r<T, TO, DVB, 128>(a, grid, s);
-    else
-        launch_tokens_r<T, TO, DVB, 256>(a, grid, s);
-    return hipGetLastError();
+    AttnArgs b = a;
+    for (int64_t first = 0; first < blocks; first += kMostThreads / 256) {
+        b.first = (int32_t)first;
+        const dim3 grid((unsigned)std::min<int64_t>(kMostThreads / 256, blocks - first));
+        if (a.dk <= 32)
+            launch_tokens_r<T, TO, DVB, 32>(b, grid, s);
+        else if (a.dk <= 64)
+            launch_tokens_r<T, TO, DVB, 64>(b, grid, s);
+        else if (a.dk <= 128)
+            launch_tokens_r<T, TO, DVB, 128>(b, grid, s);
+        else
+            launch_tokens_r<T, TO, DVB, 256>(b, grid, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, typename TO>

@@ -349,7 +349,7 @@ static void launch_rows(const AttnArgs& a, dim3 grid, hipStream_t s) {
 template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, int odt, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.ids * a.units + 7) / 8 * 8 * a.unit;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (blocks * 64 * WAVES > kMostThreads) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
     if (state_only)
         launch_rows<DKT, WAVES, true, 2>(a, grid, s);

@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * WAVES, chunk_f32_occupancy(DKT, WAVES)) void a
 template <int DKT, int WAVES>
 static hipError_t launch_one(const AttnArgs& a, bool state_only, hipStream_t s) {
     const int64_t blocks = (a.ids * a.units + 7) / 8 * 8 * a.unit;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (blocks * 64 * WAVES > kMostThreads) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(64 * WAVES);
     if (state_only) {
         if (a.vec)

@@ -149,7 +149,7 @@ static hipError_t launch(const RotaryArgs& a, hipStream_t s) {
     const int units = heads * per_head + (a.vc ? a.kv_heads * per_value : 0);
     if (a.tokens == 0 || units == 0) return hipSuccess;
     const int each = a.tokens >= 1024 ? 4 : 1;
-    constexpr int64_t MOST = 1 << 25;  // tokens of a launch, which has less than 2^32 threads
+    constexpr int64_t MOST = 1 << 25;  // tokens of a launch: up to 2^31 threads
     RotaryArgs b = a;
     for (int64_t t0 = 0; t0 < a.tokens; t0 += MOST) {
         b.tokens = std::min(MOST, a.tokens - t0);

@@ -10,6 +10,7 @@ namespace cv {
 // with residual 34.0 -> 26.4 us, 2048 rows of the two 12.4 -> 10.6 and 11.3 -> 9.6 us.  The operators after them do
 // not miss it (a layer over 8496 tokens 297 us, 296 with it): the XCDs' L2s hold little of what others wrote.
 constexpr int64_t kPastBytes = 4LL << 20;
+constexpr int64_t kMostThreads = (1LL << 32) - 1;  // of a launch: what is above is left out without an error
 constexpr int kSeqmixCUs = 256;  // plans are made without a GPU: MI355X has 256 CUs
 
 // How the rows of a call divide into sequences, and which pool entry each has.
@@ -51,6 +52,7 @@ struct AttnArgs {
     int32_t places;       // the ids of this pass number places of the workspace
     int64_t ids;          // of this pass: sequences, segments or places
     int32_t unit, units;  // workgroups of an id that stay on one XCD, such units per id
+    int32_t first;        // workgroup of a launch that is not the call's first (token kernel)
     float* ws_state;      // [nws][heads][dk][dv]
     float* ws_decay;      // [nws][heads]: log of a segment's whole decay, times log2(e)
 };

@@ -1548,7 +1548,7 @@ __attribute__((amdgpu_waves_per_eu(DKP + DVP <= 256 ? 2 : 1))) void softmax_step
 template <typename T, bool STEP, int DKP, int DVP, bool VEC>
 hipError_t launch_softmax_one(const SoftArgs& a, hipStream_t s) {
     constexpr int THREADS = 64 * (STEP ? step_waves<32 * (DKP + DVP) * sizeof(T)>() : kPromptWaves);
-    constexpr int64_t MOST = ((1LL << 32) - 1) / THREADS;  // workgroups: a launch has less than 2^32 threads
+    constexpr int64_t MOST = kMostThreads / THREADS;  // workgroups
     const int64_t all = a.shares ? a.shares : a.ids * a.blocks;
     SoftArgs b = a;
     for (int64_t first = 0; first < all; first += MOST) {
