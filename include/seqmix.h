@@ -257,8 +257,9 @@ typedef struct {
 typedef struct seqmix_softmax_desc seqmix_softmax_desc;
 
 /* E_NULL, E_INVALID (sizes out of range, a stride below the dimension inside it, a page that is no power of two),
- * E_UNSUPPORTED (dims over SEQMIX_MAX_HEAD_DIM, pages over SEQMIX_MAX_PAGE, unknown types or masks, 2^31 tokens or
- * cached rows or more).  Workspaces, streams and captures are as those of seqmix_attn. */
+ * E_UNSUPPORTED (dims over SEQMIX_MAX_HEAD_DIM, pages over SEQMIX_MAX_PAGE, unknown types or masks, 2^31 cached rows or more, keys
+ * of a sequence, or tokens and sequences times heads, beyond 2^31 - 1024).  Workspaces, streams and captures are as those of
+ * seqmix_attn. */
 int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softmax_desc** out);
 int seqmix_softmax_desc_destroy(seqmix_softmax_desc* desc);
 int seqmix_softmax_plan_query(const seqmix_softmax_desc* desc, seqmix_softmax_plan_info* out);

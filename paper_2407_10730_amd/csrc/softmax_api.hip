@@ -24,6 +24,9 @@ namespace {
 
 // Heads of one call; more make 32-bit indices of a token's elements overflow.
 constexpr int32_t kMaxHeads = 1 << 20;
+// Rows and keys of a sequence: the kernels number a tile's rows and look for the next tiles' keys, up to 640 behind the last, in 32
+// bits.
+constexpr int64_t kMaxKeys = kMaxRows - 1023;
 constexpr int kPackedShift = 10;
 
 int log2_of(int32_t page) { return 31 - __builtin_clz((unsigned)page); }
@@ -128,15 +131,14 @@ int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softm
         SM_TRY(check_table(p.max_pages, p.page));
     } else if (p.key_tokens < 0) {
         return CONV2D_E_INVALID;
-    } else if (p.key_tokens > kMaxRows) {
-        return CONV2D_E_UNSUPPORTED;
     }
+    if ((p.page ? p.max_pages * p.page : p.key_tokens) > kMaxKeys) return CONV2D_E_UNSUPPORTED;
     const int64_t rows = p.page ? p.page : p.key_tokens, pages = p.page ? p.pages : 1;
     if (!strides_ok(p.tokens, p.q_row, p.heads, p.q_head, p.dk) || !strides_ok(p.tokens, p.o_row, p.heads, p.o_head, p.dv) ||
         !cache_ok(rows, p.kv_heads, pages, p.k_row, p.k_head, p.k_page, p.dk) ||
         !cache_ok(rows, p.kv_heads, pages, p.v_row, p.v_head, p.v_page, p.dv))
         return CONV2D_E_INVALID;
-    if ((p.tokens + p.seqs) * p.heads > kMaxRows) return CONV2D_E_UNSUPPORTED;  // workgroups
+    if ((p.tokens + p.seqs) * p.heads > kMaxKeys) return CONV2D_E_UNSUPPORTED;  // (workgroups too)
     seqmix_softmax_desc* d = new (std::nothrow) seqmix_softmax_desc;
     if (!d) return CONV2D_E_ALLOC;
     d->p = p;
