@@ -210,7 +210,7 @@ int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* po
  *                       that continue the text in several ways: the bits of a token, its parent, ...)
  * Rows that see no key (n = 0, n < len, an empty mask) are zeros.  Keys that a row does not see never reach it, also where
  * they hold infinities or NaN.  Where it sees values that are not finite, its results there are NaN.  Scores are
- * compared as they are: one of +infinity makes the row NaN, ones of -infinity count nothing.
+ * compared as they are, times log2(e): one of +infinity makes the row NaN, ones of -infinity count nothing.
  *
  * Keys and values lie
  *   packed (page 0)  in key_tokens rows; sequence i holds rows [key_offsets[i], key_offsets[i+1]); key_offsets NULL: the rows
@@ -237,7 +237,7 @@ typedef struct {
     int32_t dk, dv;      /* 1 .. SEQMIX_MAX_HEAD_DIM */
     int32_t dtype;       /* q, k, v, o */
     int32_t mask;        /* SEQMIX_MASK_* */
-    float scale;         /* finite */
+    float scale;         /* times log2(e) finite */
     /* elements from a token to the next, from a head to the next, and from a page to the next (in pages) */
     int64_t q_row, q_head, o_row, o_head;
     int64_t k_row, k_head, k_page, v_row, v_head, v_page;

@@ -28,6 +28,7 @@ constexpr int32_t kMaxHeads = 1 << 20;
 // bits.
 constexpr int64_t kMaxKeys = kMaxRows - 1023;
 constexpr int kPackedShift = 10;
+constexpr float kLog2E = 1.4426950408889634f;  // exponentials are powers of two
 
 int log2_of(int32_t page) { return 31 - __builtin_clz((unsigned)page); }
 
@@ -121,7 +122,7 @@ int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softm
     if (!params || !out) return CONV2D_E_NULL;
     const seqmix_softmax_params& p = *params;
     SM_TRY(check_seqs(p.tokens, p.seqs, p.slots));
-    if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads != 0 || p.dk < 1 || p.dv < 1 || !std::isfinite(p.scale))
+    if (p.heads < 1 || p.kv_heads < 1 || p.heads % p.kv_heads != 0 || p.dk < 1 || p.dv < 1 || !std::isfinite(p.scale * kLog2E))
         return CONV2D_E_INVALID;
     if (p.mask < SEQMIX_MASK_FULL || p.mask > SEQMIX_MASK_TREE || !known_dtype(p.dtype) || p.dk > SEQMIX_MAX_HEAD_DIM ||
         p.dv > SEQMIX_MAX_HEAD_DIM || p.heads > kMaxHeads)
@@ -192,7 +193,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.by_blocks = make_fastdiv((uint32_t)a.blocks);
     a.by_groups = make_fastdiv((uint32_t)((p.dv + 3) / 4));
     a.dk = p.dk, a.dv = p.dv, a.mask = p.mask;
-    a.scale2 = std::fabs(p.scale) * 1.4426950408889634f;
+    a.scale2 = std::fabs(p.scale) * kLog2E;
     a.qsign = !(a.scale2 > 0.0f) ? 0 : p.scale < 0.0f ? -1 : 1;
     if (a.qsign == 0) a.scale2 = 1.0f;
     const bool step = d->plan.kernel == SEQMIX_KERNEL_STEP;

@@ -25,3 +25,12 @@ def test_keys_are_numbered_in_32_bits(kw):
     with pytest.raises(B.Conv2dError) as e:
         _create(**{**kw, name: kw[name] + 1})
     assert e.value.status == B.CONV2D_E_UNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", (2.4e38, -3.4e38))
+def test_scales_that_are_infinite_as_powers_of_two(scale):
+    """Scores are multiplied by scale log2(e): a finite scale above 2^128 / log2(e) made a score of zero NaN."""
+    _create(scale=2.3e38 if scale > 0 else -2.3e38)
+    with pytest.raises(B.Conv2dError) as e:
+        _create(scale=scale)
+    assert e.value.status == B.CONV2D_E_INVALID
