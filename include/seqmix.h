@@ -263,6 +263,9 @@ typedef struct seqmix_softmax_desc seqmix_softmax_desc;
 int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softmax_desc** out);
 int seqmix_softmax_desc_destroy(seqmix_softmax_desc* desc);
 int seqmix_softmax_plan_query(const seqmix_softmax_desc* desc, seqmix_softmax_plan_info* out);
+/* As seqmix_attn_reserve, but it waits for work queued on the device (counts in the workspace are cleared), and is not to be
+ * done under capture.  A first call without it clears them on its stream and does not wait; a captured one does so whenever its
+ * graph runs. */
 int seqmix_softmax_reserve(seqmix_softmax_desc* desc);
 /* q: [tokens][heads][dk], o: [tokens][heads][dv], k: [key_tokens][kv_heads][dk] or [pages][page][kv_heads][dk], v alike, by the
  * strides given; key_offsets int64 [seqs + 1] (packed; else ignored); lens int32 [slots], table int32

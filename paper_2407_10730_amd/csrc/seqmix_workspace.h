@@ -58,10 +58,10 @@ struct Workspace {
         done = nullptr;
     }
 
-    // `bytes` on the current device, once; `cleared`: zeros.
-    int ensure(int64_t bytes, bool cleared = false) {
+    // `bytes` on the current device, once.
+    int ensure(int64_t bytes) {
         if (bytes == 0) return CONV2D_OK;
-        switch (alloc(bytes, cleared)) {
+        switch (alloc(bytes)) {
             case hipSuccess: return CONV2D_OK;
             case hipErrorOutOfMemory: (void)hipGetLastError(); return CONV2D_E_ALLOC;
             case hipErrorInvalidDevice: return CONV2D_E_UNSUPPORTED;
@@ -88,30 +88,6 @@ struct Workspace {
         return CONV2D_OK;
     }
 
-private:
-    hipError_t alloc(int64_t bytes, bool cleared) {
-        int dev = -1;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return e;
-        if (device >= 0) return device == dev ? hipSuccess : hipErrorInvalidDevice;
-        e = hipEventCreateWithFlags(&done, hipEventDisableTiming);
-        if (e != hipSuccess) return e;
-        e = hipMalloc(&data, (size_t)bytes);
-        if (e == hipSuccess && cleared) {
-            e = hipMemset(data, 0, (size_t)bytes);  // waits for nothing that is queued; later calls wait for it
-            if (e == hipSuccess) e = hipDeviceSynchronize();
-            if (e != hipSuccess) (void)hipFree(data);
-        }
-        if (e != hipSuccess) {
-            (void)hipEventDestroy(done);
-            done = nullptr;
-            data = nullptr;
-            return e;
-        }
-        device = dev;
-        return hipSuccess;
-    }
-
     // Capture that stream s records into, 0: none.
     static unsigned long long capture_of(hipStream_t s) {
         hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
@@ -121,6 +97,25 @@ private:
             return 0;
         }
         return status == hipStreamCaptureStatusActive ? id : 0;
+    }
+
+private:
+    hipError_t alloc(int64_t bytes) {
+        int dev = -1;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        if (device >= 0) return device == dev ? hipSuccess : hipErrorInvalidDevice;
+        e = hipEventCreateWithFlags(&done, hipEventDisableTiming);
+        if (e != hipSuccess) return e;
+        e = hipMalloc(&data, (size_t)bytes);
+        if (e != hipSuccess) {
+            (void)hipEventDestroy(done);
+            done = nullptr;
+            data = nullptr;
+            return e;
+        }
+        device = dev;
+        return hipSuccess;
     }
 
     int wait_for(hipStream_t last, hipStream_t s) {

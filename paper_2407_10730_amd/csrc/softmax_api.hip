@@ -12,6 +12,7 @@ struct seqmix_softmax_desc {
     seqmix_softmax_plan_info plan;
     int quantum = 0;  // of shares: log2 of keys
     Workspace ws;     // of plan.workspace_bytes
+    bool counts = false;  // the step kernel's counts of parts that are done are zero, as every call leaves them
 };
 struct seqmix_rotary_desc {
     seqmix_rotary_params p;
@@ -113,6 +114,16 @@ void plan_softmax(seqmix_softmax_desc* d) {
     }
 }
 
+// What the kernels keep of each share behind the parts.
+void* marks_of(const seqmix_softmax_desc* d) {
+    return static_cast<char*>(d->ws.data) + d->plan.workspace_bytes - d->plan.shares * kMarkBytes;
+}
+bool counted(const seqmix_softmax_desc* d) { return d->plan.shares && d->plan.kernel == SEQMIX_KERNEL_STEP; }
+
+__global__ __launch_bounds__(256) void clear_counts_kernel(uint32_t* counts, int n) {
+    for (int i = threadIdx.x; i < n; i += 256) counts[i] = 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -163,7 +174,12 @@ int seqmix_softmax_plan_query(const seqmix_softmax_desc* d, seqmix_softmax_plan_
 
 int seqmix_softmax_reserve(seqmix_softmax_desc* d) {
     if (!d) return CONV2D_E_NULL;
-    return d->ws.ensure(d->plan.workspace_bytes, true);
+    SM_TRY(d->ws.ensure(d->plan.workspace_bytes));
+    if (!counted(d) || d->counts) return CONV2D_OK;
+    if (hipMemset(marks_of(d), 0, (size_t)(d->plan.shares * kMarkBytes)) != hipSuccess || hipDeviceSynchronize() != hipSuccess)
+        return CONV2D_E_HIP;
+    d->counts = true;
+    return CONV2D_OK;
 }
 
 int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, const void* v, const int64_t* offsets,
@@ -208,8 +224,14 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
     a.tile = (step ? kStepRows : kPromptRows) / a.pack;
     a.ids = seq_part_ids(a.sq, a.tile);
     if (d->plan.shares) {
-        SM_TRY(d->ws.ensure(d->plan.workspace_bytes, true));
+        SM_TRY(d->ws.ensure(d->plan.workspace_bytes));
         SM_TRY(d->ws.order_after_last(s));
+        if (counted(d) && !d->counts) {
+            // (a captured call clears them whenever its graph runs, and for no other)
+            hipLaunchKernelGGL(clear_counts_kernel, dim3(1), dim3(256), 0, s, static_cast<uint32_t*>(marks_of(d)), (int)d->plan.shares);
+            if (hipGetLastError() != hipSuccess) return CONV2D_E_HIP;
+            d->counts = Workspace::capture_of(s) == 0;
+        }
         a.shares = (int32_t)d->plan.shares;
         a.quantum = d->quantum;
         a.grow = p.mask == SEQMIX_MASK_CAUSAL && a.tile % (1 << a.quantum) == 0 ? a.tile >> a.quantum : 0;
@@ -217,7 +239,7 @@ int seqmix_softmax_fwd(seqmix_softmax_desc* d, const void* q, const void* k, con
         a.whole = division_of(step, p.dtype).whole;
         a.most = (int32_t)((1LL << 31) / a.blocks - 1);
         a.ws = d->ws.data;
-        a.marks = static_cast<char*>(d->ws.data) + 2 * d->plan.shares * part_bytes(p, step, (int64_t)a.tile * a.pack);
+        a.marks = marks_of(d);
     }
     auto launch = p.dtype == CONV2D_BF16 ? (step ? launch_softmax_step_bf16 : launch_softmax_prompt_bf16)
                                          : (step ? launch_softmax_step_f32 : launch_softmax_prompt_f32);

@@ -116,3 +116,51 @@ def test_rotary_positions_of_more_tokens_than_a_launch_holds():
         for got, one in zip(whole[2:], want[2:]):
             assert torch.equal(got.flatten(0, 1)[rows], one.flatten(0, 1)[rows])
     assert not (whole[0] == 7).all(-1).any()
+
+
+@pytest.mark.parametrize("new,keys", (([1] * 3, [5000, 70, 900]), ([300, 7], [2000, 900])))
+def test_a_first_call_does_not_wait(new, keys):
+    """A descriptor's first call, which allocates its workspace, returns while another stream has work queued; it and the next, on
+    another stream, are right."""
+    p, first = (Soft(new, keys=keys, heads=8, kv_heads=2, dk=128, dv=128, page=16) for _ in range(2))
+    assert p.op.plan().workspace_bytes > 0
+    first.run()  # (loads the kernels)
+    want = first.o
+    x = torch.randn(8192, 8192, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        x @ x
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        y = x @ x
+        for _ in range(40):
+            torch.mm(x, x, out=y)
+        done = side.record_event()
+    p.run()
+    assert not done.query(), "the call waited for another stream"
+    assert torch.equal(p.o, want)
+    p.o = torch.full_like(want, 7)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        p.run()
+    torch.cuda.synchronize()
+    assert torch.equal(p.o, want)
+
+
+def test_a_first_call_that_is_captured_in_a_reserved_workspace():
+    """Without a call before it; eager calls and replays after it give the same, in either order."""
+    for replay_first in (True, False):
+        p = Soft([1] * 3, keys=[5000, 70, 900], heads=8, kv_heads=2, dk=128, dv=128, page=16)
+        p.op.reserve()
+        g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+            p.run()
+        outs = []
+        for replay in (replay_first, not replay_first) * 2:
+            p.o.fill_(7)
+            g.replay() if replay else p.run()
+            outs.append(p.o.clone())
+        p.check()
+        assert all(torch.equal(o, outs[0]) for o in outs[1:])
