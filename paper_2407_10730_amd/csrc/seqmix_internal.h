@@ -99,7 +99,7 @@ struct NormArgs {
 };
 hipError_t launch_norm(const NormArgs& a, int dt, int rdt, hipStream_t s);
 
-// A cache of keys or values in pages, or packed rows (shift 0: row j is page j).
+// A cache of keys or values in pages, or packed rows, as many to a page as SoftArgs::shift says.
 struct CachePlace {
     int64_t page, row, head;  // elements from one to the next
 };

@@ -955,8 +955,7 @@ __device__ __forceinline__ void load_words_to_lds(__amdgpu_buffer_rsrc_t r, uint
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(r) : "memory", "m0");
 }
 typedef __attribute__((address_space(3))) const void* lds_address;
-template <int LEFT = 0>  // all but the last LEFT
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT < 63 ? LEFT : 63) : "memory"); }
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // The page that holds the rows of lane i's instruction.
 __device__ __forceinline__ int clamp_page(const SoftArgs& A, int page) { return min(max(page, 0), (int)A.pages - 1); }
@@ -1345,6 +1344,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, DKP + DVP <= 256 ? 2 : 1) void s
     // for the launch that joins: the unit that begins in this share and goes on behind it
     if (A.shares && threadIdx.x == 0) {
         if (shares.none || pl.part != 0) pl.parts = 1;
+        static_assert(sizeof(SoftPlace) <= kMarkBytes && alignof(SoftPlace) <= 8);
         static_cast<SoftPlace*>(A.marks)[shares.share] = pl;
     }
 }
