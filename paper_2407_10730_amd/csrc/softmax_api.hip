@@ -62,13 +62,13 @@ int32_t packed_heads(int64_t rows, int64_t length, int32_t rep) {
 // 128 rows per tile, keys in a cache: 4 prompts of 300 to 700 tokens that go on from up to 12000, 16 heads of 128 (304 tiles):
 // 194 us, by tiles 400; about as many keys as tokens, where tiles see half of them on average and the card overlaps short
 // and long ones: 3 of 1000 tokens (384): 54 us, by tiles 42; one of 2200 (288): 61 and 62; 10 packed ones, 12 heads of 64 x 128
-// (648): 71, by tiles 64; fp32 is slower by tiles (3 of 1300, 12 heads of 80 x 112: 222 us, by tiles 387), and so are rows that
-// are no multiple of 16 bytes (2048 tokens, 16 heads of 127, 272 tiles: 152, by tiles 184).
+// (648): 71, by tiles 64; rows that are no multiple of 16 bytes alike (2048 tokens, 16 heads of 127, 272 tiles: 118, by tiles
+// 110; of 63 53 and 56; 3 of 1000 tokens, heads of 127: 110 and 78); fp32 is slower by tiles (3 of 1300, 12 heads of 80 x 112:
+// 222 us, by tiles 387).
 // 32 rows: 64 single tokens over up to 8000 keys, 4 k/v heads (288): 111 us, by tiles 131; 2 over 65536 (8): 61 us, 700.
 int64_t full_card(const seqmix_softmax_params& p, bool step) {
     if (step) return 4 * kSeqmixCUs;
-    const bool quick = p.dtype == CONV2D_BF16 && p.dk % 8 == 0 && p.dv % 8 == 0;
-    return quick && !p.page && p.key_tokens <= 2 * p.tokens ? kSeqmixCUs : 2 * kSeqmixCUs;
+    return p.dtype == CONV2D_BF16 && !p.page && p.key_tokens <= 2 * p.tokens ? kSeqmixCUs : 2 * kSeqmixCUs;
 }
 // ... and sequences are at most this many, as each wave looks at all of them.
 constexpr int64_t kShareSeqs = 1024;
