@@ -35,7 +35,7 @@
  *   - Strides count elements.  Rows may lie apart (columns of a wider tensor); the last dimension is dense.
  *   - Any alignment of an element's size is accepted, at the same speed but for rows below 16 bytes (softmax attention: up
  *     to twice the time where k and v are not in whole 16 bytes).  Results are bitwise reproducible for the same
- *     descriptor parameters.
+ *     descriptor parameters, at whatever addresses.
  *   - Every product is summed in fp32 and states are fp32; outputs are rounded once, to nearest even.  (Attention in bf16
  *     multiplies what it has computed in fp32, scores and states, as sums of bf16 parts: 2^-16 of each term is
  *     left out where outputs are bf16, 2^-24 where they are fp32.  seqmix_softmax says for itself.)
@@ -210,7 +210,8 @@ int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* po
  *                       that continue the text in several ways: the bits of a token, its parent, ...)
  * Rows that see no key (n = 0, n < len, an empty mask) are zeros.  Keys that a row does not see never reach it, also where
  * they hold infinities or NaN.  Where it sees values that are not finite, its results there are NaN.  Scores are
- * compared as they are, times log2(e): one of +infinity makes the row NaN, ones of -infinity count nothing.
+ * compared as they are, times log2(e): one of +infinity makes the row NaN, ones of -infinity count nothing (a row of which all
+ * are is zeros).
  *
  * Keys and values lie
  *   packed (page 0)  in key_tokens rows; sequence i holds rows [key_offsets[i], key_offsets[i+1]); key_offsets NULL: the rows
@@ -219,9 +220,12 @@ int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* po
  *                    table[s][j / page], row j % page, and the slot holds lens[s] keys (the new ones among them).
  * Lengths and page numbers are clamped to what there is, so bad ones give wrong results but no access out of range.
  *
- * Precision: scores and sums are fp32 products and sums of what q, k and v hold.  bf16: the step kernel multiplies v by weights
- * in two bf16 parts (2^-16 of each is left out), so results are rounded once; the prompt kernel by weights rounded to
- * bf16 (2^-8 of each at most, about the result's own rounding), which halves its longest products. */
+ * Precision: scores and sums are fp32 products and sums of what q, k and v hold.  Sums over v are of weights up to 2^8 (they are
+ * divided at the end), so they are finite where 2^8 times the number of keys times the largest |v| is.  bf16: the step kernel
+ * multiplies v by weights in two bf16 parts (2^-16 of each is left out), so results are rounded once; the prompt kernel by
+ * weights rounded to bf16 (2^-8 of each at most, about the result's own rounding: 0.0021 off in the 2-norm, one rounding 0.0016),
+ * which halves its longest products.  Which kernel a call has, plan_query says: trees of more than a few drafts have the
+ * prompt kernel, single tokens the other, so a token that is drafted in a tree and one that is decoded alone may differ by that. */
 enum { SEQMIX_MASK_FULL = 0, SEQMIX_MASK_CAUSAL = 1, SEQMIX_MASK_TREE = 2 };
 
 #define SEQMIX_MAX_PAGE 65536
@@ -244,12 +248,18 @@ typedef struct {
 } seqmix_softmax_params;
 
 /* Kernels of a call: 128 rows of a sequence per workgroup, or 32, whose keys its waves divide; chosen by the average number of
- * rows of a sequence (times the heads that share a k/v head). */
+ * rows of a sequence (times the heads that share a k/v head).  Rows of a workgroup are of one sequence, and of `pack` heads of those
+ * that share a k/v head, a divisor of their number: as many as fill it by that average.  What this serves badly (16 heads of
+ * 128 over 4 k/v heads where nothing else is said):
+ *   - a prompt and single tokens in one call, as each single token's keys are read for every head: 2048 tokens and 32 single
+ *     ones over up to 8000 keys take 333 us, the two as calls of their own 64 and 64;
+ *   - few heads to pack, where those of a k/v head have few divisors: 16 trees of 24 drafts over up to 5000 keys take 49 us,
+ *     with 28 heads (7 of a k/v head) 201; 16 of 2 drafts with 64 heads over one 35, with 71 over one 306. */
 enum { SEQMIX_KERNEL_PROMPT = 0, SEQMIX_KERNEL_STEP = 1 };
 
 typedef struct {
     int32_t kernel;           /* SEQMIX_KERNEL_* */
-    int32_t pack;             /* heads that share a workgroup */
+    int32_t pack;             /* heads that share a workgroup, a divisor of heads / kv_heads */
     int64_t shares;           /* 0: a workgroup takes all keys of its rows; else the keys of all rows are divided in so many shares */
     int64_t workspace_bytes;  /* results of rows whose keys are in several shares */
 } seqmix_softmax_plan_info;

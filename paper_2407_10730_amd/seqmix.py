@@ -462,7 +462,8 @@ class SoftmaxAttention(_Operator):
     offsets: int64 [seqs + 1]; slot_index: int32 [seqs]; tree (mask "tree"): int64 [tokens].  Keys and values either
     packed (page 0), k: [key_tokens, kv_heads, dk], v alike, key_offsets: int64 [seqs + 1] (None: the rows of q),
     or in `pages` pages of `page` tokens, k: [pages, page, kv_heads, dk], v alike (three strides), lens: int32 [slots],
-    table: int32 [slots, max_pages].  The kernels are chosen by the average number of rows of a sequence.
+    table: int32 [slots, max_pages].  The kernels are chosen by the average number of rows of a sequence: prompts and single
+    tokens are better two calls.
     """
 
     op = "softmax"
