@@ -223,7 +223,7 @@ int seqmix_norm_fwd(const seqmix_norm_desc* desc, const void* u, const float* po
  * Precision: scores and sums are fp32 products and sums of what q, k and v hold.  Sums over v are of weights up to 2^8 (they are
  * divided at the end), so they are finite where 2^8 times the number of keys times the largest |v| is.  bf16: the step kernel
  * multiplies v by weights in two bf16 parts (2^-16 of each is left out), so results are rounded once; the prompt kernel by
- * weights rounded to bf16 (2^-8 of each at most, about the result's own rounding: 0.0021 off in the 2-norm, one rounding 0.0016),
+ * weights rounded to bf16 (2^-8 of each at most, about the result's own rounding: 0.0020 to 0.0023 off in the 2-norm, one rounding 0.0016),
  * which halves its longest products.  Which kernel a call has, plan_query says: trees of more than a few drafts have the
  * prompt kernel, single tokens the other, so a token that is drafted in a tree and one that is decoded alone may differ by that. */
 enum { SEQMIX_MASK_FULL = 0, SEQMIX_MASK_CAUSAL = 1, SEQMIX_MASK_TREE = 2 };
@@ -267,8 +267,8 @@ typedef struct {
 typedef struct seqmix_softmax_desc seqmix_softmax_desc;
 
 /* E_NULL, E_INVALID (sizes out of range, a stride below the dimension inside it, a page that is no power of two),
- * E_UNSUPPORTED (dims over SEQMIX_MAX_HEAD_DIM, pages over SEQMIX_MAX_PAGE, unknown types or masks, 2^31 cached rows or more, keys
- * of a sequence, or tokens and sequences times heads, beyond 2^31 - 1024).  Workspaces, streams and captures are as those of
+ * E_UNSUPPORTED (dims over SEQMIX_MAX_HEAD_DIM, pages over SEQMIX_MAX_PAGE, unknown types or masks, 2^31 tokens or cached rows or
+ * more; keys of a sequence, or tokens and sequences together times heads, beyond 2^31 - 1024).  Workspaces, streams and captures are as those of
  * seqmix_attn. */
 int seqmix_softmax_desc_create(const seqmix_softmax_params* params, seqmix_softmax_desc** out);
 int seqmix_softmax_desc_destroy(seqmix_softmax_desc* desc);
